@@ -249,6 +249,193 @@ dck_status dck_decode_attention_noalloc(const dck_layer_desc* desc, const void* 
                                         int32_t batch, float rope_theta, void* out, void* stream);
 
 /*
+ * Uncompressed layers: a paged key-value cache.
+ *
+ * A model whose cache is compressed keeps some layers as they were, and the
+ * uncompressed cache is what the latent one is measured against.  The entry
+ * points below (the paper has no counterpart) serve such layers: full keys,
+ * stored after rotation, and values in pages of a shared pool.
+ *   dck_page_update             block tables, free list and slot map of a step
+ *   dck_rope                    rotary positions, and the gradient through them
+ *   dck_paged_append            new tokens' rotated keys and values into their rows
+ *   dck_paged_decode_attention  one query per sequence over the pages
+ * A page holds page_size consecutive tokens of one sequence; sequence b's token
+ * t lies in page block_table[b][t / page_size] at offset t % page_size.  A slot
+ * is page * page_size + offset; the slots of dck_page_update are also valid
+ * cache rows (d_rows) of dck_latent_append.
+ *
+ * dck_paged_desc describes one layer's caches:
+ *   n_q_heads     Hq; n_kv_heads Hkv divides Hq; consecutive query heads share
+ *                 a KV head
+ *   head_dim      d, a multiple of 8, 8 .. 256
+ *   page_size     tokens per page, 1 .. 65536
+ *   n_pages       pages of the pool, 1 .. 2^31 - 1
+ *   dtype         element type of caches, queries, keys, values and outputs
+ *   k_*_stride    elements between pages, tokens of a page and heads of the key
+ *   v_*_stride    and value cache, positive multiples of 16 bytes; head elements are
+ *                 consecutive.  Any order of pages, tokens and heads, and keys
+ *                 and values in one buffer or two, are expressed by them.
+ */
+typedef struct {
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t page_size;
+  int32_t n_pages;
+  int32_t dtype; /* dck_dtype */
+  int64_t k_page_stride, k_token_stride, k_head_stride;
+  int64_t v_page_stride, v_token_stride, v_head_stride;
+} dck_paged_desc;
+
+/* Checks a descriptor without launching anything. */
+dck_status dck_validate_paged_desc(const dck_paged_desc* desc);
+
+/*
+ * One step's page bookkeeping, on the device: requests grow, shrink, start and
+ * end, pages are taken from and given back to a free list, and every new token
+ * gets its position and its slot.  With p(n) = ceil(n / page_size):
+ *   batch          requests, 0 .. 4096
+ *   d_old_len      device int32 [batch]: tokens request b holds (0: it starts)
+ *   d_new_len      device int32 [batch]: tokens it is to hold (0: it ends; less
+ *                  than before: its last tokens are given back)
+ *   d_seq_len      device int32 [batch] out: tokens it holds after the call, the
+ *                  new length or, if no pages were left for it, the old one.  May
+ *                  be d_old_len or d_new_len itself.
+ *   block_table    device int32 [batch][table_stride], 0 <= table_stride < 2^31:
+ *                  columns p(old) .. p(new)-1 of requests that grow are written,
+ *                  nothing else
+ *   free_pages     device int32 [n_pages]: the pages in [0, free_in[0]) are free.
+ *                  A page is taken from its end; pages given back (in the order
+ *                  of requests and columns) are put there first.  Written from
+ *                  free_in[0] on.
+ *   d_free_in      device int32 [2]: [0] the number of free pages
+ *   d_free_out     device int32 [2] out: [0] the number left, [1] the requests
+ *                  refused for want of pages.  May be d_free_in itself.
+ *   n_tok          capacity of d_slots and d_positions, 0 .. 2^31 - 1
+ *   d_slots        device int64 [n_tok] out: slot of each new token, requests one
+ *                  after the other; -1 for tokens of a refused request and past
+ *                  the last new token (the append skips those)
+ *   d_positions    device int32 [n_tok] out: position of each (0 past the last)
+ *   d_cu_new       device int32 [batch + 1] out: first new token of each request,
+ *                  refused ones included, and their total
+ * Pages are granted in the order of requests: with g_b the pages that requests
+ * before b ask for, b is granted if it asks for none or g_b plus its own are at
+ * most the free pages and those given back.  Want of pages is no error.  A
+ * negative length, one beyond the table, a free count outside [0, n_pages], more
+ * pages given back than the list can hold, a page number outside the pool or more
+ * new tokens than n_tok are recorded as a device error (DCK_ERR_INVALID from
+ * dck_last_device_error); the request concerned is refused (a length below 0 counts as 0), its slots are -1.
+ * Deterministic; one launch; no workspace.
+ */
+dck_status dck_page_update(int32_t batch, int32_t page_size, int32_t n_pages, const int32_t* d_old_len,
+                           const int32_t* d_new_len, int32_t* d_seq_len, int32_t* block_table, int64_t table_stride,
+                           int32_t* free_pages, const int32_t* d_free_in, int32_t* d_free_out, int64_t n_tok,
+                           int64_t* d_slots, int32_t* d_positions, int32_t* d_cu_new, void* stream);
+
+/*
+ * Rotary positions.  Pair i < R/2 of a head's first R = rotary_dim elements is
+ * turned by t w_i at position t and scaled by `magnitude`; elements from R on
+ * pass unchanged.
+ *   layout        DCK_ROPE_HALF: pairs (i, i + R/2); DCK_ROPE_INTERLEAVED: (2i, 2i + 1)
+ *   rotary_dim    R, even, 2 .. 256, at most the head dim
+ *   theta         > 0; w_i = theta^(-2i/R) before scaling
+ *   scaling       long contexts, by `factor` f >= 1:
+ *     DCK_ROPE_NONE    w_i
+ *     DCK_ROPE_LINEAR  w_i / f (position interpolation)
+ *     DCK_ROPE_NTK     theta f^(R/(R-2)) in theta's place (R > 2)
+ *     DCK_ROPE_BANDS   by the turns n_i = trained_len w_i / 2 pi that a pair makes over
+ *                      the trained length: w_i from `fast` turns on, w_i / f up to `slow`,
+ *                      linear in n_i between (0 <= slow < fast)
+ *     DCK_ROPE_YARN    w_i below pair a, w_i / f from pair b on, linear in i between,
+ *                      a = floor(c(fast)), b = ceil(c(slow)) clamped to [0, R-1],
+ *                      c(n) = R ln(trained_len / (2 pi n)) / (2 ln theta)
+ *                      (0 < slow < fast, theta > 1); its usual magnitude is 0.1 ln f + 1
+ * dck_rope_init checks the settings and fills a host structure that the caller keeps
+ * and passes by pointer (read during the call only).  Frequencies are kept as 64-bit
+ * fractions of a turn, so angles are exact to fp32 rounding at every int32 position.
+ */
+typedef enum { DCK_ROPE_HALF = 0, DCK_ROPE_INTERLEAVED = 1 } dck_rope_layout;
+typedef enum {
+  DCK_ROPE_NONE = 0,
+  DCK_ROPE_LINEAR = 1,
+  DCK_ROPE_NTK = 2,
+  DCK_ROPE_BANDS = 3,
+  DCK_ROPE_YARN = 4
+} dck_rope_scaling;
+
+typedef struct {
+  int32_t layout;
+  int32_t rotary_dim;
+  float magnitude;
+  int32_t initialised; /* set by dck_rope_init */
+  uint64_t turns[128]; /* w_i / 2 pi mod 1, times 2^64 */
+} dck_rope_table;
+
+dck_status dck_rope_init(dck_rope_table* table, int32_t layout, int32_t rotary_dim, double theta, int32_t scaling,
+                         double factor, double slow, double fast, int32_t trained_len, double magnitude);
+
+/*
+ * out = rotation of x at d_positions (device int32 [n_tok]), or with `transpose`
+ * its transpose: the gradient with respect to x, given the output's gradient.
+ * x and out are [n_tok, n_heads, head_dim] with the given element strides between
+ * tokens and heads (head elements consecutive); out may be x itself (same strides),
+ * else they must not overlap.  head_dim >= rotary_dim, at most 65536; computed in
+ * fp32, rounded once.  n_tok = 0 is a no-op.  One launch; no workspace.
+ */
+dck_status dck_rope(const dck_rope_table* table, const void* x, int32_t n_tok, int32_t n_heads, int32_t head_dim,
+                    int32_t dtype, int64_t x_token_stride, int64_t x_head_stride, const int32_t* d_positions,
+                    void* out, int64_t out_token_stride, int64_t out_head_stride, int32_t transpose, void* stream);
+
+/*
+ * Appends new tokens to a paged cache, rotated: q_out = rope(q), and for each
+ * token with slot s: K row s = rope(k), V row s = v.
+ *   table        the rotation (NULL: none, positions are not read)
+ *   q            [n_tok, Hq, d], q_stride elements between tokens; NULL: no queries
+ *   k, v         [n_tok, Hkv, d] likewise (views of one projection's rows, for instance)
+ *   d_positions  device int32 [n_tok]; d_slots device int64 [n_tok], distinct; tokens of
+ *                slot -1 are not written to the cache (their query is rotated)
+ *   q_out        [n_tok, Hq, d] dense; may be q itself if q_stride is Hq d
+ *   kcache, vcache  the caches' first elements, 16-byte aligned
+ * Any other slot outside the pool is skipped and recorded as a device error.
+ * Computed in fp32, rounded once; values are copied.  n_tok = 0 is a no-op.
+ * One launch; no workspace.
+ */
+dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* table, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n_tok,
+                            const int32_t* d_positions, const int64_t* d_slots, void* q_out, void* kcache,
+                            void* vcache, void* stream);
+
+/*
+ * Attention of one new token per sequence over a paged cache.  For query head j with
+ * KV head h = floor(j Hkv / Hq) and the keys at positions t in [max(0, L_b - window), L_b)
+ * (window = 0: all of them):
+ *   s_t = scale <q_j, k_t>, and softcap * tanh(s_t / softcap) in its place if softcap > 0
+ *   o_j = sum_t softmax_t(s) v_t,   lse_j = ln sum_t exp(s_t)
+ *   q            [batch, Hq, d], rotated, q_stride elements between sequences
+ *   kcache, vcache  the caches' first elements, 16-byte aligned
+ *   block_table  device int32 [batch][table_stride]; only the pages of the window are read
+ *   d_seq_len    device int32 [batch]: L_b, the new token included.  0 gives a zero output
+ *                row and lse = -inf.
+ *   max_seq_len  an upper bound on every L_b, 1 .. 2^31 - 1 (plans the work)
+ *   scale        finite (1/sqrt(d) as a rule); softcap >= 0; window >= 0
+ *   out          [batch, Hq, d]; lse float [batch, Hq] or NULL: with it, results over parts
+ *                of a context can be joined
+ *   workspace    at least dck_paged_decode_workspace_size bytes, 256-byte aligned; needs no
+ *                initialisation
+ * Rows past a sequence's end are never read into the sums, whatever they hold.  Scores,
+ * softmax and sums are fp32.  A length below 0, above max_seq_len or beyond the table, or a
+ * page number outside the pool among those read, is recorded as a device error; the sequence's
+ * outputs concerned are zero with lse = -inf.  At most two launches; results do not depend
+ * on the order in which blocks run.
+ */
+size_t dck_paged_decode_workspace_size(const dck_paged_desc* desc, int32_t batch, int32_t max_seq_len);
+dck_status dck_paged_decode_attention(const dck_paged_desc* desc, const void* q, int64_t q_stride, const void* kcache,
+                                      const void* vcache, const int32_t* block_table, int64_t table_stride,
+                                      const int32_t* d_seq_len, int32_t batch, int32_t max_seq_len, float scale,
+                                      int32_t window, float softcap, void* out, float* lse, void* workspace,
+                                      size_t ws_bytes, void* stream);
+
+/*
  * Synchronises `stream`, then returns and clears the device error word of the
  * current device: DCK_OK, DCK_ERR_INVALID (a length or row was outside the
  * cache) or DCK_ERR_TIMEOUT (a bounded wait inside a kernel gave up).

@@ -17,9 +17,12 @@ Contents
 * ``append.py``  - the latent projection z = x L of new tokens (Sec. III-A).
 * ``layout.py``  - parameter counts of grouped key factors (Sec. III-C,
   Table I).
+* ``paged.py``   - uncompressed layers: page bookkeeping as a program on lists,
+  rotations as complex products, attention over a paged cache.
 
 Parity status: every function is pinned by ``tests/test_oracle_pins.py`` and
-``tests/test_prefill_oracle_pins.py`` (closed forms, library routines,
+``tests/test_prefill_oracle_pins.py``, ``paged.py`` by ``tests/test_paged_abi.py``
+(closed forms, library routines,
 invariants and brute force); none is "parity unpinned".
 """
 

@@ -6,6 +6,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "api_state.h"
 #include "common.cuh"
 #include "tc_common.cuh"
 #include "tc_host.h"
@@ -51,6 +52,9 @@ thread_local int t_last_launches = 0;
 thread_local void* t_events[kMaxHookEvents] = {};
 thread_local int t_n_events = 0;
 
+}  // namespace
+
+namespace dck {
 bool device_state(int** err, int* sms) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
@@ -67,6 +71,18 @@ bool device_state(int** err, int* sms) {
   if (sms) *sms = g_sm_count[dev];
   return true;
 }
+
+LaunchHook thread_hook() {
+  LaunchHook h;
+  h.ev = t_events;
+  h.n_ev = t_n_events;
+  return h;
+}
+
+void set_last_launches(int n) { t_last_launches = n; }
+}  // namespace dck
+
+namespace {
 
 dck_status check_desc(const dck_layer_desc* d) {
   if (!d) return DCK_ERR_INVALID;

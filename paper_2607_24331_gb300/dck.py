@@ -29,7 +29,8 @@ EXPORTED = (
     "dck_decode_workspace_size", "dck_decode_attention", "dck_last_device_error", "dck_set_decode_kernel",
     "dck_last_launch_count", "dck_synth_gaussian", "dck_set_timing_events", "dck_decode_attention_noalloc",
     "dck_selftest_bounded_wait", "dck_selftest_append_timeout", "dck_decode_step", "dck_decode_step_workspace_size",
-    "dck_prefill_workspace_size", "dck_prefill_attention",
+    "dck_prefill_workspace_size", "dck_prefill_attention", "dck_validate_paged_desc", "dck_page_update",
+    "dck_rope_init", "dck_rope", "dck_paged_append", "dck_paged_decode_workspace_size", "dck_paged_decode_attention",
 )
 
 
@@ -52,6 +53,17 @@ class LayerDesc(ctypes.Structure):
         ("rank_v", ctypes.c_int32),
         ("dtype", ctypes.c_int32),
     ]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "dtype")] + [
+        (n, ctypes.c_int64) for n in ("k_page_stride", "k_token_stride", "k_head_stride", "v_page_stride",
+                                      "v_token_stride", "v_head_stride")]
+
+
+class RopeTable(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("initialised", ctypes.c_int32), ("turns", ctypes.c_uint64 * 128)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -104,6 +116,21 @@ def lib() -> ctypes.CDLL:
     L.dck_selftest_append_timeout.argtypes = [D, P, I32, P, P, P, P, P, I64, I64, P]
     L.dck_synth_gaussian.restype = I32
     L.dck_synth_gaussian.argtypes = [P, I64, U64, I64, F32, I32, P]
+    G, R, F64 = ctypes.POINTER(PagedDesc), ctypes.POINTER(RopeTable), ctypes.c_double
+    L.dck_validate_paged_desc.restype = I32
+    L.dck_validate_paged_desc.argtypes = [G]
+    L.dck_page_update.restype = I32
+    L.dck_page_update.argtypes = [I32, I32, I32, P, P, P, P, I64, P, P, P, I64, P, P, P, P]
+    L.dck_rope_init.restype = I32
+    L.dck_rope_init.argtypes = [R, I32, I32, F64, I32, F64, F64, F64, I32, F64]
+    L.dck_rope.restype = I32
+    L.dck_rope.argtypes = [R, P, I32, I32, I32, I32, I64, I64, P, P, I64, I64, I32, P]
+    L.dck_paged_append.restype = I32
+    L.dck_paged_append.argtypes = [G, R, P, I64, P, I64, P, I64, I32, P, P, P, P, P, P]
+    L.dck_paged_decode_workspace_size.restype = SZ
+    L.dck_paged_decode_workspace_size.argtypes = [G, I32, I32]
+    L.dck_paged_decode_attention.restype = I32
+    L.dck_paged_decode_attention.argtypes = [G, P, I64, P, P, P, I64, P, I32, I32, F32, I32, F32, P, P, P, SZ, P]
     _lib = L
     return L
 
@@ -140,6 +167,49 @@ class Layer:
     @property
     def ref(self):
         return ctypes.byref(self.desc)
+
+
+class PagedCache:
+    """A dck_paged_desc: one uncompressed layer's key and value caches in pages.
+
+    ``k_strides`` and ``v_strides`` are the elements between pages, tokens of a page
+    and heads; by default caches are dense [n_pages, page_size, n_kv_heads, head_dim].
+    """
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, dtype: str,
+                 k_strides: Optional[Sequence[int]] = None, v_strides: Optional[Sequence[int]] = None):
+        row = n_kv_heads * head_dim
+        dense = (page_size * row, row, head_dim)
+        self.desc = PagedDesc(n_q_heads, n_kv_heads, head_dim, page_size, n_pages,
+                              DCK_F32 if dtype == "f32" else DCK_BF16, *(k_strides or dense), *(v_strides or dense))
+        self.ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def from_tensors(cls, kcache, vcache, n_q_heads: int) -> "PagedCache":
+        """The descriptor of torch caches (or views) [n_pages, page_size, n_kv_heads, head_dim], bf16 or fp32,
+        whose head elements are consecutive."""
+        name = {"torch.bfloat16": "bf16", "torch.float32": "f32"}.get(str(kcache.dtype))
+        if kcache.shape != vcache.shape or kcache.dtype != vcache.dtype or kcache.dim() != 4 or name is None:
+            raise ValueError("kcache and vcache: [n_pages, page_size, n_kv_heads, head_dim], bfloat16 or float32 alike")
+        if kcache.stride(3) != 1 or vcache.stride(3) != 1:
+            raise ValueError("the elements of a head must be consecutive")
+        n_pages, page_size, n_kv_heads, head_dim = kcache.shape
+        return cls(n_q_heads, n_kv_heads, head_dim, page_size, n_pages, name, kcache.stride()[:3], vcache.stride()[:3])
+
+
+class Rope:
+    """A dck_rope_table (dck_rope_init): rotary dimension, base, layout and the scaling for long contexts."""
+
+    LAYOUTS = {"half": 0, "interleaved": 1}
+    SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
+
+    def __init__(self, rotary_dim: int, theta: float, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                 slow: float = 1.0, fast: float = 32.0, trained_len: int = 0, magnitude: float = 1.0):
+        self.table = RopeTable()
+        check(lib().dck_rope_init(ctypes.byref(self.table), self.LAYOUTS[layout], int(rotary_dim), float(theta),
+                                  self.SCALINGS[scaling], float(factor), float(slow), float(fast), int(trained_len),
+                                  float(magnitude)), "dck_rope_init")
+        self.ref = ctypes.byref(self.table)
 
 
 def _ptr(t) -> Optional[int]:
@@ -218,6 +288,50 @@ def dck_latent_append(layer: Layer, x, n_tok: int, A_k, A_v, rows, kcache, vcach
                       workspace, ws_bytes: int, stream=None) -> int:
     return lib().dck_latent_append(layer.ref, _ptr(x), int(n_tok), _ptr(A_k), _ptr(A_v), _ptr(rows), _ptr(kcache),
                                    _ptr(vcache), int(n_rows), _ptr(workspace), int(ws_bytes), _stream(stream))
+
+
+def dck_validate_paged_desc(cache: PagedCache) -> int:
+    return lib().dck_validate_paged_desc(cache.ref)
+
+
+def dck_page_update(batch: int, page_size: int, n_pages: int, old_len, new_len, seq_len, block_table,
+                    table_stride: int, free_pages, free_in, free_out, n_tok: int, slots, positions, cu_new,
+                    stream=None) -> int:
+    """A step's page bookkeeping: tables, free list, lengths, slots and positions of the new tokens."""
+    return lib().dck_page_update(int(batch), int(page_size), int(n_pages), _ptr(old_len), _ptr(new_len), _ptr(seq_len),
+                                 _ptr(block_table), int(table_stride), _ptr(free_pages), _ptr(free_in), _ptr(free_out),
+                                 int(n_tok), _ptr(slots), _ptr(positions), _ptr(cu_new), _stream(stream))
+
+
+def dck_rope(rope: Rope, x, n_tok: int, n_heads: int, head_dim: int, dtype: int, x_token_stride: int,
+             x_head_stride: int, positions, out, out_token_stride: int, out_head_stride: int, transpose: bool = False,
+             stream=None) -> int:
+    """Rotation of x at the given positions, or its transpose (the gradient)."""
+    return lib().dck_rope(rope.ref, _ptr(x), int(n_tok), int(n_heads), int(head_dim), int(dtype), int(x_token_stride),
+                          int(x_head_stride), _ptr(positions), _ptr(out), int(out_token_stride), int(out_head_stride),
+                          int(transpose), _stream(stream))
+
+
+def dck_paged_append(cache: PagedCache, rope: Optional[Rope], q, q_stride: int, k, k_stride: int, v, v_stride: int,
+                     n_tok: int, positions, slots, q_out, kcache, vcache, stream=None) -> int:
+    """New tokens' queries rotated to q_out, their keys (rotated) and values written to the slots' cache rows."""
+    return lib().dck_paged_append(cache.ref, rope.ref if rope is not None else None, _ptr(q), int(q_stride), _ptr(k),
+                                  int(k_stride), _ptr(v), int(v_stride), int(n_tok), _ptr(positions), _ptr(slots),
+                                  _ptr(q_out), _ptr(kcache), _ptr(vcache), _stream(stream))
+
+
+def dck_paged_decode_workspace_size(cache: PagedCache, batch: int, max_seq_len: int) -> int:
+    return lib().dck_paged_decode_workspace_size(cache.ref, int(batch), int(max_seq_len))
+
+
+def dck_paged_decode_attention(cache: PagedCache, q, q_stride: int, kcache, vcache, block_table, table_stride: int,
+                               seq_len, batch: int, max_seq_len: int, scale: float, window: int, softcap: float, out,
+                               lse, workspace, ws_bytes: int, stream=None) -> int:
+    """One query per sequence over its pages; lse (optional): the log of the softmax's sum."""
+    return lib().dck_paged_decode_attention(cache.ref, _ptr(q), int(q_stride), _ptr(kcache), _ptr(vcache),
+                                            _ptr(block_table), int(table_stride), _ptr(seq_len), int(batch),
+                                            int(max_seq_len), float(scale), int(window), float(softcap), _ptr(out),
+                                            _ptr(lse), _ptr(workspace), int(ws_bytes), _stream(stream))
 
 
 def dck_last_device_error(stream=None) -> int:
