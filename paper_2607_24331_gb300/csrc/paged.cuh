@@ -75,10 +75,11 @@ struct RopeLaunch {
   const int32_t* positions;
   const int64_t* slots;
   int32_t page, n_pages;
+  Divider by_page;
   int* err;
   RopeArgs rope;
 };
-cudaError_t launch_rope_rows(const RopeLaunch& a, int dtype, cudaStream_t s);
+cudaError_t launch_rope_rows(const RopeLaunch& a, int dtype, int sms, cudaStream_t s);
 
 struct PagedDecodeArgs {
   PagedView v;

@@ -172,7 +172,8 @@ dck_status dck_rope(const dck_rope_table* table, const void* x, int32_t n_tok, i
     if (st < 0 || st > most) return DCK_ERR_INVALID;
   if (x == out && (x_token_stride != out_token_stride || x_head_stride != out_head_stride)) return DCK_ERR_INVALID;
   if ((n_heads > 1 && out_head_stride < head_dim) || (n_tok > 1 && out_token_stride < head_dim)) return DCK_ERR_INVALID;
-  if (!device_state(&a.err, nullptr)) return DCK_ERR_CUDA;
+  int sms = 0;
+  if (!device_state(&a.err, &sms)) return DCK_ERR_CUDA;
   a.n_rows = 1;
   RopeRows& r = a.rows[0];
   r.src = x;
@@ -187,7 +188,8 @@ dck_status dck_rope(const dck_rope_table* table, const void* x, int32_t n_tok, i
   a.d = head_dim;
   a.positions = d_positions;
   a.page = a.n_pages = 1;
-  if (launch_rope_rows(a, dtype, static_cast<cudaStream_t>(stream)) != cudaSuccess) return DCK_ERR_CUDA;
+  a.by_page = divider(1);
+  if (launch_rope_rows(a, dtype, sms, static_cast<cudaStream_t>(stream)) != cudaSuccess) return DCK_ERR_CUDA;
   set_last_launches(1);
   return DCK_OK;
 }
@@ -214,7 +216,8 @@ dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* ta
   if (k_stride < 0 || v_stride < 0 || k_stride > most || v_stride > most) return DCK_ERR_INVALID;
   if (q && (q_stride < 0 || q_stride > most || (q == q_out && n_tok > 1 && q_stride != (int64_t)desc->n_q_heads * d)))
     return DCK_ERR_INVALID;
-  if (!device_state(&a.err, nullptr)) return DCK_ERR_CUDA;
+  int sms = 0;
+  if (!device_state(&a.err, &sms)) return DCK_ERR_CUDA;
   RopeRows* r = a.rows;
   r->src = k;
   r->dst = kcache;
@@ -254,7 +257,8 @@ dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* ta
   a.slots = d_slots;
   a.page = desc->page_size;
   a.n_pages = desc->n_pages;
-  if (launch_rope_rows(a, desc->dtype, static_cast<cudaStream_t>(stream)) != cudaSuccess) return DCK_ERR_CUDA;
+  a.by_page = divider((uint32_t)desc->page_size);
+  if (launch_rope_rows(a, desc->dtype, sms, static_cast<cudaStream_t>(stream)) != cudaSuccess) return DCK_ERR_CUDA;
   set_last_launches(1);
   return DCK_OK;
 }

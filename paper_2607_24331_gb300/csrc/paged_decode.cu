@@ -37,6 +37,7 @@ struct PagedPlan {
   int groups;        // head groups: Hkv * chunks / wh
   int tile;          // tokens of a CTA's tile
   int n_items;       // CTAs
+  Divider by_chunks;
 };
 
 struct Entry {  // a (head group, sequence) shared by CTAs c0 .. c1
@@ -177,7 +178,7 @@ struct Loader {
     const uint32_t col = g.a.v.by_page.div(r.valid ? t : 0);
     r.off = t - col * g.a.v.page;
     r.page = r.valid ? g.a.table[(int64_t)c.b * g.a.table_stride + col] : 0;
-    r.head = (c.group * g.p.wh + wh) / g.p.chunks;
+    r.head = g.p.by_chunks.div(c.group * g.p.wh + wh);
     return r;
   }
 
@@ -214,16 +215,42 @@ struct Loader {
   }
 };
 
-// Query head of row r of a warp's tile, or -1.
-__device__ __forceinline__ int query_head(const PagedKernelArgs& g, int group, int wh, int r) {
-  const int vh = group * g.p.wh + wh, h = vh / g.p.chunks, j = (vh - h * g.p.chunks) * g.p.rows + r;
-  return r < g.p.rows && j < g.a.v.qpg ? h * g.a.v.qpg + j : -1;
+// The queries of one head of a head group: `count` of them from query head `first` on.
+struct Queries {
+  int first, count;
+};
+__device__ __forceinline__ Queries queries_of(const PagedKernelArgs& g, int group, int wh) {
+  const int vh = group * g.p.wh + wh, h = g.p.by_chunks.div(vh), r0 = (vh - h * g.p.chunks) * g.p.rows;
+  return {h * g.a.v.qpg + r0, min(g.p.rows, g.a.v.qpg - r0)};
 }
 
-// A score in log2 units.
-__device__ __forceinline__ float to_log2(float s, const PagedDecodeArgs& a, float scale2, float inv_cap, float cap2) {
-  return a.softcap > 0.f ? cap2 * tanhf(s * inv_cap) : s * scale2;
+// tanh to 3e-7 of its value: below 1/2 an odd polynomial (least squares in x^2 on
+// tanh(x) / x, 6e-8), above it 1 - 2 / (e^2x + 1).
+__device__ __forceinline__ float tanh_of(float x) {
+  const float ax = fabsf(x), u = x * x;
+  float p = -6.6395057e-3f;
+  p = fmaf(p, u, 2.1292942e-2f);
+  p = fmaf(p, u, -5.3898074e-2f);
+  p = fmaf(p, u, 1.3332954e-1f);
+  p = fmaf(p, u, -3.3333325e-1f);
+  const float big = 1.f - __fdividef(2.f, exp2_approx(ax * 2.88539008f) + 1.f);
+  return ax < 0.5f ? fmaf(x * u, p, x) : copysignf(ax > 20.f ? 1.f : big, x);
 }
+
+// Scores in log2 units.
+struct ScoreScale {
+  float scale2, inv_cap, cap2;  // cap2 = 0: no cap
+  template <int N>
+  __device__ __forceinline__ void apply(float (&s)[N]) const {
+    if (cap2 > 0.f) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = cap2 * tanh_of(s[i] * inv_cap);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] *= scale2;
+    }
+  }
+};
 
 // ---------------------------------------------------------------------------
 // bf16: tensor cores (mma.sync m16n8k16, queries as rows)
@@ -268,24 +295,23 @@ struct TensorTile {
   float o[Z::DP / 8][4], m[kQ], l[kQ];
   uint32_t q[Z::DP / 16][2 * kQ];
 
-  __device__ __forceinline__ void begin(const PagedKernelArgs& g, const Cursor& c, int wh, int lane, int, float*) {
+  __device__ __forceinline__ void begin(const PagedKernelArgs& g, int b, const Queries& qs, int lane, float*) {
+    const int words = g.a.v.d / 8;  // runs of 8 elements in a row
 #pragma unroll
     for (int x = 0; x < kQ; ++x) {
-      const int j = query_head(g, c.group, wh, lane / 4 + 8 * x);
-      const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(g.a.q) + c.b * g.a.q_stride + (int64_t)j * g.a.v.d;
-      const bool words = (reinterpret_cast<uintptr_t>(src) & 3) == 0;
+      const int r = lane / 4 + 8 * x;
+      const uint16_t* src = static_cast<const uint16_t*>(g.a.q) + b * g.a.q_stride +
+                            (int64_t)(qs.first + (r < qs.count ? r : 0)) * g.a.v.d + (lane & 3) * 2;
+      const int have = r < qs.count ? words : 0;
+      if ((reinterpret_cast<uintptr_t>(src) & 3) == 0) {
 #pragma unroll
-      for (int k = 0; k < Z::DP / 16; ++k)
+        for (int w = 0; w < Z::DP / 8; ++w)
+          q[w / 2][w % 2 * kQ + x] = w < have ? *reinterpret_cast<const uint32_t*>(src + 8 * w) : 0u;
+      } else {
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int e = k * 16 + y * 8 + (lane & 3) * 2;
-          uint32_t w = 0;
-          if (j >= 0 && e < g.a.v.d) {
-            const uint16_t* s16 = reinterpret_cast<const uint16_t*>(src + e);
-            w = words ? *reinterpret_cast<const uint32_t*>(s16) : s16[0] | (uint32_t)s16[1] << 16;
-          }
-          q[k][y * kQ + x] = w;
-        }
+        for (int w = 0; w < Z::DP / 8; ++w)
+          q[w / 2][w % 2 * kQ + x] = w < have ? src[8 * w] | (uint32_t)src[8 * w + 1] << 16 : 0u;
+      }
       m[x] = -CUDART_INF_F;
       l[x] = 0.f;
     }
@@ -294,8 +320,7 @@ struct TensorTile {
   }
 
   // The 16 tokens of a stage, the first `live` of them present (0 or fewer: none).
-  __device__ __forceinline__ void step(const PagedKernelArgs& g, uint32_t keys, int live, int lane, float scale2,
-                                       float inv_cap, float cap2, float*) {
+  __device__ __forceinline__ void step(uint32_t keys, int live, int lane, const ScoreScale& scale, float*) {
     if (live <= 0) return;
     float s[2][4] = {};
     {
@@ -313,6 +338,21 @@ struct TensorTile {
         }
       }
     }
+    if (PACK) {  // rows 8-15 of the tile hold nothing
+      float v[4] = {s[0][0], s[0][1], s[1][0], s[1][1]};
+      scale.apply(v);
+      s[0][0] = v[0], s[0][1] = v[1], s[1][0] = v[2], s[1][1] = v[3];
+    } else {
+      scale.apply(s[0]);
+      scale.apply(s[1]);
+    }
+    if (live < 16) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (n * 8 + (lane & 3) * 2 + (y & 1) >= live) s[n][y] = -CUDART_INF_F;
+    }
     uint32_t hi[kQ][2], lo[kQ][2];
     bool raise = false;
     float top[kQ];
@@ -322,12 +362,7 @@ struct TensorTile {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          float& v = s[n][2 * x + y];
-          v = to_log2(v, g.a, scale2, inv_cap, cap2);
-          if (live < 16 && n * 8 + (lane & 3) * 2 + y >= live) v = -CUDART_INF_F;
-          mx = fmaxf(mx, v);
-        }
+        for (int y = 0; y < 2; ++y) mx = fmaxf(mx, s[n][2 * x + y]);
       mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
       mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
       raise |= mx > m[x];
@@ -384,21 +419,20 @@ struct TensorTile {
 #pragma unroll
       for (int n = 0; n < Z::DP / 8; ++n) o[n][0] += o[n][2], o[n][1] += o[n][3];
   }
-  // Calls f(row, maximum, sum) once per row, by one lane.
+  // Rows and elements of this lane: f(x, row) for each of its rows, then
+  // g(x, element, value, next value) for each pair of elements of row x.
+  static constexpr int kMine = kQ;
+  static __device__ __forceinline__ int row(int x, int lane) { return lane / 4 + 8 * x; }
+  static __device__ __forceinline__ bool speaks(int lane) { return (lane & 3) == 0; }  // one lane per row
   template <class F>
-  __device__ __forceinline__ void each_row(int lane, F f) const {
+  __device__ __forceinline__ void each(int x, int lane, int e0, int e1, F f) const {
 #pragma unroll
-    for (int x = 0; x < kQ; ++x)
-      if ((lane & 3) == 0) f(lane / 4 + 8 * x, m[x], l[x]);
+    for (int n = 0; n < Z::DP / 8; ++n)
+      if (n * 8 >= e0 && n * 8 < e1) f(n * 8 + (lane & 3) * 2, o[n][2 * x], o[n][2 * x + 1]);
   }
-  // Calls f(row, element, value, value of the next element, the row's sum) for the elements in [e0, e1).
-  template <class F>
-  __device__ __forceinline__ void each(int lane, int e0, int e1, F f) const {
+  __device__ __forceinline__ void times(int x, float c) {
 #pragma unroll
-    for (int x = 0; x < kQ; ++x)
-#pragma unroll
-      for (int n = 0; n < Z::DP / 8; ++n)
-        if (n * 8 >= e0 && n * 8 < e1) f(lane / 4 + 8 * x, n * 8 + (lane & 3) * 2, o[n][2 * x], o[n][2 * x + 1], l[x]);
+    for (int n = 0; n < Z::DP / 8; ++n) o[n][2 * x] *= c, o[n][2 * x + 1] *= c;
   }
 };
 
@@ -417,13 +451,16 @@ struct SimtTile {
   float m[ROWS], l[ROWS];
 
   // `mine`: this warp's shared memory, ROWS x DP queries, then 8 x ROWS weights.
-  __device__ __forceinline__ void begin(const PagedKernelArgs& g, const Cursor& c, int wh, int lane, int, float* mine) {
+  __device__ __forceinline__ void begin(const PagedKernelArgs& g, int b, const Queries& qs, int lane, float* mine) {
     __syncwarp();
+    const float* src = static_cast<const float*>(g.a.q) + b * g.a.q_stride + (int64_t)qs.first * g.a.v.d;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int j = query_head(g, c.group, wh, r);
-      const float* src = static_cast<const float*>(g.a.q) + c.b * g.a.q_stride + (int64_t)j * g.a.v.d;
-      for (int e = lane; e < Z::DP; e += 32) mine[r * Z::DP + e] = j >= 0 && e < g.a.v.d ? src[e] : 0.f;
+#pragma unroll
+      for (int e = 0; e < Z::DP; e += 32) {
+        const bool have = r < qs.count && e + lane < g.a.v.d;
+        mine[r * Z::DP + e + lane] = have ? src[r * g.a.v.d + e + lane] : 0.f;
+      }
       m[r] = -CUDART_INF_F;
       l[r] = 0.f;
 #pragma unroll
@@ -432,8 +469,7 @@ struct SimtTile {
     __syncwarp();
   }
 
-  __device__ __forceinline__ void step(const PagedKernelArgs& g, uint32_t keys, int live, int lane, float scale2,
-                                       float inv_cap, float cap2, float* mine) {
+  __device__ __forceinline__ void step(uint32_t keys, int live, int lane, const ScoreScale& scale, float* mine) {
     if (live <= 0) return;
     const auto chunk = [](uint32_t at) {
       float4 v;
@@ -454,23 +490,36 @@ struct SimtTile {
     }
     float* weights = mine + ROWS * Z::DP;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      float v = s[r];
-      v += __shfl_xor_sync(~0u, v, 8);
-      v += __shfl_xor_sync(~0u, v, 16);
-      v = to_log2(v, g.a, scale2, inv_cap, cap2);
-      if (t >= live) v = -CUDART_INF_F;
-      float mx = fmaxf(m[r], v);
+    for (int r = 0; r < ROWS; ++r) s[r] += __shfl_xor_sync(~0u, s[r], 8);
 #pragma unroll
-      for (int x = 1; x < 8; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, x));
-      if (mx > m[r]) {  // the same in every lane
-        const float c = exp2_approx(m[r] - mx);
-        m[r] = mx;
+    for (int r = 0; r < ROWS; ++r) s[r] += __shfl_xor_sync(~0u, s[r], 16);
+    scale.apply(s);
+    float top[ROWS];
+    bool raise = false;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (t >= live) s[r] = -CUDART_INF_F;
+      top[r] = fmaxf(m[r], s[r]);
+    }
+#pragma unroll
+    for (int x = 1; x < 8; x <<= 1)
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], x));
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) raise |= top[r] > m[r];
+    if (raise) {  // the same in every lane
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const float c = m[r] == top[r] ? 1.f : exp2_approx(m[r] - top[r]);
+        m[r] = top[r];
         l[r] *= c;
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) o[r][k].x *= c, o[r][k].y *= c, o[r][k].z *= c, o[r][k].w *= c;
       }
-      const float p = exp2_approx(v - (mx == -CUDART_INF_F ? 0.f : mx));
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const float p = exp2_approx(s[r] - (m[r] == -CUDART_INF_F ? 0.f : m[r]));
       if (quarter == 0) {
         l[r] += p;
         weights[t * ROWS + r] = p;
@@ -517,24 +566,23 @@ struct SimtTile {
       }
     }
   }
+  static constexpr int kMine = ROWS;
+  static __device__ __forceinline__ int row(int x, int) { return x; }
+  static __device__ __forceinline__ bool speaks(int lane) { return lane == 0; }
   template <class F>
-  __device__ __forceinline__ void each_row(int lane, F f) const {
+  __device__ __forceinline__ void each(int x, int lane, int e0, int e1, F f) const {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-      if (lane == 0) f(r, m[r], l[r]);
-  }
-  template <class F>
-  __device__ __forceinline__ void each(int lane, int e0, int e1, F f) const {
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-      for (int k = 0; k < kOwn; ++k) {
-        const int e = 4 * ((kSplit > 1 ? lane % Z::kChunks : lane) + 32 * k);
-        if (lane < 32 / kSplit && e >= e0 && e < e1) {
-          f(r, e, o[r][k].x, o[r][k].y, l[r]);
-          f(r, e + 2, o[r][k].z, o[r][k].w, l[r]);
-        }
+    for (int k = 0; k < kOwn; ++k) {
+      const int e = 4 * ((kSplit > 1 ? lane % Z::kChunks : lane) + 32 * k);
+      if (lane < 32 / kSplit && e >= e0 && e < e1) {
+        f(e, o[x][k].x, o[x][k].y);
+        f(e + 2, o[x][k].z, o[x][k].w);
       }
+    }
+  }
+  __device__ __forceinline__ void times(int x, float c) {
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) o[x][k].x *= c, o[x][k].y *= c, o[x][k].z *= c, o[x][k].w *= c;
   }
 };
 
@@ -606,11 +654,14 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
 
   Cursor at;
   at.enter(a, prefix, n_tiles, u0);
-  const float scale2 = a.scale * 1.44269504088896f, cap2 = a.softcap * 1.44269504088896f;
-  const float inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
+  ScoreScale scale;
+  scale.scale2 = a.scale * 1.44269504088896f;
+  scale.cap2 = a.softcap * 1.44269504088896f;
+  scale.inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
   float* mine = sh.mine + warp * (Tile::kRows * Z::DP + 8 * Tile::kRows);
   Tile tile;
-  tile.begin(g, at, wh, lane, warp, mine);
+  Queries qs = queries_of(g, at.group, wh);
+  tile.begin(g, at.b, qs, lane, mine);
 
   if (blockIdx.x == 0) {  // the list of what several CTAs share, for the second launch
     __shared__ int n_entries;
@@ -643,7 +694,7 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
     cp_async_wait<Z::S - 1>();
     __syncwarp();
     bad |= outside >> get & 1;
-    tile.step(g, load.ring + get * Z::kStage, at.len - at.token(g.p.tile) - wt * Z::TOK, lane, scale2, inv_cap, cap2, mine);
+    tile.step(load.ring + get * Z::kStage, at.len - at.token(g.p.tile) - wt * Z::TOK, lane, scale, mine);
     get = get + 1 == Z::S ? 0 : get + 1;
     const bool last = at.u + 1 == u1;
     if (at.u + 1 < at.end && !last) {
@@ -655,92 +706,77 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
     const int slot = 2 * blockIdx.x + (u0 < at.start);
     if (bad && lane == 0) atomicOr(a.err, kErrBadSeq);
     tile.finish();
-    if (g.p.wt == 1) {
-      tile.each_row(lane, [&](int r, float m, float l) {
-        const int j = query_head(g, at.group, wh, r);
-        if (j < 0) return;
-        if (whole) {
-          if (a.lse) a.lse[(int64_t)at.b * a.v.Hq + j] = bad || l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945f;
-        } else {
-          float* ml = g.part_ml + ((int64_t)(slot * g.p.wh + wh) * g.p.rows + r) * 2;
-          ml[0] = m;
-          ml[1] = bad ? -1.f : l;
-        }
-      });
-      tile.each(lane, 0, Z::DP, [&](int r, int e, float x, float y, float l) {
-        const int j = query_head(g, at.group, wh, r);
-        if (j < 0 || e >= d) return;
-        if (whole) {
-          T* p = out + ((int64_t)at.b * a.v.Hq + j) * d + e;
-          const bool none = bad || l == 0.f;
-          const float inv = 1.f / l;
-          p[0] = from_f32<T>(none ? 0.f : x * inv);
-          p[1] = from_f32<T>(none ? 0.f : y * inv);
-        } else {
-          float* p = g.part_u + ((int64_t)(slot * g.p.wh + wh) * g.p.rows + r) * Z::DP + e;
-          *reinterpret_cast<float2*>(p) = make_float2(x, y);
-        }
-      });
-    } else {
-      // runs of tokens join: all of them to the largest maximum
-      tile.each_row(lane, [&](int r, float m, float l) { sh.m[warp][r] = m, sh.l[warp][r] = l; });
+    const int64_t out_row = (int64_t)at.b * a.v.Hq + qs.first, part_row = (int64_t)(slot * g.p.wh + wh) * g.p.rows;
+    if (g.p.wt > 1) {  // the runs of tokens join: all to the largest maximum, then element by element
+#pragma unroll
+      for (int x = 0; x < Tile::kMine; ++x)
+        if (Tile::speaks(lane)) sh.m[warp][Tile::row(x, lane)] = tile.m[x], sh.l[warp][Tile::row(x, lane)] = tile.l[x];
       if (lane == 0) sh.bad[warp] = bad;
       __syncthreads();
-      const auto top = [&](int h, int r) {
-        float m = -CUDART_INF_F;
-        for (int w = h; w < Z::NW; w += g.p.wh) m = fmaxf(m, sh.m[w][r]);
-        return m;
-      };
-      const auto total = [&](int h, int r, float M) {
-        float l = 0.f;
-        for (int w = h; w < Z::NW; w += g.p.wh)
-          if (sh.m[w][r] != -CUDART_INF_F || sh.l[w][r] != 0.f) l += sh.l[w][r] * exp2_approx(sh.m[w][r] - M);
-        return l;
-      };
-      for (int x = threadIdx.x; x < g.p.wh * g.p.rows; x += Z::NW * 32) {
-        const int h = x / g.p.rows, r = x - h * g.p.rows, j = query_head(g, at.group, h, r);
-        if (j < 0) continue;
-        bool b = false;
-        for (int w = h; w < Z::NW; w += g.p.wh) b |= sh.bad[w] != 0;
-        const float M = top(h, r), l = total(h, r, M);
+      for (int w = wh; w < Z::NW; w += g.p.wh) bad |= sh.bad[w] != 0;
+#pragma unroll
+      for (int x = 0; x < Tile::kMine; ++x) {
+        const int r = Tile::row(x, lane);
+        float M = -CUDART_INF_F, sum = 0.f;
+        for (int w = wh; w < Z::NW; w += g.p.wh) M = fmaxf(M, sh.m[w][r]);
+        const float base = M == -CUDART_INF_F ? 0.f : M;
+        for (int w = wh; w < Z::NW; w += g.p.wh) sum += sh.l[w][r] * exp2_approx(sh.m[w][r] - base);
+        tile.times(x, exp2_approx(tile.m[x] - base));
+        tile.m[x] = M, tile.l[x] = sum;
+      }
+    }
+    float factor[Tile::kMine];
+#pragma unroll
+    for (int x = 0; x < Tile::kMine; ++x) {
+      const int r = Tile::row(x, lane);
+      const bool none = bad || tile.l[x] == 0.f;
+      factor[x] = !whole ? 1.f : none ? 0.f : 1.f / tile.l[x];
+      if (Tile::speaks(lane) && wt == 0 && r < qs.count) {
+        if (!whole) *reinterpret_cast<float2*>(g.part_ml + 2 * (part_row + r)) = make_float2(tile.m[x], bad ? -1.f : tile.l[x]);
+        else if (a.lse) a.lse[out_row + r] = none ? -CUDART_INF_F : (tile.m[x] + log2f(tile.l[x])) * 0.693147180559945f;
+      }
+    }
+    if (g.p.wt == 1) {
+#pragma unroll
+      for (int x = 0; x < Tile::kMine; ++x) {
+        const int r = Tile::row(x, lane);
+        if (r >= qs.count) continue;
         if (whole) {
-          if (a.lse) a.lse[(int64_t)at.b * a.v.Hq + j] = b || l == 0.f ? -CUDART_INF_F : (M + log2f(l)) * 0.693147180559945f;
+          T* p = out + (out_row + r) * d;
+          tile.each(x, lane, 0, d, [&](int e, float y, float z) {
+            p[e] = from_f32<T>(factor[x] == 0.f ? 0.f : y * factor[x]);
+            p[e + 1] = from_f32<T>(factor[x] == 0.f ? 0.f : z * factor[x]);
+          });
         } else {
-          float* ml = g.part_ml + ((int64_t)(slot * g.p.wh + h) * g.p.rows + r) * 2;
-          ml[0] = M;
-          ml[1] = b ? -1.f : l;
+          float* p = g.part_u + (part_row + r) * Z::DP;
+          tile.each(x, lane, 0, d, [&](int e, float y, float z) { *reinterpret_cast<float2*>(p + e) = make_float2(y, z); });
         }
       }
+    } else {
       for (int e0 = 0; e0 < d; e0 += kMergeDims) {
-        tile.each(lane, e0, e0 + kMergeDims, [&](int r, int e, float x, float y, float) {
-          *reinterpret_cast<float2*>(&sh.part[warp][r][e - e0]) = make_float2(x, y);
-        });
+#pragma unroll
+        for (int x = 0; x < Tile::kMine; ++x)
+          tile.each(x, lane, e0, e0 + kMergeDims, [&](int e, float y, float z) {
+            *reinterpret_cast<float2*>(&sh.part[warp][Tile::row(x, lane)][e - e0]) =
+                factor[x] == 0.f ? make_float2(0.f, 0.f) : make_float2(y * factor[x], z * factor[x]);
+          });
         __syncthreads();
-        for (int x = threadIdx.x; x < g.p.wh * g.p.rows * kMergeDims; x += Z::NW * 32) {
-          const int e = x % kMergeDims, hr = x / kMergeDims, h = hr / g.p.rows, r = hr - h * g.p.rows;
-          const int j = query_head(g, at.group, h, r);
-          if (j < 0 || e0 + e >= d) continue;
-          const float M = top(h, r);
-          float s = 0.f;
-          bool b = false;
-          for (int w = h; w < Z::NW; w += g.p.wh) {
-            if (sh.m[w][r] != -CUDART_INF_F || sh.l[w][r] != 0.f) s += sh.part[w][r][e] * exp2_approx(sh.m[w][r] - M);
-            b |= sh.bad[w] != 0;
+        // head wh of the group is summed by its own warps, a row each in turn
+        if (e0 + lane < d)
+          for (int r = wt; r < qs.count; r += g.p.wt) {
+            float sum = 0.f;
+            for (int w = wh; w < Z::NW; w += g.p.wh) sum += sh.part[w][r][lane];
+            if (whole) out[(out_row + r) * d + e0 + lane] = from_f32<T>(sum);
+            else g.part_u[(part_row + r) * Z::DP + e0 + lane] = sum;
           }
-          if (whole) {
-            const float l = total(h, r, M);
-            out[((int64_t)at.b * a.v.Hq + j) * d + e0 + e] = from_f32<T>(b || l == 0.f ? 0.f : s / l);
-          } else {
-            g.part_u[((int64_t)(slot * g.p.wh + h) * g.p.rows + r) * Z::DP + e0 + e] = s;
-          }
-        }
         __syncthreads();
       }
     }
     bad = false;
     if (last) break;
     at.next(a, prefix, n_tiles, u1);
-    tile.begin(g, at, wh, lane, warp, mine);
+    qs = queries_of(g, at.group, wh);
+    tile.begin(g, at.b, qs, lane, mine);
   }
   cp_async_wait<0>();
 }
@@ -758,8 +794,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_join_kernel(const __gri
   for (int64_t x = blockIdx.x; x < (int64_t)n * per; x += gridDim.x) {
     const Entry e = g.entries[x / per];
     const int hr = (int)(x % per), h = hr / g.p.rows, r = hr - h * g.p.rows;
-    const int group = e.pair / g.a.B, b = e.pair - group * g.a.B, j = query_head(g, group, h, r);
-    if (j < 0) continue;
+    const int group = e.pair / g.a.B, b = e.pair - group * g.a.B;
+    const Queries qs = queries_of(g, group, h);
+    if (r >= qs.count) continue;
+    const int j = qs.first + r;
     const auto row = [&](int c) { return ((int64_t)(2 * c + (c == e.c0 ? e.second : 0)) * g.p.wh + h) * g.p.rows + r; };
     float m = -CUDART_INF_F, l = 0.f, o[kMaxPagedHeadDim / 32] = {};
     bool bad = false;
@@ -812,6 +850,7 @@ PagedPlan plan_of(const PagedView& v, int dtype, int B, int max_len, int window,
   while (heads % p.wh) p.wh /= 2;
   p.wt = NW / p.wh;
   p.groups = heads / p.wh;
+  p.by_chunks = divider((uint32_t)p.chunks);
   p.tile = p.wt * (dtype == DCK_BF16 ? 16 : 8);
   const int64_t span = window > 0 ? std::min(window, max_len) : max_len;
   p.n_items = (int)std::min<int64_t>(sms, (int64_t)p.groups * std::max(B, 1) * ((span + p.tile - 1) / p.tile));
