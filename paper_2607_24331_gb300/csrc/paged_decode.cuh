@@ -1,0 +1,947 @@
+// Shared by the translation units of dck_paged_decode_attention: the work plan and
+// the device code that runs it.
+#pragma once
+
+#include <math_constants.h>
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "paged.cuh"
+
+namespace dck {
+namespace paged {
+
+constexpr int kMaxLen = 1 << 30;     // tokens of a sequence
+constexpr int kTileLimit = 1 << 30;  // tiles of one call's sequences, per head group
+constexpr int kMaxCluster = 8;
+constexpr int kClusterTiles = 4;  // tiles per CTA up to which clusters are taken
+
+// How a call is laid over warps and CTAs.
+struct Plan {
+  int chunks, rows;  // a KV head's queries: `chunks` tiles of up to `rows`
+  int wh, wt;        // warps of a CTA: wh heads (a power of two) x wt runs of tokens
+  int groups;        // head groups: Hkv * chunks / wh
+  int tile;          // tokens of a CTA's tile
+  int cluster;       // 0: tiles dealt in ranges; else CTAs of a cluster per (head group, sequence), wh = 1
+  int n_items;       // CTAs (dealt in ranges)
+  Divider by_chunks;
+};
+
+struct Entry {  // a (head group, sequence) shared by CTAs c0 .. c1
+  int pair, c0, c1, second;  // second: the partial is c0's second one
+};
+struct Header {
+  int n_entries;
+};
+
+struct Args {
+  PagedDecodeArgs a;
+  Plan p;
+  int DP;          // head dim, rounded up to the variant's
+  float* part_u;   // [2 n_items][wh][rows][DP]
+  float* part_ml;  // [2 n_items][wh][rows][2]: maximum (log2 units), sum (-1: a page outside the pool)
+  Header* header;
+  Entry* entries;  // [n_items]
+};
+
+cudaError_t launch_bf16(const Args& g, cudaStream_t s);
+cudaError_t launch_f32(const Args& g, cudaStream_t s);
+
+inline int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+inline int warps_of(int DP) { return DP == 256 ? 4 : 8; }
+inline int run_of(int dtype) { return dtype == DCK_BF16 ? 16 : 8; }  // tokens of a warp's step
+
+// Visible tokens of sequence b and the first of them; 0 for invalid lengths.
+__device__ __forceinline__ int visible(const PagedDecodeArgs& a, int b, int& first, bool& bad) {
+  const int L = a.seq_len[b];
+  bad = L < 0 || L > a.max_len || L > kMaxLen || (L > 0 && (int64_t)a.v.by_page.div(L - 1) >= a.table_stride);
+  first = a.window > 0 && L > a.window ? L - a.window : 0;
+  return bad ? 0 : L - first;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Exclusive prefix sums of the sequences' tile counts in shared memory
+// prefix[0..B].  Called by the whole block.
+template <int NW>
+__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, int* prefix, bool report) {
+  __shared__ int64_t scratch[NW];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const auto tiles_of = [&](int b) -> int64_t {
+    if (b >= a.B) return 0;
+    int first;
+    bool bad;
+    const int span = visible(a, b, first, bad);
+    if (bad && report && (a.B > 32 || warp == 0)) atomicOr(a.err, kErrBadSeq);
+    return (span + tile - 1) / tile;
+  };
+  const auto scan = [&](int64_t v) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(~0u, v, o);
+      if (lane >= o) v += y;
+    }
+    return v;
+  };
+  if (a.B <= 32) {  // every warp by itself; fewer than 2^27 + 1 tiles each: no overflow of 2^32
+    const int64_t n = tiles_of(lane), v = scan(n);
+    const int64_t all = min(__shfl_sync(~0u, v, 31), (int64_t)kTileLimit);
+    if (warp == 0) {
+      if (v > kTileLimit && n > 0 && report) atomicOr(a.err, kErrBadSeq);
+      if (lane < a.B) prefix[lane] = (int)min(v - n, (int64_t)kTileLimit);
+      if (lane == 0) prefix[a.B] = (int)all;
+    }
+    __syncthreads();
+    return (int)all;
+  }
+  int64_t base = 0;
+  for (int b0 = 0; b0 < a.B; b0 += NW * 32) {
+    const int b = b0 + tid;
+    const int64_t n = tiles_of(b), v = scan(n);
+    if (lane == 31) scratch[warp] = v;
+    __syncthreads();
+    int64_t before = base;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const int64_t y = scratch[w];
+      if (w < warp) before += y;
+      base += y;
+    }
+    if (b < a.B) {
+      if (before + v > kTileLimit && n > 0 && report) atomicOr(a.err, kErrBadSeq);
+      prefix[b] = (int)min(before + v - n, (int64_t)kTileLimit);
+    }
+    base = min(base, (int64_t)kTileLimit);
+    __syncthreads();
+  }
+  if (tid == 0) prefix[a.B] = (int)base;
+  __syncthreads();
+  return (int)base;
+}
+
+__device__ __forceinline__ int64_t range_begin(int c, int64_t units, int n) { return (int64_t)c * units / n; }
+__device__ __forceinline__ int item_of(int64_t u, int64_t units, int n) { return (int)(((u + 1) * n + units - 1) / units) - 1; }
+
+// A position in the flattened list of tiles (head groups outermost).
+struct Cursor {
+  int64_t u, start, end;  // the tile, and the range of its (head group, sequence)
+  int b, group, first, len;
+
+  __device__ __forceinline__ void enter(const PagedDecodeArgs& a, const int* prefix, int n_tiles, int64_t at) {
+    u = at;
+    group = (int)(at / n_tiles);
+    const int64_t base = (int64_t)group * n_tiles;
+    b = seq_of_tile(prefix, a.B, (int)(at - base));
+    start = base + prefix[b];
+    end = base + prefix[b + 1];
+    bool bad;
+    len = visible(a, b, first, bad) + first;
+  }
+  __device__ __forceinline__ void next(const PagedDecodeArgs& a, const int* prefix, int n_tiles, int64_t stop) {
+    if (++u < end || u >= stop) return;
+    enter(a, prefix, n_tiles, u);
+  }
+  __device__ __forceinline__ int token(int tile) const { return first + (int)(u - start) * tile; }
+};
+
+// 16-byte asynchronous copy of `bytes` (16 or 0) bytes, the rest zero.
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// Sizes of a variant: elements T, head dim up to DP, NW warps, S stages of TOK tokens.
+template <typename T_, int DP_, int NW_, int S_, int TOK_>
+struct Sizes {
+  using T = T_;
+  static constexpr int DP = DP_, NW = NW_, S = S_, TOK = TOK_;
+  static constexpr int kRow = DP * sizeof(T);   // bytes of a head's row
+  static constexpr int kChunks = kRow / 16;     // 16-byte chunks of it
+  static constexpr int kHalf = TOK * kRow;      // a stage's keys (values: the same)
+  static constexpr int kStage = 2 * kHalf;
+  static constexpr int kRing = NW * S * kStage;
+};
+
+// The page numbers and offsets of one warp's run of a tile: lane r holds token r.
+struct Pages {
+  int page, off, head;
+  bool valid;
+};
+
+template <class Z>
+struct Loader {
+  const Args& g;
+  uint32_t ring;  // this warp's stages
+  int lane, wh, wt;
+
+  __device__ __forceinline__ Pages fetch(const Cursor& c) const {
+    Pages r;
+    const int t = c.token(g.p.tile) + wt * Z::TOK + lane;
+    r.valid = lane < Z::TOK && t < c.len;
+    const uint32_t col = g.a.v.by_page.div(r.valid ? t : 0);
+    r.off = t - col * g.a.v.page;
+    r.page = r.valid ? g.a.table[(int64_t)c.b * g.a.table_stride + col] : 0;
+    r.head = g.p.by_chunks.div(c.group * g.p.wh + wh);
+    return r;
+  }
+
+  // Starts the copies of a stage; true if a page lies outside the pool (its tokens read as zeros).
+  __device__ __forceinline__ bool issue(const Pages& r, int stage) const {
+    const PagedView& v = g.a.v;
+    const bool outside = r.valid && (r.page < 0 || r.page >= v.n_pages);
+    const bool ok = r.valid && !outside;
+    const int page = ok ? r.page : 0, off = ok ? r.off : 0;
+    const int64_t ko = (int64_t)page * v.k_page + (int64_t)off * v.k_tok + (int64_t)r.head * v.k_head;
+    const int64_t vo = (int64_t)page * v.v_page + (int64_t)off * v.v_tok + (int64_t)r.head * v.v_head;
+    const uint32_t mask = __ballot_sync(~0u, ok);
+    const uint32_t at = ring + stage * Z::kStage;
+    constexpr int kPer = Z::kChunks < 32 ? 32 / Z::kChunks : 1;    // rows per instruction
+    constexpr int kTurns = Z::kChunks > 32 ? Z::kChunks / 32 : 1;  // instructions per row
+    const char* kc = static_cast<const char*>(g.a.kc);
+    const char* vc = static_cast<const char*>(g.a.vc);
+    const int have = v.d * (int)sizeof(typename Z::T) / 16;  // chunks of a row
+#pragma unroll
+    for (int i = 0; i < Z::TOK / kPer; ++i) {
+      const int row = i * kPer + lane / (32 / kPer);
+      const int64_t kr = __shfl_sync(~0u, ko, row), vr = __shfl_sync(~0u, vo, row);
+#pragma unroll
+      for (int j = 0; j < kTurns; ++j) {
+        const int c = lane % (32 / kPer) + 32 * j;
+        const int bytes = (mask >> row & 1) && c < have ? 16 : 0;
+        const int64_t ce = bytes ? c * 16 : 0;
+        const uint32_t dst = at + row * Z::kRow + ((c ^ (row & 7)) * 16);
+        cp_async16_or_zero(dst, kc + kr * (int64_t)sizeof(typename Z::T) + ce, bytes);
+        cp_async16_or_zero(dst + Z::kHalf, vc + vr * (int64_t)sizeof(typename Z::T) + ce, bytes);
+      }
+    }
+    return __any_sync(~0u, outside);
+  }
+};
+
+// The queries of one head of a head group: `count` of them from query head `first` on.
+struct Queries {
+  int first, count;
+};
+__device__ __forceinline__ Queries queries_of(const Args& g, int group, int wh) {
+  const int vh = group * g.p.wh + wh, h = g.p.by_chunks.div(vh), r0 = (vh - h * g.p.chunks) * g.p.rows;
+  return {h * g.a.v.qpg + r0, min(g.p.rows, g.a.v.qpg - r0)};
+}
+
+// tanh to 3e-7 of its value: below 1/2 an odd polynomial (least squares in x^2 on
+// tanh(x) / x, 6e-8), above it 1 - 2 / (e^2x + 1).
+__device__ __forceinline__ float tanh_of(float x) {
+  const float ax = fabsf(x), u = x * x;
+  float p = -6.6395057e-3f;
+  p = fmaf(p, u, 2.1292942e-2f);
+  p = fmaf(p, u, -5.3898074e-2f);
+  p = fmaf(p, u, 1.3332954e-1f);
+  p = fmaf(p, u, -3.3333325e-1f);
+  const float big = 1.f - __fdividef(2.f, exp2_approx(ax * 2.88539008f) + 1.f);
+  return ax < 0.5f ? fmaf(x * u, p, x) : copysignf(ax > 20.f ? 1.f : big, x);
+}
+
+// Scores in log2 units.
+struct ScoreScale {
+  float scale2, inv_cap, cap2;  // cap2 = 0: no cap
+  template <int N>
+  __device__ __forceinline__ void apply(float (&s)[N]) const {
+    if (cap2 > 0.f) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = cap2 * tanh_of(s[i] * inv_cap);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] *= scale2;
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// bf16: tensor cores (mma.sync m16n8k16, queries as rows)
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Two weights as bf16 pairs hi + lo.  Rounding weights to one bf16 would add 2^-9 to
+// the output's own rounding; two of them leave 2^-16.  hi lies below the weight, so lo
+// is positive too: an infinite value gives an infinity, never inf - inf or 0 inf.
+__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t& hi, uint32_t& lo) {
+  const uint32_t h0 = __float_as_uint(p0 * 0.998f) & 0xffff0000u, h1 = __float_as_uint(p1 * 0.998f) & 0xffff0000u;
+  hi = h0 >> 16 | h1;
+  const __nv_bfloat162 l = __floats2bfloat162_rn(p0 - __uint_as_float(h0), p1 - __uint_as_float(h1));
+  lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+
+// One warp's tile of queries and its running sums.  PACK: up to 8 queries, rows 0-7
+// of the tile; the value product's rows 8-15 take the low halves of the weights, so
+// that two-term weights cost no further MMA.  Otherwise up to 16 queries and two MMAs.
+template <class Z, bool PACK>
+struct TensorTile {
+  static constexpr int kQ = PACK ? 1 : 2;  // query rows per lane
+  static constexpr int kRows = PACK ? 8 : 16;
+  float o[Z::DP / 8][4], m[kQ], l[kQ];
+  uint32_t q[Z::DP / 16][2 * kQ];
+
+  __device__ __forceinline__ void begin(const Args& g, int b, const Queries& qs, int lane, float*) {
+    const int words = g.a.v.d / 8;  // runs of 8 elements in a row
+#pragma unroll
+    for (int x = 0; x < kQ; ++x) {
+      const int r = lane / 4 + 8 * x;
+      const uint16_t* src = static_cast<const uint16_t*>(g.a.q) + b * g.a.q_stride +
+                            (int64_t)(qs.first + (r < qs.count ? r : 0)) * g.a.v.d + (lane & 3) * 2;
+      const int have = r < qs.count ? words : 0;
+      if ((reinterpret_cast<uintptr_t>(src) & 3) == 0) {
+#pragma unroll
+        for (int w = 0; w < Z::DP / 8; ++w)
+          q[w / 2][w % 2 * kQ + x] = w < have ? *reinterpret_cast<const uint32_t*>(src + 8 * w) : 0u;
+      } else {
+#pragma unroll
+        for (int w = 0; w < Z::DP / 8; ++w)
+          q[w / 2][w % 2 * kQ + x] = w < have ? src[8 * w] | (uint32_t)src[8 * w + 1] << 16 : 0u;
+      }
+      m[x] = -CUDART_INF_F;
+      l[x] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < Z::DP / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+  }
+
+  // The 16 tokens of a stage, the first `live` of them present (0 or fewer: none).
+  __device__ __forceinline__ void step(uint32_t keys, int live, int lane, const ScoreScale& scale, float*) {
+    if (live <= 0) return;
+    float s[2][4] = {};
+    {
+      const int row = (lane & 7) + (lane >> 4) * 8, c = lane >> 3 & 1;
+#pragma unroll
+      for (int k = 0; k < Z::DP / 16; ++k) {
+        uint32_t b[4];
+        ldmatrix4(b, keys + row * Z::kRow + (((2 * k + c) ^ (row & 7)) * 16));
+        if (PACK) {
+          mma16816(s[0], q[k][0], 0u, q[k][1], 0u, b[0], b[1]);
+          mma16816(s[1], q[k][0], 0u, q[k][1], 0u, b[2], b[3]);
+        } else {
+          mma16816(s[0], q[k][0], q[k][1], q[k][2 % (2 * kQ)], q[k][3 % (2 * kQ)], b[0], b[1]);
+          mma16816(s[1], q[k][0], q[k][1], q[k][2 % (2 * kQ)], q[k][3 % (2 * kQ)], b[2], b[3]);
+        }
+      }
+    }
+    if (PACK) {  // rows 8-15 of the tile hold nothing
+      float v[4] = {s[0][0], s[0][1], s[1][0], s[1][1]};
+      scale.apply(v);
+      s[0][0] = v[0], s[0][1] = v[1], s[1][0] = v[2], s[1][1] = v[3];
+    } else {
+      scale.apply(s[0]);
+      scale.apply(s[1]);
+    }
+    if (live < 16) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if (n * 8 + (lane & 3) * 2 + (y & 1) >= live) s[n][y] = -CUDART_INF_F;
+    }
+    uint32_t hi[kQ][2], lo[kQ][2];
+    bool raise = false;
+    float top[kQ];
+#pragma unroll
+    for (int x = 0; x < kQ; ++x) {
+      float mx = m[x];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) mx = fmaxf(mx, s[n][2 * x + y]);
+      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
+      raise |= mx > m[x];
+      top[x] = mx;
+    }
+    if (__any_sync(~0u, raise)) {
+#pragma unroll
+      for (int x = 0; x < kQ; ++x) {
+        const float c = m[x] == top[x] ? 1.f : exp2_approx(m[x] - top[x]);
+        m[x] = top[x];
+        l[x] *= c;
+#pragma unroll
+        for (int n = 0; n < Z::DP / 8; ++n) {
+          o[n][2 * x] *= c, o[n][2 * x + 1] *= c;
+          if (PACK) o[n][2] *= c, o[n][3] *= c;
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kQ; ++x) {
+      const float base = m[x] == -CUDART_INF_F ? 0.f : m[x];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const float p0 = exp2_approx(s[n][2 * x] - base), p1 = exp2_approx(s[n][2 * x + 1] - base);
+        l[x] += p0 + p1;
+        split_weights(p0, p1, hi[x][n], lo[x][n]);
+      }
+    }
+    const uint32_t vals = keys + Z::kHalf;
+    const int row = lane & 15, c = lane >> 4;
+#pragma unroll
+    for (int n = 0; n < Z::DP / 16; ++n) {
+      uint32_t b[4];
+      ldmatrix4_trans(b, vals + row * Z::kRow + (((2 * n + c) ^ (row & 7)) * 16));
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        if (PACK) {
+          mma16816(o[2 * n + y], hi[0][0], lo[0][0], hi[0][1], lo[0][1], b[2 * y], b[2 * y + 1]);
+        } else {
+          mma16816(o[2 * n + y], hi[0][0], hi[kQ - 1][0], hi[0][1], hi[kQ - 1][1], b[2 * y], b[2 * y + 1]);
+          mma16816(o[2 * n + y], lo[0][0], lo[kQ - 1][0], lo[0][1], lo[kQ - 1][1], b[2 * y], b[2 * y + 1]);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int x = 0; x < kQ; ++x) {
+      l[x] += __shfl_xor_sync(~0u, l[x], 1);
+      l[x] += __shfl_xor_sync(~0u, l[x], 2);
+    }
+    if (PACK)
+#pragma unroll
+      for (int n = 0; n < Z::DP / 8; ++n) o[n][0] += o[n][2], o[n][1] += o[n][3];
+  }
+  // This lane's kMine rows, and f(element, value, next value) for its pairs of elements below d of row x.
+  static constexpr int kMine = kQ;
+  static __device__ __forceinline__ int row(int x, int lane) { return lane / 4 + 8 * x; }
+  static __device__ __forceinline__ bool speaks(int lane) { return (lane & 3) == 0; }  // one lane per row
+  template <class F>
+  __device__ __forceinline__ void each(int x, int lane, int d, F f) const {
+#pragma unroll
+    for (int n = 0; n < Z::DP / 8; ++n)
+      if (n * 8 < d) f(n * 8 + (lane & 3) * 2, o[n][2 * x], o[n][2 * x + 1]);
+  }
+};
+
+// ---------------------------------------------------------------------------
+// fp32: CUDA cores
+// ---------------------------------------------------------------------------
+
+// Up to ROWS queries, 8 tokens a stage.  Scores: lane = (token, quarter of the
+// chunks), the queries from shared memory; values: a lane owns chunks of the output.
+template <class Z, int ROWS>
+struct SimtTile {
+  static constexpr int kRows = ROWS;
+  static constexpr int kOwn = Z::kChunks >= 32 ? Z::kChunks / 32 : 1;  // chunks per lane
+  static constexpr int kSplit = Z::kChunks >= 32 ? 1 : 32 / Z::kChunks;  // lanes that share a chunk, by tokens
+  float4 o[ROWS][kOwn];
+  float m[ROWS], l[ROWS];
+
+  // `mine`: this warp's shared memory, ROWS x DP queries, then 8 x ROWS weights.
+  __device__ __forceinline__ void begin(const Args& g, int b, const Queries& qs, int lane, float* mine) {
+    __syncwarp();
+    const float* src = static_cast<const float*>(g.a.q) + b * g.a.q_stride + (int64_t)qs.first * g.a.v.d;
+    float x[ROWS][Z::DP / 32];  // all loads before the first store
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int e = 0; e < Z::DP / 32; ++e) {
+        const bool have = r < qs.count && e * 32 + lane < g.a.v.d;
+        x[r][e] = have ? src[r * g.a.v.d + e * 32 + lane] : 0.f;
+      }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+      for (int e = 0; e < Z::DP / 32; ++e) mine[r * Z::DP + e * 32 + lane] = x[r][e];
+      m[r] = -CUDART_INF_F;
+      l[r] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) o[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __syncwarp();
+  }
+
+  __device__ __forceinline__ void step(uint32_t keys, int live, int lane, const ScoreScale& scale, float* mine) {
+    if (live <= 0) return;
+    const auto chunk = [](uint32_t at) {
+      float4 v;
+      asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+      return v;
+    };
+    const int t = lane & 7, quarter = lane >> 3;
+    float s[ROWS] = {};
+#pragma unroll
+    for (int k = 0; k < Z::kChunks / 4; ++k) {
+      const int c = 4 * k + quarter;
+      const float4 x = chunk(keys + t * Z::kRow + ((c ^ t) * 16));
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const float4 y = *reinterpret_cast<const float4*>(mine + r * Z::DP + 4 * c);
+        s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
+      }
+    }
+    float* weights = mine + ROWS * Z::DP;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) s[r] += __shfl_xor_sync(~0u, s[r], 8);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) s[r] += __shfl_xor_sync(~0u, s[r], 16);
+    scale.apply(s);
+    float top[ROWS];
+    bool raise = false;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      if (t >= live) s[r] = -CUDART_INF_F;
+      top[r] = fmaxf(m[r], s[r]);
+    }
+#pragma unroll
+    for (int x = 1; x < 8; x <<= 1)
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], x));
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) raise |= top[r] > m[r];
+    if (raise) {  // the same in every lane
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const float c = m[r] == top[r] ? 1.f : exp2_approx(m[r] - top[r]);
+        m[r] = top[r];
+        l[r] *= c;
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) o[r][k].x *= c, o[r][k].y *= c, o[r][k].z *= c, o[r][k].w *= c;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const float p = exp2_approx(s[r] - (m[r] == -CUDART_INF_F ? 0.f : m[r]));
+      if (quarter == 0) {
+        l[r] += p;
+        weights[t * ROWS + r] = p;
+      }
+    }
+    __syncwarp();
+    const uint32_t vals = keys + Z::kHalf;
+#pragma unroll
+    for (int i = 0; i < Z::TOK / kSplit; ++i) {
+      const int tok = i * kSplit + (kSplit > 1 ? lane / Z::kChunks : 0);
+      float p[ROWS];
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) p[r] = weights[tok * ROWS + r];
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        const int c = (kSplit > 1 ? lane % Z::kChunks : lane) + 32 * k;
+        const float4 x = chunk(vals + tok * Z::kRow + ((c ^ (tok & 7)) * 16));
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          o[r][k].x = fmaf(p[r], x.x, o[r][k].x);
+          o[r][k].y = fmaf(p[r], x.y, o[r][k].y);
+          o[r][k].z = fmaf(p[r], x.z, o[r][k].z);
+          o[r][k].w = fmaf(p[r], x.w, o[r][k].w);
+        }
+      }
+    }
+    __syncwarp();  // the weights are read
+  }
+
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+      for (int x = 1; x < 32; x <<= 1) l[r] += __shfl_xor_sync(~0u, l[r], x);  // lanes past 7 hold zero
+#pragma unroll
+      for (int x = 32 / kSplit; x < 32; x <<= 1) {
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+          o[r][k].x += __shfl_xor_sync(~0u, o[r][k].x, x);
+          o[r][k].y += __shfl_xor_sync(~0u, o[r][k].y, x);
+          o[r][k].z += __shfl_xor_sync(~0u, o[r][k].z, x);
+          o[r][k].w += __shfl_xor_sync(~0u, o[r][k].w, x);
+        }
+      }
+    }
+  }
+  static constexpr int kMine = ROWS;
+  static __device__ __forceinline__ int row(int x, int) { return x; }
+  static __device__ __forceinline__ bool speaks(int lane) { return lane == 0; }
+  template <class F>
+  __device__ __forceinline__ void each(int x, int lane, int d, F f) const {
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int e = 4 * ((kSplit > 1 ? lane % Z::kChunks : lane) + 32 * k);
+      if (lane < 32 / kSplit && e < d) {
+        f(e, o[x][k].x, o[x][k].y);
+        f(e + 2, o[x][k].z, o[x][k].w);
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// the kernel
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// The address in CTA `rank`'s shared memory of what `p` is in this one's.
+__device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void store_remote(uint32_t at, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void store_remote(uint32_t at, float2 v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(at), "f"(v.x), "f"(v.y) : "memory");
+}
+
+// Four elements of an output row, 4-byte aligned for bf16 where `even`.
+__device__ __forceinline__ void put4(float* p, float4 v, bool) { p[0] = v.x, p[1] = v.y, p[2] = v.z, p[3] = v.w; }
+__device__ __forceinline__ void put4(__nv_bfloat16* p, float4 v, bool even) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  if (even) {
+    reinterpret_cast<__nv_bfloat162*>(p)[0] = a;
+    reinterpret_cast<__nv_bfloat162*>(p)[1] = b;
+  } else {
+    p[0] = a.x, p[1] = a.y, p[2] = b.x, p[3] = b.y;
+  }
+}
+
+template <class Z, class Tile>
+struct Shared {  // after the rings
+  float4 part[Tile::kRows * Z::DP / 4];              // of the cluster's CTAs, this one's share of the elements
+  float2 cluster_ml[kMaxCluster][Tile::kRows];
+  float mine[std::is_same<typename Z::T, float>::value ? Z::NW * (Tile::kRows * Z::DP + 8 * Tile::kRows) : 4];
+  float2 ml[Z::NW][Tile::kRows];  // sum -1: a page outside the pool
+};
+
+template <class Z, class Tile>
+constexpr size_t shared_bytes(int B) {
+  return Z::kRing + sizeof(Shared<Z, Tile>) + sizeof(int) * (B + 1);
+}
+
+// The maximum and sum that `n` partial sums have together, and each one's weight.
+struct Joined {
+  float m, l;
+  bool bad;
+};
+template <int MOST, class F>
+__device__ __forceinline__ Joined join_rows(int n, float (&weight)[MOST], F ml_of) {
+  Joined r = {-CUDART_INF_F, 0.f, false};
+  float l[MOST];
+#pragma unroll
+  for (int k = 0; k < MOST; ++k) {
+    weight[k] = -CUDART_INF_F;
+    l[k] = 0.f;
+    if (k < n) {
+      const float2 v = ml_of(k);
+      weight[k] = v.x, l[k] = v.y;
+      r.bad |= v.y < 0.f;
+      r.m = fmaxf(r.m, v.x);
+    }
+  }
+  const float base = r.m == -CUDART_INF_F ? 0.f : r.m;
+#pragma unroll
+  for (int k = 0; k < MOST; ++k) {
+    weight[k] = exp2_approx(weight[k] - base);
+    r.l += l[k] * weight[k];
+  }
+  return r;
+}
+
+template <class Z, class Tile, bool CLUSTER>
+__global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __grid_constant__ Args g) {
+  using T = typename Z::T;
+  extern __shared__ __align__(128) uint8_t raw[];
+  Shared<Z, Tile>& sh = *reinterpret_cast<Shared<Z, Tile>*>(raw + Z::kRing);
+  int* prefix = reinterpret_cast<int*>(raw + Z::kRing + sizeof(sh));
+  const PagedDecodeArgs& a = g.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int wh = CLUSTER ? 0 : warp & (g.p.wh - 1), wt = CLUSTER ? warp : warp / g.p.wh;
+  const int n_heads = CLUSTER ? 1 : g.p.wh, n_runs = CLUSTER ? Z::NW : g.p.wt;
+  const int d = a.v.d;
+  T* out = static_cast<T*>(a.out);
+  const bool even = (reinterpret_cast<uintptr_t>(out) & 3) == 0;
+  pdl_launch_dependents();
+  pdl_wait();
+
+  int n_tiles = 0, n = 0;
+  int64_t u0, u1;
+  Cursor ahead;
+  uint32_t rank = 0;
+  if (CLUSTER) {
+    cluster_arrive();  // remote stores must find the other CTAs running: waited for before the first
+    rank = cluster_rank();
+    const int pair = blockIdx.x / g.p.cluster;
+    ahead.group = pair / a.B;
+    ahead.b = pair - ahead.group * a.B;
+    bool bad;
+    const int span = visible(a, ahead.b, ahead.first, bad);
+    if (bad && ahead.group == 0 && rank == 0 && threadIdx.x == 0) atomicOr(a.err, kErrBadSeq);
+    ahead.len = span + ahead.first;
+    ahead.start = 0;
+    ahead.end = (span + g.p.tile - 1) / g.p.tile;
+    u0 = rank * ahead.end / g.p.cluster;
+    u1 = (rank + 1) * ahead.end / g.p.cluster;
+    ahead.u = u0;
+  } else {
+    n_tiles = tile_prefix<Z::NW>(a, g.p.tile, prefix, blockIdx.x == 0);
+    const int64_t units = (int64_t)g.p.groups * n_tiles;
+    n = (int)min((int64_t)g.p.n_items, units);
+    // empty sequences
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+      if (prefix[b + 1] == prefix[b]) {
+        for (int e = threadIdx.x; e < a.v.Hq * d; e += Z::NW * 32) out[(int64_t)b * a.v.Hq * d + e] = from_f32<T>(0.f);
+        if (a.lse)
+          for (int j = threadIdx.x; j < a.v.Hq; j += Z::NW * 32) a.lse[(int64_t)b * a.v.Hq + j] = -CUDART_INF_F;
+      }
+    if ((int)blockIdx.x >= n) {
+      if (blockIdx.x == 0 && threadIdx.x == 0) g.header->n_entries = 0;
+      return;
+    }
+    u0 = range_begin(blockIdx.x, units, n);
+    u1 = range_begin(blockIdx.x + 1, units, n);
+    ahead.enter(a, prefix, n_tiles, u0);
+  }
+
+  const Loader<Z> load{g, (uint32_t)__cvta_generic_to_shared(raw) + warp * Z::S * Z::kStage, lane, wh, wt};
+  Cursor at = ahead;
+  Pages pages = {0, 0, 0, false};
+  if (u0 < u1) pages = load.fetch(ahead);
+  uint32_t outside = 0;  // bit s: stage s has a page outside the pool
+  int put = 0;           // stage that the next copies go to
+  const auto copy_next = [&]() {
+    if (ahead.u < u1) {
+      const bool bad = load.issue(pages, put);
+      outside = (outside & ~(1u << put)) | (uint32_t)bad << put;
+      if (CLUSTER) ++ahead.u;
+      else ahead.next(a, prefix, n_tiles, u1);
+      if (ahead.u < u1) pages = load.fetch(ahead);
+      put = put + 1 == Z::S ? 0 : put + 1;
+    }
+    cp_async_commit();
+  };
+#pragma unroll 1
+  for (int i = 0; i < Z::S - 1; ++i) copy_next();
+
+  ScoreScale scale;
+  scale.scale2 = a.scale * 1.44269504088896f;
+  scale.cap2 = a.softcap * 1.44269504088896f;
+  scale.inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
+  float* mine = sh.mine + warp * (Tile::kRows * Z::DP + 8 * Tile::kRows);
+  Tile tile;
+  Queries qs = queries_of(g, at.group, wh);
+  tile.begin(g, at.b, qs, lane, mine);
+
+  if (!CLUSTER && blockIdx.x == 0) {  // the list of what several CTAs share, for the second launch
+    __shared__ int n_entries;
+    if (threadIdx.x == 0) n_entries = 0;
+    __syncthreads();
+    const int64_t units = (int64_t)g.p.groups * n_tiles;
+    for (int c = threadIdx.x; c + 1 < n; c += Z::NW * 32) {
+      const int64_t x = range_begin(c + 1, units, n);
+      const int group = (int)(x / n_tiles);
+      const int64_t base = (int64_t)group * n_tiles;
+      const int b = seq_of_tile(prefix, a.B, (int)(x - base));
+      const int64_t start = base + prefix[b], begin = range_begin(c, units, n);
+      if (x > start && begin <= start) {
+        Entry e;
+        e.pair = group * a.B + b;
+        e.c0 = c;
+        e.c1 = item_of(base + prefix[b + 1] - 1, units, n);
+        e.second = begin < start;
+        g.entries[atomicAdd(&n_entries, 1)] = e;
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) g.header->n_entries = n_entries;
+  }
+
+  int get = 0;
+  bool bad = false;
+  while (true) {
+    if (!CLUSTER || at.u < u1) {
+      __syncwarp();  // the stage that is filled next has been read
+      copy_next();
+      cp_async_wait<Z::S - 1>();
+      __syncwarp();
+      bad |= outside >> get & 1;
+      tile.step(load.ring + get * Z::kStage, at.len - at.token(g.p.tile) - wt * Z::TOK, lane, scale, mine);
+    }
+    const int used = get;
+    get = get + 1 == Z::S ? 0 : get + 1;
+    const bool last = at.u + 1 >= u1;
+    if (at.u + 1 < at.end && !last) {
+      ++at.u;
+      continue;
+    }
+    // the end of a (head group, sequence), or of this CTA's part of it
+    const bool whole = CLUSTER ? g.p.cluster == 1 : at.start >= u0 && at.end <= u1;
+    if (bad && lane == 0) atomicOr(a.err, kErrBadSeq);
+    tile.finish();
+    const int64_t out_row = (int64_t)at.b * a.v.Hq + qs.first;
+    const int64_t part_row = CLUSTER ? 0 : (int64_t)((2 * blockIdx.x + (u0 < at.start)) * n_heads + wh) * g.p.rows;
+    // the sum of row r (lse, or the partial's maximum and sum)
+    const auto put_sum = [&](int r, const Joined& j) {
+      if (!whole) *reinterpret_cast<float2*>(g.part_ml + 2 * (part_row + r)) = make_float2(j.m, j.bad ? -1.f : j.l);
+      else if (a.lse) a.lse[out_row + r] = j.bad || j.l == 0.f ? -CUDART_INF_F : (j.m + log2f(j.l)) * 0.693147180559945f;
+    };
+    if (!CLUSTER && n_runs == 1) {
+#pragma unroll
+      for (int x = 0; x < Tile::kMine; ++x) {
+        const int r = Tile::row(x, lane);
+        if (r >= qs.count) continue;
+        const bool none = bad || tile.l[x] == 0.f;
+        if (Tile::speaks(lane)) put_sum(r, {tile.m[x], tile.l[x], bad});
+        if (whole) {
+          const float f = 1.f / tile.l[x];
+          T* p = out + (out_row + r) * d;
+          tile.each(x, lane, d, [&](int e, float y, float z) {
+            p[e] = from_f32<T>(none ? 0.f : y * f);
+            p[e + 1] = from_f32<T>(none ? 0.f : z * f);
+          });
+        } else {
+          float* p = g.part_u + (part_row + r) * Z::DP;
+          tile.each(x, lane, d, [&](int e, float y, float z) { *reinterpret_cast<float2*>(p + e) = make_float2(y, z); });
+        }
+      }
+    } else {
+      // The head's runs of tokens join: each warp leaves its sums in the stage that it has
+      // just read (not filled again before the barrier behind), then all of them add up.
+      float* left = reinterpret_cast<float*>(raw + (warp * Z::S + used) * Z::kStage);
+#pragma unroll
+      for (int x = 0; x < Tile::kMine; ++x) {
+        const int r = Tile::row(x, lane);
+        if (Tile::speaks(lane)) sh.ml[warp][r] = make_float2(tile.m[x], bad ? -1.f : tile.l[x]);
+        tile.each(x, lane, d, [&](int e, float y, float z) {
+          *reinterpret_cast<float2*>(left + r * Z::DP + (e ^ (r & 7) * 8)) = make_float2(y, z);
+        });
+      }
+      __syncthreads();
+      if (CLUSTER && g.p.cluster > 1) cluster_wait();
+      for (int i = wt * 32 + lane; i < qs.count * (Z::DP / 4); i += n_runs * 32) {
+        const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
+        if (e >= d) continue;
+        float w[Z::NW];
+        const Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < Z::NW; ++k)
+          if (k < n_runs && w[k] != 0.f) {
+            const float* from = reinterpret_cast<const float*>(raw + ((k * n_heads + wh) * Z::S + used) * Z::kStage);
+            const float4 v = *reinterpret_cast<const float4*>(from + r * Z::DP + (e ^ (r & 7) * 8));
+            sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
+          }
+        if (CLUSTER && g.p.cluster > 1) {
+          store_remote(remote(&sh.part[i / g.p.cluster + rank * (Tile::kRows * Z::DP / 4 / g.p.cluster)], i % g.p.cluster), sum);
+          if (e == 0)
+            for (int c = 0; c < g.p.cluster; ++c)
+              store_remote(remote(&sh.cluster_ml[rank][r], c), make_float2(j.m, j.bad ? -1.f : j.l));
+        } else if (whole) {
+          const float f = j.bad || j.l == 0.f ? 0.f : 1.f / j.l;
+          put4(out + (out_row + r) * d + e,
+               f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f), even);
+          if (e == 0) put_sum(r, j);
+        } else {
+          *reinterpret_cast<float4*>(g.part_u + (part_row + r) * Z::DP + e) = sum;
+          if (e == 0) put_sum(r, j);
+        }
+      }
+      if (!CLUSTER) __syncthreads();
+    }
+    if (last) break;
+    bad = false;
+    at.next(a, prefix, n_tiles, u1);
+    qs = queries_of(g, at.group, wh);
+    tile.begin(g, at.b, qs, lane, mine);
+  }
+  cp_async_wait<0>();
+  if (!CLUSTER) return;
+  if (g.p.cluster == 1) {
+    cluster_wait();
+    return;
+  }
+  // Every CTA of the cluster has sent its sums: each joins its share of the elements.
+  cluster_arrive();
+  cluster_wait();
+  const int per = Tile::kRows * Z::DP / 4 / g.p.cluster;
+  for (int i = threadIdx.x * g.p.cluster + rank; i < qs.count * (Z::DP / 4); i += Z::NW * 32 * g.p.cluster) {
+    const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
+    if (e >= d) continue;
+    float w[kMaxCluster];
+    const Joined j = join_rows<kMaxCluster>(g.p.cluster, w, [&](int k) { return sh.cluster_ml[k][r]; });
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kMaxCluster; ++k)
+      if (k < g.p.cluster && w[k] != 0.f) {
+        const float4 v = sh.part[i / g.p.cluster + k * per];
+        sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
+      }
+    const int64_t row = (int64_t)at.b * a.v.Hq + qs.first + r;
+    const float f = j.bad || j.l == 0.f ? 0.f : 1.f / j.l;
+    put4(out + row * d + e, f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f),
+         even);
+    if (e == 0 && a.lse) a.lse[row] = j.bad || j.l == 0.f ? -CUDART_INF_F : (j.m + log2f(j.l)) * 0.693147180559945f;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launch
+// ---------------------------------------------------------------------------
+
+template <class Z, class Tile, bool CLUSTER>
+cudaError_t launch_kernel(const Args& g, cudaStream_t s) {
+  const auto k = paged_decode_kernel<Z, Tile, CLUSTER>;
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes<Z, Tile>(CLUSTER ? 0 : kMaxBatch));
+    if (e != cudaSuccess) return e;
+    if (dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = CLUSTER ? g.p.groups * g.a.B * g.p.cluster : g.p.n_items;
+  cfg.blockDim = Z::NW * 32;
+  cfg.dynamicSmemBytes = shared_bytes<Z, Tile>(CLUSTER ? 0 : g.a.B);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CLUSTER ? g.p.cluster : 1;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CLUSTER ? 2 : 1;
+  e = cudaLaunchKernelEx(&cfg, k, g);
+  if (e != cudaSuccess) return e;
+  return hook_launched(g.a.hook, s);
+}
+
+template <class Z, class Tile>
+cudaError_t launch_tile(const Args& g, cudaStream_t s) {
+  return g.p.cluster ? launch_kernel<Z, Tile, true>(g, s) : launch_kernel<Z, Tile, false>(g, s);
+}
+
+}  // namespace paged
+}  // namespace dck
