@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     float M = -CUDART_INF_F, total = 0.f;
     bool bad = false;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = 0; i0 < parts; i0 += kJoinThreads) {  // once, but on a GPU of more than kJoinThreads SMs
+    for (int i0 = 0; i0 < parts; i0 += kJoinThreads) {  // twice at most: CTAs are two per SM
       const int count = min(kJoinThreads, parts - i0);
       // the loads of the first partials go out before the weights are known
       float4 v[kJoinBatch];
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
 
 Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int sms) {
   Plan p;
-  const int DP = padded_dim(v.d), NW = warps_of(DP);
+  const int DP = padded_dim(v.d);
   const int most = dtype == DCK_BF16 && DP <= 128 && v.qpg > 8 ? 16 : 8;
   p.chunks = (v.qpg + most - 1) / most;
   p.rows = (v.qpg + p.chunks - 1) / p.chunks;
@@ -136,18 +136,20 @@ Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int 
   const int64_t span = window > 0 ? std::min(window, max_len) : max_len;
   // Clusters: one (head, sequence) each, as many CTAs as have a tile and one SM each
   p.cluster = 0;
-  const int64_t pairs = (int64_t)heads * std::max(B, 1), tiles = (span + NW * run_of(dtype) - 1) / (NW * run_of(dtype));
+  const int of_cluster = warps_of(DP, true) * run_of(dtype);
+  const int64_t pairs = (int64_t)heads * std::max(B, 1), tiles = (span + of_cluster - 1) / of_cluster;
   if (pairs <= sms) {
     int c = 1;
     while (2 * c <= kMaxCluster && 2 * c * pairs <= sms && c < tiles) c *= 2;
     if (tiles <= kClusterTiles * c) p.cluster = c;
   }
+  const int NW = warps_of(DP, p.cluster != 0);
   p.wh = p.cluster ? 1 : NW;
   while (heads % p.wh) p.wh /= 2;
   p.wt = NW / p.wh;
   p.groups = heads / p.wh;
   p.tile = p.wt * run_of(dtype);
-  p.n_items = (int)std::min<int64_t>(sms, (int64_t)p.groups * std::max(B, 1) * ((span + p.tile - 1) / p.tile));
+  p.n_items = (int)std::min<int64_t>(kPerSm * sms, (int64_t)p.groups * std::max(B, 1) * ((span + p.tile - 1) / p.tile));
   return p;
 }
 

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cstddef>
 #include <type_traits>
 
 #include "paged.cuh"
@@ -50,7 +51,8 @@ cudaError_t launch_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_f32(const Args& g, cudaStream_t s);
 
 inline int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-inline int warps_of(int DP) { return DP == 256 ? 4 : 8; }
+constexpr int warps_of(int DP, bool cluster) { return (DP == 256 ? 2 : 4) * (cluster ? 2 : 1); }
+constexpr int kPerSm = 2;  // CTAs per SM of tiles dealt in ranges
 inline int run_of(int dtype) { return dtype == DCK_BF16 ? 16 : 8; }  // tokens of a warp's step
 
 // Visible tokens of sequence b and the first of them; 0 for invalid lengths.
@@ -68,9 +70,9 @@ __device__ __forceinline__ float exp2_approx(float x) {
 }
 
 // Exclusive prefix sums of the sequences' tile counts in shared memory
-// prefix[0..B].  Called by the whole block.
+// prefix[0..B], and their lengths (len may be null).  Called by the whole block.
 template <int NW>
-__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, int* prefix, bool report) {
+__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, int* prefix, int* len, bool report) {
   __shared__ int64_t scratch[NW];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const auto tiles_of = [&](int b) -> int64_t {
@@ -79,6 +81,7 @@ __device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, i
     bool bad;
     const int span = visible(a, b, first, bad);
     if (bad && report && (a.B > 32 || warp == 0)) atomicOr(a.err, kErrBadSeq);
+    if (len && (a.B > 32 || warp == 0)) len[b] = span + first;
     return (span + tile - 1) / tile;
   };
   const auto scan = [&](int64_t v) {
@@ -128,24 +131,46 @@ __device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, i
 __device__ __forceinline__ int64_t range_begin(int c, int64_t units, int n) { return (int64_t)c * units / n; }
 __device__ __forceinline__ int item_of(int64_t u, int64_t units, int n) { return (int)(((u + 1) * n + units - 1) / units) - 1; }
 
+// What the plan keeps of the sequences in shared memory.
+struct Batch {
+  int* prefix;  // [B + 1] exclusive prefix sums of the tile counts
+  int* len;     // [B] lengths, 0 for invalid ones (null: more than kKeptLens sequences, lengths from memory)
+};
+constexpr int kKeptLens = 1024;
+
 // A position in the flattened list of tiles (head groups outermost).
 struct Cursor {
   int64_t u, start, end;  // the tile, and the range of its (head group, sequence)
   int b, group, first, len;
 
-  __device__ __forceinline__ void enter(const PagedDecodeArgs& a, const int* prefix, int n_tiles, int64_t at) {
+  __device__ __forceinline__ void see(const PagedDecodeArgs& a, const Batch& q) {
+    if (q.len) {
+      len = q.len[b];
+      first = a.window > 0 && len > a.window ? len - a.window : 0;
+    } else {
+      bool bad;
+      len = visible(a, b, first, bad) + first;
+    }
+  }
+  __device__ __forceinline__ void enter(const PagedDecodeArgs& a, const Batch& q, int n_tiles, int64_t at) {
     u = at;
     group = (int)(at / n_tiles);
     const int64_t base = (int64_t)group * n_tiles;
-    b = seq_of_tile(prefix, a.B, (int)(at - base));
-    start = base + prefix[b];
-    end = base + prefix[b + 1];
-    bool bad;
-    len = visible(a, b, first, bad) + first;
+    b = seq_of_tile(q.prefix, a.B, (int)(at - base));
+    start = base + q.prefix[b];
+    end = base + q.prefix[b + 1];
+    see(a, q);
   }
-  __device__ __forceinline__ void next(const PagedDecodeArgs& a, const int* prefix, int n_tiles, int64_t stop) {
+  __device__ __forceinline__ void next(const PagedDecodeArgs& a, const Batch& q, int64_t stop) {
     if (++u < end || u >= stop) return;
-    enter(a, prefix, n_tiles, u);
+    int n;
+    do {
+      if (++b == a.B) b = 0, ++group;
+      n = q.prefix[b + 1] - q.prefix[b];
+    } while (n == 0);
+    start = end;
+    end = start + n;
+    see(a, q);
   }
   __device__ __forceinline__ int token(int tile) const { return first + (int)(u - start) * tile; }
 };
@@ -614,7 +639,13 @@ __device__ __forceinline__ void store_remote(uint32_t at, float2 v) {
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(at), "f"(v.x), "f"(v.y) : "memory");
 }
 
-// Four elements of an output row, 4-byte aligned for bf16 where `even`.
+// Two or four elements of an output row, 4-byte aligned for bf16 where `even`.
+__device__ __forceinline__ void put2(float* p, float x, float y, bool) { p[0] = x, p[1] = y; }
+__device__ __forceinline__ void put2(__nv_bfloat16* p, float x, float y, bool even) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x, y);
+  if (even) *reinterpret_cast<__nv_bfloat162*>(p) = a;
+  else p[0] = a.x, p[1] = a.y;
+}
 __device__ __forceinline__ void put4(float* p, float4 v, bool) { p[0] = v.x, p[1] = v.y, p[2] = v.z, p[3] = v.w; }
 __device__ __forceinline__ void put4(__nv_bfloat16* p, float4 v, bool even) {
   const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
@@ -626,17 +657,17 @@ __device__ __forceinline__ void put4(__nv_bfloat16* p, float4 v, bool even) {
   }
 }
 
-template <class Z, class Tile>
+template <class Z, class Tile, bool CLUSTER>
 struct Shared {  // after the rings
-  float4 part[Tile::kRows * Z::DP / 4];              // of the cluster's CTAs, this one's share of the elements
-  float2 cluster_ml[kMaxCluster][Tile::kRows];
-  float mine[std::is_same<typename Z::T, float>::value ? Z::NW * (Tile::kRows * Z::DP + 8 * Tile::kRows) : 4];
-  float2 ml[Z::NW][Tile::kRows];  // sum -1: a page outside the pool
+  float4 part[CLUSTER ? Tile::kRows * Z::DP / 4 : 1];  // of the cluster's CTAs, this one's share of the elements
+  float2 cluster_ml[CLUSTER ? kMaxCluster : 1][Tile::kRows];
+  alignas(16) float mine[std::is_same<typename Z::T, float>::value ? Z::NW * (Tile::kRows * Z::DP + 8 * Tile::kRows) : 4];
+  alignas(16) float2 ml[Z::NW][Tile::kRows];  // sum -1: a page outside the pool
 };
 
-template <class Z, class Tile>
+template <class Z, class Tile, bool CLUSTER>
 constexpr size_t shared_bytes(int B) {
-  return Z::kRing + sizeof(Shared<Z, Tile>) + sizeof(int) * (B + 1);
+  return Z::kRing + sizeof(Shared<Z, Tile, CLUSTER>) + (CLUSTER ? 0 : sizeof(int) * (B + 1 + (B <= kKeptLens ? B : 0)));
 }
 
 // The maximum and sum that `n` partial sums have together, and each one's weight.
@@ -669,12 +700,17 @@ __device__ __forceinline__ Joined join_rows(int n, float (&weight)[MOST], F ml_o
 }
 
 template <class Z, class Tile, bool CLUSTER>
-__global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(Z::NW * 32, CLUSTER ? 1 : kPerSm) paged_decode_kernel(const __grid_constant__ Args g) {
   using T = typename Z::T;
   extern __shared__ __align__(128) uint8_t raw[];
-  Shared<Z, Tile>& sh = *reinterpret_cast<Shared<Z, Tile>*>(raw + Z::kRing);
-  int* prefix = reinterpret_cast<int*>(raw + Z::kRing + sizeof(sh));
+  using Shm = Shared<Z, Tile, CLUSTER>;
+  Shm& sh = *reinterpret_cast<Shm*>(raw + Z::kRing);
   const PagedDecodeArgs& a = g.a;
+  static_assert(Z::kRing % 16 == 0 && offsetof(Shm, mine) % 16 == 0 && sizeof(Shm) % 16 == 0, "16-byte accesses");
+  static_assert((Tile::kRows * Z::DP + 8 * Tile::kRows) % 4 == 0 && Z::kStage >= Tile::kRows * Z::DP * 4, "a warp's queries, its sums in a stage");
+  Batch batch;
+  batch.prefix = reinterpret_cast<int*>(raw + Z::kRing + sizeof(sh));
+  batch.len = a.B <= kKeptLens ? batch.prefix + a.B + 1 : nullptr;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int wh = CLUSTER ? 0 : warp & (g.p.wh - 1), wt = CLUSTER ? warp : warp / g.p.wh;
   const int n_heads = CLUSTER ? 1 : g.p.wh, n_runs = CLUSTER ? Z::NW : g.p.wt;
@@ -704,12 +740,12 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
     u1 = (rank + 1) * ahead.end / g.p.cluster;
     ahead.u = u0;
   } else {
-    n_tiles = tile_prefix<Z::NW>(a, g.p.tile, prefix, blockIdx.x == 0);
+    n_tiles = tile_prefix<Z::NW>(a, g.p.tile, batch.prefix, batch.len, blockIdx.x == 0);
     const int64_t units = (int64_t)g.p.groups * n_tiles;
     n = (int)min((int64_t)g.p.n_items, units);
     // empty sequences
     for (int b = blockIdx.x; b < a.B; b += gridDim.x)
-      if (prefix[b + 1] == prefix[b]) {
+      if (batch.prefix[b + 1] == batch.prefix[b]) {
         for (int e = threadIdx.x; e < a.v.Hq * d; e += Z::NW * 32) out[(int64_t)b * a.v.Hq * d + e] = from_f32<T>(0.f);
         if (a.lse)
           for (int j = threadIdx.x; j < a.v.Hq; j += Z::NW * 32) a.lse[(int64_t)b * a.v.Hq + j] = -CUDART_INF_F;
@@ -720,7 +756,7 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
     }
     u0 = range_begin(blockIdx.x, units, n);
     u1 = range_begin(blockIdx.x + 1, units, n);
-    ahead.enter(a, prefix, n_tiles, u0);
+    ahead.enter(a, batch, n_tiles, u0);
   }
 
   const Loader<Z> load{g, (uint32_t)__cvta_generic_to_shared(raw) + warp * Z::S * Z::kStage, lane, wh, wt};
@@ -734,7 +770,7 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
       const bool bad = load.issue(pages, put);
       outside = (outside & ~(1u << put)) | (uint32_t)bad << put;
       if (CLUSTER) ++ahead.u;
-      else ahead.next(a, prefix, n_tiles, u1);
+      else ahead.next(a, batch, u1);
       if (ahead.u < u1) pages = load.fetch(ahead);
       put = put + 1 == Z::S ? 0 : put + 1;
     }
@@ -761,13 +797,13 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
       const int64_t x = range_begin(c + 1, units, n);
       const int group = (int)(x / n_tiles);
       const int64_t base = (int64_t)group * n_tiles;
-      const int b = seq_of_tile(prefix, a.B, (int)(x - base));
-      const int64_t start = base + prefix[b], begin = range_begin(c, units, n);
+      const int b = seq_of_tile(batch.prefix, a.B, (int)(x - base));
+      const int64_t start = base + batch.prefix[b], begin = range_begin(c, units, n);
       if (x > start && begin <= start) {
         Entry e;
         e.pair = group * a.B + b;
         e.c0 = c;
-        e.c1 = item_of(base + prefix[b + 1] - 1, units, n);
+        e.c1 = item_of(base + batch.prefix[b + 1] - 1, units, n);
         e.second = begin < start;
         g.entries[atomicAdd(&n_entries, 1)] = e;
       }
@@ -816,8 +852,7 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
           const float f = 1.f / tile.l[x];
           T* p = out + (out_row + r) * d;
           tile.each(x, lane, d, [&](int e, float y, float z) {
-            p[e] = from_f32<T>(none ? 0.f : y * f);
-            p[e + 1] = from_f32<T>(none ? 0.f : z * f);
+            put2(p + e, none ? 0.f : y * f, none ? 0.f : z * f, even);
           });
         } else {
           float* p = g.part_u + (part_row + r) * Z::DP;
@@ -870,7 +905,7 @@ __global__ void __launch_bounds__(Z::NW * 32, 1) paged_decode_kernel(const __gri
     }
     if (last) break;
     bad = false;
-    at.next(a, prefix, n_tiles, u1);
+    at.next(a, batch, u1);
     qs = queries_of(g, at.group, wh);
     tile.begin(g, at.b, qs, lane, mine);
   }
@@ -916,14 +951,14 @@ cudaError_t launch_kernel(const Args& g, cudaStream_t s) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes<Z, Tile>(CLUSTER ? 0 : kMaxBatch));
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(shared_bytes<Z, Tile, CLUSTER>(kMaxBatch), shared_bytes<Z, Tile, CLUSTER>(kKeptLens)));
     if (e != cudaSuccess) return e;
     if (dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = CLUSTER ? g.p.groups * g.a.B * g.p.cluster : g.p.n_items;
   cfg.blockDim = Z::NW * 32;
-  cfg.dynamicSmemBytes = shared_bytes<Z, Tile>(CLUSTER ? 0 : g.a.B);
+  cfg.dynamicSmemBytes = shared_bytes<Z, Tile, CLUSTER>(g.a.B);
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -936,11 +971,6 @@ cudaError_t launch_kernel(const Args& g, cudaStream_t s) {
   e = cudaLaunchKernelEx(&cfg, k, g);
   if (e != cudaSuccess) return e;
   return hook_launched(g.a.hook, s);
-}
-
-template <class Z, class Tile>
-cudaError_t launch_tile(const Args& g, cudaStream_t s) {
-  return g.p.cluster ? launch_kernel<Z, Tile, true>(g, s) : launch_kernel<Z, Tile, false>(g, s);
 }
 
 }  // namespace paged

@@ -3,19 +3,25 @@
 
 namespace dck {
 namespace paged {
+namespace {
+
+// S_R, S_C: stages per warp of tiles dealt in ranges and of clusters.
+template <int DP, int S_R, int S_C, bool PACK>
+cudaError_t launch_pack(const Args& g, cudaStream_t s) {
+  if (g.p.cluster) {
+    using Z = Sizes<__nv_bfloat16, DP, warps_of(DP, true), S_C, 16>;
+    return launch_kernel<Z, TensorTile<Z, PACK>, true>(g, s);
+  }
+  using Z = Sizes<__nv_bfloat16, DP, warps_of(DP, false), S_R, 16>;
+  return launch_kernel<Z, TensorTile<Z, PACK>, false>(g, s);
+}
+
+}  // namespace
 
 cudaError_t launch_bf16(const Args& g, cudaStream_t s) {
-  using bf16 = __nv_bfloat16;
-  if (g.DP == 256) {
-    using Z = Sizes<bf16, 256, 4, 3, 16>;
-    return launch_tile<Z, TensorTile<Z, true>>(g, s);
-  }
-  if (g.DP == 128) {
-    using Z = Sizes<bf16, 128, 8, 3, 16>;
-    return g.p.rows > 8 ? launch_tile<Z, TensorTile<Z, false>>(g, s) : launch_tile<Z, TensorTile<Z, true>>(g, s);
-  }
-  using Z = Sizes<bf16, 64, 8, 6, 16>;
-  return g.p.rows > 8 ? launch_tile<Z, TensorTile<Z, false>>(g, s) : launch_tile<Z, TensorTile<Z, true>>(g, s);
+  if (g.DP == 256) return launch_pack<256, 3, 3, true>(g, s);
+  if (g.DP == 128) return g.p.rows > 8 ? launch_pack<128, 3, 3, false>(g, s) : launch_pack<128, 3, 3, true>(g, s);
+  return g.p.rows > 8 ? launch_pack<64, 6, 6, false>(g, s) : launch_pack<64, 6, 6, true>(g, s);
 }
 
 }  // namespace paged

@@ -5,19 +5,29 @@ namespace dck {
 namespace paged {
 namespace {
 
-template <class Z>
+template <int DP, int S_R, int S_C, int ROWS>
+cudaError_t launch_rows(const Args& g, cudaStream_t s) {
+  if (g.p.cluster) {
+    using Z = Sizes<float, DP, warps_of(DP, true), S_C, 8>;
+    return launch_kernel<Z, SimtTile<Z, ROWS>, true>(g, s);
+  }
+  using Z = Sizes<float, DP, warps_of(DP, false), S_R, 8>;
+  return launch_kernel<Z, SimtTile<Z, ROWS>, false>(g, s);
+}
+
+template <int DP, int S_R, int S_C>
 cudaError_t by_rows(const Args& g, cudaStream_t s) {
-  if (g.p.rows == 1) return launch_tile<Z, SimtTile<Z, 1>>(g, s);
-  if (g.p.rows <= 4) return launch_tile<Z, SimtTile<Z, 4>>(g, s);
-  return launch_tile<Z, SimtTile<Z, 8>>(g, s);
+  if (g.p.rows == 1) return launch_rows<DP, S_R, S_C, 1>(g, s);
+  if (g.p.rows <= 4) return launch_rows<DP, S_R, S_C, 4>(g, s);
+  return launch_rows<DP, DP == 64 ? S_R : S_R - 1, S_C, 8>(g, s);  // the queries take the room of a stage
 }
 
 }  // namespace
 
 cudaError_t launch_f32(const Args& g, cudaStream_t s) {
-  if (g.DP == 64) return by_rows<Sizes<float, 64, 8, 4, 8>>(g, s);
-  if (g.DP == 128) return by_rows<Sizes<float, 128, 8, 2, 8>>(g, s);
-  return by_rows<Sizes<float, 256, 4, 2, 8>>(g, s);
+  if (g.DP == 64) return by_rows<64, 6, 4>(g, s);
+  if (g.DP == 128) return by_rows<128, 3, 2>(g, s);
+  return by_rows<256, 3, 2>(g, s);
 }
 
 }  // namespace paged
