@@ -31,24 +31,41 @@ namespace dck {
 namespace paged {
 namespace {
 
-// Joins the partial sums of what several CTAs share: a block per (entry, row).  Weights
-// first (a thread per partial), then 16-byte loads of the partials by kJoinWarps warps'
-// groups of lanes, several in flight.
+// Joins the partial sums of what several CTAs share: per (entry, row) weights first,
+// then 16-byte loads of the partials, several in flight.  A block takes a row (BLOCK),
+// or each of its warps takes one: few partials of many rows.
 constexpr int kJoinThreads = 256;
 constexpr int kJoinBatch = 8;
 
 template <typename T>
+__device__ __forceinline__ void put_joined(const Args& g, int64_t out_row, int e, float4 sum, float m, float l, bool bad) {
+  const bool none = bad || l == 0.f;
+  const float f = 1.f / l;
+  put4(static_cast<T*>(g.a.out) + out_row * g.a.v.d + e,
+       none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f),
+       (reinterpret_cast<uintptr_t>(g.a.out) & 3) == 0);
+  if (g.a.lse && e == 0) g.a.lse[out_row] = none ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945f;
+}
+
+template <typename T, bool BLOCK>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args g) {
-  __shared__ float weight[kJoinThreads];
   __shared__ float2 warp_ml[kJoinThreads / 32];
+  __shared__ float weights[kJoinThreads];
   __shared__ int any_bad;
-  __shared__ float4 sums[kJoinThreads];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = g.p.wh * g.p.rows, d = g.a.v.d;
-  const int quads = g.DP / 4, lanes = kJoinThreads / quads, quad = tid % quads, turn = tid / quads;
+  __shared__ float4 sums[BLOCK ? kJoinThreads : 1];
+  constexpr int kTeam = BLOCK ? kJoinThreads : 32;  // threads of a row
+  const int team = threadIdx.x / kTeam, tid = threadIdx.x % kTeam, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = g.p.wh * g.p.rows, d = g.a.v.d;
+  const int quads = min(g.DP / 4, kTeam), lanes = kTeam / quads, quad = tid % quads, turn = tid / quads;
+  const auto sync = [] {
+    if (BLOCK) __syncthreads();
+    else __syncwarp();
+  };
+  float* weight = weights + team * kTeam;
   pdl_launch_dependents();
   pdl_wait();
-  const int n = g.header->n_entries;
-  for (int64_t x = blockIdx.x; x < (int64_t)n * per; x += gridDim.x) {
+  const int64_t n = (int64_t)g.header->n_entries * per;
+  for (int64_t x = (int64_t)blockIdx.x * (kJoinThreads / kTeam) + team; x < n; x += (int64_t)gridDim.x * (kJoinThreads / kTeam)) {
     const Entry e = g.entries[x / per];
     const int hr = (int)(x % per), h = hr / g.p.rows, r = hr - h * g.p.rows;
     const int group = e.pair / g.a.B, b = e.pair - group * g.a.B;
@@ -57,71 +74,87 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     const int64_t out_row = (int64_t)b * g.a.v.Hq + qs.first + r;
     const auto row = [&](int i) { return ((int64_t)(2 * (e.c0 + i) + (i == 0 ? e.second : 0)) * g.p.wh + h) * g.p.rows + r; };
     const int parts = e.c1 - e.c0 + 1;
-    float M = -CUDART_INF_F, total = 0.f;
-    bool bad = false;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = 0; i0 < parts; i0 += kJoinThreads) {  // twice at most: CTAs are two per SM
-      const int count = min(kJoinThreads, parts - i0);
-      // the loads of the first partials go out before the weights are known
-      float4 v[kJoinBatch];
-      const auto fetch = [&](int i) {
+    for (int q0 = 0; q0 < g.DP / 4; q0 += quads) {  // once, but for a warp on heads above 128
+      const int el = 4 * (q0 + quad);
+      float M = -CUDART_INF_F, total = 0.f;
+      bool bad = false;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i0 = 0; i0 < parts; i0 += kTeam) {
+        const int count = min(kTeam, parts - i0);
+        // the loads of the first partials go out before the weights are known
+        float4 v[kJoinBatch];
+        const auto fetch = [&](int i) {
 #pragma unroll
-        for (int k = 0; k < kJoinBatch; ++k)
-          if (i + k * lanes < count && 4 * quad < d)
-            v[k] = *reinterpret_cast<const float4*>(g.part_u + row(i0 + i + k * lanes) * g.DP + 4 * quad);
-      };
-      fetch(turn);
-      float2 ml = make_float2(-CUDART_INF_F, 0.f);
-      if (tid < count) ml = *reinterpret_cast<const float2*>(g.part_ml + 2 * row(i0 + tid));
-      if (tid == 0) any_bad = 0;
-      float m = ml.x;
+          for (int k = 0; k < kJoinBatch; ++k)
+            if (i + k * lanes < count && el < d)
+              v[k] = *reinterpret_cast<const float4*>(g.part_u + row(i0 + i + k * lanes) * g.DP + el);
+        };
+        fetch(turn);
+        float2 ml = make_float2(-CUDART_INF_F, 0.f);
+        if (tid < count) ml = *reinterpret_cast<const float2*>(g.part_ml + 2 * row(i0 + tid));
+        float m = ml.x;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-      if (lane == 0) warp_ml[warp].x = m;
-      __syncthreads();
-      if (ml.y < 0.f) any_bad = 1;
-      float top = M;
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+        if (BLOCK) {
+          if (tid == 0) any_bad = 0;
+          if (lane == 0) warp_ml[warp].x = m;
+          __syncthreads();
+          if (ml.y < 0.f) any_bad = 1;
 #pragma unroll
-      for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, warp_ml[w].x);
-      const float base = top == -CUDART_INF_F ? 0.f : top, w = exp2_approx(ml.x - base), before = exp2_approx(M - base);
-      weight[tid] = w;
-      float l = ml.y * w;
+          for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, warp_ml[w].x);
+        }
+        const float top = fmaxf(M, m);
+        const float base = top == -CUDART_INF_F ? 0.f : top, w = exp2_approx(ml.x - base), before = exp2_approx(M - base);
+        weight[tid] = w;
+        float l = ml.y * w;
 #pragma unroll
-      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
-      if (lane == 0) warp_ml[warp].y = l;
-      __syncthreads();
-      bad |= any_bad != 0;
-      total *= before;
+        for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+        if (BLOCK) {
+          if (lane == 0) warp_ml[warp].y = l;
+          __syncthreads();
+          l = 0.f;
 #pragma unroll
-      for (int k = 0; k < kJoinThreads / 32; ++k) total += warp_ml[k].y;
-      sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
-      M = top;
-      for (int i = turn; i < count; i += kJoinBatch * lanes) {
-        if (i != turn) fetch(i);
+          for (int k = 0; k < kJoinThreads / 32; ++k) l += warp_ml[k].y;
+          bad |= any_bad != 0;
+        } else {
+          bad |= __any_sync(~0u, ml.y < 0.f) != 0;
+          __syncwarp();
+        }
+        total = total * before + l;
+        sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
+        M = top;
+        for (int i = turn; i < count; i += kJoinBatch * lanes) {
+          if (i != turn) fetch(i);
 #pragma unroll
-        for (int k = 0; k < kJoinBatch; ++k)
-          if (i + k * lanes < count && 4 * quad < d && weight[i + k * lanes] != 0.f) {
-            const float c = weight[i + k * lanes];
-            sum.x += v[k].x * c, sum.y += v[k].y * c, sum.z += v[k].z * c, sum.w += v[k].w * c;
+          for (int k = 0; k < kJoinBatch; ++k)
+            if (i + k * lanes < count && el < d && weight[i + k * lanes] != 0.f) {
+              const float c = weight[i + k * lanes];
+              sum.x += v[k].x * c, sum.y += v[k].y * c, sum.z += v[k].z * c, sum.w += v[k].w * c;
+            }
+        }
+        sync();
+      }
+      if (BLOCK) {
+        sums[tid] = sum;
+        __syncthreads();
+        if (turn == 0 && el < d) {
+          for (int k = 1; k < lanes; ++k) {
+            const float4 y = sums[k * quads + quad];
+            sum.x += y.x, sum.y += y.y, sum.z += y.z, sum.w += y.w;
           }
+          put_joined<T>(g, out_row, el, sum, M, total, bad);
+        }
+        __syncthreads();
+      } else {
+        for (int k = quads; k < 32; k <<= 1) {  // the lanes that share a quad of elements
+          sum.x += __shfl_xor_sync(~0u, sum.x, k);
+          sum.y += __shfl_xor_sync(~0u, sum.y, k);
+          sum.z += __shfl_xor_sync(~0u, sum.z, k);
+          sum.w += __shfl_xor_sync(~0u, sum.w, k);
+        }
+        if (turn == 0 && el < d) put_joined<T>(g, out_row, el, sum, M, total, bad);
       }
-      __syncthreads();
     }
-    sums[tid] = sum;
-    __syncthreads();
-    if (turn == 0 && 4 * quad < d) {
-      for (int k = 1; k < lanes; ++k) {
-        const float4 y = sums[k * quads + quad];
-        sum.x += y.x, sum.y += y.y, sum.z += y.z, sum.w += y.w;
-      }
-      const float f = bad || total == 0.f ? 0.f : 1.f / total;
-      put4(static_cast<T*>(g.a.out) + out_row * d + 4 * quad,
-           f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f),
-           (reinterpret_cast<uintptr_t>(g.a.out) & 3) == 0);
-      if (g.a.lse && quad == 0)
-        g.a.lse[out_row] = bad || total == 0.f ? -CUDART_INF_F : (M + log2f(total)) * 0.693147180559945f;
-    }
-    __syncthreads();
   }
 }
 
@@ -134,22 +167,28 @@ Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int 
   p.by_chunks = divider((uint32_t)p.chunks);
   const int heads = v.Hkv * p.chunks;
   const int64_t span = window > 0 ? std::min(window, max_len) : max_len;
+  const int64_t batch = std::max(B, 1);
+  const auto tiles_of = [&](int tokens) { return (span + tokens - 1) / tokens; };
+  const int few = warps_of(DP, false), many = warps_of(DP, true), run = run_of(dtype);
   // Clusters: one (head, sequence) each, as many CTAs as have a tile and one SM each
   p.cluster = 0;
-  const int of_cluster = warps_of(DP, true) * run_of(dtype);
-  const int64_t pairs = (int64_t)heads * std::max(B, 1), tiles = (span + of_cluster - 1) / of_cluster;
-  if (pairs <= sms) {
-    int c = 1;
-    while (2 * c <= kMaxCluster && 2 * c * pairs <= sms && c < tiles) c *= 2;
-    if (tiles <= kClusterTiles * c) p.cluster = c;
-  }
-  const int NW = warps_of(DP, p.cluster != 0);
-  p.wh = p.cluster ? 1 : NW;
+  p.warps = few;
+  p.wh = few;
   while (heads % p.wh) p.wh /= 2;
-  p.wt = NW / p.wh;
+  if (heads * batch <= sms) {
+    int c = 1;
+    while (2 * c <= kMaxCluster && 2 * c * heads * batch <= sms && c < tiles_of(many * run)) c *= 2;
+    if (tiles_of(many * run) <= kClusterTiles * c) p.cluster = c, p.warps = many, p.wh = 1;
+  } else if (tiles_of(run) <= kDirectRuns) {
+    // A CTA per (head group, sequence): the fewest heads that still make one wave, or all
+    int w = 1;
+    while (w < p.wh && heads / w * batch > kPerSm * sms) w *= 2;
+    p.cluster = 1, p.wh = w;
+  }
+  p.wt = p.warps / p.wh;
   p.groups = heads / p.wh;
-  p.tile = p.wt * run_of(dtype);
-  p.n_items = (int)std::min<int64_t>(kPerSm * sms, (int64_t)p.groups * std::max(B, 1) * ((span + p.tile - 1) / p.tile));
+  p.tile = p.wt * run;
+  p.n_items = (int)std::min<int64_t>(kPerSm * sms, p.groups * batch * tiles_of(p.tile));
   return p;
 }
 
@@ -183,10 +222,14 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cu
   if (e != cudaSuccess || g.p.cluster) return e;
   // one tile per (head group, sequence) at most: nothing is shared
   if ((a.window > 0 ? std::min(a.window, a.max_len) : a.max_len) <= g.p.tile) return cudaSuccess;
-  const int64_t work = (int64_t)g.p.n_items * g.p.wh * g.p.rows;
+  // partials per entry, on average, where all sequences are alike
+  const bool block = (int64_t)g.p.groups * a.B * 16 <= g.p.n_items;
+  const int64_t work = ((int64_t)g.p.n_items * g.p.wh * g.p.rows + (block ? 0 : 7)) / (block ? 1 : kJoinThreads / 32);
   const int grid = (int)std::min<int64_t>(work, 4 * sms);
-  e = dtype == DCK_F32 ? launch_pdl(join_kernel<float>, grid, kJoinThreads, 0, s, g)
-                       : launch_pdl(join_kernel<__nv_bfloat16>, grid, kJoinThreads, 0, s, g);
+  using bf16 = __nv_bfloat16;
+  const auto k = dtype == DCK_F32 ? (block ? join_kernel<float, true> : join_kernel<float, false>)
+                                  : (block ? join_kernel<bf16, true> : join_kernel<bf16, false>);
+  e = launch_pdl(k, grid, kJoinThreads, 0, s, g);
   if (e != cudaSuccess) return e;
   return hook_launched(a.hook, s);
 }

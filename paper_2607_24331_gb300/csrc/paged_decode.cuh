@@ -18,6 +18,7 @@ constexpr int kMaxLen = 1 << 30;     // tokens of a sequence
 constexpr int kTileLimit = 1 << 30;  // tiles of one call's sequences, per head group
 constexpr int kMaxCluster = 8;
 constexpr int kClusterTiles = 4;  // tiles per CTA up to which clusters are taken
+constexpr int kDirectRuns = 16;   // runs of tokens up to which a CTA takes a sequence whole
 
 // How a call is laid over warps and CTAs.
 struct Plan {
@@ -25,7 +26,8 @@ struct Plan {
   int wh, wt;        // warps of a CTA: wh heads (a power of two) x wt runs of tokens
   int groups;        // head groups: Hkv * chunks / wh
   int tile;          // tokens of a CTA's tile
-  int cluster;       // 0: tiles dealt in ranges; else CTAs of a cluster per (head group, sequence), wh = 1
+  int cluster;       // 0: tiles dealt in ranges; else the CTAs per (head group, sequence): 1, or a cluster of them and wh = 1
+  int warps;         // of a CTA
   int n_items;       // CTAs (dealt in ranges)
   Divider by_chunks;
 };
@@ -51,8 +53,9 @@ cudaError_t launch_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_f32(const Args& g, cudaStream_t s);
 
 inline int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-constexpr int warps_of(int DP, bool cluster) { return (DP == 256 ? 2 : 4) * (cluster ? 2 : 1); }
-constexpr int kPerSm = 2;  // CTAs per SM of tiles dealt in ranges
+// Warps of a CTA: two CTAs per SM fill its shared memory with rings, or one of twice the warps.
+constexpr int warps_of(int DP, bool one_per_sm) { return (DP == 256 ? 2 : 4) * (one_per_sm ? 2 : 1); }
+constexpr int kPerSm = 2;
 inline int run_of(int dtype) { return dtype == DCK_BF16 ? 16 : 8; }  // tokens of a warp's step
 
 // Visible tokens of sequence b and the first of them; 0 for invalid lengths.
@@ -700,7 +703,7 @@ __device__ __forceinline__ Joined join_rows(int n, float (&weight)[MOST], F ml_o
 }
 
 template <class Z, class Tile, bool CLUSTER>
-__global__ void __launch_bounds__(Z::NW * 32, CLUSTER ? 1 : kPerSm) paged_decode_kernel(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1 : kPerSm) paged_decode_kernel(const __grid_constant__ Args g) {
   using T = typename Z::T;
   extern __shared__ __align__(128) uint8_t raw[];
   using Shm = Shared<Z, Tile, CLUSTER>;
@@ -712,8 +715,7 @@ __global__ void __launch_bounds__(Z::NW * 32, CLUSTER ? 1 : kPerSm) paged_decode
   batch.prefix = reinterpret_cast<int*>(raw + Z::kRing + sizeof(sh));
   batch.len = a.B <= kKeptLens ? batch.prefix + a.B + 1 : nullptr;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int wh = CLUSTER ? 0 : warp & (g.p.wh - 1), wt = CLUSTER ? warp : warp / g.p.wh;
-  const int n_heads = CLUSTER ? 1 : g.p.wh, n_runs = CLUSTER ? Z::NW : g.p.wt;
+  const int n_heads = g.p.wh, n_runs = g.p.wt, wh = warp & (n_heads - 1), wt = warp / n_heads;
   const int d = a.v.d;
   T* out = static_cast<T*>(a.out);
   const bool even = (reinterpret_cast<uintptr_t>(out) & 3) == 0;
@@ -841,7 +843,7 @@ __global__ void __launch_bounds__(Z::NW * 32, CLUSTER ? 1 : kPerSm) paged_decode
       if (!whole) *reinterpret_cast<float2*>(g.part_ml + 2 * (part_row + r)) = make_float2(j.m, j.bad ? -1.f : j.l);
       else if (a.lse) a.lse[out_row + r] = j.bad || j.l == 0.f ? -CUDART_INF_F : (j.m + log2f(j.l)) * 0.693147180559945f;
     };
-    if (!CLUSTER && n_runs == 1) {
+    if (n_runs == 1) {
 #pragma unroll
       for (int x = 0; x < Tile::kMine; ++x) {
         const int r = Tile::row(x, lane);

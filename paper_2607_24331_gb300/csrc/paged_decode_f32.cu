@@ -5,29 +5,29 @@ namespace dck {
 namespace paged {
 namespace {
 
-template <int DP, int S_R, int S_C, int ROWS>
+template <int DP, int S, int ROWS>
 cudaError_t launch_rows(const Args& g, cudaStream_t s) {
-  if (g.p.cluster) {
-    using Z = Sizes<float, DP, warps_of(DP, true), S_C, 8>;
+  if (g.p.warps == warps_of(DP, true)) {
+    using Z = Sizes<float, DP, warps_of(DP, true), S, 8>;
     return launch_kernel<Z, SimtTile<Z, ROWS>, true>(g, s);
   }
-  using Z = Sizes<float, DP, warps_of(DP, false), S_R, 8>;
-  return launch_kernel<Z, SimtTile<Z, ROWS>, false>(g, s);
+  using Z = Sizes<float, DP, warps_of(DP, false), S, 8>;
+  return g.p.cluster ? launch_kernel<Z, SimtTile<Z, ROWS>, true>(g, s) : launch_kernel<Z, SimtTile<Z, ROWS>, false>(g, s);
 }
 
-template <int DP, int S_R, int S_C>
+template <int DP, int S>
 cudaError_t by_rows(const Args& g, cudaStream_t s) {
-  if (g.p.rows == 1) return launch_rows<DP, S_R, S_C, 1>(g, s);
-  if (g.p.rows <= 4) return launch_rows<DP, S_R, S_C, 4>(g, s);
-  return launch_rows<DP, DP == 64 ? S_R : S_R - 1, S_C, 8>(g, s);  // the queries take the room of a stage
+  if (g.p.rows == 1) return launch_rows<DP, S, 1>(g, s);
+  if (g.p.rows <= 4) return launch_rows<DP, S, 4>(g, s);
+  return launch_rows<DP, DP == 64 ? S : S - 1, 8>(g, s);  // the queries take the room of a stage
 }
 
 }  // namespace
 
 cudaError_t launch_f32(const Args& g, cudaStream_t s) {
-  if (g.DP == 64) return by_rows<64, 6, 4>(g, s);
-  if (g.DP == 128) return by_rows<128, 3, 2>(g, s);
-  return by_rows<256, 3, 2>(g, s);
+  if (g.DP == 64) return by_rows<64, 6>(g, s);
+  if (g.DP == 128) return by_rows<128, 3>(g, s);
+  return by_rows<256, 3>(g, s);
 }
 
 }  // namespace paged
