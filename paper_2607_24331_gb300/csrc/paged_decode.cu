@@ -165,6 +165,7 @@ Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int 
   p.chunks = (v.qpg + most - 1) / most;
   p.rows = (v.qpg + p.chunks - 1) / p.chunks;
   p.by_chunks = divider((uint32_t)p.chunks);
+  p.alike = v.k_page == v.v_page && v.k_tok == v.v_tok && v.k_head == v.v_head;
   const int heads = v.Hkv * p.chunks;
   const int64_t span = window > 0 ? std::min(window, max_len) : max_len;
   const int64_t batch = std::max(B, 1);

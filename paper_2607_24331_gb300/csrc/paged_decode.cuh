@@ -29,6 +29,7 @@ struct Plan {
   int cluster;       // 0: tiles dealt in ranges; else the CTAs per (head group, sequence): 1, or a cluster of them and wh = 1
   int warps;         // of a CTA
   int n_items;       // CTAs (dealt in ranges)
+  int alike;         // keys and values have the same strides
   Divider by_chunks;
 };
 
@@ -38,6 +39,8 @@ struct Entry {  // a (head group, sequence) shared by CTAs c0 .. c1
 struct Header {
   int n_entries;
 };
+
+constexpr float kHeadroom = 8.f;  // log2 units that a score may lie above the running reference
 
 struct Args {
   PagedDecodeArgs a;
@@ -218,33 +221,36 @@ struct Loader {
     return r;
   }
 
-  // Starts the copies of a stage; true if a page lies outside the pool (its tokens read as zeros).
+  // Starts the copies of a stage; true if a page lies outside the pool (its tokens read as
+  // zeros).  Eight lanes copy 128 bytes of a row, a warp four rows at a time.
   __device__ __forceinline__ bool issue(const Pages& r, int stage) const {
     const PagedView& v = g.a.v;
+    constexpr int el = sizeof(typename Z::T);
     const bool outside = r.valid && (r.page < 0 || r.page >= v.n_pages);
     const bool ok = r.valid && !outside;
     const int page = ok ? r.page : 0, off = ok ? r.off : 0;
-    const int64_t ko = (int64_t)page * v.k_page + (int64_t)off * v.k_tok + (int64_t)r.head * v.k_head;
-    const int64_t vo = (int64_t)page * v.v_page + (int64_t)off * v.v_tok + (int64_t)r.head * v.v_head;
+    const int64_t ko = ((int64_t)page * v.k_page + (int64_t)off * v.k_tok + (int64_t)r.head * v.k_head) * el;
+    int64_t vo = 0;
+    if (!g.p.alike) vo = ((int64_t)page * v.v_page + (int64_t)off * v.v_tok + (int64_t)r.head * v.v_head) * el;
     const uint32_t mask = __ballot_sync(~0u, ok);
-    const uint32_t at = ring + stage * Z::kStage;
-    constexpr int kPer = Z::kChunks < 32 ? 32 / Z::kChunks : 1;    // rows per instruction
-    constexpr int kTurns = Z::kChunks > 32 ? Z::kChunks / 32 : 1;  // instructions per row
-    const char* kc = static_cast<const char*>(g.a.kc);
-    const char* vc = static_cast<const char*>(g.a.vc);
-    const int have = v.d * (int)sizeof(typename Z::T) / 16;  // chunks of a row
+    const int sub = lane >> 3, c = lane & 7;
+    const uint32_t at = ring + stage * Z::kStage + sub * Z::kRow;
+    const char* kc = static_cast<const char*>(g.a.kc) + c * 16;
+    const char* vc = static_cast<const char*>(g.a.vc) + c * 16;
+    const int have = v.d * el / 16 - c;  // chunks of a row from this lane's first on
 #pragma unroll
-    for (int i = 0; i < Z::TOK / kPer; ++i) {
-      const int row = i * kPer + lane / (32 / kPer);
-      const int64_t kr = __shfl_sync(~0u, ko, row), vr = __shfl_sync(~0u, vo, row);
+    for (int i = 0; i < Z::TOK / 4; ++i) {
+      const int row = i * 4 + sub;
+      const int64_t kr = __shfl_sync(~0u, ko, row);
+      const int64_t vr = g.p.alike ? kr : __shfl_sync(~0u, vo, row);
+      const int bytes = mask >> row & 1 ? 16 : 0;
+      const uint32_t dst = at + i * 4 * Z::kRow + ((c ^ (row & 7)) * 16);
 #pragma unroll
-      for (int j = 0; j < kTurns; ++j) {
-        const int c = lane % (32 / kPer) + 32 * j;
-        const int bytes = (mask >> row & 1) && c < have ? 16 : 0;
-        const int64_t ce = bytes ? c * 16 : 0;
-        const uint32_t dst = at + row * Z::kRow + ((c ^ (row & 7)) * 16);
-        cp_async16_or_zero(dst, kc + kr * (int64_t)sizeof(typename Z::T) + ce, bytes);
-        cp_async16_or_zero(dst + Z::kHalf, vc + vr * (int64_t)sizeof(typename Z::T) + ce, bytes);
+      for (int j = 0; j < Z::kChunks / 8; ++j) {
+        const bool in = 8 * j < have;  // (past the row: zeros, from an address of the row)
+        const int from = in ? 128 * j : -16 * c;
+        cp_async16_or_zero(dst + 128 * j, kc + kr + from, in ? bytes : 0);
+        cp_async16_or_zero(dst + 128 * j + Z::kHalf, vc + vr + from, in ? bytes : 0);
       }
     }
     return __any_sync(~0u, outside);
@@ -361,18 +367,24 @@ struct TensorTile {
     float s[2][4] = {};
     {
       const int row = (lane & 7) + (lane >> 4) * 8, c = lane >> 3 & 1;
+      float s2[2][4] = {};  // every other k-step: chains of half the length
 #pragma unroll
       for (int k = 0; k < Z::DP / 16; ++k) {
         uint32_t b[4];
         ldmatrix4(b, keys + row * Z::kRow + (((2 * k + c) ^ (row & 7)) * 16));
+        float(&t)[2][4] = k & 1 ? s2 : s;
         if (PACK) {
-          mma16816(s[0], q[k][0], 0u, q[k][1], 0u, b[0], b[1]);
-          mma16816(s[1], q[k][0], 0u, q[k][1], 0u, b[2], b[3]);
+          mma16816(t[0], q[k][0], 0u, q[k][1], 0u, b[0], b[1]);
+          mma16816(t[1], q[k][0], 0u, q[k][1], 0u, b[2], b[3]);
         } else {
-          mma16816(s[0], q[k][0], q[k][1], q[k][2 % (2 * kQ)], q[k][3 % (2 * kQ)], b[0], b[1]);
-          mma16816(s[1], q[k][0], q[k][1], q[k][2 % (2 * kQ)], q[k][3 % (2 * kQ)], b[2], b[3]);
+          mma16816(t[0], q[k][0], q[k][1], q[k][2 % (2 * kQ)], q[k][3 % (2 * kQ)], b[0], b[1]);
+          mma16816(t[1], q[k][0], q[k][1], q[k][2 % (2 * kQ)], q[k][3 % (2 * kQ)], b[2], b[3]);
         }
       }
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int y = 0; y < (PACK ? 2 : 4); ++y) s[n][y] += s2[n][y];
     }
     if (PACK) {  // rows 8-15 of the tile hold nothing
       float v[4] = {s[0][0], s[0][1], s[1][0], s[1][1]};
@@ -390,25 +402,20 @@ struct TensorTile {
           if (n * 8 + (lane & 3) * 2 + (y & 1) >= live) s[n][y] = -CUDART_INF_F;
     }
     uint32_t hi[kQ][2], lo[kQ][2];
+    // m need not be the maximum, only near it: raised where a score is 2^8 above
     bool raise = false;
-    float top[kQ];
 #pragma unroll
-    for (int x = 0; x < kQ; ++x) {
-      float mx = m[x];
+    for (int x = 0; x < kQ; ++x)
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) mx = fmaxf(mx, s[n][2 * x + y]);
-      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
-      raise |= mx > m[x];
-      top[x] = mx;
-    }
+      for (int n = 0; n < 2; ++n) raise |= fmaxf(s[n][2 * x], s[n][2 * x + 1]) > m[x] + kHeadroom;
     if (__any_sync(~0u, raise)) {
 #pragma unroll
       for (int x = 0; x < kQ; ++x) {
-        const float c = m[x] == top[x] ? 1.f : exp2_approx(m[x] - top[x]);
-        m[x] = top[x];
+        float top = fmaxf(fmaxf(fmaxf(s[0][2 * x], s[0][2 * x + 1]), fmaxf(s[1][2 * x], s[1][2 * x + 1])), m[x]);
+        top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+        const float c = m[x] == top ? 1.f : exp2_approx(m[x] - top);
+        m[x] = top;
         l[x] *= c;
 #pragma unroll
         for (int n = 0; n < Z::DP / 8; ++n) {
@@ -530,24 +537,20 @@ struct SimtTile {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) s[r] += __shfl_xor_sync(~0u, s[r], 16);
     scale.apply(s);
-    float top[ROWS];
-    bool raise = false;
+    bool raise = false;  // as in TensorTile
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       if (t >= live) s[r] = -CUDART_INF_F;
-      top[r] = fmaxf(m[r], s[r]);
+      raise |= s[r] > m[r] + kHeadroom;
     }
-#pragma unroll
-    for (int x = 1; x < 8; x <<= 1)
-#pragma unroll
-      for (int r = 0; r < ROWS; ++r) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], x));
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) raise |= top[r] > m[r];
-    if (raise) {  // the same in every lane
+    if (__any_sync(~0u, raise)) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        const float c = m[r] == top[r] ? 1.f : exp2_approx(m[r] - top[r]);
-        m[r] = top[r];
+        float top = fmaxf(m[r], s[r]);
+#pragma unroll
+        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+        const float c = m[r] == top ? 1.f : exp2_approx(m[r] - top);
+        m[r] = top;
         l[r] *= c;
 #pragma unroll
         for (int k = 0; k < kOwn; ++k) o[r][k].x *= c, o[r][k].y *= c, o[r][k].z *= c, o[r][k].w *= c;
@@ -556,10 +559,8 @@ struct SimtTile {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
       const float p = exp2_approx(s[r] - (m[r] == -CUDART_INF_F ? 0.f : m[r]));
-      if (quarter == 0) {
-        l[r] += p;
-        weights[t * ROWS + r] = p;
-      }
+      l[r] += quarter == 0 ? p : 0.f;
+      if (quarter == 0) weights[t * ROWS + r] = p;
     }
     __syncwarp();
     const uint32_t vals = keys + Z::kHalf;
