@@ -764,17 +764,29 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
 
   const Loader<Z> load{g, (uint32_t)__cvta_generic_to_shared(raw) + warp * Z::S * Z::kStage, lane, wh, wt};
   Cursor at = ahead;
-  Pages pages = {0, 0, 0, false};
-  if (u0 < u1) pages = load.fetch(ahead);
+  // page numbers are read two tiles ahead of the copies: a read takes longer than a tile's arithmetic
+  Pages pages = {0, 0, 0, false}, pages2 = {0, 0, 0, false};
+  const auto fetch_next = [&]() {
+    pages2 = load.fetch(ahead);
+    if (CLUSTER) ++ahead.u;
+    else ahead.next(a, batch, u1);
+  };
+  if (u0 < u1) {
+    pages = load.fetch(ahead);
+    if (CLUSTER) ++ahead.u;
+    else ahead.next(a, batch, u1);
+    if (ahead.u < u1) fetch_next();
+  }
   uint32_t outside = 0;  // bit s: stage s has a page outside the pool
   int put = 0;           // stage that the next copies go to
+  int64_t to_copy = u1 - u0;
   const auto copy_next = [&]() {
-    if (ahead.u < u1) {
+    if (to_copy > 0) {
+      --to_copy;
       const bool bad = load.issue(pages, put);
       outside = (outside & ~(1u << put)) | (uint32_t)bad << put;
-      if (CLUSTER) ++ahead.u;
-      else ahead.next(a, batch, u1);
-      if (ahead.u < u1) pages = load.fetch(ahead);
+      pages = pages2;
+      if (ahead.u < u1) fetch_next();
       put = put + 1 == Z::S ? 0 : put + 1;
     }
     cp_async_commit();
