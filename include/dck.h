@@ -272,7 +272,7 @@ dck_status dck_decode_attention_noalloc(const dck_layer_desc* desc, const void* 
  *   n_pages       pages of the pool, 1 .. 2^31 - 1
  *   dtype         element type of caches, queries, keys, values and outputs
  *   k_*_stride    elements between pages, tokens of a page and heads of the key
- *   v_*_stride    and value cache, positive multiples of 16 bytes; head elements are
+ *   v_*_stride    and value cache, positive multiples of 16 bytes below 2^30; head elements are
  *                 consecutive.  Any order of pages, tokens and heads, and keys
  *                 and values in one buffer or two, are expressed by them.
  */
@@ -425,8 +425,8 @@ dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* ta
  * Rows past a sequence's end are never read into the sums, whatever they hold.  Scores,
  * softmax and sums are fp32.  A length below 0, above max_seq_len, 2^30 or the table, or a
  * page number outside the pool among those read, is recorded as a device error; the sequence's
- * outputs are zero with lse = -inf.  (So are more than 2^33 tokens in one call, which leave out
- * undefined.)  At most two launches; results do not depend on the order in which blocks run.
+ * outputs are zero with lse = -inf.  (So are more than 2^33 tokens times query heads in one call,
+ * which leave out undefined.)  At most two launches; results do not depend on the order in which blocks run.
  */
 size_t dck_paged_decode_workspace_size(const dck_paged_desc* desc, int32_t batch, int32_t max_seq_len);
 dck_status dck_paged_decode_attention(const dck_paged_desc* desc, const void* q, int64_t q_stride, const void* kcache,

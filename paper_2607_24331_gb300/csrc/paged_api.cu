@@ -24,8 +24,8 @@ dck_status check_paged(const dck_paged_desc* p) {
   if (p->head_dim % 8 || p->head_dim > kMaxPagedHeadDim || p->page_size > kMaxPageSize || p->n_q_heads > 65536)
     return DCK_ERR_UNSUPPORTED;
   const int64_t el = (int64_t)element(p->dtype);
-  // a bound on each stride keeps every byte offset (fewer than 2^31 strides) inside 64 bits
-  const int64_t most = int64_t(1) << 30;
+  // bytes of a stride in 32 bits, and with that every offset (fewer than 2^31 strides) in 64
+  const int64_t most = (int64_t(1) << 30) - 1;
   for (int64_t st : {p->k_page_stride, p->k_token_stride, p->k_head_stride, p->v_page_stride, p->v_token_stride,
                      p->v_head_stride})
     if (st <= 0 || st > most || st * el % 16 != 0) return DCK_ERR_INVALID;
@@ -46,6 +46,13 @@ PagedView make_view(const dck_paged_desc* p) {
   v.v_page = p->v_page_stride;
   v.v_tok = p->v_token_stride;
   v.v_head = p->v_head_stride;
+  const uint32_t el = (uint32_t)element(p->dtype);
+  v.k_page_b = (uint32_t)v.k_page * el;
+  v.k_tok_b = (uint32_t)v.k_tok * el;
+  v.k_head_b = (uint32_t)v.k_head * el;
+  v.v_page_b = (uint32_t)v.v_page * el;
+  v.v_tok_b = (uint32_t)v.v_tok * el;
+  v.v_head_b = (uint32_t)v.v_head * el;
   v.by_page = divider((uint32_t)p->page_size);
   return v;
 }

@@ -15,7 +15,7 @@ namespace dck {
 namespace paged {
 
 constexpr int kMaxLen = 1 << 30;     // tokens of a sequence
-constexpr int kTileLimit = 1 << 30;  // tiles of one call's sequences, per head group
+constexpr int kUnitLimit = 1 << 30;  // tiles of one call, over all head groups
 constexpr int kMaxCluster = 8;
 constexpr int kClusterTiles = 4;  // tiles per CTA up to which clusters are taken
 constexpr int kDirectRuns = 16;   // runs of tokens up to which a CTA takes a sequence whole
@@ -78,7 +78,8 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // Exclusive prefix sums of the sequences' tile counts in shared memory
 // prefix[0..B], and their lengths (len may be null).  Called by the whole block.
 template <int NW>
-__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, int* prefix, int* len, bool report) {
+__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, int groups, int* prefix, int* len, bool report) {
+  const int64_t limit = kUnitLimit / groups;
   __shared__ int64_t scratch[NW];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const auto tiles_of = [&](int b) -> int64_t {
@@ -100,10 +101,10 @@ __device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, i
   };
   if (a.B <= 32) {  // every warp by itself; fewer than 2^27 + 1 tiles each: no overflow of 2^32
     const int64_t n = tiles_of(lane), v = scan(n);
-    const int64_t all = min(__shfl_sync(~0u, v, 31), (int64_t)kTileLimit);
+    const int64_t all = min(__shfl_sync(~0u, v, 31), limit);
     if (warp == 0) {
-      if (v > kTileLimit && n > 0 && report) atomicOr(a.err, kErrBadSeq);
-      if (lane < a.B) prefix[lane] = (int)min(v - n, (int64_t)kTileLimit);
+      if (v > limit && n > 0 && report) atomicOr(a.err, kErrBadSeq);
+      if (lane < a.B) prefix[lane] = (int)min(v - n, limit);
       if (lane == 0) prefix[a.B] = (int)all;
     }
     __syncthreads();
@@ -123,10 +124,10 @@ __device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, i
       base += y;
     }
     if (b < a.B) {
-      if (before + v > kTileLimit && n > 0 && report) atomicOr(a.err, kErrBadSeq);
-      prefix[b] = (int)min(before + v - n, (int64_t)kTileLimit);
+      if (before + v > limit && n > 0 && report) atomicOr(a.err, kErrBadSeq);
+      prefix[b] = (int)min(before + v - n, limit);
     }
-    base = min(base, (int64_t)kTileLimit);
+    base = min(base, limit);
     __syncthreads();
   }
   if (tid == 0) prefix[a.B] = (int)base;
@@ -134,8 +135,9 @@ __device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, i
   return (int)base;
 }
 
-__device__ __forceinline__ int64_t range_begin(int c, int64_t units, int n) { return (int64_t)c * units / n; }
-__device__ __forceinline__ int item_of(int64_t u, int64_t units, int n) { return (int)(((u + 1) * n + units - 1) / units) - 1; }
+// CTA c of n has tiles [range_begin(c), range_begin(c + 1)) of `units`.
+__device__ __forceinline__ int range_begin(int c, int units, int n) { return (int)((int64_t)c * units / n); }
+__device__ __forceinline__ int item_of(int u, int units, int n) { return (int)(((int64_t)(u + 1) * n + units - 1) / units) - 1; }
 
 // What the plan keeps of the sequences in shared memory.
 struct Batch {
@@ -145,40 +147,38 @@ struct Batch {
 constexpr int kKeptLens = 1024;
 
 // A position in the flattened list of tiles (head groups outermost).
-struct Cursor {
-  int64_t u, start, end;  // the tile, and the range of its (head group, sequence)
-  int b, group, first, len;
+struct Walk {
+  int token, left;  // the tile's first token, and the tiles from it to the end of its (head group, sequence)
+  int b, group, len;
 
+  // Sets len, and token to the first visible one.
   __device__ __forceinline__ void see(const PagedDecodeArgs& a, const Batch& q) {
     if (q.len) {
       len = q.len[b];
-      first = a.window > 0 && len > a.window ? len - a.window : 0;
+      token = a.window > 0 && len > a.window ? len - a.window : 0;
     } else {
       bool bad;
-      len = visible(a, b, first, bad) + first;
+      len = visible(a, b, token, bad) + token;
     }
   }
-  __device__ __forceinline__ void enter(const PagedDecodeArgs& a, const Batch& q, int n_tiles, int64_t at) {
-    u = at;
-    group = (int)(at / n_tiles);
-    const int64_t base = (int64_t)group * n_tiles;
-    b = seq_of_tile(q.prefix, a.B, (int)(at - base));
-    start = base + q.prefix[b];
-    end = base + q.prefix[b + 1];
+  // Enters at tile u; true if that is the first of its (head group, sequence).
+  __device__ __forceinline__ bool enter(const PagedDecodeArgs& a, const Batch& q, int n_tiles, int tile, int u) {
+    group = u / n_tiles;
+    const int x = u - group * n_tiles;
+    b = seq_of_tile(q.prefix, a.B, x);
     see(a, q);
+    token += (x - q.prefix[b]) * tile;
+    left = q.prefix[b + 1] - x;
+    return x == q.prefix[b];
   }
-  __device__ __forceinline__ void next(const PagedDecodeArgs& a, const Batch& q, int64_t stop) {
-    if (++u < end || u >= stop) return;
-    int n;
+  // The next (head group, sequence) that has tiles.
+  __device__ __forceinline__ void leave(const PagedDecodeArgs& a, const Batch& q) {
     do {
       if (++b == a.B) b = 0, ++group;
-      n = q.prefix[b + 1] - q.prefix[b];
-    } while (n == 0);
-    start = end;
-    end = start + n;
+      left = q.prefix[b + 1] - q.prefix[b];
+    } while (left == 0);
     see(a, q);
   }
-  __device__ __forceinline__ int token(int tile) const { return first + (int)(u - start) * tile; }
 };
 
 // 16-byte asynchronous copy of `bytes` (16 or 0) bytes, the rest zero.
@@ -198,26 +198,53 @@ struct Sizes {
   static constexpr int kRing = NW * S * kStage;
 };
 
-// The page numbers and offsets of one warp's run of a tile: lane r holds token r.
+// The page number and offset of a token of one warp's run of a tile: lane r holds token r.
 struct Pages {
-  int page, off, head;
-  bool valid;
+  int page, off;  // off < 0: no token
+  int head;
 };
 
 template <class Z>
 struct Loader {
+  static constexpr int el = sizeof(typename Z::T);
   const Args& g;
-  uint32_t ring;  // this warp's stages
-  int lane, wh, wt;
+  const char *kc, *vc;    // with this lane's chunk
+  uint32_t ring, even, odd;  // this warp's stages; where this lane's chunk of rows 4 i + sub lies, i even or odd
+  int lane, run, wh;      // run: the warp's first token of a tile
+  int have;               // chunks of a row from this lane's first on
 
-  __device__ __forceinline__ Pages fetch(const Cursor& c) const {
+  __device__ __forceinline__ Loader(const Args& g, const uint8_t* raw, int warp, int lane, int wh, int wt)
+      : g(g), lane(lane), run(wt * Z::TOK), wh(wh) {
+    const int sub = lane >> 3, c = lane & 7;
+    kc = static_cast<const char*>(g.a.kc) + c * 16;
+    vc = static_cast<const char*>(g.a.vc) + c * 16;
+    ring = (uint32_t)__cvta_generic_to_shared(raw) + warp * Z::S * Z::kStage;
+    even = sub * Z::kRow + (c ^ sub) * 16;
+    odd = sub * Z::kRow + (c ^ (sub + 4)) * 16;
+    have = g.a.v.d * el / 16 - c;
+  }
+
+  // Heads shorter than the variant's: the rest of each row stays zero.
+  __device__ __forceinline__ void clear(uint8_t* raw) const {
+    if (g.a.v.d == Z::DP) return;
+    for (int i = threadIdx.x; i < Z::kRing / 16; i += Z::NW * 32) reinterpret_cast<uint4*>(raw)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+  }
+
+  // The same for a stage of this warp that has held something else.
+  __device__ __forceinline__ void clear_stage(uint8_t* stage) const {
+    if (g.a.v.d == Z::DP) return;
+    for (int i = lane; i < Z::kStage / 16; i += 32) reinterpret_cast<uint4*>(stage)[i] = make_uint4(0, 0, 0, 0);
+  }
+
+  __device__ __forceinline__ Pages fetch(const Walk& w) const {
     Pages r;
-    const int t = c.token(g.p.tile) + wt * Z::TOK + lane;
-    r.valid = lane < Z::TOK && t < c.len;
-    const uint32_t col = g.a.v.by_page.div(r.valid ? t : 0);
-    r.off = t - col * g.a.v.page;
-    r.page = r.valid ? g.a.table[(int64_t)c.b * g.a.table_stride + col] : 0;
-    r.head = g.p.by_chunks.div(c.group * g.p.wh + wh);
+    const int t = w.token + run + lane;
+    const bool have_it = lane < Z::TOK && t < w.len;
+    const uint32_t col = g.a.v.by_page.div(have_it ? t : 0);
+    r.off = have_it ? t - (int)col * g.a.v.page : -1;
+    r.page = have_it ? g.a.table[w.b * g.a.table_stride + col] : 0;
+    r.head = g.p.by_chunks.div(w.group * g.p.wh + wh);
     return r;
   }
 
@@ -225,35 +252,30 @@ struct Loader {
   // zeros).  Eight lanes copy 128 bytes of a row, a warp four rows at a time.
   __device__ __forceinline__ bool issue(const Pages& r, int stage) const {
     const PagedView& v = g.a.v;
-    constexpr int el = sizeof(typename Z::T);
-    const bool outside = r.valid && (r.page < 0 || r.page >= v.n_pages);
-    const bool ok = r.valid && !outside;
-    const int page = ok ? r.page : 0, off = ok ? r.off : 0;
-    const int64_t ko = ((int64_t)page * v.k_page + (int64_t)off * v.k_tok + (int64_t)r.head * v.k_head) * el;
-    int64_t vo = 0;
-    if (!g.p.alike) vo = ((int64_t)page * v.v_page + (int64_t)off * v.v_tok + (int64_t)r.head * v.v_head) * el;
-    const uint32_t mask = __ballot_sync(~0u, ok);
-    const int sub = lane >> 3, c = lane & 7;
-    const uint32_t at = ring + stage * Z::kStage + sub * Z::kRow;
-    const char* kc = static_cast<const char*>(g.a.kc) + c * 16;
-    const char* vc = static_cast<const char*>(g.a.vc) + c * 16;
-    const int have = v.d * el / 16 - c;  // chunks of a row from this lane's first on
+    const bool inside = (uint32_t)r.page < (uint32_t)v.n_pages, ok = inside && r.off >= 0;
+    const uint32_t page = inside ? r.page : 0, off = max(r.off, 0);
+    const int64_t ko = (int64_t)((uint64_t)page * v.k_page_b + (uint64_t)off * v.k_tok_b + (uint64_t)(uint32_t)r.head * v.k_head_b);
+    int64_t vo = ko;
+    if (!g.p.alike)
+      vo = (int64_t)((uint64_t)page * v.v_page_b + (uint64_t)off * v.v_tok_b + (uint64_t)(uint32_t)r.head * v.v_head_b);
+    const uint32_t mask = __ballot_sync(~0u, ok), at = ring + stage * Z::kStage;
+    const int sub = lane >> 3;
 #pragma unroll
     for (int i = 0; i < Z::TOK / 4; ++i) {
       const int row = i * 4 + sub;
       const int64_t kr = __shfl_sync(~0u, ko, row);
       const int64_t vr = g.p.alike ? kr : __shfl_sync(~0u, vo, row);
       const int bytes = mask >> row & 1 ? 16 : 0;
-      const uint32_t dst = at + i * 4 * Z::kRow + ((c ^ (row & 7)) * 16);
+      const uint32_t dst = at + (i & 1 ? odd : even) + i * 4 * Z::kRow;
+      const char *kp = kc + kr, *vp = vc + vr;
 #pragma unroll
-      for (int j = 0; j < Z::kChunks / 8; ++j) {
-        const bool in = 8 * j < have;  // (past the row: zeros, from an address of the row)
-        const int from = in ? 128 * j : -16 * c;
-        cp_async16_or_zero(dst + 128 * j, kc + kr + from, in ? bytes : 0);
-        cp_async16_or_zero(dst + 128 * j + Z::kHalf, vc + vr + from, in ? bytes : 0);
-      }
+      for (int j = 0; j < Z::kChunks / 8; ++j)
+        if (8 * j < have) {
+          cp_async16_or_zero(dst + 128 * j, kp + 128 * j, bytes);
+          cp_async16_or_zero(dst + 128 * j + Z::kHalf, vp + 128 * j, bytes);
+        }
     }
-    return __any_sync(~0u, outside);
+    return __any_sync(~0u, !inside);
   }
 };
 
@@ -298,16 +320,18 @@ struct ScoreScale {
 // bf16: tensor cores (mma.sync m16n8k16, queries as rows)
 // ---------------------------------------------------------------------------
 
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+// Matrices 16-byte chunks 2 k and 2 k + 1 of rows whose chunk 0 or 1 is at `at`: the swizzle
+// flips bits 4 to 6 of the address, whole 128-byte lines add.
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at, int k) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(at)
+               : "r"((at ^ (k % 4 * 32)) + k / 4 * 128)
                : "memory");
 }
-__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at, int k) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(at)
+               : "r"((at ^ (k % 4 * 32)) + k / 4 * 128)
                : "memory");
 }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -367,11 +391,12 @@ struct TensorTile {
     float s[2][4] = {};
     {
       const int row = (lane & 7) + (lane >> 4) * 8, c = lane >> 3 & 1;
+      const uint32_t at = keys + row * Z::kRow + (c ^ (row & 7)) * 16;
       float s2[2][4] = {};  // every other k-step: chains of half the length
 #pragma unroll
       for (int k = 0; k < Z::DP / 16; ++k) {
         uint32_t b[4];
-        ldmatrix4(b, keys + row * Z::kRow + (((2 * k + c) ^ (row & 7)) * 16));
+        ldmatrix4(b, at, k);
         float(&t)[2][4] = k & 1 ? s2 : s;
         if (PACK) {
           mma16816(t[0], q[k][0], 0u, q[k][1], 0u, b[0], b[1]);
@@ -436,10 +461,11 @@ struct TensorTile {
     }
     const uint32_t vals = keys + Z::kHalf;
     const int row = lane & 15, c = lane >> 4;
+    const uint32_t at = vals + row * Z::kRow + (c ^ (row & 7)) * 16;
 #pragma unroll
     for (int n = 0; n < Z::DP / 16; ++n) {
       uint32_t b[4];
-      ldmatrix4_trans(b, vals + row * Z::kRow + (((2 * n + c) ^ (row & 7)) * 16));
+      ldmatrix4_trans(b, at, n);
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         if (PACK) {
@@ -723,10 +749,13 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   pdl_launch_dependents();
   pdl_wait();
 
-  int n_tiles = 0, n = 0;
-  int64_t u0, u1;
-  Cursor ahead;
+  int n_tiles = 0, n = 0, units = 0;
+  int u0, u1;
+  Walk ahead;
+  bool begins = true;  // the first (head group, sequence) is this CTA's from its first tile on
   uint32_t rank = 0;
+  const Loader<Z> load(g, raw, warp, lane, wh, wt);
+  load.clear(raw);
   if (CLUSTER) {
     cluster_arrive();  // remote stores must find the other CTAs running: waited for before the first
     rank = cluster_rank();
@@ -734,18 +763,17 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     ahead.group = pair / a.B;
     ahead.b = pair - ahead.group * a.B;
     bool bad;
-    const int span = visible(a, ahead.b, ahead.first, bad);
+    const int span = visible(a, ahead.b, ahead.token, bad), tiles = (span + g.p.tile - 1) / g.p.tile;
     if (bad && ahead.group == 0 && rank == 0 && threadIdx.x == 0) atomicOr(a.err, kErrBadSeq);
-    ahead.len = span + ahead.first;
-    ahead.start = 0;
-    ahead.end = (span + g.p.tile - 1) / g.p.tile;
-    u0 = rank * ahead.end / g.p.cluster;
-    u1 = (rank + 1) * ahead.end / g.p.cluster;
-    ahead.u = u0;
+    ahead.len = span + ahead.token;
+    u0 = (int)rank * tiles / g.p.cluster;
+    u1 = ((int)rank + 1) * tiles / g.p.cluster;
+    ahead.token += u0 * g.p.tile;
+    ahead.left = u1 - u0;
   } else {
-    n_tiles = tile_prefix<Z::NW>(a, g.p.tile, batch.prefix, batch.len, blockIdx.x == 0);
-    const int64_t units = (int64_t)g.p.groups * n_tiles;
-    n = (int)min((int64_t)g.p.n_items, units);
+    n_tiles = tile_prefix<Z::NW>(a, g.p.tile, g.p.groups, batch.prefix, batch.len, blockIdx.x == 0);
+    units = g.p.groups * n_tiles;
+    n = min(g.p.n_items, units);
     // empty sequences
     for (int b = blockIdx.x; b < a.B; b += gridDim.x)
       if (batch.prefix[b + 1] == batch.prefix[b]) {
@@ -759,34 +787,30 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     }
     u0 = range_begin(blockIdx.x, units, n);
     u1 = range_begin(blockIdx.x + 1, units, n);
-    ahead.enter(a, batch, n_tiles, u0);
+    begins = ahead.enter(a, batch, n_tiles, g.p.tile, u0);
   }
 
-  const Loader<Z> load{g, (uint32_t)__cvta_generic_to_shared(raw) + warp * Z::S * Z::kStage, lane, wh, wt};
-  Cursor at = ahead;
+  Walk at = ahead;
+  int to_compute = u1 - u0, to_copy = to_compute, to_fetch = to_compute;
   // page numbers are read two tiles ahead of the copies: a read takes longer than a tile's arithmetic
-  Pages pages = {0, 0, 0, false}, pages2 = {0, 0, 0, false};
+  Pages pages = {0, -1, 0}, pages2 = {0, -1, 0};
   const auto fetch_next = [&]() {
-    pages2 = load.fetch(ahead);
-    if (CLUSTER) ++ahead.u;
-    else ahead.next(a, batch, u1);
+    const Pages p = load.fetch(ahead);
+    ahead.token += g.p.tile;
+    if (--to_fetch > 0 && --ahead.left == 0 && !CLUSTER) ahead.leave(a, batch);
+    return p;
   };
-  if (u0 < u1) {
-    pages = load.fetch(ahead);
-    if (CLUSTER) ++ahead.u;
-    else ahead.next(a, batch, u1);
-    if (ahead.u < u1) fetch_next();
-  }
+  if (to_fetch > 0) pages = fetch_next();
+  if (to_fetch > 0) pages2 = fetch_next();
   uint32_t outside = 0;  // bit s: stage s has a page outside the pool
   int put = 0;           // stage that the next copies go to
-  int64_t to_copy = u1 - u0;
   const auto copy_next = [&]() {
     if (to_copy > 0) {
       --to_copy;
       const bool bad = load.issue(pages, put);
       outside = (outside & ~(1u << put)) | (uint32_t)bad << put;
       pages = pages2;
-      if (ahead.u < u1) fetch_next();
+      if (to_fetch > 0) pages2 = fetch_next();
       put = put + 1 == Z::S ? 0 : put + 1;
     }
     cp_async_commit();
@@ -807,13 +831,10 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     __shared__ int n_entries;
     if (threadIdx.x == 0) n_entries = 0;
     __syncthreads();
-    const int64_t units = (int64_t)g.p.groups * n_tiles;
     for (int c = threadIdx.x; c + 1 < n; c += Z::NW * 32) {
-      const int64_t x = range_begin(c + 1, units, n);
-      const int group = (int)(x / n_tiles);
-      const int64_t base = (int64_t)group * n_tiles;
-      const int b = seq_of_tile(batch.prefix, a.B, (int)(x - base));
-      const int64_t start = base + batch.prefix[b], begin = range_begin(c, units, n);
+      const int x = range_begin(c + 1, units, n), group = x / n_tiles, base = group * n_tiles;
+      const int b = seq_of_tile(batch.prefix, a.B, x - base);
+      const int start = base + batch.prefix[b], begin = range_begin(c, units, n);
       if (x > start && begin <= start) {
         Entry e;
         e.pair = group * a.B + b;
@@ -827,30 +848,28 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     if (threadIdx.x == 0) g.header->n_entries = n_entries;
   }
 
-  int get = 0;
+  int get = 0, nth = 0;  // nth: this (head group, sequence) among the CTA's
   bool bad = false;
   while (true) {
-    if (!CLUSTER || at.u < u1) {
+    if (!CLUSTER || to_compute > 0) {
       __syncwarp();  // the stage that is filled next has been read
       copy_next();
       cp_async_wait<Z::S - 1>();
       __syncwarp();
       bad |= outside >> get & 1;
-      tile.step(load.ring + get * Z::kStage, at.len - at.token(g.p.tile) - wt * Z::TOK, lane, scale, mine);
+      tile.step(load.ring + get * Z::kStage, at.len - at.token - load.run, lane, scale, mine);
     }
     const int used = get;
     get = get + 1 == Z::S ? 0 : get + 1;
-    const bool last = at.u + 1 >= u1;
-    if (at.u + 1 < at.end && !last) {
-      ++at.u;
-      continue;
-    }
+    at.token += g.p.tile;
+    const bool ends = --at.left <= 0, last = --to_compute <= 0;
+    if (!ends && !last) continue;
     // the end of a (head group, sequence), or of this CTA's part of it
-    const bool whole = CLUSTER ? g.p.cluster == 1 : at.start >= u0 && at.end <= u1;
+    const bool whole = CLUSTER ? g.p.cluster == 1 : begins && ends;
     if (bad && lane == 0) atomicOr(a.err, kErrBadSeq);
     tile.finish();
     const int64_t out_row = (int64_t)at.b * a.v.Hq + qs.first;
-    const int64_t part_row = CLUSTER ? 0 : (int64_t)((2 * blockIdx.x + (u0 < at.start)) * n_heads + wh) * g.p.rows;
+    const int64_t part_row = CLUSTER ? 0 : (int64_t)((2 * blockIdx.x + (nth > 0)) * n_heads + wh) * g.p.rows;
     // the sum of row r (lse, or the partial's maximum and sum)
     const auto put_sum = [&](int r, const Joined& j) {
       if (!whole) *reinterpret_cast<float2*>(g.part_ml + 2 * (part_row + r)) = make_float2(j.m, j.bad ? -1.f : j.l);
@@ -916,11 +935,16 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
           if (e == 0) put_sum(r, j);
         }
       }
-      if (!CLUSTER) __syncthreads();
+      if (!CLUSTER) {
+        __syncthreads();
+        load.clear_stage(reinterpret_cast<uint8_t*>(left));
+      }
     }
     if (last) break;
     bad = false;
-    at.next(a, batch, u1);
+    begins = true;
+    ++nth;
+    at.leave(a, batch);
     qs = queries_of(g, at.group, wh);
     tile.begin(g, at.b, qs, lane, mine);
   }
