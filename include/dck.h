@@ -423,7 +423,7 @@ dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* ta
  *   workspace    at least dck_paged_decode_workspace_size bytes, 256-byte aligned; needs no
  *                initialisation
  * Rows past a sequence's end are never read into the sums, whatever they hold.  Scores,
- * softmax and sums are fp32.  A length below 0, above max_seq_len, 2^30 or the table, or a
+ * softmax and sums are fp32.  A length below 0, above max_seq_len, 2^29 or the table, or a
  * page number outside the pool among those read, is recorded as a device error; the sequence's
  * outputs are zero with lse = -inf.  (So are more than 2^33 tokens times query heads in one call,
  * which leave out undefined.)  At most two launches; results do not depend on the order in which blocks run.

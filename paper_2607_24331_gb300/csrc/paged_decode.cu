@@ -48,14 +48,14 @@ __device__ __forceinline__ void put_joined(const Args& g, int64_t out_row, int e
 }
 
 template <typename T, bool BLOCK>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args g, const Divider by_per, const Divider by_rows) {
   __shared__ float2 warp_ml[kJoinThreads / 32];
   __shared__ float weights[kJoinThreads];
   __shared__ int any_bad;
   __shared__ float4 sums[BLOCK ? kJoinThreads : 1];
   constexpr int kTeam = BLOCK ? kJoinThreads : 32;  // threads of a row
   const int team = threadIdx.x / kTeam, tid = threadIdx.x % kTeam, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int per = g.p.wh * g.p.rows, d = g.a.v.d;
+  const int d = g.a.v.d;
   const int quads = min(g.DP / 4, kTeam), lanes = kTeam / quads, quad = tid % quads, turn = tid / quads;
   const auto sync = [] {
     if (BLOCK) __syncthreads();
@@ -64,16 +64,33 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   float* weight = weights + team * kTeam;
   pdl_launch_dependents();
   pdl_wait();
-  const int64_t n = (int64_t)g.header->n_entries * per;
-  for (int64_t x = (int64_t)blockIdx.x * (kJoinThreads / kTeam) + team; x < n; x += (int64_t)gridDim.x * (kJoinThreads / kTeam)) {
-    const Entry e = g.entries[x / per];
-    const int hr = (int)(x % per), h = hr / g.p.rows, r = hr - h * g.p.rows;
-    const int group = e.pair / g.a.B, b = e.pair - group * g.a.B;
-    const Queries qs = queries_of(g, group, h);
+  // the entries that are any, in the order of CTAs
+  __shared__ uint16_t shared_by[kMaxItems];
+  __shared__ int counts[kJoinThreads / 32];
+  int n_entries = 0;
+  for (int c0 = 0; c0 < g.p.n_items; c0 += kJoinThreads) {
+    const int c = c0 + threadIdx.x;
+    const uint32_t any = __ballot_sync(~0u, c < g.p.n_items && g.entries[c].last >= 0);
+    if (lane == 0) counts[warp] = __popc(any);
+    __syncthreads();
+    int before = n_entries;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) {
+      if (w < warp) before += counts[w];
+      n_entries += counts[w];
+    }
+    if (any >> lane & 1) shared_by[before + __popc(any & ((1u << lane) - 1))] = (uint16_t)c;
+    __syncthreads();
+  }
+  const int per = g.p.wh * g.p.rows;
+  for (int x = blockIdx.x * (kJoinThreads / kTeam) + team; x < n_entries * per; x += gridDim.x * (kJoinThreads / kTeam)) {
+    const int c0 = shared_by[by_per.div(x)], hr = x - by_per.div(x) * per, h = by_rows.div(hr), r = hr - h * g.p.rows;
+    const Entry e = g.entries[c0];
+    const Queries qs = queries_of(g, e.group, h);
     if (r >= qs.count) continue;
-    const int64_t out_row = (int64_t)b * g.a.v.Hq + qs.first + r;
-    const auto row = [&](int i) { return ((int64_t)(2 * (e.c0 + i) + (i == 0 ? e.second : 0)) * g.p.wh + h) * g.p.rows + r; };
-    const int parts = e.c1 - e.c0 + 1;
+    const int64_t out_row = (int64_t)e.b * g.a.v.Hq + qs.first + r;
+    const auto row = [&](int i) { return ((int64_t)(2 * (c0 + i) + (i == 0 ? e.second : 0)) * g.p.wh + h) * g.p.rows + r; };
+    const int parts = e.last - c0 + 1;
     for (int q0 = 0; q0 < g.DP / 4; q0 += quads) {  // once, but for a warp on heads above 128
       const int el = 4 * (q0 + quad);
       float M = -CUDART_INF_F, total = 0.f;
@@ -189,7 +206,8 @@ Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int 
   p.wt = p.warps / p.wh;
   p.groups = heads / p.wh;
   p.tile = p.wt * run;
-  p.n_items = (int)std::min<int64_t>(kPerSm * sms, p.groups * batch * tiles_of(p.tile));
+  p.by_tile = divider((uint32_t)p.tile);
+  p.n_items = (int)std::min<int64_t>(std::min(kPerSm * sms, kMaxItems), p.groups * batch * tiles_of(p.tile));
   return p;
 }
 
@@ -205,7 +223,7 @@ size_t paged_decode_workspace(const PagedView& v, int dtype, int B, int max_len,
   // windows only make calls smaller: fewer CTAs, and clusters where the whole length has them
   const Plan p = plan_of(v, dtype, std::max(B, 1), max_len, 0, sms);
   if (p.cluster) return 0;
-  return 256 + align_up(p.n_items * sizeof(Entry), 256) + bytes_ml(p) + bytes_u(p, padded_dim(v.d));
+  return align_up(p.n_items * sizeof(Entry), 256) + bytes_ml(p) + bytes_u(p, padded_dim(v.d));
 }
 
 cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cudaStream_t s) {
@@ -214,9 +232,8 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cu
   g.p = plan_of(a.v, dtype, a.B, a.max_len, a.window, sms);
   g.DP = padded_dim(a.v.d);
   char* ws = static_cast<char*>(a.ws);
-  g.header = reinterpret_cast<Header*>(ws);
-  g.entries = reinterpret_cast<Entry*>(ws + 256);
-  ws += 256 + align_up(g.p.n_items * sizeof(Entry), 256);
+  g.entries = reinterpret_cast<Entry*>(ws);
+  ws += align_up(g.p.n_items * sizeof(Entry), 256);
   g.part_ml = reinterpret_cast<float*>(ws);
   g.part_u = reinterpret_cast<float*>(ws + bytes_ml(g.p));
   cudaError_t e = dtype == DCK_F32 ? launch_f32(g, s) : launch_bf16(g, s);
@@ -230,7 +247,7 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cu
   using bf16 = __nv_bfloat16;
   const auto k = dtype == DCK_F32 ? (block ? join_kernel<float, true> : join_kernel<float, false>)
                                   : (block ? join_kernel<bf16, true> : join_kernel<bf16, false>);
-  e = launch_pdl(k, grid, kJoinThreads, 0, s, g);
+  e = launch_pdl(k, grid, kJoinThreads, 0, s, g, divider(g.p.wh * g.p.rows), divider(g.p.rows));
   if (e != cudaSuccess) return e;
   return hook_launched(a.hook, s);
 }

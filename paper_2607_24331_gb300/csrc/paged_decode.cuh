@@ -14,7 +14,7 @@
 namespace dck {
 namespace paged {
 
-constexpr int kMaxLen = 1 << 30;     // tokens of a sequence
+constexpr int kMaxLen = 1 << 29;     // tokens of a sequence
 constexpr int kUnitLimit = 1 << 30;  // tiles of one call, over all head groups
 constexpr int kMaxCluster = 8;
 constexpr int kClusterTiles = 4;  // tiles per CTA up to which clusters are taken
@@ -30,15 +30,16 @@ struct Plan {
   int warps;         // of a CTA
   int n_items;       // CTAs (dealt in ranges)
   int alike;         // keys and values have the same strides
-  Divider by_chunks;
+  Divider by_chunks, by_tile;
 };
 
-struct Entry {  // a (head group, sequence) shared by CTAs c0 .. c1
-  int pair, c0, c1, second;  // second: the partial is c0's second one
+// What CTA c of tiles dealt in ranges leaves to the second launch: the (head group,
+// sequence) that it begins and that other CTAs, up to `last`, go on with.
+struct Entry {
+  int b, group, last;  // last < 0: none
+  int second;          // the CTA's partial of it is its second one
 };
-struct Header {
-  int n_entries;
-};
+constexpr int kMaxItems = 512;  // CTAs of tiles dealt in ranges
 
 constexpr float kHeadroom = 8.f;  // log2 units that a score may lie above the running reference
 
@@ -48,7 +49,6 @@ struct Args {
   int DP;          // head dim, rounded up to the variant's
   float* part_u;   // [2 n_items][wh][rows][DP]
   float* part_ml;  // [2 n_items][wh][rows][2]: maximum (log2 units), sum (-1: a page outside the pool)
-  Header* header;
   Entry* entries;  // [n_items]
 };
 
@@ -78,33 +78,33 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // Exclusive prefix sums of the sequences' tile counts in shared memory
 // prefix[0..B], and their lengths (len may be null).  Called by the whole block.
 template <int NW>
-__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, int tile, int groups, int* prefix, int* len, bool report) {
+__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, const Divider& by_tile, int groups, int* prefix, int* len, bool report) {
   const int64_t limit = kUnitLimit / groups;
   __shared__ int64_t scratch[NW];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const auto tiles_of = [&](int b) -> int64_t {
+  const auto tiles_of = [&](int b) -> uint32_t {  // at most 2^26
     if (b >= a.B) return 0;
     int first;
     bool bad;
     const int span = visible(a, b, first, bad);
     if (bad && report && (a.B > 32 || warp == 0)) atomicOr(a.err, kErrBadSeq);
     if (len && (a.B > 32 || warp == 0)) len[b] = span + first;
-    return (span + tile - 1) / tile;
+    return by_tile.div(span + by_tile.d - 1);
   };
-  const auto scan = [&](int64_t v) {
+  const auto scan = [&](auto v) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(~0u, v, o);
+      const auto y = __shfl_up_sync(~0u, v, o);
       if (lane >= o) v += y;
     }
     return v;
   };
-  if (a.B <= 32) {  // every warp by itself; fewer than 2^27 + 1 tiles each: no overflow of 2^32
-    const int64_t n = tiles_of(lane), v = scan(n);
-    const int64_t all = min(__shfl_sync(~0u, v, 31), limit);
+  if (a.B <= 32) {  // every warp by itself
+    const uint32_t n = tiles_of(lane), v = scan(n), most = (uint32_t)limit;
+    const uint32_t all = min(__shfl_sync(~0u, v, 31), most);
     if (warp == 0) {
-      if (v > limit && n > 0 && report) atomicOr(a.err, kErrBadSeq);
-      if (lane < a.B) prefix[lane] = (int)min(v - n, limit);
+      if (v > most && n > 0 && report) atomicOr(a.err, kErrBadSeq);
+      if (lane < a.B) prefix[lane] = (int)min(v - n, most);
       if (lane == 0) prefix[a.B] = (int)all;
     }
     __syncthreads();
@@ -771,7 +771,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     ahead.token += u0 * g.p.tile;
     ahead.left = u1 - u0;
   } else {
-    n_tiles = tile_prefix<Z::NW>(a, g.p.tile, g.p.groups, batch.prefix, batch.len, blockIdx.x == 0);
+    n_tiles = tile_prefix<Z::NW>(a, g.p.by_tile, g.p.groups, batch.prefix, batch.len, blockIdx.x == 0);
     units = g.p.groups * n_tiles;
     n = min(g.p.n_items, units);
     // empty sequences
@@ -782,7 +782,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
           for (int j = threadIdx.x; j < a.v.Hq; j += Z::NW * 32) a.lse[(int64_t)b * a.v.Hq + j] = -CUDART_INF_F;
       }
     if ((int)blockIdx.x >= n) {
-      if (blockIdx.x == 0 && threadIdx.x == 0) g.header->n_entries = 0;
+      if (threadIdx.x == 0) g.entries[blockIdx.x].last = -1;
       return;
     }
     u0 = range_begin(blockIdx.x, units, n);
@@ -826,27 +826,6 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   Tile tile;
   Queries qs = queries_of(g, at.group, wh);
   tile.begin(g, at.b, qs, lane, mine);
-
-  if (!CLUSTER && blockIdx.x == 0) {  // the list of what several CTAs share, for the second launch
-    __shared__ int n_entries;
-    if (threadIdx.x == 0) n_entries = 0;
-    __syncthreads();
-    for (int c = threadIdx.x; c + 1 < n; c += Z::NW * 32) {
-      const int x = range_begin(c + 1, units, n), group = x / n_tiles, base = group * n_tiles;
-      const int b = seq_of_tile(batch.prefix, a.B, x - base);
-      const int start = base + batch.prefix[b], begin = range_begin(c, units, n);
-      if (x > start && begin <= start) {
-        Entry e;
-        e.pair = group * a.B + b;
-        e.c0 = c;
-        e.c1 = item_of(base + batch.prefix[b + 1] - 1, units, n);
-        e.second = begin < start;
-        g.entries[atomicAdd(&n_entries, 1)] = e;
-      }
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) g.header->n_entries = n_entries;
-  }
 
   int get = 0, nth = 0;  // nth: this (head group, sequence) among the CTA's
   bool bad = false;
@@ -940,7 +919,11 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
         load.clear_stage(reinterpret_cast<uint8_t*>(left));
       }
     }
-    if (last) break;
+    if (last) {
+      if (!CLUSTER && threadIdx.x == 0)
+        g.entries[blockIdx.x] = {at.b, at.group, begins && !ends ? item_of(u1 + at.left - 1, units, n) : -1, nth > 0};
+      break;
+    }
     bad = false;
     begins = true;
     ++nth;

@@ -213,19 +213,23 @@ class Rope:
 
 
 def _ptr(t) -> Optional[int]:
-    if t is None:
-        return None
-    if isinstance(t, int):
+    try:
+        return t.data_ptr()
+    except AttributeError:  # an address, or None
         return t
-    return t.data_ptr()
+
+
+_torch = None
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        if torch.cuda.is_initialized():  # the handle alone: a Stream object takes 3 us to make, a fifth of a short call
-            return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream
+        global _torch
+        if _torch is None:
+            import torch as _torch
+        if _torch.cuda.is_initialized():  # the handle alone: a Stream object takes 3 us to make, a fifth of a short call
+            return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
+        return _torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -298,40 +302,40 @@ def dck_page_update(batch: int, page_size: int, n_pages: int, old_len, new_len, 
                     table_stride: int, free_pages, free_in, free_out, n_tok: int, slots, positions, cu_new,
                     stream=None) -> int:
     """A step's page bookkeeping: tables, free list, lengths, slots and positions of the new tokens."""
-    return lib().dck_page_update(int(batch), int(page_size), int(n_pages), _ptr(old_len), _ptr(new_len), _ptr(seq_len),
-                                 _ptr(block_table), int(table_stride), _ptr(free_pages), _ptr(free_in), _ptr(free_out),
-                                 int(n_tok), _ptr(slots), _ptr(positions), _ptr(cu_new), _stream(stream))
+    return lib().dck_page_update(batch, page_size, n_pages, _ptr(old_len), _ptr(new_len), _ptr(seq_len),
+                                 _ptr(block_table), table_stride, _ptr(free_pages), _ptr(free_in), _ptr(free_out),
+                                 n_tok, _ptr(slots), _ptr(positions), _ptr(cu_new), _stream(stream))
 
 
 def dck_rope(rope: Rope, x, n_tok: int, n_heads: int, head_dim: int, dtype: int, x_token_stride: int,
              x_head_stride: int, positions, out, out_token_stride: int, out_head_stride: int, transpose: bool = False,
              stream=None) -> int:
     """Rotation of x at the given positions, or its transpose (the gradient)."""
-    return lib().dck_rope(rope.ref, _ptr(x), int(n_tok), int(n_heads), int(head_dim), int(dtype), int(x_token_stride),
-                          int(x_head_stride), _ptr(positions), _ptr(out), int(out_token_stride), int(out_head_stride),
-                          int(transpose), _stream(stream))
+    return lib().dck_rope(rope.ref, _ptr(x), n_tok, n_heads, head_dim, dtype, x_token_stride,
+                          x_head_stride, _ptr(positions), _ptr(out), out_token_stride, out_head_stride,
+                          transpose, _stream(stream))
 
 
 def dck_paged_append(cache: PagedCache, rope: Optional[Rope], q, q_stride: int, k, k_stride: int, v, v_stride: int,
                      n_tok: int, positions, slots, q_out, kcache, vcache, stream=None) -> int:
     """New tokens' queries rotated to q_out, their keys (rotated) and values written to the slots' cache rows."""
-    return lib().dck_paged_append(cache.ref, rope.ref if rope is not None else None, _ptr(q), int(q_stride), _ptr(k),
-                                  int(k_stride), _ptr(v), int(v_stride), int(n_tok), _ptr(positions), _ptr(slots),
+    return lib().dck_paged_append(cache.ref, rope.ref if rope is not None else None, _ptr(q), q_stride, _ptr(k),
+                                  k_stride, _ptr(v), v_stride, n_tok, _ptr(positions), _ptr(slots),
                                   _ptr(q_out), _ptr(kcache), _ptr(vcache), _stream(stream))
 
 
 def dck_paged_decode_workspace_size(cache: PagedCache, batch: int, max_seq_len: int) -> int:
-    return lib().dck_paged_decode_workspace_size(cache.ref, int(batch), int(max_seq_len))
+    return lib().dck_paged_decode_workspace_size(cache.ref, batch, max_seq_len)
 
 
 def dck_paged_decode_attention(cache: PagedCache, q, q_stride: int, kcache, vcache, block_table, table_stride: int,
                                seq_len, batch: int, max_seq_len: int, scale: float, window: int, softcap: float, out,
                                lse, workspace, ws_bytes: int, stream=None) -> int:
     """One query per sequence over its pages; lse (optional): the log of the softmax's sum."""
-    return lib().dck_paged_decode_attention(cache.ref, _ptr(q), int(q_stride), _ptr(kcache), _ptr(vcache),
-                                            _ptr(block_table), int(table_stride), _ptr(seq_len), int(batch),
-                                            int(max_seq_len), float(scale), int(window), float(softcap), _ptr(out),
-                                            _ptr(lse), _ptr(workspace), int(ws_bytes), _stream(stream))
+    return lib().dck_paged_decode_attention(cache.ref, _ptr(q), q_stride, _ptr(kcache), _ptr(vcache),
+                                            _ptr(block_table), table_stride, _ptr(seq_len), batch,
+                                            max_seq_len, scale, window, softcap, _ptr(out),
+                                            _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream))
 
 
 def dck_last_device_error(stream=None) -> int:
