@@ -32,11 +32,10 @@ namespace paged {
 namespace {
 
 // Joins the partial sums of what several CTAs share: per (entry, row) weights first,
-// then 16-byte loads of the partials, several in flight.  A block takes a row (BLOCK),
-// or each of its warps takes one: few partials of many rows.
-constexpr int kJoinThreads = 256;
-constexpr int kJoinBatch = 8;
-
+// then 16-byte loads of the partials, several in flight.  Few entries of many partials
+// (LIST): blocks of 256 threads list the entries that are any and take their rows in turn.
+// Many entries of few partials: a block of 64 threads per CTA's entry and row, whether
+// there is one or not.
 template <typename T>
 __device__ __forceinline__ void put_joined(const Args& g, int64_t out_row, int e, float4 sum, float m, float l, bool bad) {
   const bool none = bad || l == 0.f;
@@ -47,132 +46,120 @@ __device__ __forceinline__ void put_joined(const Args& g, int64_t out_row, int e
   if (g.a.lse && e == 0) g.a.lse[out_row] = none ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945f;
 }
 
-template <typename T, bool BLOCK>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args g, const Divider by_per, const Divider by_rows) {
-  __shared__ float2 warp_ml[kJoinThreads / 32];
-  __shared__ float weights[kJoinThreads];
+template <typename T, int THREADS, bool LIST>
+__global__ void __launch_bounds__(THREADS, LIST ? 2 : 16) join_kernel(const __grid_constant__ Args g, const Divider by_per, const Divider by_rows) {
+  constexpr int kBatch = LIST ? 8 : 4;  // loads in flight per thread
+  __shared__ float2 warp_ml[THREADS / 32];
+  __shared__ float weight[THREADS];
   __shared__ int any_bad;
-  __shared__ float4 sums[BLOCK ? kJoinThreads : 1];
-  constexpr int kTeam = BLOCK ? kJoinThreads : 32;  // threads of a row
-  const int team = threadIdx.x / kTeam, tid = threadIdx.x % kTeam, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int d = g.a.v.d;
-  const int quads = min(g.DP / 4, kTeam), lanes = kTeam / quads, quad = tid % quads, turn = tid / quads;
-  const auto sync = [] {
-    if (BLOCK) __syncthreads();
-    else __syncwarp();
-  };
-  float* weight = weights + team * kTeam;
+  __shared__ float4 sums[THREADS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, d = g.a.v.d, per = g.p.wh * g.p.rows;
+  const int quads = g.DP / 4, lanes = THREADS / quads, quad = tid % quads, turn = tid / quads, el = 4 * quad;
   pdl_launch_dependents();
   pdl_wait();
   // the entries that are any, in the order of CTAs
-  __shared__ uint16_t shared_by[kMaxItems];
-  __shared__ int counts[kJoinThreads / 32];
-  int n_entries = 0;
-  for (int c0 = 0; c0 < g.p.n_items; c0 += kJoinThreads) {
-    const int c = c0 + threadIdx.x;
-    const uint32_t any = __ballot_sync(~0u, c < g.p.n_items && g.entries[c].last >= 0);
-    if (lane == 0) counts[warp] = __popc(any);
-    __syncthreads();
-    int before = n_entries;
+  __shared__ uint16_t shared_by[LIST ? kMaxItems : 1];
+  __shared__ int counts[THREADS / 32];
+  int n_rows = g.p.n_items * per;
+  if (LIST) {
+    int n_entries = 0;
+    for (int c0 = 0; c0 < g.p.n_items; c0 += THREADS) {
+      const int c = c0 + tid;
+      const uint32_t any = __ballot_sync(~0u, c < g.p.n_items && g.entries[c].last >= 0);
+      if (lane == 0) counts[warp] = __popc(any);
+      __syncthreads();
+      int before = n_entries;
 #pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) {
-      if (w < warp) before += counts[w];
-      n_entries += counts[w];
+      for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) before += counts[w];
+        n_entries += counts[w];
+      }
+      if (any >> lane & 1) shared_by[before + __popc(any & ((1u << lane) - 1))] = (uint16_t)c;
+      __syncthreads();
     }
-    if (any >> lane & 1) shared_by[before + __popc(any & ((1u << lane) - 1))] = (uint16_t)c;
-    __syncthreads();
+    n_rows = n_entries * per;
   }
-  const int per = g.p.wh * g.p.rows;
-  for (int x = blockIdx.x * (kJoinThreads / kTeam) + team; x < n_entries * per; x += gridDim.x * (kJoinThreads / kTeam)) {
-    const int c0 = shared_by[by_per.div(x)], hr = x - by_per.div(x) * per, h = by_rows.div(hr), r = hr - h * g.p.rows;
+  for (int x = blockIdx.x; x < n_rows; x += gridDim.x) {
+    const int nth = by_per.div(x), c0 = LIST ? shared_by[nth] : nth, hr = x - nth * per, h = by_rows.div(hr), r = hr - h * g.p.rows;
     const Entry e = g.entries[c0];
+    if (!LIST && e.last < 0) continue;
     const Queries qs = queries_of(g, e.group, h);
     if (r >= qs.count) continue;
     const int64_t out_row = (int64_t)e.b * g.a.v.Hq + qs.first + r;
-    const auto row = [&](int i) { return ((int64_t)(2 * (c0 + i) + (i == 0 ? e.second : 0)) * g.p.wh + h) * g.p.rows + r; };
-    const int parts = e.last - c0 + 1;
-    for (int q0 = 0; q0 < g.DP / 4; q0 += quads) {  // once, but for a warp on heads above 128
-      const int el = 4 * (q0 + quad);
-      float M = -CUDART_INF_F, total = 0.f;
-      bool bad = false;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i0 = 0; i0 < parts; i0 += kTeam) {
-        const int count = min(kTeam, parts - i0);
-        // the loads of the first partials go out before the weights are known
-        float4 v[kJoinBatch];
-        const auto fetch = [&](int i) {
+    const int parts = e.last - c0 + 1, stride = 2 * g.p.wh * g.p.rows;  // partial rows from CTA to CTA
+    const int row0 = (2 * c0 * g.p.wh + h) * g.p.rows + r;
+    const auto row = [&](int i) { return (int64_t)(row0 + i * stride + (i == 0 && e.second ? stride / 2 : 0)); };
+    float M = -CUDART_INF_F, total = 0.f;
+    bool bad = false;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < parts; i0 += THREADS) {
+      const int count = min(THREADS, parts - i0);
+      // the loads of the first partials go out before the weights are known
+      float4 v[kBatch];
+      const auto fetch = [&](int i) {
 #pragma unroll
-          for (int k = 0; k < kJoinBatch; ++k)
-            if (i + k * lanes < count && el < d)
-              v[k] = *reinterpret_cast<const float4*>(g.part_u + row(i0 + i + k * lanes) * g.DP + el);
-        };
-        fetch(turn);
-        float2 ml = make_float2(-CUDART_INF_F, 0.f);
-        if (tid < count) ml = *reinterpret_cast<const float2*>(g.part_ml + 2 * row(i0 + tid));
-        float m = ml.x;
+        for (int k = 0; k < kBatch; ++k)
+          if (i + k * lanes < count && el < d)
+            v[k] = *reinterpret_cast<const float4*>(g.part_u + row(i0 + i + k * lanes) * g.DP + el);
+      };
+      float2 ml = make_float2(-CUDART_INF_F, 0.f);
+      if (tid < count) ml = *reinterpret_cast<const float2*>(g.part_ml + 2 * row(i0 + tid));
+      fetch(turn);
+      if (tid == 0) any_bad = 0;
+      float m = ml.x;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-        if (BLOCK) {
-          if (tid == 0) any_bad = 0;
-          if (lane == 0) warp_ml[warp].x = m;
-          __syncthreads();
-          if (ml.y < 0.f) any_bad = 1;
+      for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+      if (lane == 0) warp_ml[warp].x = m;
+      __syncthreads();
+      if (ml.y < 0.f) any_bad = 1;
+      float top = M;
 #pragma unroll
-          for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, warp_ml[w].x);
-        }
-        const float top = fmaxf(M, m);
-        const float base = top == -CUDART_INF_F ? 0.f : top, w = exp2_approx(ml.x - base), before = exp2_approx(M - base);
-        weight[tid] = w;
-        float l = ml.y * w;
+      for (int w = 0; w < THREADS / 32; ++w) top = fmaxf(top, warp_ml[w].x);
+      const float base = top == -CUDART_INF_F ? 0.f : top, w = exp2_approx(ml.x - base), before = exp2_approx(M - base);
+      weight[tid] = w;
+      float l = ml.y * w;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
-        if (BLOCK) {
-          if (lane == 0) warp_ml[warp].y = l;
-          __syncthreads();
-          l = 0.f;
+      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+      if (lane == 0) warp_ml[warp].y = l;
+      __syncthreads();
+      bad |= any_bad != 0;
+      total *= before;
 #pragma unroll
-          for (int k = 0; k < kJoinThreads / 32; ++k) l += warp_ml[k].y;
-          bad |= any_bad != 0;
-        } else {
-          bad |= __any_sync(~0u, ml.y < 0.f) != 0;
-          __syncwarp();
-        }
-        total = total * before + l;
-        sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
-        M = top;
-        for (int i = turn; i < count; i += kJoinBatch * lanes) {
-          if (i != turn) fetch(i);
+      for (int k = 0; k < THREADS / 32; ++k) total += warp_ml[k].y;
+      sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
+      M = top;
+      for (int i = turn; i < count; i += kBatch * lanes) {
+        if (i != turn) fetch(i);
 #pragma unroll
-          for (int k = 0; k < kJoinBatch; ++k)
-            if (i + k * lanes < count && el < d && weight[i + k * lanes] != 0.f) {
-              const float c = weight[i + k * lanes];
-              sum.x += v[k].x * c, sum.y += v[k].y * c, sum.z += v[k].z * c, sum.w += v[k].w * c;
-            }
-        }
-        sync();
-      }
-      if (BLOCK) {
-        sums[tid] = sum;
-        __syncthreads();
-        if (turn == 0 && el < d) {
-          for (int k = 1; k < lanes; ++k) {
-            const float4 y = sums[k * quads + quad];
-            sum.x += y.x, sum.y += y.y, sum.z += y.z, sum.w += y.w;
+        for (int k = 0; k < kBatch; ++k)
+          if (i + k * lanes < count && el < d && weight[i + k * lanes] != 0.f) {
+            const float c = weight[i + k * lanes];
+            sum.x += v[k].x * c, sum.y += v[k].y * c, sum.z += v[k].z * c, sum.w += v[k].w * c;
           }
-          put_joined<T>(g, out_row, el, sum, M, total, bad);
-        }
-        __syncthreads();
-      } else {
-        for (int k = quads; k < 32; k <<= 1) {  // the lanes that share a quad of elements
-          sum.x += __shfl_xor_sync(~0u, sum.x, k);
-          sum.y += __shfl_xor_sync(~0u, sum.y, k);
-          sum.z += __shfl_xor_sync(~0u, sum.z, k);
-          sum.w += __shfl_xor_sync(~0u, sum.w, k);
-        }
-        if (turn == 0 && el < d) put_joined<T>(g, out_row, el, sum, M, total, bad);
       }
+      __syncthreads();
     }
+    if (lanes > 1) {
+      sums[tid] = sum;
+      __syncthreads();
+    }
+    if (turn == 0 && el < d) {
+      for (int k = 1; k < lanes; ++k) {
+        const float4 y = sums[k * quads + quad];
+        sum.x += y.x, sum.y += y.y, sum.z += y.z, sum.w += y.w;
+      }
+      put_joined<T>(g, out_row, el, sum, M, total, bad);
+    }
+    __syncthreads();
   }
+}
+
+template <typename T, int THREADS, bool LIST>
+cudaError_t launch_join(const Args& g, int64_t most, cudaStream_t s) {
+  const int per = g.p.wh * g.p.rows;
+  const int grid = (int)std::min<int64_t>((int64_t)g.p.n_items * per, most);
+  cudaError_t e = launch_pdl(join_kernel<T, THREADS, LIST>, grid, THREADS, 0, s, g, divider(per), divider(g.p.rows));
+  return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
 }
 
 Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int sms) {
@@ -240,16 +227,11 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cu
   if (e != cudaSuccess || g.p.cluster) return e;
   // one tile per (head group, sequence) at most: nothing is shared
   if ((a.window > 0 ? std::min(a.window, a.max_len) : a.max_len) <= g.p.tile) return cudaSuccess;
-  // partials per entry, on average, where all sequences are alike
-  const bool block = (int64_t)g.p.groups * a.B * 16 <= g.p.n_items;
-  const int64_t work = ((int64_t)g.p.n_items * g.p.wh * g.p.rows + (block ? 0 : 7)) / (block ? 1 : kJoinThreads / 32);
-  const int grid = (int)std::min<int64_t>(work, 4 * sms);
+  // partials per entry, on average, where all sequences are alike: 16 or more
   using bf16 = __nv_bfloat16;
-  const auto k = dtype == DCK_F32 ? (block ? join_kernel<float, true> : join_kernel<float, false>)
-                                  : (block ? join_kernel<bf16, true> : join_kernel<bf16, false>);
-  e = launch_pdl(k, grid, kJoinThreads, 0, s, g, divider(g.p.wh * g.p.rows), divider(g.p.rows));
-  if (e != cudaSuccess) return e;
-  return hook_launched(a.hook, s);
+  if ((int64_t)g.p.groups * a.B * 16 <= g.p.n_items)
+    return dtype == DCK_F32 ? launch_join<float, 256, true>(g, 4 * sms, s) : launch_join<bf16, 256, true>(g, 4 * sms, s);
+  return dtype == DCK_F32 ? launch_join<float, 64, false>(g, 1 << 30, s) : launch_join<bf16, 64, false>(g, 1 << 30, s);
 }
 
 }  // namespace dck

@@ -135,9 +135,13 @@ __device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, const Divid
   return (int)base;
 }
 
-// CTA c of n has tiles [range_begin(c), range_begin(c + 1)) of `units`.
-__device__ __forceinline__ int range_begin(int c, int units, int n) { return (int)((int64_t)c * units / n); }
-__device__ __forceinline__ int item_of(int u, int units, int n) { return (int)(((int64_t)(u + 1) * n + units - 1) / units) - 1; }
+// CTA c of n has tiles [begin(c), begin(c + 1)) of `units`, begin(c) = floor(c units / n).
+struct Ranges {
+  int units, n, each, rest;
+  __device__ __forceinline__ Ranges(int units, int n) : units(units), n(n), each(n ? units / n : 0), rest(units - each * n) {}
+  __device__ __forceinline__ int begin(int c) const { return c * each + c * rest / n; }
+  __device__ __forceinline__ int item_of(int u) const { return (int)(((int64_t)(u + 1) * n + units - 1) / units) - 1; }
+};
 
 // What the plan keeps of the sequences in shared memory.
 struct Batch {
@@ -749,7 +753,8 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   pdl_launch_dependents();
   pdl_wait();
 
-  int n_tiles = 0, n = 0, units = 0;
+  int n_tiles = 0;
+  Ranges ranges(0, 0);
   int u0, u1;
   Walk ahead;
   bool begins = true;  // the first (head group, sequence) is this CTA's from its first tile on
@@ -772,8 +777,8 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     ahead.left = u1 - u0;
   } else {
     n_tiles = tile_prefix<Z::NW>(a, g.p.by_tile, g.p.groups, batch.prefix, batch.len, blockIdx.x == 0);
-    units = g.p.groups * n_tiles;
-    n = min(g.p.n_items, units);
+    const int units = g.p.groups * n_tiles;
+    ranges = Ranges(units, min(g.p.n_items, units));
     // empty sequences
     for (int b = blockIdx.x; b < a.B; b += gridDim.x)
       if (batch.prefix[b + 1] == batch.prefix[b]) {
@@ -781,12 +786,12 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
         if (a.lse)
           for (int j = threadIdx.x; j < a.v.Hq; j += Z::NW * 32) a.lse[(int64_t)b * a.v.Hq + j] = -CUDART_INF_F;
       }
-    if ((int)blockIdx.x >= n) {
+    if ((int)blockIdx.x >= ranges.n) {
       if (threadIdx.x == 0) g.entries[blockIdx.x].last = -1;
       return;
     }
-    u0 = range_begin(blockIdx.x, units, n);
-    u1 = range_begin(blockIdx.x + 1, units, n);
+    u0 = ranges.begin(blockIdx.x);
+    u1 = ranges.begin(blockIdx.x + 1);
     begins = ahead.enter(a, batch, n_tiles, g.p.tile, u0);
   }
 
@@ -921,7 +926,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     }
     if (last) {
       if (!CLUSTER && threadIdx.x == 0)
-        g.entries[blockIdx.x] = {at.b, at.group, begins && !ends ? item_of(u1 + at.left - 1, units, n) : -1, nth > 0};
+        g.entries[blockIdx.x] = {at.b, at.group, begins && !ends ? ranges.item_of(u1 + at.left - 1) : -1, nth > 0};
       break;
     }
     bad = false;

@@ -35,6 +35,8 @@ __device__ __forceinline__ CacheRow cache_row(const RopeLaunch& a, int64_t i, bo
 // elements (or single element past the rotary dimension).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rope_any_kernel(const __grid_constant__ RopeLaunch a) {
+  pdl_launch_dependents();
+  pdl_wait();
   const int64_t i = blockIdx.x;
   const uint32_t pos = a.rope.rot ? (uint32_t)a.positions[i] : 0u;
   const CacheRow to = cache_row(a, i, threadIdx.x == 0);
@@ -98,104 +100,91 @@ struct Vec<__nv_bfloat16> {
 
 // Rows of whole 16-byte vectors, a rotary dimension of whole pairs of vectors.  A
 // thread's unit is two vectors of a head: those of N pairs, or of elements past the
-// rotary dimension.  Threads are laid out (token, head, unit); each visits its unit of
-// further heads and tokens, with the loads of kUnroll of them in flight, the first of
-// them while the block computes its tokens' sines and cosines (once per token, for all
-// heads) into shared memory.
+// rotary dimension.  Threads are laid out (head, unit) over the heads of all the block's
+// tokens, and each visits its unit of every across-th head.  The first loads are under way
+// while the block computes its tokens' sines and cosines (once per token, for all heads)
+// into shared memory.  One unit in flight per thread and six blocks per SM: with two or
+// four units in flight and as many blocks as their registers leave, 16384 x 32 heads of 128
+// took 42.8 and 49.5 us for 42.3 (268 MB, 93% of the copy bandwidth); with eight blocks 42.0,
+// but small fp32 calls 15% more.
 struct VecLaunch {
   int turned;   // units of pairs per head
   int units;    // units per head
-  int across;   // heads that a token's threads cover at a time
-  int abreast;  // tokens that a block's threads cover at a time
+  int across;   // heads that a block's threads cover at a time
   int tokens;   // tokens per block
   int heads;    // heads of all row sets
-  Divider by_token, by_head;  // threads per token, units per head
-  Divider by_turned;
+  Divider by_units, by_heads, by_turned;
 };
-constexpr int kUnroll = 4;
+constexpr int kRounds = 2;  // units per thread that a block's tokens are chosen for (1, 4 or 8: 43, 44, 48 us there)
 
 template <typename T, bool HALF>
-__global__ void __launch_bounds__(kThreads, 3) rope_vec_kernel(const __grid_constant__ RopeLaunch a,
+__global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_constant__ RopeLaunch a,
                                                                const __grid_constant__ VecLaunch v) {
   constexpr int N = Vec<T>::N;
   // [tokens][N][turned] (cos, sin) of pair j N + k at k turned + j; then the tokens' cache rows
   extern __shared__ float2 turn[];
   const int pairs = a.rope.rot / 2;
   CacheRow* rows_to = reinterpret_cast<CacheRow*>(turn + v.tokens * pairs);
-  const int tid = threadIdx.x;
-  const int tok = v.by_token.div(tid), in_tok = tid - tok * v.by_token.d;
-  const int h0 = v.by_head.div(in_tok), j = in_tok - h0 * v.units;
+  const int tid = threadIdx.x, h0 = v.by_units.div(tid), j = tid - h0 * v.units;
   const int64_t first = (int64_t)blockIdx.x * v.tokens;
-  const int n_here = (int)min((int64_t)v.tokens, a.n_tok - first);
+  const int n_here = (int)min((int64_t)v.tokens, a.n_tok - first), n_heads = n_here * v.heads;
   // the unit's two vectors: pairs (x, y) side by side or half the rotary dimension apart
   const int past = 2 * v.turned + 2 * (j - v.turned);
-  const int va = j >= v.turned ? past : HALF ? j : 2 * j, vb = j >= v.turned ? past + 1 : HALF ? j + v.turned : 2 * j + 1;
-  const bool two = vb * N < a.d;
+  const int va = (j >= v.turned ? past : HALF ? j : 2 * j) * N, vb = (j >= v.turned ? past + 1 : HALF ? j + v.turned : 2 * j + 1) * N;
+  const bool two = vb < a.d;
 
-  struct Unit {
-    int t, set, head;  // t < 0: none
-  };
-  int t_next = tok < v.abreast ? tok : n_here, h_next = h0;
-  Unit unit[kUnroll];
-  uint4 x[kUnroll], y[kUnroll];
+  int next = h0 < v.across ? h0 : n_heads, t, head, set;
+  uint4 x, y;
   const auto load = [&]() {
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      unit[u].t = -1;
-      if (t_next >= n_here) continue;
-      int hh = h_next, r = 0;
-      while (r + 1 < a.n_rows && hh >= a.rows[r].heads) hh -= a.rows[r++].heads;
-      unit[u] = {t_next, r, hh};
-      const T* src = static_cast<const T*>(a.rows[r].src) + (first + t_next) * a.rows[r].src_tok + hh * a.rows[r].src_head;
-      x[u] = *reinterpret_cast<const uint4*>(src + va * N);
-      if (two) y[u] = *reinterpret_cast<const uint4*>(src + vb * N);
-      h_next += v.across;
-      if (h_next >= v.heads) h_next = h0, t_next += v.abreast;
-    }
+    if (next >= n_heads) return;
+    t = v.by_heads.div(next);
+    head = next - t * v.heads;
+    set = 0;
+    while (set + 1 < a.n_rows && head >= a.rows[set].heads) head -= a.rows[set++].heads;
+    const T* src = static_cast<const T*>(a.rows[set].src) + (first + t) * a.rows[set].src_tok + head * a.rows[set].src_head;
+    x = *reinterpret_cast<const uint4*>(src + va);
+    if (two) y = *reinterpret_cast<const uint4*>(src + vb);
   };
+  pdl_launch_dependents();
+  pdl_wait();
   load();
   for (int z = tid; z < n_here * pairs; z += kThreads) {
-    const int q = v.by_turned.div(z), jj = z - q * v.turned, t = q / N, k = q - t * N;
+    const int q = v.by_turned.div(z), jj = z - q * v.turned, tok = q / N, k = q - tok * N;
     float sn, cs;
-    rope_sincos(a.rope.f[jj * N + k], (uint32_t)a.positions[first + t], sn, cs);
+    rope_sincos(a.rope.f[jj * N + k], (uint32_t)a.positions[first + tok], sn, cs);
     turn[z] = make_float2(cs * a.rope.magnitude, sn * (a.rope.sign * a.rope.magnitude));
   }
   if (a.slots)
-    for (int t = tid; t < n_here; t += kThreads) rows_to[t] = cache_row(a, first + t, true);
+    for (int i = tid; i < n_here; i += kThreads) rows_to[i] = cache_row(a, first + i, true);
   __syncthreads();
-  while (unit[0].t >= 0) {
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (unit[u].t < 0) continue;
-      const RopeRows& rows = a.rows[unit[u].set];
-      int64_t at = (first + unit[u].t) * rows.dst_tok;
-      if (rows.cached) {
-        const CacheRow to = rows_to[unit[u].t];
-        if (!to.have) continue;
-        at = to.page * rows.dst_page + to.off * rows.dst_tok;
-      }
-      T* dst = static_cast<T*>(rows.dst) + at + unit[u].head * rows.dst_head;
-      if (rows.rotate && j < v.turned) {
-        const float2* cs = turn + unit[u].t * pairs + j;
-        float p[N], q[N];
-        Vec<T>::open(x[u], p);
-        Vec<T>::open(y[u], q);
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const float2 z = cs[k * v.turned];
-          float& e0 = HALF ? p[k] : k < N / 2 ? p[2 * k % N] : q[2 * k % N];
-          float& e1 = HALF ? q[k] : k < N / 2 ? p[(2 * k + 1) % N] : q[(2 * k + 1) % N];
-          const float w = e0 * z.x - e1 * z.y;
-          e1 = e0 * z.y + e1 * z.x;
-          e0 = w;
-        }
-        x[u] = Vec<T>::close(p);
-        y[u] = Vec<T>::close(q);
-      }
-      *reinterpret_cast<uint4*>(dst + va * N) = x[u];
-      if (two) *reinterpret_cast<uint4*>(dst + vb * N) = y[u];
+  for (; next < n_heads; next += v.across, load()) {
+    const RopeRows& rows = a.rows[set];
+    int64_t at = (first + t) * rows.dst_tok;
+    if (rows.cached) {
+      const CacheRow to = rows_to[t];
+      if (!to.have) continue;
+      at = to.page * rows.dst_page + to.off * rows.dst_tok;
     }
-    load();
+    T* dst = static_cast<T*>(rows.dst) + at + head * rows.dst_head;
+    if (rows.rotate && j < v.turned) {
+      const float2* cs = turn + t * pairs + j;
+      float p[N], q[N];
+      Vec<T>::open(x, p);
+      Vec<T>::open(y, q);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float2 z = cs[k * v.turned];
+        float& e0 = HALF ? p[k] : k < N / 2 ? p[2 * k % N] : q[2 * k % N];
+        float& e1 = HALF ? q[k] : k < N / 2 ? p[(2 * k + 1) % N] : q[(2 * k + 1) % N];
+        const float w = e0 * z.x - e1 * z.y;
+        e1 = e0 * z.y + e1 * z.x;
+        e0 = w;
+      }
+      x = Vec<T>::close(p);
+      y = Vec<T>::close(q);
+    }
+    *reinterpret_cast<uint4*>(dst + va) = x;
+    if (two) *reinterpret_cast<uint4*>(dst + vb) = y;
   }
 }
 
@@ -214,14 +203,12 @@ bool vec_plan(const RopeLaunch& a, int sms, VecLaunch* v) {
   v->turned = a.rope.rot / (2 * N);
   v->units = v->turned + ((a.d - a.rope.rot) / N + 1) / 2;
   if (v->units > kThreads) return false;
-  v->across = std::min(v->heads, kThreads / v->units);
-  v->abreast = (int)std::min<int64_t>(kThreads / (v->across * v->units), a.n_tok);
-  // enough tokens for a few rounds of loads per thread, as long as four blocks per SM remain
-  const int rounds = (v->heads + v->across - 1) / v->across;
-  const int64_t spread = a.n_tok / ((int64_t)v->abreast * 4 * sms);
-  v->tokens = v->abreast * (int)std::max<int64_t>(1, std::min<int64_t>(spread, (2 * kUnroll + rounds - 1) / rounds));
-  v->by_token = divider(v->across * v->units);
-  v->by_head = divider(v->units);
+  v->across = kThreads / v->units;
+  // as many tokens as give every thread a few units, if eight blocks per SM remain
+  const int64_t full = (kRounds * v->across + v->heads - 1) / v->heads, one = (v->across + v->heads - 1) / v->heads;
+  v->tokens = (int)std::min<int64_t>(std::max<int64_t>(std::min(full, (int64_t)a.n_tok / (8 * sms)), one), a.n_tok);
+  v->by_units = divider(v->units);
+  v->by_heads = divider(v->heads);
   v->by_turned = divider(std::max(1, v->turned));
   return true;
 }
@@ -230,14 +217,12 @@ template <typename T>
 cudaError_t launch(const RopeLaunch& a, int sms, cudaStream_t s) {
   VecLaunch v;
   if (!vec_plan<T>(a, sms, &v)) {
-    rope_any_kernel<T><<<a.n_tok, kThreads, 0, s>>>(a);
-    return cudaGetLastError();
+    return launch_pdl(rope_any_kernel<T>, a.n_tok, kThreads, 0, s, a);
   }
   const int grid = (a.n_tok + v.tokens - 1) / v.tokens;
   const size_t smem = (size_t)v.tokens * (a.rope.rot / 2 * sizeof(float2) + sizeof(CacheRow));
-  if (a.rope.layout == DCK_ROPE_HALF) rope_vec_kernel<T, true><<<grid, kThreads, smem, s>>>(a, v);
-  else rope_vec_kernel<T, false><<<grid, kThreads, smem, s>>>(a, v);
-  return cudaGetLastError();
+  return launch_pdl(a.rope.layout == DCK_ROPE_HALF ? rope_vec_kernel<T, true> : rope_vec_kernel<T, false>, grid, kThreads,
+                    smem, s, a, v);
 }
 
 }  // namespace
