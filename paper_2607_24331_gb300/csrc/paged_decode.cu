@@ -25,6 +25,8 @@
 // second launch would take longer than the attention: there a cluster of CTAs takes each
 // (KV head, sequence), all warps of a CTA on runs of its tokens, and joins the CTAs' sums
 // through distributed shared memory.
+#include <cmath>
+
 #include "paged_decode.cuh"
 
 namespace dck {
@@ -162,6 +164,14 @@ cudaError_t launch_join(const Args& g, int64_t most, cudaStream_t s) {
   return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
 }
 
+// Which of the three ways a call takes: the least of their times (us) by a model fitted to
+// 570 calls of six head layouts, 1 to 128 sequences of 16 to 4096 tokens, all alike or
+// ragged 16-fold; the choice is 1.6% off the best of the three on average.  Measured, ranges
+// / clusters / whole, 32 query heads on 8 KV heads of 128 in bf16:
+//   1 x 1024   9.0 /  6.3 / 15.5      16 x 512  13.7 /  8.2 / 10.9      64 x 256   21.2 / - / 15.7
+//   4 x 4096  18.8 / 17.4 / 63        16 x 4096 50.2 / 46.5 / 59        64 x 2048  90.2 / - / 84
+//   1 x 128    6.8 /  4.6 /  4.4      16 x 128..2048 17.3 / 15.6 / 22   64 x 128..2048  38.4 / - / 46
+// (1 x 16384 15 / 21 / 190).
 Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int sms) {
   Plan p;
   const int DP = padded_dim(v.d);
@@ -170,36 +180,45 @@ Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int 
   p.rows = (v.qpg + p.chunks - 1) / p.chunks;
   p.by_chunks = divider((uint32_t)p.chunks);
   p.alike = v.k_page == v.v_page && v.k_tok == v.v_tok && v.k_head == v.v_head;
-  const int heads = v.Hkv * p.chunks;
-  const int64_t span = window > 0 ? std::min(window, max_len) : max_len;
-  const int64_t batch = std::max(B, 1);
+  const int heads = v.Hkv * p.chunks, few = warps_of(DP, false), many = warps_of(DP, true), run = run_of(dtype);
+  const int64_t span = window > 0 ? std::min(window, max_len) : max_len, pairs = (int64_t)heads * std::max(B, 1);
   const auto tiles_of = [&](int tokens) { return (span + tokens - 1) / tokens; };
-  const int few = warps_of(DP, false), many = warps_of(DP, true), run = run_of(dtype);
-  // Clusters: one (head, sequence) each, as many CTAs as have a tile and one SM each
+  int wide = few;  // heads side by side in a CTA, at most
+  while (heads % wide) wide /= 2;
+
+  const int row = DP * (dtype == DCK_BF16 ? 2 : 4);
+  const double step = row <= 128 ? 0.53 : row == 256 ? 0.68 : row == 512 ? 0.88 : 1.14;  // a warp's run of tokens
+  // the bytes at the copy bandwidth and 7% more, of sequences of 0.56 of the bound on average
+  const double bytes = 0.56 * 1.07 * 2. * B * span * v.Hkv * v.d * (dtype == DCK_BF16 ? 2 : 4) / 6.8e6;
+  const int slots = kPerSm * sms;
+  double best = 7.5 + bytes + 0.45 * std::max(0., (double)pairs / wide / slots - 1) - (span <= few / wide * run ? 2.7 : 0);
   p.cluster = 0;
   p.warps = few;
-  p.wh = few;
-  while (heads % p.wh) p.wh /= 2;
-  if (heads * batch <= sms) {
-    int c = 1;
-    while (2 * c <= kMaxCluster && 2 * c * heads * batch <= sms && c < tiles_of(many * run)) c *= 2;
-    if (tiles_of(many * run) <= kClusterTiles * c) p.cluster = c, p.warps = many, p.wh = 1;
-  } else if (tiles_of(run) <= kDirectRuns) {
-    // A CTA per (head group, sequence): the fewest heads that still make one wave, or all
-    int w = 1;
-    while (w < p.wh && heads / w * batch > kPerSm * sms) w *= 2;
-    p.cluster = 1, p.wh = w;
+  p.wh = wide;
+  // clusters of c (not all SMs take part in those of 8: 15 of them on 152)
+  for (int c = 1; c <= kMaxCluster && c * pairs <= sms - (c > 1 ? 4 * c : 0); c *= 2) {
+    const double t = (c > 1 ? 5.2 : 4.1) + std::max(tiles_of(many * run * c) * step, bytes);
+    if (t < best) best = t, p.cluster = c, p.warps = many, p.wh = 1;
+  }
+  // a CTA of `few` warps for w heads of a sequence
+  for (int w = 1; w <= wide; w *= 2) {
+    const double waves = std::ceil((double)(pairs / w) / slots);
+    const double t = 4.0 * (1 + 0.5 * (waves - 1)) + std::max(waves * tiles_of(few / w * run) * step * 0.93, bytes);
+    if (t < best) best = t, p.cluster = 1, p.warps = few, p.wh = w;
   }
   p.wt = p.warps / p.wh;
   p.groups = heads / p.wh;
   p.tile = p.wt * run;
   p.by_tile = divider((uint32_t)p.tile);
-  p.n_items = (int)std::min<int64_t>(std::min(kPerSm * sms, kMaxItems), p.groups * batch * tiles_of(p.tile));
+  // CTAs of tiles dealt in ranges (whichever way this call takes: it sizes the workspace)
+  p.n_items = (int)std::min<int64_t>(std::min(slots, kMaxItems), pairs / wide * tiles_of(few / wide * run));
+  p.part_rows = wide * p.rows;
   return p;
 }
 
-size_t bytes_u(const Plan& p, int DP) { return align_up((size_t)2 * p.n_items * p.wh * p.rows * DP * sizeof(float), 256); }
-size_t bytes_ml(const Plan& p) { return align_up((size_t)2 * p.n_items * p.wh * p.rows * 2 * sizeof(float), 256); }
+size_t bytes_entries(const Plan& p) { return align_up(p.n_items * sizeof(Entry), 256); }
+size_t bytes_ml(const Plan& p) { return align_up((size_t)2 * p.n_items * p.part_rows * 2 * sizeof(float), 256); }
+size_t bytes_u(const Plan& p, int DP) { return align_up((size_t)2 * p.n_items * p.part_rows * DP * sizeof(float), 256); }
 
 }  // namespace
 }  // namespace paged
@@ -207,10 +226,8 @@ size_t bytes_ml(const Plan& p) { return align_up((size_t)2 * p.n_items * p.wh * 
 using namespace paged;
 
 size_t paged_decode_workspace(const PagedView& v, int dtype, int B, int max_len, int sms) {
-  // windows only make calls smaller: fewer CTAs, and clusters where the whole length has them
-  const Plan p = plan_of(v, dtype, std::max(B, 1), max_len, 0, sms);
-  if (p.cluster) return 0;
-  return align_up(p.n_items * sizeof(Entry), 256) + bytes_ml(p) + bytes_u(p, padded_dim(v.d));
+  const Plan p = plan_of(v, dtype, std::max(B, 1), max_len, 0, sms);  // a window only takes CTAs away
+  return bytes_entries(p) + bytes_ml(p) + bytes_u(p, padded_dim(v.d));
 }
 
 cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cudaStream_t s) {
@@ -218,9 +235,11 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cu
   g.a = a;
   g.p = plan_of(a.v, dtype, a.B, a.max_len, a.window, sms);
   g.DP = padded_dim(a.v.d);
+  const int el = dtype == DCK_F32 ? 4 : 2;
+  g.p.q_copied = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride * el % 16 == 0;
   char* ws = static_cast<char*>(a.ws);
   g.entries = reinterpret_cast<Entry*>(ws);
-  ws += align_up(g.p.n_items * sizeof(Entry), 256);
+  ws += bytes_entries(g.p);
   g.part_ml = reinterpret_cast<float*>(ws);
   g.part_u = reinterpret_cast<float*>(ws + bytes_ml(g.p));
   cudaError_t e = dtype == DCK_F32 ? launch_f32(g, s) : launch_bf16(g, s);

@@ -17,8 +17,6 @@ namespace paged {
 constexpr int kMaxLen = 1 << 29;     // tokens of a sequence
 constexpr int kUnitLimit = 1 << 30;  // tiles of one call, over all head groups
 constexpr int kMaxCluster = 8;
-constexpr int kClusterTiles = 4;  // tiles per CTA up to which clusters are taken
-constexpr int kDirectRuns = 16;   // runs of tokens up to which a CTA takes a sequence whole
 
 // How a call is laid over warps and CTAs.
 struct Plan {
@@ -28,8 +26,10 @@ struct Plan {
   int tile;          // tokens of a CTA's tile
   int cluster;       // 0: tiles dealt in ranges; else the CTAs per (head group, sequence): 1, or a cluster of them and wh = 1
   int warps;         // of a CTA
-  int n_items;       // CTAs (dealt in ranges)
+  int n_items;       // CTAs of tiles dealt in ranges
+  int part_rows;     // rows of partial sums that each of them has twice
   int alike;         // keys and values have the same strides
+  int q_copied;      // queries in whole aligned 16-byte chunks
   Divider by_chunks, by_tile;
 };
 
@@ -202,27 +202,41 @@ struct Sizes {
   static constexpr int kRing = NW * S * kStage;
 };
 
+// The queries of one head of a head group: `count` of them from query head `first` on.
+struct Queries {
+  int first, count;
+};
+__device__ __forceinline__ Queries queries_of(const Args& g, int group, int wh) {
+  const int vh = group * g.p.wh + wh, h = g.p.by_chunks.div(vh), r0 = (vh - h * g.p.chunks) * g.p.rows;
+  return {h * g.a.v.qpg + r0, min(g.p.rows, g.a.v.qpg - r0)};
+}
+
 // The page number and offset of a token of one warp's run of a tile: lane r holds token r.
 struct Pages {
   int page, off;  // off < 0: no token
-  int head;
+  int group;
+  int b;          // the sequence whose queries come with this tile, or -1
 };
 
-template <class Z>
+// ROWS: queries of a warp; they are copied along with the first tile of a (head group,
+// sequence), QS places for them per warp.
+template <class Z, int ROWS, int QS>
 struct Loader {
   static constexpr int el = sizeof(typename Z::T);
+  static constexpr int kPlace = ROWS * Z::kRow;
   const Args& g;
   const char *kc, *vc;    // with this lane's chunk
-  uint32_t ring, even, odd;  // this warp's stages; where this lane's chunk of rows 4 i + sub lies, i even or odd
+  uint32_t ring, places, even, odd;  // this warp's stages and places; where this lane's chunk of rows 4 i + sub lies, i even or odd
   int lane, run, wh;      // run: the warp's first token of a tile
   int have;               // chunks of a row from this lane's first on
 
-  __device__ __forceinline__ Loader(const Args& g, const uint8_t* raw, int warp, int lane, int wh, int wt)
+  __device__ __forceinline__ Loader(const Args& g, const uint8_t* raw, const void* q, int warp, int lane, int wh, int wt)
       : g(g), lane(lane), run(wt * Z::TOK), wh(wh) {
     const int sub = lane >> 3, c = lane & 7;
     kc = static_cast<const char*>(g.a.kc) + c * 16;
     vc = static_cast<const char*>(g.a.vc) + c * 16;
     ring = (uint32_t)__cvta_generic_to_shared(raw) + warp * Z::S * Z::kStage;
+    places = (uint32_t)__cvta_generic_to_shared(q) + warp * QS * kPlace;
     even = sub * Z::kRow + (c ^ sub) * 16;
     odd = sub * Z::kRow + (c ^ (sub + 4)) * 16;
     have = g.a.v.d * el / 16 - c;
@@ -241,27 +255,58 @@ struct Loader {
     for (int i = lane; i < Z::kStage / 16; i += 32) reinterpret_cast<uint4*>(stage)[i] = make_uint4(0, 0, 0, 0);
   }
 
-  __device__ __forceinline__ Pages fetch(const Walk& w) const {
+  __device__ __forceinline__ Pages fetch(const Walk& w, bool first) const {
     Pages r;
+    r.b = first ? w.b : -1;
+    r.group = w.group;
     const int t = w.token + run + lane;
     const bool have_it = lane < Z::TOK && t < w.len;
     const uint32_t col = g.a.v.by_page.div(have_it ? t : 0);
     r.off = have_it ? t - (int)col * g.a.v.page : -1;
     r.page = have_it ? g.a.table[w.b * g.a.table_stride + col] : 0;
-    r.head = g.p.by_chunks.div(w.group * g.p.wh + wh);
     return r;
+  }
+
+  // Starts the copy of the queries to place `at`: rows past them, and rows' ends, as zeros.
+  __device__ __forceinline__ void copy_queries(const Pages& r, int at) const {
+    const Queries qs = queries_of(g, r.group, wh);
+    const char* q = static_cast<const char*>(g.a.q) + ((int64_t)r.b * g.a.q_stride + (int64_t)qs.first * g.a.v.d) * el;
+    const int row_bytes = g.a.v.d * el;
+    const uint32_t to = places + at * kPlace;
+#pragma unroll
+    for (int i = 0; i < ROWS * Z::kChunks / 32 + (ROWS * Z::kChunks % 32 != 0); ++i) {
+      const int x = i * 32 + lane, row = x / Z::kChunks, c = x % Z::kChunks;
+      const bool have = row < qs.count && c * 16 < row_bytes;
+      if (ROWS * Z::kChunks % 32 == 0 || row < ROWS)
+        cp_async16_or_zero(to + row * Z::kRow + (c ^ (row & 7)) * 16, q + (have ? row * row_bytes + c * 16 : 0), have ? 16 : 0);
+    }
+  }
+  // The same by single elements, for queries off 16-byte boundaries.
+  __device__ __forceinline__ void read_queries(const Queries& qs, int b, uint8_t* q_all, int warp, int at) const {
+    using T = typename Z::T;
+    T* to = reinterpret_cast<T*>(q_all + (warp * QS + at) * kPlace);
+    const T* q = static_cast<const T*>(g.a.q) + (int64_t)b * g.a.q_stride + (int64_t)qs.first * g.a.v.d;
+    constexpr int per = 16 / el;
+    for (int x = lane; x < ROWS * Z::DP; x += 32) {
+      const int row = x / Z::DP, e = x % Z::DP;
+      to[row * Z::DP + ((e / per) ^ (row & 7)) * per + e % per] =
+          row < qs.count && e < g.a.v.d ? q[row * g.a.v.d + e] : from_f32<T>(0.f);
+    }
+    __syncwarp();
   }
 
   // Starts the copies of a stage; true if a page lies outside the pool (its tokens read as
   // zeros).  Eight lanes copy 128 bytes of a row, a warp four rows at a time.
   __device__ __forceinline__ bool issue(const Pages& r, int stage) const {
     const PagedView& v = g.a.v;
+    if (QS > 1 && r.b >= 0 && g.p.q_copied) copy_queries(r, stage);
+    const uint32_t head = g.p.by_chunks.div(r.group * g.p.wh + wh);
     const bool inside = (uint32_t)r.page < (uint32_t)v.n_pages, ok = inside && r.off >= 0;
     const uint32_t page = inside ? r.page : 0, off = max(r.off, 0);
-    const int64_t ko = (int64_t)((uint64_t)page * v.k_page_b + (uint64_t)off * v.k_tok_b + (uint64_t)(uint32_t)r.head * v.k_head_b);
+    const int64_t ko = (int64_t)((uint64_t)page * v.k_page_b + (uint64_t)off * v.k_tok_b + (uint64_t)head * v.k_head_b);
     int64_t vo = ko;
     if (!g.p.alike)
-      vo = (int64_t)((uint64_t)page * v.v_page_b + (uint64_t)off * v.v_tok_b + (uint64_t)(uint32_t)r.head * v.v_head_b);
+      vo = (int64_t)((uint64_t)page * v.v_page_b + (uint64_t)off * v.v_tok_b + (uint64_t)head * v.v_head_b);
     const uint32_t mask = __ballot_sync(~0u, ok), at = ring + stage * Z::kStage;
     const int sub = lane >> 3;
 #pragma unroll
@@ -282,15 +327,6 @@ struct Loader {
     return __any_sync(~0u, !inside);
   }
 };
-
-// The queries of one head of a head group: `count` of them from query head `first` on.
-struct Queries {
-  int first, count;
-};
-__device__ __forceinline__ Queries queries_of(const Args& g, int group, int wh) {
-  const int vh = group * g.p.wh + wh, h = g.p.by_chunks.div(vh), r0 = (vh - h * g.p.chunks) * g.p.rows;
-  return {h * g.a.v.qpg + r0, min(g.p.rows, g.a.v.qpg - r0)};
-}
 
 // tanh to 3e-7 of its value: below 1/2 an odd polynomial (least squares in x^2 on
 // tanh(x) / x, 6e-8), above it 1 - 2 / (e^2x + 1).
@@ -324,6 +360,12 @@ struct ScoreScale {
 // bf16: tensor cores (mma.sync m16n8k16, queries as rows)
 // ---------------------------------------------------------------------------
 
+__device__ __forceinline__ void ldmatrix4_plain(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
 // Matrices 16-byte chunks 2 k and 2 k + 1 of rows whose chunk 0 or 1 is at `at`: the swizzle
 // flips bits 4 to 6 of the address, whole 128-byte lines add.
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at, int k) {
@@ -365,23 +407,22 @@ struct TensorTile {
   float o[Z::DP / 8][4], m[kQ], l[kQ];
   uint32_t q[Z::DP / 16][2 * kQ];
 
-  __device__ __forceinline__ void begin(const Args& g, int b, const Queries& qs, int lane, float*) {
-    const int words = g.a.v.d / 8;  // runs of 8 elements in a row
+  // `place`: the queries in shared memory.
+  __device__ __forceinline__ void begin(uint32_t place, int lane, float*) {
+    const int row = PACK ? lane & 7 : lane & 15, c = PACK ? lane >> 3 : lane >> 4;
 #pragma unroll
-    for (int x = 0; x < kQ; ++x) {
-      const int r = lane / 4 + 8 * x;
-      const uint16_t* src = static_cast<const uint16_t*>(g.a.q) + b * g.a.q_stride +
-                            (int64_t)(qs.first + (r < qs.count ? r : 0)) * g.a.v.d + (lane & 3) * 2;
-      const int have = r < qs.count ? words : 0;
-      if ((reinterpret_cast<uintptr_t>(src) & 3) == 0) {
-#pragma unroll
-        for (int w = 0; w < Z::DP / 8; ++w)
-          q[w / 2][w % 2 * kQ + x] = w < have ? *reinterpret_cast<const uint32_t*>(src + 8 * w) : 0u;
+    for (int k = 0; k < Z::DP / 16; k += PACK ? 2 : 1) {
+      uint32_t r[4];
+      ldmatrix4_plain(r, place + row * Z::kRow + ((2 * k + c) ^ (row & 7)) * 16);
+      if (PACK) {
+        q[k][0] = r[0], q[k][1] = r[1], q[k + 1][0] = r[2], q[k + 1][1] = r[3];
       } else {
 #pragma unroll
-        for (int w = 0; w < Z::DP / 8; ++w)
-          q[w / 2][w % 2 * kQ + x] = w < have ? src[8 * w] | (uint32_t)src[8 * w + 1] << 16 : 0u;
+        for (int y = 0; y < 4; ++y) q[k][y % (2 * kQ)] = r[y];
       }
+    }
+#pragma unroll
+    for (int x = 0; x < kQ; ++x) {
       m[x] = -CUDART_INF_F;
       l[x] = 0.f;
     }
@@ -518,22 +559,22 @@ struct SimtTile {
   float4 o[ROWS][kOwn];
   float m[ROWS], l[ROWS];
 
-  // `mine`: this warp's shared memory, ROWS x DP queries, then 8 x ROWS weights.
-  __device__ __forceinline__ void begin(const Args& g, int b, const Queries& qs, int lane, float* mine) {
-    __syncwarp();
-    const float* src = static_cast<const float*>(g.a.q) + b * g.a.q_stride + (int64_t)qs.first * g.a.v.d;
-    float x[ROWS][Z::DP / 32];  // all loads before the first store
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-      for (int e = 0; e < Z::DP / 32; ++e) {
-        const bool have = r < qs.count && e * 32 + lane < g.a.v.d;
-        x[r][e] = have ? src[r * g.a.v.d + e * 32 + lane] : 0.f;
-      }
+  // `place`: the queries in shared memory, as long as it lasts; `mine`: this warp's, ROWS x DP
+  // queries for all of the sequence, then 8 x ROWS weights.
+  __device__ __forceinline__ void begin(uint32_t place, int lane, float* mine) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
-      for (int e = 0; e < Z::DP / 32; ++e) mine[r * Z::DP + e * 32 + lane] = x[r][e];
+      for (int k = 0; k < (Z::kChunks + 31) / 32; ++k) {
+        const int c = k * 32 + lane;
+        float4 v;
+        if (c < Z::kChunks) {
+          asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];"
+                       : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                       : "r"(place + r * Z::kRow + (c ^ (r & 7)) * 16));
+          *reinterpret_cast<float4*>(mine + r * Z::DP + 4 * c) = v;
+        }
+      }
       m[r] = -CUDART_INF_F;
       l[r] = 0.f;
 #pragma unroll
@@ -693,6 +734,9 @@ __device__ __forceinline__ void put4(__nv_bfloat16* p, float4 v, bool even) {
 
 template <class Z, class Tile, bool CLUSTER>
 struct Shared {  // after the rings
+  // places for queries: as many segments as tiles are copied ahead
+  static constexpr int kPlaces = CLUSTER ? 1 : Z::S;
+  alignas(16) uint8_t q[Z::NW * kPlaces * Tile::kRows * Z::kRow];
   float4 part[CLUSTER ? Tile::kRows * Z::DP / 4 : 1];  // of the cluster's CTAs, this one's share of the elements
   float2 cluster_ml[CLUSTER ? kMaxCluster : 1][Tile::kRows];
   alignas(16) float mine[std::is_same<typename Z::T, float>::value ? Z::NW * (Tile::kRows * Z::DP + 8 * Tile::kRows) : 4];
@@ -759,7 +803,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   Walk ahead;
   bool begins = true;  // the first (head group, sequence) is this CTA's from its first tile on
   uint32_t rank = 0;
-  const Loader<Z> load(g, raw, warp, lane, wh, wt);
+  const Loader<Z, Tile::kRows, Shm::kPlaces> load(g, raw, sh.q, warp, lane, wh, wt);
   load.clear(raw);
   if (CLUSTER) {
     cluster_arrive();  // remote stores must find the other CTAs running: waited for before the first
@@ -798,11 +842,16 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   Walk at = ahead;
   int to_compute = u1 - u0, to_copy = to_compute, to_fetch = to_compute;
   // page numbers are read two tiles ahead of the copies: a read takes longer than a tile's arithmetic
-  Pages pages = {0, -1, 0}, pages2 = {0, -1, 0};
+  Pages pages = {0, -1, 0, -1}, pages2 = {0, -1, 0, -1};
+  bool first = true;  // of its (head group, sequence), for this CTA
   const auto fetch_next = [&]() {
-    const Pages p = load.fetch(ahead);
+    const Pages p = load.fetch(ahead, first);
+    first = false;
     ahead.token += g.p.tile;
-    if (--to_fetch > 0 && --ahead.left == 0 && !CLUSTER) ahead.leave(a, batch);
+    if (--to_fetch > 0 && --ahead.left == 0 && !CLUSTER) {
+      ahead.leave(a, batch);
+      first = true;
+    }
     return p;
   };
   if (to_fetch > 0) pages = fetch_next();
@@ -820,26 +869,41 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     }
     cp_async_commit();
   };
-#pragma unroll 1
-  for (int i = 0; i < Z::S - 1; ++i) copy_next();
-
   ScoreScale scale;
   scale.scale2 = a.scale * 1.44269504088896f;
   scale.cap2 = a.softcap * 1.44269504088896f;
   scale.inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
   float* mine = sh.mine + warp * (Tile::kRows * Z::DP + 8 * Tile::kRows);
   Tile tile;
-  Queries qs = queries_of(g, at.group, wh);
-  tile.begin(g, at.b, qs, lane, mine);
+  Queries qs;
+  if (CLUSTER) {  // the queries by themselves, before the copies
+    qs = queries_of(g, at.group, wh);
+    if (g.p.q_copied) load.copy_queries({0, 0, at.group, at.b}, 0);
+    else load.read_queries(qs, at.b, sh.q, warp, 0);
+    cp_async_commit();
+  }
+#pragma unroll 1
+  for (int i = 0; i < Z::S - 1; ++i) copy_next();
 
   int get = 0, nth = 0;  // nth: this (head group, sequence) among the CTA's
-  bool bad = false;
+  bool bad = false, fresh = !CLUSTER;
+  if (CLUSTER) {
+    cp_async_wait<Z::S - 1>();
+    __syncwarp();
+    tile.begin(load.places, lane, mine);
+  }
   while (true) {
     if (!CLUSTER || to_compute > 0) {
       __syncwarp();  // the stage that is filled next has been read
       copy_next();
       cp_async_wait<Z::S - 1>();
       __syncwarp();
+      if (!CLUSTER && fresh) {
+        qs = queries_of(g, at.group, wh);
+        if (!g.p.q_copied) load.read_queries(qs, at.b, sh.q, warp, get);
+        tile.begin(load.places + get * load.kPlace, lane, mine);
+        fresh = false;
+      }
       bad |= outside >> get & 1;
       tile.step(load.ring + get * Z::kStage, at.len - at.token - load.run, lane, scale, mine);
     }
@@ -930,11 +994,9 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
       break;
     }
     bad = false;
-    begins = true;
+    begins = fresh = true;
     ++nth;
     at.leave(a, batch);
-    qs = queries_of(g, at.group, wh);
-    tile.begin(g, at.b, qs, lane, mine);
   }
   cp_async_wait<0>();
   if (!CLUSTER) return;

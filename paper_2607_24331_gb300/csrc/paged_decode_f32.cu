@@ -19,15 +19,15 @@ template <int DP, int S>
 cudaError_t by_rows(const Args& g, cudaStream_t s) {
   if (g.p.rows == 1) return launch_rows<DP, S, 1>(g, s);
   if (g.p.rows <= 4) return launch_rows<DP, S, 4>(g, s);
-  return launch_rows<DP, DP == 64 ? S : S - 1, 8>(g, s);  // the queries take the room of a stage
+  return launch_rows<DP, S, 8>(g, s);
 }
 
 }  // namespace
 
 cudaError_t launch_f32(const Args& g, cudaStream_t s) {
-  if (g.DP == 64) return by_rows<64, 6>(g, s);
-  if (g.DP == 128) return by_rows<128, 3>(g, s);
-  return by_rows<256, 3>(g, s);
+  if (g.DP == 64) return by_rows<64, 4>(g, s);
+  if (g.DP == 128) return by_rows<128, 2>(g, s);
+  return by_rows<256, 2>(g, s);
 }
 
 }  // namespace paged
