@@ -164,14 +164,15 @@ cudaError_t launch_join(const Args& g, int64_t most, cudaStream_t s) {
   return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
 }
 
-// Which of the three ways a call takes: the least of their times (us) by a model fitted to
-// 570 calls of six head layouts, 1 to 128 sequences of 16 to 4096 tokens, all alike or
-// ragged 16-fold; the choice is 1.6% off the best of the three on average.  Measured, ranges
-// / clusters / whole, 32 query heads on 8 KV heads of 128 in bf16:
-//   1 x 1024   9.0 /  6.3 / 15.5      16 x 512  13.7 /  8.2 / 10.9      64 x 256   21.2 / - / 15.7
-//   4 x 4096  18.8 / 17.4 / 63        16 x 4096 50.2 / 46.5 / 59        64 x 2048  90.2 / - / 84
-//   1 x 128    6.8 /  4.6 /  4.4      16 x 128..2048 17.3 / 15.6 / 22   64 x 128..2048  38.4 / - / 46
-// (1 x 16384 15 / 21 / 190).
+// Which of the three ways a call takes: the one of the least time by a model in us, fitted
+// to 650 measured calls (six head layouts, bf16 and fp32, 1 to 128 sequences of 16 to 4096
+// tokens, half of them ragged 16-fold); its choice is 1.4% off the best of the three on
+// average.  The host knows a bound on the lengths only, so a way is judged by the geometric
+// mean of its times for sequences of that length and for ragged ones, 0.34 of it on average.
+// Measured, ranges / clusters / whole, 32 query heads on 8 KV heads of 128 in bf16:
+//   1 x 128   6.9 /  4.6 /  4.4     16 x 512       13.6 /  8.4 / 10.5    64 x 256        21 / - / 15
+//   1 x 1024  9.1 /  6.4 / 14.6     16 x 4096      49.8 / 46.3 / 56      64 x 2048       87 / - / 83
+//   4 x 4096 18.6 / 17.4 / 58       16 x 128..2048 17.3 / 16.1 / 21      64 x 128..2048  37 / - / 44
 Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int sms) {
   Plan p;
   const int DP = padded_dim(v.d);
@@ -186,24 +187,27 @@ Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int 
   int wide = few;  // heads side by side in a CTA, at most
   while (heads % wide) wide /= 2;
 
-  const int row = DP * (dtype == DCK_BF16 ? 2 : 4);
-  const double step = row <= 128 ? 0.53 : row == 256 ? 0.68 : row == 512 ? 0.88 : 1.14;  // a warp's run of tokens
-  // the bytes at the copy bandwidth and 7% more, of sequences of 0.56 of the bound on average
-  const double bytes = 0.56 * 1.07 * 2. * B * span * v.Hkv * v.d * (dtype == DCK_BF16 ? 2 : 4) / 6.8e6;
-  const int slots = kPerSm * sms;
-  double best = 7.5 + bytes + 0.45 * std::max(0., (double)pairs / wide / slots - 1) - (span <= few / wide * run ? 2.7 : 0);
+  const int row = DP * (dtype == DCK_BF16 ? 2 : 4), slots = kPerSm * sms;
+  const double step = row <= 128 ? 0.45 : row == 256 ? 0.65 : row == 512 ? 0.95 : 1.37;  // a warp's run of tokens
+  const double bytes = 1.07 * 2. * B * span * v.Hkv * v.d * (dtype == DCK_BF16 ? 2 : 4) / 6.8e6;
+  // (product of the two times) of a way with a fixed part and the longest CTA's part
+  const auto times = [&](double fixed, double longest) {
+    return (fixed + std::max(longest, bytes)) * (fixed + std::max(longest, 0.34 * bytes));
+  };
+  double best = times((dtype == DCK_BF16 ? 7.5 : 12.7) + 0.45 * std::max(0., (double)pairs / wide / slots - 1) -
+                          (span <= few / wide * run ? 2.8 : 0), 0);
   p.cluster = 0;
   p.warps = few;
   p.wh = wide;
   // clusters of c (not all SMs take part in those of 8: 15 of them on 152)
   for (int c = 1; c <= kMaxCluster && c * pairs <= sms - (c > 1 ? 4 * c : 0); c *= 2) {
-    const double t = (c > 1 ? 5.2 : 4.1) + std::max(tiles_of(many * run * c) * step, bytes);
+    const double t = times(c > 1 ? 5.4 : 4.3, tiles_of(many * run * c) * step);
     if (t < best) best = t, p.cluster = c, p.warps = many, p.wh = 1;
   }
   // a CTA of `few` warps for w heads of a sequence
   for (int w = 1; w <= wide; w *= 2) {
     const double waves = std::ceil((double)(pairs / w) / slots);
-    const double t = 4.0 * (1 + 0.5 * (waves - 1)) + std::max(waves * tiles_of(few / w * run) * step * 0.93, bytes);
+    const double t = times(4.1 * (1 + 0.43 * (waves - 1)), waves * tiles_of(few / w * run) * step * 0.89);
     if (t < best) best = t, p.cluster = 1, p.warps = few, p.wh = w;
   }
   p.wt = p.warps / p.wh;
