@@ -34,10 +34,10 @@ namespace paged {
 namespace {
 
 // Joins the partial sums of what several CTAs share: per (entry, row) weights first,
-// then 16-byte loads of the partials, several in flight.  Few entries of many partials
-// (LIST): blocks of 256 threads list the entries that are any and take their rows in turn.
-// Many entries of few partials: a block of 64 threads per CTA's entry and row, whether
-// there is one or not.
+// then 16-byte loads of the partials, several in flight.  Few entries of many partials:
+// blocks of 256 threads list the entries that are any and take their rows in turn.
+constexpr int kJoinThreads = 256;
+
 template <typename T>
 __device__ __forceinline__ void put_joined(const Args& g, int64_t out_row, int e, float4 sum, float m, float l, bool bad) {
   const bool none = bad || l == 0.f;
@@ -48,9 +48,9 @@ __device__ __forceinline__ void put_joined(const Args& g, int64_t out_row, int e
   if (g.a.lse && e == 0) g.a.lse[out_row] = none ? -CUDART_INF_F : (m + log2f(l)) * 0.693147180559945f;
 }
 
-template <typename T, int THREADS, bool LIST>
-__global__ void __launch_bounds__(THREADS, LIST ? 2 : 16) join_kernel(const __grid_constant__ Args g, const Divider by_per, const Divider by_rows) {
-  constexpr int kBatch = LIST ? 8 : 4;  // loads in flight per thread
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_constant__ Args g, const Divider by_per, const Divider by_rows) {
+  constexpr int THREADS = kJoinThreads, kBatch = 8;  // kBatch: loads in flight per thread
   __shared__ float2 warp_ml[THREADS / 32];
   __shared__ float weight[THREADS];
   __shared__ int any_bad;
@@ -60,31 +60,27 @@ __global__ void __launch_bounds__(THREADS, LIST ? 2 : 16) join_kernel(const __gr
   pdl_launch_dependents();
   pdl_wait();
   // the entries that are any, in the order of CTAs
-  __shared__ uint16_t shared_by[LIST ? kMaxItems : 1];
+  __shared__ uint16_t shared_by[kMaxItems];
   __shared__ int counts[THREADS / 32];
-  int n_rows = g.p.n_items * per;
-  if (LIST) {
-    int n_entries = 0;
-    for (int c0 = 0; c0 < g.p.n_items; c0 += THREADS) {
-      const int c = c0 + tid;
-      const uint32_t any = __ballot_sync(~0u, c < g.p.n_items && g.entries[c].last >= 0);
-      if (lane == 0) counts[warp] = __popc(any);
-      __syncthreads();
-      int before = n_entries;
+  int n_entries = 0;
+  for (int i0 = 0; i0 < g.p.n_items; i0 += THREADS) {
+    const int c = i0 + tid;
+    const uint32_t any = __ballot_sync(~0u, c < g.p.n_items && g.entries[c].last >= 0);
+    if (lane == 0) counts[warp] = __popc(any);
+    __syncthreads();
+    int before = n_entries;
 #pragma unroll
-      for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < warp) before += counts[w];
-        n_entries += counts[w];
-      }
-      if (any >> lane & 1) shared_by[before + __popc(any & ((1u << lane) - 1))] = (uint16_t)c;
-      __syncthreads();
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) before += counts[w];
+      n_entries += counts[w];
     }
-    n_rows = n_entries * per;
+    if (any >> lane & 1) shared_by[before + __popc(any & ((1u << lane) - 1))] = (uint16_t)c;
+    __syncthreads();
   }
+  const int n_rows = n_entries * per;
   for (int x = blockIdx.x; x < n_rows; x += gridDim.x) {
-    const int nth = by_per.div(x), c0 = LIST ? shared_by[nth] : nth, hr = x - nth * per, h = by_rows.div(hr), r = hr - h * g.p.rows;
+    const int nth = by_per.div(x), c0 = shared_by[nth], hr = x - nth * per, h = by_rows.div(hr), r = hr - h * g.p.rows;
     const Entry e = g.entries[c0];
-    if (!LIST && e.last < 0) continue;
     const Queries qs = queries_of(g, e.group, h);
     if (r >= qs.count) continue;
     const int64_t out_row = (int64_t)e.b * g.a.v.Hq + qs.first + r;
@@ -156,11 +152,83 @@ __global__ void __launch_bounds__(THREADS, LIST ? 2 : 16) join_kernel(const __gr
   }
 }
 
-template <typename T, int THREADS, bool LIST>
-cudaError_t launch_join(const Args& g, int64_t most, cudaStream_t s) {
-  const int per = g.p.wh * g.p.rows;
-  const int grid = (int)std::min<int64_t>((int64_t)g.p.n_items * per, most);
-  cudaError_t e = launch_pdl(join_kernel<T, THREADS, LIST>, grid, THREADS, 0, s, g, divider(per), divider(g.p.rows));
+// Many entries of few partials: a warp per CTA's entry and row, whether there is one or
+// not, two warps a block, so that all are on the GPU at once.
+constexpr int kFewThreads = 64;
+
+template <typename T>
+__global__ void __launch_bounds__(kFewThreads, 16) join_few_kernel(const __grid_constant__ Args g, const Divider by_per, const Divider by_rows) {
+  constexpr int kBatch = 4;
+  const int lane = threadIdx.x & 31, d = g.a.v.d, per = g.p.wh * g.p.rows;
+  const int x = (blockIdx.x * kFewThreads + threadIdx.x) / 32;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (x >= g.p.n_items * per) return;
+  const int c0 = by_per.div(x), hr = x - c0 * per, h = by_rows.div(hr), r = hr - h * g.p.rows;
+  const Entry e = g.entries[c0];
+  if (e.last < 0) return;
+  const Queries qs = queries_of(g, e.group, h);
+  if (r >= qs.count) return;
+  const int64_t out_row = (int64_t)e.b * g.a.v.Hq + qs.first + r;
+  const int parts = e.last - c0 + 1, stride = 2 * per, row0 = (2 * c0 * g.p.wh + h) * g.p.rows + r;
+  const auto row = [&](int i) { return (int64_t)(row0 + i * stride + (i == 0 && e.second ? per : 0)); };
+  const int quads = min(g.DP / 4, 32), lanes = 32 / quads, turn = lane / quads;
+  for (int q0 = 0; q0 < g.DP / 4; q0 += quads) {  // once, but twice for heads above 128
+    const int el = 4 * (q0 + lane % quads);
+    float M = -CUDART_INF_F, total = 0.f;
+    bool bad = false;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < parts; i0 += 32) {
+      const int count = min(32, parts - i0);
+      float4 v[kBatch];
+      const auto fetch = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+          if (i + k * lanes < count && el < d)
+            v[k] = *reinterpret_cast<const float4*>(g.part_u + row(i0 + i + k * lanes) * g.DP + el);
+      };
+      float2 ml = make_float2(-CUDART_INF_F, 0.f);
+      if (lane < count) ml = *reinterpret_cast<const float2*>(g.part_ml + 2 * row(i0 + lane));
+      fetch(turn);
+      float top = fmaxf(M, ml.x);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+      const float base = top == -CUDART_INF_F ? 0.f : top, w = exp2_approx(ml.x - base), before = exp2_approx(M - base);
+      float l = ml.y * w;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+      bad |= __any_sync(~0u, ml.y < 0.f) != 0;
+      total = total * before + l;
+      sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
+      M = top;
+      for (int i = 0; i < count; i += kBatch * lanes) {
+        if (i) fetch(i + turn);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          const int p = i + turn + k * lanes;
+          const float c = __shfl_sync(~0u, w, p & 31);
+          if (p < count && el < d && c != 0.f) sum.x += v[k].x * c, sum.y += v[k].y * c, sum.z += v[k].z * c, sum.w += v[k].w * c;
+        }
+      }
+    }
+    for (int k = quads; k < 32; k <<= 1) {  // the lanes that share a quad of elements
+      sum.x += __shfl_xor_sync(~0u, sum.x, k);
+      sum.y += __shfl_xor_sync(~0u, sum.y, k);
+      sum.z += __shfl_xor_sync(~0u, sum.z, k);
+      sum.w += __shfl_xor_sync(~0u, sum.w, k);
+    }
+    if (turn == 0 && el < d) put_joined<T>(g, out_row, el, sum, M, total, bad);
+  }
+}
+
+template <typename T>
+cudaError_t launch_join(const Args& g, int sms, cudaStream_t s) {
+  const int per = g.p.wh * g.p.rows, rows = g.p.n_items * per;
+  // partials per entry, on average, where all sequences are alike: 16 or more
+  cudaError_t e = (int64_t)g.p.groups * g.a.B * 16 <= g.p.n_items
+                      ? launch_pdl(join_kernel<T>, std::min(rows, 4 * sms), kJoinThreads, 0, s, g, divider(per), divider(g.p.rows))
+                      : launch_pdl(join_few_kernel<T>, (rows * 32 + kFewThreads - 1) / kFewThreads, kFewThreads, 0, s, g,
+                                   divider(per), divider(g.p.rows));
   return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
 }
 
@@ -250,11 +318,7 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cu
   if (e != cudaSuccess || g.p.cluster) return e;
   // one tile per (head group, sequence) at most: nothing is shared
   if ((a.window > 0 ? std::min(a.window, a.max_len) : a.max_len) <= g.p.tile) return cudaSuccess;
-  // partials per entry, on average, where all sequences are alike: 16 or more
-  using bf16 = __nv_bfloat16;
-  if ((int64_t)g.p.groups * a.B * 16 <= g.p.n_items)
-    return dtype == DCK_F32 ? launch_join<float, 256, true>(g, 4 * sms, s) : launch_join<bf16, 256, true>(g, 4 * sms, s);
-  return dtype == DCK_F32 ? launch_join<float, 64, false>(g, 1 << 30, s) : launch_join<bf16, 64, false>(g, 1 << 30, s);
+  return dtype == DCK_F32 ? launch_join<float>(g, sms, s) : launch_join<__nv_bfloat16>(g, sms, s);
 }
 
 }  // namespace dck
