@@ -28,8 +28,7 @@ inline Divider divider(uint32_t d) {
 // One layer's paged caches, by value.
 struct PagedView {
   int32_t Hq, Hkv, d, qpg, page, n_pages;
-  int64_t k_page, k_tok, k_head, v_page, v_tok, v_head;  // strides, in elements
-  uint32_t k_page_b, k_tok_b, k_head_b, v_page_b, v_tok_b, v_head_b;  // the same in bytes
+  uint32_t k_page_b, k_tok_b, k_head_b, v_page_b, v_tok_b, v_head_b;  // strides, in bytes
   Divider by_page;
 };
 

@@ -40,19 +40,13 @@ PagedView make_view(const dck_paged_desc* p) {
   v.qpg = p->n_q_heads / p->n_kv_heads;
   v.page = p->page_size;
   v.n_pages = p->n_pages;
-  v.k_page = p->k_page_stride;
-  v.k_tok = p->k_token_stride;
-  v.k_head = p->k_head_stride;
-  v.v_page = p->v_page_stride;
-  v.v_tok = p->v_token_stride;
-  v.v_head = p->v_head_stride;
   const uint32_t el = (uint32_t)element(p->dtype);
-  v.k_page_b = (uint32_t)v.k_page * el;
-  v.k_tok_b = (uint32_t)v.k_tok * el;
-  v.k_head_b = (uint32_t)v.k_head * el;
-  v.v_page_b = (uint32_t)v.v_page * el;
-  v.v_tok_b = (uint32_t)v.v_tok * el;
-  v.v_head_b = (uint32_t)v.v_head * el;
+  v.k_page_b = (uint32_t)p->k_page_stride * el;
+  v.k_tok_b = (uint32_t)p->k_token_stride * el;
+  v.k_head_b = (uint32_t)p->k_head_stride * el;
+  v.v_page_b = (uint32_t)p->v_page_stride * el;
+  v.v_tok_b = (uint32_t)p->v_token_stride * el;
+  v.v_head_b = (uint32_t)p->v_head_stride * el;
   v.by_page = divider((uint32_t)p->page_size);
   return v;
 }

@@ -24,7 +24,7 @@ struct Plan {
   int wh, wt;        // warps of a CTA: wh heads (a power of two) x wt runs of tokens
   int groups;        // head groups: Hkv * chunks / wh
   int tile;          // tokens of a CTA's tile
-  int cluster;       // 0: tiles dealt in ranges; else the CTAs per (head group, sequence): 1, or a cluster of them and wh = 1
+  int cluster;       // 0: tiles dealt in ranges; else CTAs per (head group, sequence), where more than 1 a cluster
   int warps;         // of a CTA
   int n_items;       // CTAs of tiles dealt in ranges
   int part_rows;     // rows of partial sums that each of them has twice
@@ -78,7 +78,8 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // Exclusive prefix sums of the sequences' tile counts in shared memory
 // prefix[0..B], and their lengths (len may be null).  Called by the whole block.
 template <int NW>
-__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, const Divider& by_tile, int groups, int* prefix, int* len, bool report) {
+__device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, const Divider& by_tile, int groups, int* prefix,
+                                           int* len, bool report) {
   const int64_t limit = kUnitLimit / groups;
   __shared__ int64_t scratch[NW];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -138,7 +139,8 @@ __device__ __forceinline__ int tile_prefix(const PagedDecodeArgs& a, const Divid
 // CTA c of n has tiles [begin(c), begin(c + 1)) of `units`, begin(c) = floor(c units / n).
 struct Ranges {
   int units, n, each, rest;
-  __device__ __forceinline__ Ranges(int units, int n) : units(units), n(n), each(n ? units / n : 0), rest(units - each * n) {}
+  __device__ __forceinline__ Ranges(int units, int n)
+      : units(units), n(n), each(n ? units / n : 0), rest(units - each * n) {}
   __device__ __forceinline__ int begin(int c) const { return c * each + c * rest / n; }
   __device__ __forceinline__ int item_of(int u) const { return (int)(((int64_t)(u + 1) * n + units - 1) / units) - 1; }
 };
@@ -226,7 +228,8 @@ struct Loader {
   static constexpr int kPlace = ROWS * Z::kRow;
   const Args& g;
   const char *kc, *vc;    // with this lane's chunk
-  uint32_t ring, places, even, odd;  // this warp's stages and places; where this lane's chunk of rows 4 i + sub lies, i even or odd
+  uint32_t ring, places;     // this warp's stages and places
+  uint32_t even, odd;        // where this lane's chunk of rows 4 i + sub lies in a stage, i even or odd
   int lane, run, wh;      // run: the warp's first token of a tile
   int have;               // chunks of a row from this lane's first on
 
@@ -278,7 +281,8 @@ struct Loader {
       const int x = i * 32 + lane, row = x / Z::kChunks, c = x % Z::kChunks;
       const bool have = row < qs.count && c * 16 < row_bytes;
       if (ROWS * Z::kChunks % 32 == 0 || row < ROWS)
-        cp_async16_or_zero(to + row * Z::kRow + (c ^ (row & 7)) * 16, q + (have ? row * row_bytes + c * 16 : 0), have ? 16 : 0);
+        cp_async16_or_zero(to + row * Z::kRow + (c ^ (row & 7)) * 16, q + (have ? row * row_bytes + c * 16 : 0),
+                           have ? 16 : 0);
     }
   }
   // The same by single elements, for queries off 16-byte boundaries.
@@ -397,7 +401,9 @@ __device__ __forceinline__ void split_weights(float p0, float p1, uint32_t& hi, 
   lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
-// One warp's tile of queries and its running sums.  PACK: up to 8 queries, rows 0-7
+// One warp's tile of queries and its running sums, 16 tokens a step: keys and values are read
+// from shared memory once, straight into MMA operands, whatever the number of queries; at 1.1
+// to 1.4 us per step of an SM's eight warps HBM is the slower (0.65 us alone).  PACK: up to 8 queries, rows 0-7
 // of the tile; the value product's rows 8-15 take the low halves of the weights, so
 // that two-term weights cost no further MMA.  Otherwise up to 16 queries and two MMAs.
 template <class Z, bool PACK>
@@ -549,8 +555,10 @@ struct TensorTile {
 // fp32: CUDA cores
 // ---------------------------------------------------------------------------
 
-// Up to ROWS queries, 8 tokens a stage.  Scores: lane = (token, quarter of the
-// chunks), the queries from shared memory; values: a lane owns chunks of the output.
+// Up to ROWS queries, 8 tokens a stage (products on tensor cores would round to 10 bits).
+// Scores: lane = (token, quarter of the chunks), the queries from shared memory; values: a
+// lane owns chunks of the output.  HBM bounds it up to four queries: 16 x 4096 tokens of 32
+// query heads on 8 KV heads, 537 MB, 86 us.
 template <class Z, int ROWS>
 struct SimtTile {
   static constexpr int kRows = ROWS;
@@ -778,14 +786,16 @@ __device__ __forceinline__ Joined join_rows(int n, float (&weight)[MOST], F ml_o
 }
 
 template <class Z, class Tile, bool CLUSTER>
-__global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1 : kPerSm) paged_decode_kernel(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1 : kPerSm)
+    paged_decode_kernel(const __grid_constant__ Args g) {
   using T = typename Z::T;
   extern __shared__ __align__(128) uint8_t raw[];
   using Shm = Shared<Z, Tile, CLUSTER>;
   Shm& sh = *reinterpret_cast<Shm*>(raw + Z::kRing);
   const PagedDecodeArgs& a = g.a;
   static_assert(Z::kRing % 16 == 0 && offsetof(Shm, mine) % 16 == 0 && sizeof(Shm) % 16 == 0, "16-byte accesses");
-  static_assert((Tile::kRows * Z::DP + 8 * Tile::kRows) % 4 == 0 && Z::kStage >= Tile::kRows * Z::DP * 4, "a warp's queries, its sums in a stage");
+  static_assert((Tile::kRows * Z::DP + 8 * Tile::kRows) % 4 == 0 && Z::kStage >= Tile::kRows * Z::DP * 4,
+                "a warp's queries, its sums in a stage");
   Batch batch;
   batch.prefix = reinterpret_cast<int*>(raw + Z::kRing + sizeof(sh));
   batch.len = a.B <= kKeptLens ? batch.prefix + a.B + 1 : nullptr;
@@ -969,7 +979,8 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
             sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
           }
         if (CLUSTER && g.p.cluster > 1) {
-          store_remote(remote(&sh.part[i / g.p.cluster + rank * (Tile::kRows * Z::DP / 4 / g.p.cluster)], i % g.p.cluster), sum);
+          const int at_rank = rank * (Tile::kRows * Z::DP / 4 / g.p.cluster);
+          store_remote(remote(&sh.part[i / g.p.cluster + at_rank], i % g.p.cluster), sum);
           if (e == 0)
             for (int c = 0; c < g.p.cluster; ++c)
               store_remote(remote(&sh.cluster_ml[rank][r], c), make_float2(j.m, j.bad ? -1.f : j.l));
@@ -1022,8 +1033,8 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
       }
     const int64_t row = (int64_t)at.b * a.v.Hq + qs.first + r;
     const float f = j.bad || j.l == 0.f ? 0.f : 1.f / j.l;
-    put4(out + row * d + e, f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f),
-         even);
+    put4(out + row * d + e,
+         f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f), even);
     if (e == 0 && a.lse) a.lse[row] = j.bad || j.l == 0.f ? -CUDART_INF_F : (j.m + log2f(j.l)) * 0.693147180559945f;
   }
 }
@@ -1040,7 +1051,8 @@ cudaError_t launch_kernel(const Args& g, cudaStream_t s) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(shared_bytes<Z, Tile, CLUSTER>(kMaxBatch), shared_bytes<Z, Tile, CLUSTER>(kKeptLens)));
+    const size_t most = std::max(shared_bytes<Z, Tile, CLUSTER>(kMaxBatch), shared_bytes<Z, Tile, CLUSTER>(kKeptLens));
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
     if (e != cudaSuccess) return e;
     if (dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
   }
