@@ -219,9 +219,9 @@ cudaError_t launch(const RopeLaunch& a, int sms, cudaStream_t s) {
   if (!vec_plan<T>(a, sms, &v)) {
     return launch_pdl(rope_any_kernel<T>, a.n_tok, kThreads, 0, s, a);
   }
-  const int grid = (a.n_tok + v.tokens - 1) / v.tokens;
+  const int64_t grid = ((int64_t)a.n_tok + v.tokens - 1) / v.tokens;
   const size_t smem = (size_t)v.tokens * (a.rope.rot / 2 * sizeof(float2) + sizeof(CacheRow));
-  return launch_pdl(a.rope.layout == DCK_ROPE_HALF ? rope_vec_kernel<T, true> : rope_vec_kernel<T, false>, grid, kThreads,
+  return launch_pdl(a.rope.layout == DCK_ROPE_HALF ? rope_vec_kernel<T, true> : rope_vec_kernel<T, false>, (unsigned)grid, kThreads,
                     smem, s, a, v);
 }
 

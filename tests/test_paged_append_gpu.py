@@ -201,3 +201,18 @@ def test_queries_in_place_and_offsets_beyond_32_bits():
                                    kc, vc), "dck_paged_append")
     assert dck.dck_last_device_error() == dck.DCK_OK
     _near(q, *_expected(ref, [7, 90000], s), "bf16")
+
+
+def test_as_many_tokens_as_an_int32_counts():
+    n, d = (1 << 31) - 1, 8
+    kc, vc = cache_pair("rows", 2, 4, 1, d, "bf16", fill=3.0)
+    k, v = (torch.full((1, 1, d), x, dtype=torch.bfloat16, device="cuda") for x in (1.0, 2.0))
+    slots = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    slots[0], slots[n // 2], slots[n - 1] = 1, 6, 4
+    dck.check(dck.dck_paged_append(dck.PagedCache.from_tensors(kc, vc, 1), None, None, 0, k, 0, v, 0, n, None, slots, None,
+                                   kc, vc), "dck_paged_append")
+    assert dck.dck_last_device_error() == dck.DCK_OK
+    for c, x in ((kc, 1.0), (vc, 2.0)):
+        want = torch.full((8, d), 3.0)
+        want[[1, 4, 6]] = x
+        assert torch.equal(c.reshape(8, d).float().cpu(), want)
