@@ -324,7 +324,8 @@ dck_status dck_validate_paged_desc(const dck_paged_desc* desc);
  * negative length, one beyond the table, a free count outside [0, n_pages], more
  * pages given back than the list can hold, a page number outside the pool or more
  * new tokens than n_tok are recorded as a device error (DCK_ERR_INVALID from
- * dck_last_device_error); the request concerned is refused (a length below 0 counts as 0), its slots are -1.
+ * dck_last_device_error); the request concerned is refused (an old length that is
+ * negative or beyond the table counts as 0), its slots are -1.
  * Deterministic; one launch; no workspace.
  */
 dck_status dck_page_update(int32_t batch, int32_t page_size, int32_t n_pages, const int32_t* d_old_len,
