@@ -555,91 +555,137 @@ struct TensorTile {
 // fp32: CUDA cores
 // ---------------------------------------------------------------------------
 
-// Up to ROWS queries, 8 tokens a stage (products on tensor cores would round to 10 bits).
-// Scores: lane = (token, quarter of the chunks), the queries from shared memory; values: a
-// lane owns chunks of the output.  HBM bounds it up to four queries: 16 x 4096 tokens of 32
-// query heads on 8 KV heads, 537 MB, 86 us.
+// Up to ROWS queries, 8 tokens a stage (products on tensor cores would round to 10 bits).  A
+// lane owns chunks of four elements, of the queries and the output in registers and of each key
+// and value it reads once; a token's products with all queries are summed up over the lanes by
+// exchanging halves (5 steps for all tokens and rows), so that lane 4 t + j ends with token t and
+// the rows of row_of.  HBM bounds it up to four queries: 64 x 4096 tokens of 32 query heads on 8
+// KV heads, 2.1 GB, 309 us.  With 16 queries on one KV head (268 MB there) 91 us, bound by the
+// length of a step with eight warps on an SM; with queries in shared memory, read by eight lanes
+// a token (no exchanges, but eight times the loads), 128.
 template <class Z, int ROWS>
 struct SimtTile {
   static constexpr int kRows = ROWS;
   static constexpr int kOwn = Z::kChunks >= 32 ? Z::kChunks / 32 : 1;  // chunks per lane
   static constexpr int kSplit = Z::kChunks >= 32 ? 1 : 32 / Z::kChunks;  // lanes that share a chunk, by tokens
-  float4 o[ROWS][kOwn];
-  float m[ROWS], l[ROWS];
+  static constexpr int kVals = ROWS > 4 ? ROWS / 4 : 1;                  // scores per lane
+  static_assert(Z::TOK == 8 && kSplit <= 2 && (ROWS & (ROWS - 1)) == 0 && ROWS <= 8, "lanes by tokens and rows");
+  float4 q[ROWS][kOwn], o[ROWS][kOwn];
+  float near[kVals], sum[kVals];  // this lane's reference maxima and sums
+  float m[ROWS], l[ROWS];         // all of them, after finish
 
-  // `place`: the queries in shared memory, as long as it lasts; `mine`: this warp's, ROWS x DP
-  // queries for all of the sequence, then 8 x ROWS weights.
-  __device__ __forceinline__ void begin(uint32_t place, int lane, float* mine) {
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-      for (int k = 0; k < (Z::kChunks + 31) / 32; ++k) {
-        const int c = k * 32 + lane;
-        float4 v;
-        if (c < Z::kChunks) {
-          asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];"
-                       : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                       : "r"(place + r * Z::kRow + (c ^ (r & 7)) * 16));
-          *reinterpret_cast<float4*>(mine + r * Z::DP + 4 * c) = v;
-        }
-      }
-      m[r] = -CUDART_INF_F;
-      l[r] = 0.f;
-#pragma unroll
-      for (int k = 0; k < kOwn; ++k) o[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    __syncwarp();
+  static __device__ __forceinline__ int row_of(int i, int lane) { return (lane & 3) * ROWS / 4 + i; }
+  static __device__ __forceinline__ int chunk_of(int k, int lane) { return (kSplit > 1 ? lane % Z::kChunks : lane) + 32 * k; }
+  static __device__ __forceinline__ float4 chunk(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+    return v;
+  }
+  // x of row r from the lane that has it to all
+  static __device__ __forceinline__ float of_row(const float (&x)[kVals], int r) {
+    return __shfl_sync(~0u, x[r % kVals], r * 4 / ROWS);
   }
 
-  __device__ __forceinline__ void step(uint32_t keys, int live, int lane, const ScoreScale& scale, float* mine) {
-    if (live <= 0) return;
-    const auto chunk = [](uint32_t at) {
-      float4 v;
-      asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
-      return v;
-    };
-    const int t = lane & 7, quarter = lane >> 3;
-    float s[ROWS] = {};
+  // `place`: the queries in shared memory, as long as it lasts.
+  __device__ __forceinline__ void begin(uint32_t place, int lane, float*) {
 #pragma unroll
-    for (int k = 0; k < Z::kChunks / 4; ++k) {
-      const int c = 4 * k + quarter;
-      const float4 x = chunk(keys + t * Z::kRow + ((c ^ t) * 16));
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        q[r][k] = chunk(place + r * Z::kRow + (chunk_of(k, lane) ^ (r & 7)) * 16);
+        o[r][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) near[i] = -CUDART_INF_F, sum[i] = 0.f;
+  }
+
+  // This lane's share of the products of a token with all queries.
+  __device__ __forceinline__ void products(uint32_t keys, int tok, int lane, float (&s)[ROWS]) const {
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const float4 x = chunk(keys + tok * Z::kRow + (chunk_of(k, lane) ^ tok) * 16);
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        const float4 y = *reinterpret_cast<const float4*>(mine + r * Z::DP + 4 * c);
-        s[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[r]))));
+        const float4 y = q[r][k];
+        const float rest = fmaf(x.y, y.y, fmaf(x.z, y.z, x.w * y.w));
+        s[r] = k ? s[r] + fmaf(x.x, y.x, rest) : fmaf(x.x, y.x, rest);
       }
     }
-    float* weights = mine + ROWS * Z::DP;
+  }
+  // Sums over the lanes that differ in bit O, of the lower half of s where it is clear, else the upper.
+  template <int N, int O>
+  static __device__ __forceinline__ void halve(float (&s)[4 * ROWS], int lane) {
+    const bool up = lane & O;
+    if (N == 1) {
+      s[0] += __shfl_xor_sync(~0u, s[0], O);
+    } else {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) s[r] += __shfl_xor_sync(~0u, s[r], 8);
+      for (int i = 0; i < N / 2; ++i) {
+        const float give = up ? s[i] : s[i + N / 2], keep = up ? s[i + N / 2] : s[i];
+        s[i] = keep + __shfl_xor_sync(~0u, give, O);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void step(uint32_t keys, int live, int lane, const ScoreScale& scale, float* weights) {
+    if (live <= 0) return;
+    const int t = lane >> 2;
+    float s[4 * ROWS];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) s[r] += __shfl_xor_sync(~0u, s[r], 16);
-    scale.apply(s);
+    for (int i = 0; i < 4; ++i) {
+      float x[ROWS];
+      if (kSplit > 1) {
+        products(keys, i + (lane >> 4) * 4, lane, x);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) s[i * ROWS + r] = x[r];
+      } else {
+        float y[ROWS];
+        products(keys, i, lane, x);
+        products(keys, i + 4, lane, y);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          const float give = lane & 16 ? x[r] : y[r], keep = lane & 16 ? y[r] : x[r];
+          s[i * ROWS + r] = keep + __shfl_xor_sync(~0u, give, 16);
+        }
+      }
+    }
+    halve<4 * ROWS, 8>(s, lane);
+    halve<2 * ROWS, 4>(s, lane);
+    halve<ROWS, 2>(s, lane);
+    halve<(ROWS > 1 ? ROWS / 2 : 1), 1>(s, lane);
+    float v[kVals];
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) v[i] = s[i];
+    scale.apply(v);
     bool raise = false;  // as in TensorTile
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      if (t >= live) s[r] = -CUDART_INF_F;
-      raise |= s[r] > m[r] + kHeadroom;
+    for (int i = 0; i < kVals; ++i) {
+      if (t >= live) v[i] = -CUDART_INF_F;
+      raise |= v[i] > near[i] + kHeadroom;
     }
     if (__any_sync(~0u, raise)) {
+      float c[kVals];
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        float top = fmaxf(near[i], v[i]);
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+        c[i] = near[i] == top ? 1.f : exp2_approx(near[i] - top);
+        near[i] = top;
+        sum[i] *= c[i];
+      }
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
-        float top = fmaxf(m[r], s[r]);
+        const float cr = of_row(c, r);
 #pragma unroll
-        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
-        const float c = m[r] == top ? 1.f : exp2_approx(m[r] - top);
-        m[r] = top;
-        l[r] *= c;
-#pragma unroll
-        for (int k = 0; k < kOwn; ++k) o[r][k].x *= c, o[r][k].y *= c, o[r][k].z *= c, o[r][k].w *= c;
+        for (int k = 0; k < kOwn; ++k) o[r][k].x *= cr, o[r][k].y *= cr, o[r][k].z *= cr, o[r][k].w *= cr;
       }
     }
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const float p = exp2_approx(s[r] - (m[r] == -CUDART_INF_F ? 0.f : m[r]));
-      l[r] += quarter == 0 ? p : 0.f;
-      if (quarter == 0) weights[t * ROWS + r] = p;
+    for (int i = 0; i < kVals; ++i) {
+      v[i] = exp2_approx(v[i] - (near[i] == -CUDART_INF_F ? 0.f : near[i]));
+      sum[i] += v[i];
+      weights[t * ROWS + row_of(i, lane)] = v[i];  // (the same from lanes that share a score)
     }
     __syncwarp();
     const uint32_t vals = keys + Z::kHalf;
@@ -647,12 +693,19 @@ struct SimtTile {
     for (int i = 0; i < Z::TOK / kSplit; ++i) {
       const int tok = i * kSplit + (kSplit > 1 ? lane / Z::kChunks : 0);
       float p[ROWS];
+      if (ROWS >= 4) {
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) p[r] = weights[tok * ROWS + r];
+        for (int r = 0; r < ROWS; r += 4) {
+          const float4 w = *reinterpret_cast<const float4*>(weights + tok * ROWS + r);
+          p[r] = w.x, p[(r + 1) % ROWS] = w.y, p[(r + 2) % ROWS] = w.z, p[(r + 3) % ROWS] = w.w;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) p[r] = weights[tok * ROWS + r];
+      }
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) {
-        const int c = (kSplit > 1 ? lane % Z::kChunks : lane) + 32 * k;
-        const float4 x = chunk(vals + tok * Z::kRow + ((c ^ (tok & 7)) * 16));
+        const float4 x = chunk(vals + tok * Z::kRow + (chunk_of(k, lane) ^ (tok & 7)) * 16);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
           o[r][k].x = fmaf(p[r], x.x, o[r][k].x);
@@ -667,9 +720,13 @@ struct SimtTile {
 
   __device__ __forceinline__ void finish() {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
+    for (int i = 0; i < kVals; ++i)
 #pragma unroll
-      for (int x = 1; x < 32; x <<= 1) l[r] += __shfl_xor_sync(~0u, l[r], x);  // lanes past 7 hold zero
+      for (int x = 4; x < 32; x <<= 1) sum[i] += __shfl_xor_sync(~0u, sum[i], x);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      m[r] = of_row(near, r);
+      l[r] = of_row(sum, r);
 #pragma unroll
       for (int x = 32 / kSplit; x < 32; x <<= 1) {
 #pragma unroll
@@ -689,7 +746,7 @@ struct SimtTile {
   __device__ __forceinline__ void each(int x, int lane, int d, F f) const {
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) {
-      const int e = 4 * ((kSplit > 1 ? lane % Z::kChunks : lane) + 32 * k);
+      const int e = 4 * chunk_of(k, lane);
       if (lane < 32 / kSplit && e < d) {
         f(e, o[x][k].x, o[x][k].y);
         f(e + 2, o[x][k].z, o[x][k].w);
@@ -747,7 +804,7 @@ struct Shared {  // after the rings
   alignas(16) uint8_t q[Z::NW * kPlaces * Tile::kRows * Z::kRow];
   float4 part[CLUSTER ? Tile::kRows * Z::DP / 4 : 1];  // of the cluster's CTAs, this one's share of the elements
   float2 cluster_ml[CLUSTER ? kMaxCluster : 1][Tile::kRows];
-  alignas(16) float mine[std::is_same<typename Z::T, float>::value ? Z::NW * (Tile::kRows * Z::DP + 8 * Tile::kRows) : 4];
+  alignas(16) float mine[std::is_same<typename Z::T, float>::value ? Z::NW * 8 * Tile::kRows : 4];  // fp32: a warp's weights
   alignas(16) float2 ml[Z::NW][Tile::kRows];  // sum -1: a page outside the pool
 };
 
@@ -794,8 +851,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   Shm& sh = *reinterpret_cast<Shm*>(raw + Z::kRing);
   const PagedDecodeArgs& a = g.a;
   static_assert(Z::kRing % 16 == 0 && offsetof(Shm, mine) % 16 == 0 && sizeof(Shm) % 16 == 0, "16-byte accesses");
-  static_assert((Tile::kRows * Z::DP + 8 * Tile::kRows) % 4 == 0 && Z::kStage >= Tile::kRows * Z::DP * 4,
-                "a warp's queries, its sums in a stage");
+  static_assert(Z::kStage >= Tile::kRows * Z::DP * 4, "a warp's sums in a stage");
   Batch batch;
   batch.prefix = reinterpret_cast<int*>(raw + Z::kRing + sizeof(sh));
   batch.len = a.B <= kKeptLens ? batch.prefix + a.B + 1 : nullptr;
@@ -883,7 +939,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   scale.scale2 = a.scale * 1.44269504088896f;
   scale.cap2 = a.softcap * 1.44269504088896f;
   scale.inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
-  float* mine = sh.mine + warp * (Tile::kRows * Z::DP + 8 * Tile::kRows);
+  float* mine = sh.mine + warp * 8 * Tile::kRows;
   Tile tile;
   Queries qs;
   if (CLUSTER) {  // the queries by themselves, before the copies
