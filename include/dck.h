@@ -353,7 +353,8 @@ dck_status dck_page_update(int32_t batch, int32_t page_size, int32_t n_pages, co
  *                      (0 < slow < fast, theta > 1); its usual magnitude is 0.1 ln f + 1
  * dck_rope_init checks the settings and fills a host structure that the caller keeps
  * and passes by pointer (read during the call only).  Frequencies are kept as 64-bit
- * fractions of a turn, so angles are exact to fp32 rounding at every int32 position.
+ * fractions of a turn, so angles are exact to fp32 rounding at every int32 position,
+ * negative ones (turning back) included.
  */
 typedef enum { DCK_ROPE_HALF = 0, DCK_ROPE_INTERLEAVED = 1 } dck_rope_layout;
 typedef enum {

@@ -12,6 +12,13 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// sin and cos at a signed position: read as unsigned, t < 0 is t + 2^32, which turns by
+// 2^32 f more: the fraction's low word as the angle's high one (2^64 of a turn are none).
+__device__ __forceinline__ void signed_sincos(uint2 f, int t, float& sn, float& cs) {
+  const uint32_t u = (uint32_t)t;
+  turn_sincos(__umulhi(u, f.x) + u * f.y - (t < 0 ? f.x : 0u), sn, cs);
+}
+
 // Where token i's rows go in a cache.
 struct CacheRow {
   int64_t page, off;
@@ -38,7 +45,7 @@ __global__ void __launch_bounds__(kThreads) rope_any_kernel(const __grid_constan
   pdl_launch_dependents();
   pdl_wait();
   const int64_t i = blockIdx.x;
-  const uint32_t pos = a.rope.rot ? (uint32_t)a.positions[i] : 0u;
+  const int pos = a.rope.rot ? a.positions[i] : 0;
   const CacheRow to = cache_row(a, i, threadIdx.x == 0);
   for (int r = 0; r < a.n_rows; ++r) {
     const RopeRows& rows = a.rows[r];
@@ -54,7 +61,7 @@ __global__ void __launch_bounds__(kThreads) rope_any_kernel(const __grid_constan
       if (j < half) {
         const int i0 = a.rope.layout == DCK_ROPE_HALF ? j : 2 * j, i1 = a.rope.layout == DCK_ROPE_HALF ? j + half : 2 * j + 1;
         float sn, cs;
-        rope_sincos(a.rope.f[j], pos, sn, cs);
+        signed_sincos(a.rope.f[j], pos, sn, cs);
         sn *= a.rope.sign * a.rope.magnitude;
         cs *= a.rope.magnitude;
         const float x = to_f32(sp[i0]), y = to_f32(sp[i1]);
@@ -151,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_cons
   for (int z = tid; z < n_here * pairs; z += kThreads) {
     const int q = v.by_turned.div(z), jj = z - q * v.turned, tok = q / N, k = q - tok * N;
     float sn, cs;
-    rope_sincos(a.rope.f[jj * N + k], (uint32_t)a.positions[first + tok], sn, cs);
+    signed_sincos(a.rope.f[jj * N + k], a.positions[first + tok], sn, cs);
     turn[z] = make_float2(cs * a.rope.magnitude, sn * (a.rope.sign * a.rope.magnitude));
   }
   if (a.slots)
