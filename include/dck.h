@@ -320,12 +320,18 @@ dck_status dck_validate_paged_desc(const dck_paged_desc* desc);
  *                  refused ones included, and their total
  * Pages are granted in the order of requests: with g_b the pages that requests
  * before b ask for, b is granted if it asks for none or g_b plus its own are at
- * most the free pages and those given back.  Want of pages is no error.  A
- * negative length, one beyond the table, a free count outside [0, n_pages], more
- * pages given back than the list can hold, a page number outside the pool or more
- * new tokens than n_tok are recorded as a device error (DCK_ERR_INVALID from
- * dck_last_device_error); the request concerned is refused (an old length that is
- * negative or beyond the table counts as 0), its slots are -1.
+ * most the free pages and those given back.  Want of pages is no error.  The
+ * following are recorded as a device error (DCK_ERR_INVALID from
+ * dck_last_device_error):
+ *  - A negative length or one beyond the table: the request is refused, it keeps
+ *    its old length and pages, its slots are -1 (an old length that is itself
+ *    negative or beyond the table becomes 0).
+ *  - More new tokens than n_tok: a request whose last new token has no slot is
+ *    refused the same way, and so are all after it that have new tokens; those
+ *    that have none are not.  (Tokens of refused requests count, as in d_cu_new.)
+ *  - A free count outside [0, n_pages]: counts as 0.  More pages given back than
+ *    the list can hold: the last of them are lost.
+ *  - A page number outside the pool; the slots of its tokens are -1.
  * Deterministic; one launch; no workspace.
  */
 dck_status dck_page_update(int32_t batch, int32_t page_size, int32_t n_pages, const int32_t* d_old_len,

@@ -18,28 +18,33 @@ def page_update(page_size, old_len, new_len, block_table, free_pages, n_free, n_
     pages = lambda n: -(-int(n) // page_size)  # noqa: E731
     for b, (o, n) in enumerate(zip(old_len, new_len)):
         pool += [int(table[b, c]) for c in range(pages(n), pages(o))]
-    total, asked, refused, seq_len = len(pool), 0, 0, []
+    total = len(pool)
+    asked = refused = tokens = 0
+    granted, seq_len = [], []
     for b, (o, n) in enumerate(zip(old_len, new_len)):
         want = max(0, pages(n) - pages(o))
         asked += want
-        if want and asked > total:
-            refused += 1
-            seq_len.append(int(o))
-            continue
-        for c in range(pages(o), pages(o) + want):
-            table[b, c] = pool.pop()
-        seq_len.append(int(n))
+        tokens += max(0, int(n) - int(o))
+        late = n > o and tokens > n_tok  # no room for its slots
+        short = want > 0 and asked > total
+        refused += short
+        granted.append(not (late or short))
+        seq_len.append(int(n) if granted[b] else int(o))
+        if granted[b]:
+            for c in range(pages(o), pages(o) + want):
+                table[b, c] = pool.pop()
     slots, positions, cu = [], [], [0]
     for b, (o, n) in enumerate(zip(old_len, new_len)):
         for t in range(int(o), int(n)):
             positions.append(t)
-            slots.append(int(table[b, t // page_size]) * page_size + t % page_size if seq_len[b] == n else -1)
+            slots.append(int(table[b, t // page_size]) * page_size + t % page_size if granted[b] else -1)
         cu.append(len(positions))
     pad = n_tok - len(slots)
     free = np.array(free_pages, dtype=np.int64)
     free[n_free:max(n_free, len(pool))] = pool[n_free:]
     return dict(block_table=table, free_pages=free, free=np.array([len(pool), refused]), seq_len=np.array(seq_len),
-                slots=np.array(slots + [-1] * pad), positions=np.array(positions + [0] * pad), cu_new=np.array(cu))
+                slots=np.array((slots + [-1] * pad)[:n_tok]), positions=np.array((positions + [0] * pad)[:n_tok]),
+                cu_new=np.array(cu))
 
 
 def rope_frequencies(rotary_dim, theta, scaling="none", factor=1.0, slow=1.0, fast=32.0, trained_len=0):

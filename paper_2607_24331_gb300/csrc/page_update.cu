@@ -100,13 +100,20 @@ __global__ void __launch_bounds__(kThreads) page_update_kernel(const PageUpdateA
     if (tid == 0) atomicOr(a.err, kErrBadSeq);
     have = a.n_pages;
   }
-  const auto granted = [&](int b) { return grow[b + 1] == grow[b] || grow[b + 1] <= have; };
-  // Requests are granted up to the first whose pages go beyond what there is: the largest
-  // prefix sum that does not is what they take.
-  const int64_t used = base.grow <= have ? base.grow : grow[request_of(grow, a.B, have)], left = have - used;
+  // Requests are granted pages up to the first whose own go beyond what there is, and tokens
+  // up to the first whose own go beyond the slots: of those that grow, the ones before both,
+  // so a prefix sum is what they take.
+  const auto enough = [&](int b) { return grow[b + 1] == grow[b] || grow[b + 1] <= have; };
+  const auto granted = [&](int b) { return enough(b) && (tok[b + 1] == tok[b] || tok[b + 1] <= a.n_tok); };
+  int64_t used = base.grow <= have ? base.grow : grow[request_of(grow, a.B, have)];
+  if (base.tok > a.n_tok) {
+    if (tid == 0) atomicOr(a.err, kErrBadSeq);
+    used = min(used, grow[request_of(tok, a.B, a.n_tok)]);
+  }
+  const int64_t left = have - used;
   if (base.grow > have) {
     for (int b = tid; b < a.B; b += kThreads)
-      if (!granted(b)) atomicAdd(&refused_s, 1);
+      if (!enough(b)) atomicAdd(&refused_s, 1);
     __syncthreads();
   }
 
@@ -148,7 +155,6 @@ __global__ void __launch_bounds__(kThreads) page_update_kernel(const PageUpdateA
     a.slots[i] = slot;
     a.positions[i] = pos;
   }
-  if (base.tok > a.n_tok && tid == 0) atomicOr(a.err, kErrBadSeq);
   if (shares > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   for (int b = me; b <= a.B; b += all) {
     a.cu_new[b] = (int)min(tok[b], (int64_t)0x7fffffff);
