@@ -331,7 +331,13 @@ dck_status dck_validate_paged_desc(const dck_paged_desc* desc);
  *    that have none are not.  (Tokens of refused requests count, as in d_cu_new.)
  *  - A free count outside [0, n_pages]: counts as 0.  More pages given back than
  *    the list can hold: the last of them are lost.
- *  - A page number outside the pool; the slots of its tokens are -1.
+ *  - A page number outside the pool.  In the partly filled last page of a request
+ *    with new tokens: the request is refused.  Among the pages that would be taken:
+ *    the list ends there, so that the request that would take it and those after it
+ *    that ask for pages are refused, and count in d_free_out[1]; it stays in the
+ *    list, where the next call meets it again.  Among the pages given back and not
+ *    taken: it joins the list like any other.
+ * So the tokens of a granted request all have slots inside the pool.
  * Deterministic; one launch; no workspace.
  */
 dck_status dck_page_update(int32_t batch, int32_t page_size, int32_t n_pages, const int32_t* d_old_len,

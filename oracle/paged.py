@@ -9,26 +9,36 @@ import math
 import numpy as np
 
 
-def page_update(page_size, old_len, new_len, block_table, free_pages, n_free, n_tok):
-    """One step's bookkeeping, request by request, on lists.
+def page_update(page_size, old_len, new_len, block_table, free_pages, n_free, n_tok, n_pages=None):
+    """One step's bookkeeping, request by request, on lists.  With n_pages, page numbers outside [0, n_pages) refuse:
+    one in the partly filled last page of a request that grows refuses that request alone; one among the pages that
+    would be taken ends the list, so that its request and the later ones that ask for pages are refused.
 
     Returns a dict with block_table, free_pages, free (left, refused), seq_len, slots, positions, cu_new."""
     table = np.array(block_table, dtype=np.int64)
     pool = [int(p) for p in free_pages[:n_free]]
     pages = lambda n: -(-int(n) // page_size)  # noqa: E731
+    outside = lambda p: n_pages is not None and not 0 <= p < n_pages  # noqa: E731
+    broken = [n > o and o % page_size and outside(table[b, int(o) // page_size])
+              for b, (o, n) in enumerate(zip(old_len, new_len))]
     for b, (o, n) in enumerate(zip(old_len, new_len)):
         pool += [int(table[b, c]) for c in range(pages(n), pages(o))]
-    total = len(pool)
+    total = limit = len(pool)
     asked = refused = tokens = 0
     granted, seq_len = [], []
     for b, (o, n) in enumerate(zip(old_len, new_len)):
-        want = max(0, pages(n) - pages(o))
+        want = 0 if broken[b] else max(0, pages(n) - pages(o))
         asked += want
         tokens += max(0, int(n) - int(o))
         late = n > o and tokens > n_tok  # no room for its slots
-        short = want > 0 and asked > total
+        if want and not late and asked <= limit:
+            for x in range(asked - want, asked):  # the x-th page from the list's end
+                if outside(pool[total - 1 - x]):
+                    limit = x
+                    break
+        short = want > 0 and asked > limit
         refused += short
-        granted.append(not (late or short))
+        granted.append(not (broken[b] or late or short))
         seq_len.append(int(n) if granted[b] else int(o))
         if granted[b]:
             for c in range(pages(o), pages(o) + want):

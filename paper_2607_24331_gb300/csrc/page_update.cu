@@ -6,7 +6,8 @@
 // on to a slot: page number a of those taken is a function of the prefix sums and
 // of entries that the call does not write (free_pages below the old count, table
 // columns that a request had before).  So one launch suffices, and a token's slot
-// does not wait for the table entry that it equals.
+// does not wait for the table entry that it equals.  The pages that would be taken are all
+// looked at before the first is written: a number outside the pool ends the list there.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -15,6 +16,18 @@ namespace dck {
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kNone = 0x7fffffff;
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// What CTA `rank` of the cluster holds where `p` is in this one's shared memory.
+__device__ __forceinline__ int read_remote(const int* p, int rank) {
+  uint32_t at;
+  int v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
 
 struct Sums {
   int64_t rel, grow, tok;
@@ -61,8 +74,15 @@ __global__ void __launch_bounds__(kThreads) page_update_kernel(const PageUpdateA
         atomicOr(a.err, kErrBadSeq);
         o = -1 - (old_ok ? o : 0);
       } else {
-        v.rel = po > pn ? po - pn : 0;
-        v.grow = pn > po ? pn - po : 0;
+        // the page that a request goes on filling: a table entry that it has already
+        const int last = n > o && po * a.page > o ? a.table[(int64_t)b * a.table_stride + po - 1] : 0;
+        if (last < 0 || last >= a.n_pages) {
+          atomicOr(a.err, kErrBadRow);
+          o = -1 - o;
+        } else {
+          v.rel = po > pn ? po - pn : 0;
+          v.grow = pn > po ? pn - po : 0;
+        }
       }
       olen[b] = o;
       nlen[b] = n;
@@ -89,34 +109,15 @@ __global__ void __launch_bounds__(kThreads) page_update_kernel(const PageUpdateA
     __syncthreads();
   }
   if (tid == 0) rel[a.B] = base.rel, grow[a.B] = base.grow, tok[a.B] = base.tok;
-  __shared__ int refused_s;
-  if (tid == 0) refused_s = 0;
+  __shared__ int refused_s, first_outside;
+  if (tid == 0) refused_s = 0, first_outside = kNone;
   __syncthreads();
-  // Every CTA has read the lengths and the free count: they may be written after the wait.
-  if (shares > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 
   int64_t have = f + base.rel;  // free pages and those given back
   if (have > a.n_pages) {
     if (tid == 0) atomicOr(a.err, kErrBadSeq);
     have = a.n_pages;
   }
-  // Requests are granted pages up to the first whose own go beyond what there is, and tokens
-  // up to the first whose own go beyond the slots: of those that grow, the ones before both,
-  // so a prefix sum is what they take.
-  const auto enough = [&](int b) { return grow[b + 1] == grow[b] || grow[b + 1] <= have; };
-  const auto granted = [&](int b) { return enough(b) && (tok[b + 1] == tok[b] || tok[b + 1] <= a.n_tok); };
-  int64_t used = base.grow <= have ? base.grow : grow[request_of(grow, a.B, have)];
-  if (base.tok > a.n_tok) {
-    if (tid == 0) atomicOr(a.err, kErrBadSeq);
-    used = min(used, grow[request_of(tok, a.B, a.n_tok)]);
-  }
-  const int64_t left = have - used;
-  if (base.grow > have) {
-    for (int b = tid; b < a.B; b += kThreads)
-      if (!enough(b)) atomicAdd(&refused_s, 1);
-    __syncthreads();
-  }
-
   const auto pages_of = [&](int len) { return ((int64_t)len + a.page - 1) / a.page; };
   // page j of the free list with the pages given back behind it
   const auto page_at = [&](int64_t j) -> int {
@@ -126,11 +127,47 @@ __global__ void __launch_bounds__(kThreads) page_update_kernel(const PageUpdateA
   };
   const auto taken = [&](int64_t x) { return page_at(have - 1 - x); };  // the x-th page that is taken
   const int me = share * kThreads + tid, all = shares * kThreads;
+  // Requests are granted pages up to the first whose own go beyond what there is, and tokens
+  // up to the first whose own go beyond the slots: of those that grow, the ones before both,
+  // so a prefix sum is what they take.
+  const auto pages_within = [&](int64_t most) { return base.grow <= most ? base.grow : grow[request_of(grow, a.B, most)]; };
+  int64_t used = pages_within(have);
+  if (base.tok > a.n_tok) {
+    if (tid == 0) atomicOr(a.err, kErrBadSeq);
+    used = min(used, grow[request_of(tok, a.B, a.n_tok)]);
+  }
+  int page0 = 0;  // this thread's first page of those taken
+  for (int64_t x = me; x < used; x += all) {
+    const int p = taken(x);
+    if (x == me) page0 = p;
+    if (p < 0 || p >= a.n_pages) atomicMin(&first_outside, (int)x);
+  }
+  __syncthreads();
+  int outside = first_outside;
+  if (shares > 1) {
+    // Every CTA has read the lengths, the free count and the pages: they may be written after the wait.
+    cluster_arrive();
+    cluster_wait();
+    outside = __reduce_min_sync(~0u, read_remote(&first_outside, lane % shares));
+    cluster_arrive();  // no CTA ends before the others have read its first_outside
+  }
+  const int64_t there = min(have, (int64_t)outside);  // pages that can be taken
+  if (outside != kNone) {
+    if (me == 0) atomicOr(a.err, kErrBadRow);
+    used = pages_within(there);
+  }
+  const auto enough = [&](int b) { return grow[b + 1] == grow[b] || grow[b + 1] <= there; };
+  const auto granted = [&](int b) { return enough(b) && (tok[b + 1] == tok[b] || tok[b + 1] <= a.n_tok); };
+  const int64_t left = have - used;
+  if (base.grow > there) {
+    for (int b = tid; b < a.B; b += kThreads)
+      if (!enough(b)) atomicAdd(&refused_s, 1);
+    __syncthreads();
+  }
+
   for (int64_t x = me; x < used; x += all) {
     const int b = request_of(grow, a.B, x);
-    const int p = taken(x);
-    if (p < 0 || p >= a.n_pages) atomicOr(a.err, kErrBadRow);
-    a.table[(int64_t)b * a.table_stride + pages_of(olen[b]) + (x - grow[b])] = p;
+    a.table[(int64_t)b * a.table_stride + pages_of(olen[b]) + (x - grow[b])] = x == me ? page0 : taken(x);
   }
   for (int64_t j = f + me; j < left; j += all) {
     const int p = page_at(j);
@@ -148,19 +185,18 @@ __global__ void __launch_bounds__(kThreads) page_update_kernel(const PageUpdateA
       if (o >= 0 && granted(b)) {
         const int64_t c = pos / a.page, had = pages_of(o);
         const int p = c < had ? a.table[(int64_t)b * a.table_stride + c] : taken(grow[b] + (c - had));
-        if (p < 0 || p >= a.n_pages) atomicOr(a.err, kErrBadRow);
-        else slot = (int64_t)p * a.page + pos % a.page;
+        slot = (int64_t)p * a.page + pos % a.page;
       }
     }
     a.slots[i] = slot;
     a.positions[i] = pos;
   }
-  if (shares > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   for (int b = me; b <= a.B; b += all) {
     a.cu_new[b] = (int)min(tok[b], (int64_t)0x7fffffff);
     if (b < a.B) a.seq_len[b] = olen[b] < 0 ? -1 - olen[b] : granted(b) ? nlen[b] : olen[b];
   }
   if (me == 0) a.free_out[0] = (int)left, a.free_out[1] = refused_s;
+  if (shares > 1) cluster_wait();
 }
 
 }  // namespace

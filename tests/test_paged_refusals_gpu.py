@@ -1,5 +1,5 @@
-"""What dck_page_update does with more new tokens than there are slots for, value for value against the sequential
-program: lengths, tables, free list and slots, of the requests concerned and the others."""
+"""What dck_page_update does with more new tokens than there are slots for, and with page numbers outside the pool, value
+for value against the sequential program: lengths, tables, free list and slots, of the requests concerned and the others."""
 
 import numpy as np
 import pytest
@@ -9,11 +9,12 @@ from oracle import paged as P
 from paper_2607_24331_gb300 import dck
 
 pytestmark = pytest.mark.gpu
+BAD = (-1, -(1 << 31), 1 << 30)
 
 
 def _step(page, n_pages, old, new, table, free_pages, n_free, n_tok):
     """(what the program on lists gives, what the call gives, its device error), on copies."""
-    want = P.page_update(page, old, new, table, free_pages, n_free, n_tok)
+    want = P.page_update(page, old, new, table, free_pages, n_free, n_tok, n_pages)
     i32 = lambda v: torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")  # noqa: E731
     B, t, length, pool, free = len(old), i32(table), i32(old), i32(free_pages), i32([n_free, 0])
     slots = torch.full((n_tok,), -77, dtype=torch.int64, device="cuda")
@@ -87,10 +88,45 @@ def test_a_request_beyond_the_table_keeps_its_places():
         assert (slots[:95] == -1).all() and (n_tok < 96 or slots[95] == 19)
 
 
+@pytest.mark.parametrize("bad", BAD)
+def test_a_page_outside_the_pool_in_the_list_ends_it(bad):
+    table = [[0, -9, -9], [1, -9, -9], [2, -9, -9], [3, -9, -9], [4, 5, -9]]
+    # two, two, one page asked for (the third request none), the last gives one back; taken from the end: 5, 9, 8, bad, 7
+    want, got, err = _step(16, 12, [16, 10, 3, 16, 32], [40, 40, 4, 17, 16], table,
+                           [6, 7, bad, 8, 9, 0, 0, 0, 0, 0, 0, 0], 5, 100)
+    assert err == dck.DCK_ERR_INVALID
+    _same(want, got)
+    assert got["seq_len"].tolist() == [40, 10, 4, 16, 16] and got["free"].tolist() == [4, 2]
+    assert got["free_pages"][:4].tolist() == [6, 7, bad, 8] and got["block_table"][1].tolist() == table[1]
+    # the next step meets it again, and without it all is well
+    for page, held, error in ((bad, 10, dck.DCK_ERR_INVALID), (10, 40, dck.DCK_OK)):
+        want, got, err = _step(16, 12, [40, 10], [40, 40], [[0, 5, 9], [1, -9, -9]], [6, 7, page, 8] + [0] * 8, 4, 40)
+        assert err == error
+        _same(want, got)
+        assert got["seq_len"].tolist() == [40, held]
+    # a page given back counts among those of the list
+    want, got, err = _step(16, 12, [16, 32], [17, 0], [[0, -9], [1, bad]], [6, 7] + [0] * 10, 2, 5)
+    assert err == dck.DCK_ERR_INVALID
+    _same(want, got)
+    assert got["seq_len"].tolist() == [16, 0] and got["free"].tolist() == [4, 1]
+
+
+@pytest.mark.parametrize("bad", BAD)
+def test_a_page_outside_the_pool_in_a_table_refuses_its_request(bad):
+    table = [[0, -9, -9], [bad, -9, -9], [2, bad, -9], [3, bad, -9]]
+    # the first two grow within and beyond their page, the third beyond a full table column, the fourth stays
+    want, got, err = _step(16, 8, [10, 10, 32, 20], [20, 40, 33, 20], table, [4, 5, 6, 7, 0, 0, 0, 0], 4, 60)
+    assert err == dck.DCK_ERR_INVALID
+    _same(want, got)
+    assert got["seq_len"].tolist() == [20, 10, 33, 20] and got["free"].tolist() == [2, 0]
+    assert (got["slots"][10:40] == -1).all() and got["slots"][40] >= 0
+    assert np.array_equal(got["block_table"][1], table[1])
+
+
 @pytest.mark.parametrize("batch", [9, 32, 33, 200, 700])
 @pytest.mark.parametrize("page", [1, 16, 100])
 def test_random_steps(batch, page):
-    """One CTA and a cluster; slots for all tokens or for some."""
+    """One CTA and a cluster; slots for all tokens or for some, bad numbers in the list, the tables, or nowhere."""
     rng = np.random.default_rng(batch * 7 + page)
     refused = errors = 0
     for turn in range(12):
@@ -98,6 +134,12 @@ def test_random_steps(batch, page):
         spare = n_pages - int((-(-old // page)).sum())
         n_new = int(np.maximum(0, new - old).sum())
         n_tok = n_new + int(rng.integers(0, 20)) if turn % 3 else int(rng.integers(0, n_new + 1))
+        for _ in range(turn % 4):
+            if rng.random() < 0.5:
+                free_pages[rng.integers(0, spare)] = rng.choice(BAD)
+            else:
+                b = int(rng.integers(0, batch))
+                table[b, rng.integers(0, max(1, -(-old[b] // page)))] = rng.choice(BAD)
         want, got, err = _step(page, n_pages, old, new, table, free_pages, spare, n_tok)
         _same(want, got)
         refused += int((got["seq_len"] != new).sum())
