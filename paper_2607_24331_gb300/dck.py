@@ -215,8 +215,10 @@ class Rope:
 def _ptr(t) -> Optional[int]:
     try:
         return t.data_ptr()
-    except AttributeError:  # an address, or None
-        return t
+    except AttributeError:
+        if t is None or isinstance(t, int):  # an address
+            return t
+        raise  # ctypes would take bytes or str for one
 
 
 _torch = None
