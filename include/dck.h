@@ -431,7 +431,8 @@ dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* ta
  *   d_seq_len    device int32 [batch]: L_b, the new token included.  0 gives a zero output
  *                row and lse = -inf.
  *   max_seq_len  an upper bound on every L_b, 1 .. 2^31 - 1 (plans the work)
- *   scale        finite (1/sqrt(d) as a rule); softcap >= 0; window >= 0
+ *   scale        finite (1/sqrt(d) as a rule); softcap >= 0, finite (from 2^100 on it
+ *                caps nothing); window >= 0
  *   out          [batch, Hq, d]; lse float [batch, Hq] or NULL: with it, results over parts
  *                of a context can be joined
  *   workspace    at least dck_paged_decode_workspace_size bytes, 256-byte aligned; needs no

@@ -311,6 +311,7 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cu
   g.a = a;
   g.p = plan_of(a.v, dtype, a.B, a.max_len, a.window, sms);
   g.DP = padded_dim(a.v.d);
+  g.score.set(a.scale, a.softcap);
   const int el = dtype == DCK_F32 ? 4 : 2;
   g.p.q_copied = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride * el % 16 == 0;
   char* ws = static_cast<char*>(a.ws);

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <cstddef>
 #include <type_traits>
 
@@ -43,9 +44,35 @@ constexpr int kMaxItems = 512;  // CTAs of tiles dealt in ranges
 
 constexpr float kHeadroom = 8.f;  // log2 units that a score may lie above the running reference
 
+// Scores in log2 units.
+__device__ __forceinline__ float tanh_of(float x);
+struct ScoreScale {
+  float scale2, inv_cap, cap2;  // cap2 = 0: no cap
+  // Factors that stay finite, so that a product of 0 stays 0.  c tanh(s / c) is s to fp32
+  // rounding for |s| < 2^-12 c: a cap from 2^100 on is none.
+  void set(float scale, float softcap) {
+    const auto finite = [](float x) { return std::min(std::max(x, -FLT_MAX), FLT_MAX); };
+    const bool capped = softcap > 0.f && softcap < 1.2676506e30f;
+    scale2 = finite(scale * 1.44269504088896f);
+    cap2 = capped ? softcap * 1.44269504088896f : 0.f;
+    inv_cap = capped ? finite(scale / softcap) : 0.f;
+  }
+  template <int N>
+  __device__ __forceinline__ void apply(float (&s)[N]) const {
+    if (cap2 > 0.f) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = cap2 * tanh_of(s[i] * inv_cap);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] *= scale2;
+    }
+  }
+};
+
 struct Args {
   PagedDecodeArgs a;
   Plan p;
+  ScoreScale score;
   int DP;          // head dim, rounded up to the variant's
   float* part_u;   // [2 n_items][wh][rows][DP]
   float* part_ml;  // [2 n_items][wh][rows][2]: maximum (log2 units), sum (-1: a page outside the pool)
@@ -344,21 +371,6 @@ __device__ __forceinline__ float tanh_of(float x) {
   const float big = 1.f - __fdividef(2.f, exp2_approx(ax * 2.88539008f) + 1.f);
   return ax < 0.5f ? fmaf(x * u, p, x) : copysignf(ax > 20.f ? 1.f : big, x);
 }
-
-// Scores in log2 units.
-struct ScoreScale {
-  float scale2, inv_cap, cap2;  // cap2 = 0: no cap
-  template <int N>
-  __device__ __forceinline__ void apply(float (&s)[N]) const {
-    if (cap2 > 0.f) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) s[i] = cap2 * tanh_of(s[i] * inv_cap);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) s[i] *= scale2;
-    }
-  }
-};
 
 // ---------------------------------------------------------------------------
 // bf16: tensor cores (mma.sync m16n8k16, queries as rows)
@@ -935,10 +947,6 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     }
     cp_async_commit();
   };
-  ScoreScale scale;
-  scale.scale2 = a.scale * 1.44269504088896f;
-  scale.cap2 = a.softcap * 1.44269504088896f;
-  scale.inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
   float* mine = sh.mine + warp * 8 * Tile::kRows;
   Tile tile;
   Queries qs;
@@ -971,7 +979,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
         fresh = false;
       }
       bad |= outside >> get & 1;
-      tile.step(load.ring + get * Z::kStage, at.len - at.token - load.run, lane, scale, mine);
+      tile.step(load.ring + get * Z::kStage, at.len - at.token - load.run, lane, g.score, mine);
     }
     const int used = get;
     get = get + 1 == Z::S ? 0 : get + 1;
