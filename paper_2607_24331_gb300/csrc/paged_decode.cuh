@@ -191,7 +191,8 @@ struct Walk {
       token = a.window > 0 && len > a.window ? len - a.window : 0;
     } else {
       bool bad;
-      len = visible(a, b, token, bad) + token;
+      const int span = visible(a, b, token, bad);  // (sets token)
+      len = span + token;
     }
   }
   // Enters at tile u; true if that is the first of its (head group, sequence).
