@@ -94,8 +94,10 @@ def serve(requests=24, pages=400, page=16, batch=8, dtype="bf16", check=False, s
     dt = torch.float32 if dtype == "f32" else torch.bfloat16
     hidden, chunk = 512, 64
     width = -(-longest // page)
-    layer = Layer(hidden, n_q, n_kv, d, page, pages, batch, width, batch * chunk, dt, seed)
     waiting = [(rng.randint(1, longest // 2), rng.randint(1, longest // 8)) for _ in range(requests)]  # (prompt, answers)
+    if requests and max(-(-(p + a) // page) for p, a in waiting) > pages:
+        raise ValueError("a request needs more pages than there are: it would wait for ever")
+    layer = Layer(hidden, n_q, n_kv, d, page, pages, batch, width, batch * chunk, dt, seed)
     slots = [None] * batch  # [prompt left, answers left, qkv rows so far, the request]
     done = tokens = steps = refused = restarted = 0
     worst = 0.0
