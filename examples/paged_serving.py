@@ -6,7 +6,8 @@ Requests arrive with prompts, give a token per step and end; every step
   3. ``dck_paged_append`` rotates them and writes keys and values into their pages,
   4. ``dck_paged_decode_attention`` attends: each new token, of a prompt's chunk too, is a row of
      the call with its request's block table and its own position + 1 as length.
-Requests that find no page wait for the next step; where none can grow, one gives its pages back and starts anew later.
+Requests that find no page wait for the next step; where none can grow, one gives its pages back and starts anew later
+(``Scheduler``).
 
     python examples/paged_serving.py [--requests 24] [--pages 400] [--dtype bf16|f32] [--check]
 
@@ -88,64 +89,95 @@ def plain(layer, qkv, n_before):
     return torch.einsum("hij,jhd->ihd", torch.softmax(w.masked_fill(late, -math.inf), -1), v)
 
 
+class Scheduler:
+    """Which requests run and how many tokens each takes, on the host; a request is (prompt tokens, answer tokens).
+
+    While a request waits for pages none is admitted.  Where no request can grow, the last that holds pages gives them
+    back: the first is never it, since with all other pages free it can grow.  So the first always ends, and so do all."""
+
+    def __init__(self, requests, batch, chunk):
+        self.waiting, self.batch, self.chunk = list(requests), batch, chunk
+        self.running = [None] * batch  # [prompt left, answers left, the request]
+        self.held = [0] * batch
+        self.done = self.tokens = self.steps = self.refused = self.restarted = 0
+        self.starved = False
+
+    def ask(self):
+        """(tokens that each slot is to hold, the slot of each new token)."""
+        new, owner = [], []
+        for b in range(self.batch):
+            if self.running[b] is None and self.held[b] == 0 and self.waiting and not self.starved:
+                request = self.waiting.pop()
+                self.running[b] = [*request, request]
+            r = self.running[b]
+            n = 0 if r is None else min(self.chunk, r[0]) if r[0] else 1
+            new.append(0 if r is None else self.held[b] + n)
+            owner += [b] * n
+        return new, owner
+
+    def answer(self, new, got):
+        """Takes the tokens that each slot holds now; returns the slots whose requests have ended, restarted ones among them."""
+        ended, grown, self.starved = [], False, False
+        for b, r in enumerate(self.running):
+            n, self.held[b] = new[b] - self.held[b], got[b]
+            if r is None:
+                continue
+            if got[b] != new[b]:
+                self.starved = True
+                self.refused += 1
+                continue
+            r[0], r[1] = (r[0] - n, r[1]) if r[0] else (0, r[1] - 1)
+            self.tokens += n
+            grown = True
+            if r[0] == 0 and r[1] == 0:
+                ended.append(b)
+                self.done += 1
+        if self.starved and not grown:
+            last = max(b for b in range(self.batch) if self.running[b] and self.held[b])
+            self.waiting.append(self.running[last][2])
+            ended.append(last)
+            self.restarted += 1
+        for b in ended:
+            self.running[b] = None
+        self.steps += 1
+        return ended
+
+
 def serve(requests=24, pages=400, page=16, batch=8, dtype="bf16", check=False, seed=0, longest=600, n_q=8, n_kv=2, d=128):
     """Runs all requests to their ends; returns a dict of figures (worst error against plain attention if check)."""
     rng = random.Random(seed)
     dt = torch.float32 if dtype == "f32" else torch.bfloat16
     hidden, chunk = 512, 64
     width = -(-longest // page)
-    waiting = [(rng.randint(1, longest // 2), rng.randint(1, longest // 8)) for _ in range(requests)]  # (prompt, answers)
-    if requests and max(-(-(p + a) // page) for p, a in waiting) > pages:
+    work = [(rng.randint(1, longest // 2), rng.randint(1, longest // 8)) for _ in range(requests)]
+    if requests and max(-(-(p + a) // page) for p, a in work) > pages:
         raise ValueError("a request needs more pages than there are: it would wait for ever")
     layer = Layer(hidden, n_q, n_kv, d, page, pages, batch, width, batch * chunk, dt, seed)
-    slots = [None] * batch  # [prompt left, answers left, qkv rows so far, the request]
-    done = tokens = steps = refused = restarted = 0
+    plan = Scheduler(work, batch, chunk)
+    rows = [[] for _ in range(batch)]  # each running request's qkv rows so far
     worst = 0.0
     gen = torch.Generator(device="cuda").manual_seed(seed + 1)
-    held = [0] * batch
     begin = time.perf_counter()
-    while done < requests:
-        new, owner = [], []
-        for b in range(batch):
-            if slots[b] is None and held[b] == 0 and waiting:
-                p, a = waiting.pop()
-                slots[b] = [p, a, [], (p, a)]
-            r = slots[b]
-            n = 0 if r is None else min(chunk, r[0]) if r[0] else 1
-            new.append(0 if r is None else held[b] + n)
-            owner += [b] * n
+    while plan.done < requests:
+        held = list(plan.held)
+        new, owner = plan.ask()
         x = torch.randn((len(owner), hidden), generator=gen, device="cuda", dtype=dt)
-        out, qkv = layer.step(torch.tensor(new, dtype=torch.int32, device="cuda"), torch.tensor(owner, device="cuda"), x)
+        out, qkv = layer.step(torch.tensor(new, dtype=torch.int32, device="cuda"), torch.tensor(owner, dtype=torch.int64, device="cuda"), x)
         got = layer.len.tolist()  # the scheduler's look at what was granted
-        at, grown = 0, False
+        at = 0
         for b in range(batch):
             n = max(0, new[b] - held[b])
-            granted = got[b] == new[b]
-            if n and granted:
-                r = slots[b]
-                r[2].append(qkv[at:at + n])
+            if n and got[b] == new[b]:
+                rows[b].append(qkv[at:at + n])
                 if check:
-                    rows = torch.cat(r[2])
-                    want = plain(layer, rows, rows.shape[0] - n)
+                    mine = torch.cat(rows[b])
+                    want = plain(layer, mine, mine.shape[0] - n)
                     worst = max(worst, float((out[at:at + n].double() - want).abs().max() / want.abs().max()))
-                r[0], r[1] = (r[0] - n, r[1]) if r[0] else (0, r[1] - 1)
-                tokens += n
-                grown = True
-                if r[0] == 0 and r[1] == 0:
-                    slots[b] = None
-                    done += 1
-            elif n:
-                refused += 1
-                if check:
-                    assert (out[at:at + n] == 0).all()
-            held[b] = got[b]
+            elif n and check:
+                assert (out[at:at + n] == 0).all()
             at += n
-        if owner and not grown:
-            last = max(b for b in range(batch) if slots[b])
-            waiting.append(slots[last][3])
-            slots[last] = None
-            restarted += 1
-        steps += 1
+        for b in plan.answer(new, got):
+            rows[b] = []
     torch.cuda.synchronize()
     took = time.perf_counter() - begin
     # give back the last pages
@@ -153,7 +185,8 @@ def serve(requests=24, pages=400, page=16, batch=8, dtype="bf16", check=False, s
                torch.zeros((1, hidden), dtype=dt, device="cuda"))
     dck.check(dck.dck_last_device_error(), "device error")
     assert int(layer.free[0]) == pages and sorted(layer.free_pages.tolist()) == list(range(pages))
-    return dict(requests=done, tokens=tokens, steps=steps, refused=refused, restarted=restarted, seconds=took, worst=worst)
+    return dict(requests=plan.done, tokens=plan.tokens, steps=plan.steps, refused=plan.refused, restarted=plan.restarted,
+                seconds=took, worst=worst)
 
 
 if __name__ == "__main__":
