@@ -178,6 +178,8 @@ class PagedCache:
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, dtype: str,
                  k_strides: Optional[Sequence[int]] = None, v_strides: Optional[Sequence[int]] = None):
+        if dtype not in ("bf16", "f32"):
+            raise ValueError(f"dtype: bf16 or f32, not {dtype!r}")
         row = n_kv_heads * head_dim
         dense = (page_size * row, row, head_dim)
         self.desc = PagedDesc(n_q_heads, n_kv_heads, head_dim, page_size, n_pages,

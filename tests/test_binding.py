@@ -1,4 +1,4 @@
-"""What the binding takes for an address: tensors, integers and None, nothing else."""
+"""What the binding takes for an address (tensors, integers and None, nothing else) and for a type."""
 
 import pytest
 
@@ -20,3 +20,10 @@ def test_tensors_integers_and_none():
     import torch
     t = torch.zeros(3)
     assert dck._ptr(t) == t.data_ptr() and dck._ptr(A) == A and dck._ptr(None) is None
+
+
+@pytest.mark.parametrize("name", ["float32", "fp32", "f16", "torch.bfloat16", "", None])
+def test_a_cache_of_another_type_is_refused(name):
+    """Anything but f32 was taken for bf16."""
+    with pytest.raises(ValueError):
+        dck.PagedCache(8, 2, 64, 16, 10, name)
