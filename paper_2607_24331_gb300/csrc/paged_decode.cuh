@@ -427,7 +427,7 @@ struct TensorTile {
   uint32_t q[Z::DP / 16][2 * kQ];
 
   // `place`: the queries in shared memory.
-  __device__ __forceinline__ void begin(uint32_t place, int lane, float*) {
+  __device__ __forceinline__ void begin(uint32_t place, int lane) {
     const int row = PACK ? lane & 7 : lane & 15, c = PACK ? lane >> 3 : lane >> 4;
 #pragma unroll
     for (int k = 0; k < Z::DP / 16; k += PACK ? 2 : 1) {
@@ -600,7 +600,7 @@ struct SimtTile {
   }
 
   // `place`: the queries in shared memory, as long as it lasts.
-  __device__ __forceinline__ void begin(uint32_t place, int lane, float*) {
+  __device__ __forceinline__ void begin(uint32_t place, int lane) {
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
@@ -965,7 +965,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   if (CLUSTER) {
     cp_async_wait<Z::S - 1>();
     __syncwarp();
-    tile.begin(load.places, lane, mine);
+    tile.begin(load.places, lane);
   }
   while (true) {
     if (!CLUSTER || to_compute > 0) {
@@ -976,7 +976,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
       if (!CLUSTER && fresh) {
         qs = queries_of(g, at.group, wh);
         if (!g.p.q_copied) load.read_queries(qs, at.b, sh.q, warp, get);
-        tile.begin(load.places + get * load.kPlace, lane, mine);
+        tile.begin(load.places + get * load.kPlace, lane);
         fresh = false;
       }
       bad |= outside >> get & 1;
