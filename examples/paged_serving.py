@@ -11,7 +11,8 @@ Requests that find no page wait for the next step; where none can grow, one give
 
     python examples/paged_serving.py [--requests 24] [--pages 400] [--dtype bf16|f32] [--check]
 
-``--check`` recomputes every output with plain attention over each request's own keys and values.
+``--check`` recomputes every output with plain attention over each request's own keys and values, and turns the cached
+keys of each request that ends back by their positions (``dck_rope``'s transpose), to what was projected.
 """
 
 import argparse
@@ -71,6 +72,16 @@ class Layer:
                                                  self.width, seen, n, self.max_len, 1 / math.sqrt(self.d), 0, 0.0, out,
                                                  None, self.ws, self.ws_bytes), "dck_paged_decode_attention")
         return out, qkv
+
+
+    def keys_as_projected(self, b, n):
+        """The keys of request b's first n tokens, read from its pages and turned back by their positions."""
+        t = torch.arange(n, device="cuda")
+        rows = self.k[self.table[b, t // self.page].long(), t % self.page]
+        dtype = dck.DCK_F32 if rows.dtype == torch.float32 else dck.DCK_BF16
+        dck.check(dck.dck_rope(self.rope, rows, n, self.n_kv, self.d, dtype, self.n_kv * self.d, self.d, t.to(torch.int32), rows,
+                               self.n_kv * self.d, self.d, transpose=True), "dck_rope")
+        return rows
 
 
 def plain(layer, qkv, n_before):
@@ -177,6 +188,10 @@ def serve(requests=24, pages=400, page=16, batch=8, dtype="bf16", check=False, s
                 assert (out[at:at + n] == 0).all()
             at += n
         for b in plan.answer(new, got):
+            if check and got[b]:  # its pages are given back in the next step
+                keys = torch.cat(rows[b])[:, n_q:n_q + n_kv].double()
+                back = layer.keys_as_projected(b, got[b]).double()
+                worst = max(worst, float((back - keys).abs().max() / keys.abs().max()))
             rows[b] = []
     torch.cuda.synchronize()
     took = time.perf_counter() - begin
