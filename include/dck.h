@@ -438,7 +438,9 @@ dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* ta
  *   workspace    at least dck_paged_decode_workspace_size bytes, 256-byte aligned; needs no
  *                initialisation
  * Rows past a sequence's end are never read into the sums, whatever they hold.  Scores,
- * softmax and sums are fp32.  A length below 0, above max_seq_len, 2^29 or the table, or a
+ * their maximum and all sums are fp32, exponentials are good to 2^-22; the weights that
+ * multiply the values are fp32 too on fp32 caches, and two bf16 terms (2^-16) on bf16
+ * ones.  A length below 0, above max_seq_len, 2^29 or the table, or a
  * page number outside the pool among those read, is recorded as a device error; the sequence's
  * outputs are zero with lse = -inf.  (So are more than 2^33 tokens times query heads in one call,
  * which leave out undefined.)  At most two launches; results do not depend on the order in which blocks run.
@@ -470,7 +472,8 @@ dck_status dck_last_device_error(void* stream);
 int32_t dck_set_decode_kernel(int32_t which);
 
 /*
- * dck_set_timing_events - timing hook of dck_decode_attention: `events` holds
+ * dck_set_timing_events - timing hook of the decode calls
+ * (dck_paged_decode_attention among them): `events` holds
  * n CUDA events (cudaEvent_t, owned by the caller, 2 <= n <= 16).  Each later
  * decode call records events[0] on its stream before its first kernel,
  * events[k] after its k-th kernel for k < n - 1 (k = 1, 2, ...) and
@@ -484,7 +487,7 @@ int32_t dck_set_decode_kernel(int32_t which);
  */
 dck_status dck_set_timing_events(void* const* events, int32_t n);
 
-/* Number of kernels this thread's last decode / append call launched. */
+/* Number of kernels this thread's last decode, append or paged-cache call launched. */
 int32_t dck_last_launch_count(void);
 
 /*

@@ -209,8 +209,8 @@ cudaError_t launch_page_update(const PageUpdateArgs& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
   }
   // A cluster where there is more than a CTA's worth of tokens or requests (finished requests
-  // give back many pages each): 256 requests, 128-token chunks among them, 12.5 us on one CTA
-  // and 7.0 on eight; 16 requests of one token each take 3.7 on one, a cluster's launch 0.9 more.
+  // give back many pages each): 256 requests, 128-token chunks among them, 12.2 us on one CTA
+  // and 8.1 on eight; 16 requests of one token each take 3.9 on one, a cluster 1.0 more.
   const int shares = a.B > 32 || a.n_tok > kThreads ? 8 : 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = shares;
