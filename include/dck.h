@@ -453,6 +453,99 @@ dck_status dck_paged_decode_attention(const dck_paged_desc* desc, const void* q,
                                       size_t ws_bytes, void* stream);
 
 /*
+ * 8-bit caches: half the bytes of bf16 ones, for a paged cache as above.
+ *   dck_quant_append            new tokens rotated, rounded to 8 bits and written to their rows
+ *   dck_quant_read              rows of the cache as the values they stand for
+ *   dck_quant_decode_attention  dck_paged_decode_attention on such a cache
+ * A head's row of a token (a key after rotation, or a value; rounded to the descriptor's type) is
+ * kept as d codes of one byte, e4m3 (1 sign, 4 exponent and 3 mantissa bits, largest 448), and a scale of 32 bits:
+ * s = 2^e with the least whole e >= -126 for which no magnitude is above 448 s, codes the roundings
+ * (to nearest, ties to even) of x / s, which is exact.  Infinities and NaN count as 0 for the scale and are
+ * stored as NaN.
+ *
+ * dck_quant_desc: `cache` as in dck_paged_desc, its dtype that of queries, new keys and values, outputs and
+ * what is read back; its strides (in elements, of one byte) multiples of 16.  The scales are arrays
+ * of their own, float [pages, tokens, heads] in any order:
+ *   k_scale_*_stride  elements between pages, tokens of a page and heads of the keys'
+ *   v_scale_*_stride  and the values' scales, 1 .. 2^30 - 1
+ */
+typedef struct {
+  dck_paged_desc cache;
+  int64_t k_scale_page_stride, k_scale_token_stride, k_scale_head_stride;
+  int64_t v_scale_page_stride, v_scale_token_stride, v_scale_head_stride;
+} dck_quant_desc;
+
+/* Checks a descriptor without launching anything. */
+dck_status dck_validate_quant_desc(const dck_quant_desc* desc);
+
+/*
+ * dck_paged_append to an 8-bit cache: arguments as there, with the caches' codes (16-byte aligned)
+ * and scales (4-byte aligned).  One launch; no workspace.
+ */
+dck_status dck_quant_append(const dck_quant_desc* desc, const dck_rope_table* table, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* v, int64_t v_stride, int32_t n_tok,
+                            const int32_t* d_positions, const int64_t* d_slots, void* q_out, void* kcache,
+                            float* k_scale, void* vcache, float* v_scale, void* stream);
+
+/*
+ * Rows of an 8-bit cache in full width: k[i] and v[i] = code times scale of slot d_slots[i], rounded once to the
+ * descriptor's type (keys stay rotated; dck_rope's transpose turns them back).
+ *   d_slots   device int64 [n_tok], the same slot any number of times; -1 reads as zeros.  Any other
+ *             slot outside the pool reads as zeros too and is recorded as a device error.
+ *   k, v      [n_tok, Hkv, d], k_stride and v_stride elements between tokens (Hkv d or more)
+ * n_tok = 0 is a no-op.  One launch; no workspace.
+ */
+dck_status dck_quant_read(const dck_quant_desc* desc, int32_t n_tok, const int64_t* d_slots, const void* kcache,
+                          const float* k_scale, const void* vcache, const float* v_scale, void* k, int64_t k_stride,
+                          void* v, int64_t v_stride, void* stream);
+
+/*
+ * dck_paged_decode_attention on an 8-bit cache: keys and values are code times scale.  Any finite scales >= 0 do,
+ * powers of two or not.  Codes are multiplied exactly; queries are held to 2^-29 (bf16) or 2^-22 (fp32) of themselves,
+ * or 2^-39 of their row's largest element, and weights to 2^-22 of themselves, or 2^-31 of the largest (2^-11 of
+ * themselves on bf16 calls with more than 8 query heads on a KV head); all sums are fp32.  Otherwise as there.
+ */
+size_t dck_quant_decode_workspace_size(const dck_quant_desc* desc, int32_t batch, int32_t max_seq_len);
+dck_status dck_quant_decode_attention(const dck_quant_desc* desc, const void* q, int64_t q_stride, const void* kcache,
+                                      const float* k_scale, const void* vcache, const float* v_scale,
+                                      const int32_t* block_table, int64_t table_stride, const int32_t* d_seq_len,
+                                      int32_t batch, int32_t max_seq_len, float scale, int32_t window, float softcap,
+                                      void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * The same attention (dck_paged_decode_attention's, dck_quant_decode_attention's) for rows that share the beginnings
+ * of their sequences: requests that begin with one prompt, or the new tokens of one request's chunk, each with its
+ * own position + 1 as length.  What a group's rows share is read once for all of them.
+ *   batch          rows, each with its query, block table row and length
+ *   n_groups       groups of consecutive rows, 1 .. batch (0 if batch is 0)
+ *   d_group_start  device int32 [n_groups + 1]: group g has rows d_group_start[g] .. d_group_start[g + 1] - 1;
+ *                  0 first, batch last, none smaller than the one before
+ *   d_shared_len   device int32 [n_groups]: the tokens that the rows of g share.  Of those a row sees the ones
+ *                  below its length (and in its window): they lie, for all rows, where the block table of the group's
+ *                  longest row (the first of them) has them.  Of groups of one row nothing counts as shared.
+ *   max_own        upper bound on the tokens that a row sees beyond its group's shared ones, 1 .. 2^31 - 1
+ * Other arguments as there.  Results differ from those calls' by roundings only.  A row with more than max_own tokens
+ * of its own is treated like one with a bad length, a page outside the pool like one for every row that sees it; a
+ * shared length below 0 counts as 0 and is recorded; where d_group_start is not as described, every output is zero with
+ * lse = -inf, and it is recorded.  At most three launches; results do not depend on the order in which blocks run.
+ */
+size_t dck_paged_shared_workspace_size(const dck_paged_desc* desc, int32_t batch, int32_t max_seq_len, int32_t max_own);
+dck_status dck_paged_shared_attention(const dck_paged_desc* desc, const void* q, int64_t q_stride, const void* kcache,
+                                      const void* vcache, const int32_t* block_table, int64_t table_stride,
+                                      const int32_t* d_seq_len, int32_t batch, int32_t max_seq_len, int32_t max_own,
+                                      int32_t n_groups, const int32_t* d_group_start, const int32_t* d_shared_len,
+                                      float scale, int32_t window, float softcap, void* out, float* lse, void* workspace,
+                                      size_t ws_bytes, void* stream);
+size_t dck_quant_shared_workspace_size(const dck_quant_desc* desc, int32_t batch, int32_t max_seq_len, int32_t max_own);
+dck_status dck_quant_shared_attention(const dck_quant_desc* desc, const void* q, int64_t q_stride, const void* kcache,
+                                      const float* k_scale, const void* vcache, const float* v_scale,
+                                      const int32_t* block_table, int64_t table_stride, const int32_t* d_seq_len,
+                                      int32_t batch, int32_t max_seq_len, int32_t max_own, int32_t n_groups,
+                                      const int32_t* d_group_start, const int32_t* d_shared_len, float scale,
+                                      int32_t window, float softcap, void* out, float* lse, void* workspace,
+                                      size_t ws_bytes, void* stream);
+
+/*
  * Synchronises `stream`, then returns and clears the device error word of the
  * current device: DCK_OK, DCK_ERR_INVALID (a length or row was outside the
  * cache) or DCK_ERR_TIMEOUT (a bounded wait inside a kernel gave up).

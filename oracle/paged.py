@@ -116,3 +116,41 @@ def paged_decode(q, kcache, vcache, block_table, seq_len, scale, window=0, softc
                 lse[b, j] = m + math.log(e.sum())
                 slack[b, j] = abs(scale) * (np.abs(k) @ np.abs(q[b, j])).max()
     return out, lse, weight, slack
+
+
+def code_values():
+    """The 256 numbers of e4m3 codes: 1 sign, 4 exponent (bias 7) and 3 mantissa bits; all ones: NaN."""
+    out = np.empty(256)
+    for c in range(256):
+        e, f = c >> 3 & 15, c & 7
+        x = math.ldexp(f, -9) if e == 0 else math.ldexp(8 + f, e - 10)
+        out[c] = math.nan if c & 127 == 127 else -x if c & 128 else x
+    return out
+
+
+def quantise(x):
+    """(codes, scales) of rows x [..., d]: the least power of two (2^-126 at least) that leaves no magnitude above 448 of it,
+    and of each quotient the nearest code, ties to even; infinities and NaN count as 0 there and become NaN."""
+    x = np.asarray(x, dtype=np.float64)
+    table = code_values()[:127]
+    middle = (table[1:] + table[:-1]) / 2
+    codes, scales = np.empty(x.shape, dtype=np.uint8), np.empty(x.shape[:-1])
+    for at in np.ndindex(*x.shape[:-1]):
+        row = x[at]
+        fine = np.isfinite(row)
+        top = np.abs(row[fine]).max() if fine.any() else 0.0
+        e = -126
+        while top > 448 * 2.0 ** e:
+            e += 1
+        y = np.abs(np.where(fine, row, 0.0)) / 2.0 ** e
+        c = np.searchsorted(middle, y, side="left")  # at a middle: the lower one
+        c = c + ((c < 126) & (y == middle[np.minimum(c, 125)]) & (c % 2 == 1))
+        c = np.where(fine, c, 127)
+        codes[at] = c | np.where(np.signbit(row), 128, 0)
+        scales[at] = 2.0 ** e
+    return codes, scales
+
+
+def stand_for(codes, scales):
+    """The values of an 8-bit cache."""
+    return code_values()[np.asarray(codes)] * np.asarray(scales, dtype=np.float64)[..., None]

@@ -30,6 +30,8 @@ struct PagedView {
   int32_t Hq, Hkv, d, qpg, page, n_pages;
   uint32_t k_page_b, k_tok_b, k_head_b, v_page_b, v_tok_b, v_head_b;  // strides, in bytes
   Divider by_page;
+  // 8-bit caches: the strides of the scales, in elements
+  uint32_t ks_page, ks_tok, ks_head, vs_page, vs_tok, vs_head;
 };
 
 // The rotation, by value (dck_rope_table).
@@ -68,6 +70,8 @@ struct RopeRows {
   int32_t rotate;  // 0: copy
   int32_t cached;  // dst is a cache: rows by slot (dst_tok between a page's tokens, dst_page between pages)
   int64_t dst_page;
+  float* scale;  // not null: dst is an 8-bit cache (strides in bytes), this its scales
+  int64_t scale_page, scale_tok, scale_head;
 };
 struct RopeLaunch {
   RopeRows rows[3];
@@ -80,6 +84,19 @@ struct RopeLaunch {
   RopeArgs rope;
 };
 cudaError_t launch_rope_rows(const RopeLaunch& a, int dtype, int sms, cudaStream_t s);
+
+// Rows of an 8-bit cache in full width.
+struct QuantReadArgs {
+  PagedView v;
+  int32_t n_tok;
+  const int64_t* slots;
+  const void *kc, *vc;
+  const float *ks, *vs;
+  void *k, *v_out;
+  int64_t k_stride, v_stride;
+  int* err;
+};
+cudaError_t launch_quant_read(const QuantReadArgs& a, int dtype, int sms, cudaStream_t s);
 
 struct PagedDecodeArgs {
   PagedView v;
@@ -97,8 +114,19 @@ struct PagedDecodeArgs {
   void* ws;
   int* err;
   LaunchHook* hook;
+  const float *ks, *vs;  // 8-bit caches: the scales
+  // calls over shared prefixes: rows group_start[g] .. group_start[g + 1] - 1 share their first shared_len[g] tokens
+  int32_t n_groups, max_own;
+  const int32_t *group_start, *shared_len;
 };
-size_t paged_decode_workspace(const PagedView& v, int dtype, int B, int max_len, int sms);
-cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cudaStream_t s);
+// What an attention call works on: the type of queries and outputs, and whether caches are 8-bit.
+struct DecodeKind {
+  int dtype;
+  bool quant;
+};
+size_t paged_decode_workspace(const PagedView& v, DecodeKind kind, int B, int max_len, int sms);
+cudaError_t launch_paged_decode(const PagedDecodeArgs& a, DecodeKind kind, int sms, cudaStream_t s);
+size_t paged_shared_workspace(const PagedView& v, DecodeKind kind, int B, int max_len, int max_own, int sms);
+cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int sms, cudaStream_t s);
 
 }  // namespace dck

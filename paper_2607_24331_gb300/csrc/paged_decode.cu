@@ -245,23 +245,24 @@ cudaError_t launch_join(const Args& g, int sms, cudaStream_t s) {
 //   1 x 128   6.9 /  4.6 /  4.4     16 x 512       13.6 /  8.4 / 10.5    64 x 256        21 / - / 15
 //   1 x 1024  9.1 /  6.4 / 14.6     16 x 4096      49.8 / 46.3 / 56      64 x 2048       87 / - / 83
 //   4 x 4096 18.6 / 17.4 / 58       16 x 128..2048 17.3 / 16.1 / 21      64 x 128..2048  37 / - / 44
-Plan plan_of(const PagedView& v, int dtype, int B, int max_len, int window, int sms) {
+Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window, int sms) {
   Plan p;
-  const int DP = padded_dim(v.d);
+  const int DP = padded_dim(v.d), dtype = kind.dtype;
   const int most = dtype == DCK_BF16 && DP <= 128 && v.qpg > 8 ? 16 : 8;
   p.chunks = (v.qpg + most - 1) / most;
   p.rows = (v.qpg + p.chunks - 1) / p.chunks;
   p.by_chunks = divider((uint32_t)p.chunks);
   p.alike = v.k_page_b == v.v_page_b && v.k_tok_b == v.v_tok_b && v.k_head_b == v.v_head_b;
-  const int heads = v.Hkv * p.chunks, few = warps_of(DP, false), many = warps_of(DP, true), run = run_of(dtype);
+  const int el = kind.quant ? 1 : dtype == DCK_BF16 ? 2 : 4;  // bytes of a cached element
+  const int heads = v.Hkv * p.chunks, few = warps_of(DP, false), many = warps_of(DP, true), run = run_of(kind);
   const int64_t span = window > 0 ? std::min(window, max_len) : max_len, pairs = (int64_t)heads * std::max(B, 1);
   const auto tiles_of = [&](int tokens) { return (span + tokens - 1) / tokens; };
   int wide = few;  // heads side by side in a CTA, at most
   while (heads % wide) wide /= 2;
 
-  const int row = DP * (dtype == DCK_BF16 ? 2 : 4), slots = kPerSm * sms;
+  const int row = DP * el, slots = kPerSm * sms;
   const double step = row <= 128 ? 0.45 : row == 256 ? 0.65 : row == 512 ? 0.95 : 1.37;  // a warp's run of tokens
-  const double bytes = 1.07 * 2. * B * span * v.Hkv * v.d * (dtype == DCK_BF16 ? 2 : 4) / 6.8e6;
+  const double bytes = 1.07 * 2. * B * span * v.Hkv * (v.d * el + (kind.quant ? 4 : 0)) / 6.8e6;
   // (product of the two times) of a way with a fixed part and the longest CTA's part
   const auto times = [&](double fixed, double longest) {
     return (fixed + std::max(longest, bytes)) * (fixed + std::max(longest, 0.34 * bytes));
@@ -301,25 +302,25 @@ size_t bytes_u(const Plan& p, int DP) { return align_up((size_t)2 * p.n_items * 
 
 using namespace paged;
 
-size_t paged_decode_workspace(const PagedView& v, int dtype, int B, int max_len, int sms) {
-  const Plan p = plan_of(v, dtype, std::max(B, 1), max_len, 0, sms);  // a window only takes CTAs away
+size_t paged_decode_workspace(const PagedView& v, DecodeKind kind, int B, int max_len, int sms) {
+  const Plan p = plan_of(v, kind, std::max(B, 1), max_len, 0, sms);  // a window only takes CTAs away
   return bytes_entries(p) + bytes_ml(p) + bytes_u(p, padded_dim(v.d));
 }
 
-cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int dtype, int sms, cudaStream_t s) {
+cudaError_t launch_paged_decode(const PagedDecodeArgs& a, DecodeKind kind, int sms, cudaStream_t s) {
   Args g;
   g.a = a;
-  g.p = plan_of(a.v, dtype, a.B, a.max_len, a.window, sms);
+  g.p = plan_of(a.v, kind, a.B, a.max_len, a.window, sms);
   g.DP = padded_dim(a.v.d);
   g.score.set(a.scale, a.softcap);
-  const int el = dtype == DCK_F32 ? 4 : 2;
+  const int dtype = kind.dtype, el = dtype == DCK_F32 ? 4 : 2;
   g.p.q_copied = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride * el % 16 == 0;
   char* ws = static_cast<char*>(a.ws);
   g.entries = reinterpret_cast<Entry*>(ws);
   ws += bytes_entries(g.p);
   g.part_ml = reinterpret_cast<float*>(ws);
   g.part_u = reinterpret_cast<float*>(ws + bytes_ml(g.p));
-  cudaError_t e = dtype == DCK_F32 ? launch_f32(g, s) : launch_bf16(g, s);
+  cudaError_t e = kind.quant ? launch_q8(g, dtype, s) : dtype == DCK_F32 ? launch_f32(g, s) : launch_bf16(g, s);
   if (e != cudaSuccess || g.p.cluster) return e;
   // one tile per (head group, sequence) at most: nothing is shared
   if ((a.window > 0 ? std::min(a.window, a.max_len) : a.max_len) <= g.p.tile) return cudaSuccess;

@@ -81,12 +81,13 @@ struct Args {
 
 cudaError_t launch_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_f32(const Args& g, cudaStream_t s);
+cudaError_t launch_q8(const Args& g, int dtype, cudaStream_t s);
 
 inline int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // Warps of a CTA: two CTAs per SM fill its shared memory with rings, or one of twice the warps.
 constexpr int warps_of(int DP, bool one_per_sm) { return (DP == 256 ? 2 : 4) * (one_per_sm ? 2 : 1); }
 constexpr int kPerSm = 2;
-inline int run_of(int dtype) { return dtype == DCK_BF16 ? 16 : 8; }  // tokens of a warp's step
+inline int run_of(DecodeKind k) { return k.quant ? 32 : k.dtype == DCK_BF16 ? 16 : 8; }  // tokens of a warp's step
 
 // Visible tokens of sequence b and the first of them; 0 for invalid lengths.
 __device__ __forceinline__ int visible(const PagedDecodeArgs& a, int b, int& first, bool& bad) {
@@ -225,8 +226,10 @@ template <typename T_, int DP_, int NW_, int S_, int TOK_>
 struct Sizes {
   using T = T_;
   static constexpr int DP = DP_, NW = NW_, S = S_, TOK = TOK_;
+  static constexpr bool kQuant = false;
   static constexpr int kRow = DP * sizeof(T);   // bytes of a head's row
   static constexpr int kChunks = kRow / 16;     // 16-byte chunks of it
+  static constexpr int kQRow = kRow;            // bytes of a query
   static constexpr int kHalf = TOK * kRow;      // a stage's keys (values: the same)
   static constexpr int kStage = 2 * kHalf;
   static constexpr int kRing = NW * S * kStage;
@@ -248,29 +251,21 @@ struct Pages {
   int b;          // the sequence whose queries come with this tile, or -1
 };
 
-// ROWS: queries of a warp; they are copied along with the first tile of a (head group,
-// sequence), QS places for them per warp.
+// What copies have in common, whatever the caches' type.  ROWS: queries of a warp; they are
+// copied along with the first tile of a (head group, sequence), QS places for them per warp.
 template <class Z, int ROWS, int QS>
-struct Loader {
+struct LoaderBase {
   static constexpr int el = sizeof(typename Z::T);
-  static constexpr int kPlace = ROWS * Z::kRow;
+  static constexpr int kPlace = ROWS * Z::kQRow;
+  static constexpr int kQChunks = Z::kQRow / 16;
   const Args& g;
-  const char *kc, *vc;    // with this lane's chunk
   uint32_t ring, places;     // this warp's stages and places
-  uint32_t even, odd;        // where this lane's chunk of rows 4 i + sub lies in a stage, i even or odd
   int lane, run, wh;      // run: the warp's first token of a tile
-  int have;               // chunks of a row from this lane's first on
 
-  __device__ __forceinline__ Loader(const Args& g, const uint8_t* raw, const void* q, int warp, int lane, int wh, int wt)
+  __device__ __forceinline__ LoaderBase(const Args& g, const uint8_t* raw, const void* q, int warp, int lane, int wh, int wt)
       : g(g), lane(lane), run(wt * Z::TOK), wh(wh) {
-    const int sub = lane >> 3, c = lane & 7;
-    kc = static_cast<const char*>(g.a.kc) + c * 16;
-    vc = static_cast<const char*>(g.a.vc) + c * 16;
     ring = (uint32_t)__cvta_generic_to_shared(raw) + warp * Z::S * Z::kStage;
     places = (uint32_t)__cvta_generic_to_shared(q) + warp * QS * kPlace;
-    even = sub * Z::kRow + (c ^ sub) * 16;
-    odd = sub * Z::kRow + (c ^ (sub + 4)) * 16;
-    have = g.a.v.d * el / 16 - c;
   }
 
   // Heads shorter than the variant's: the rest of each row stays zero.
@@ -305,11 +300,11 @@ struct Loader {
     const int row_bytes = g.a.v.d * el;
     const uint32_t to = places + at * kPlace;
 #pragma unroll
-    for (int i = 0; i < ROWS * Z::kChunks / 32 + (ROWS * Z::kChunks % 32 != 0); ++i) {
-      const int x = i * 32 + lane, row = x / Z::kChunks, c = x % Z::kChunks;
+    for (int i = 0; i < ROWS * kQChunks / 32 + (ROWS * kQChunks % 32 != 0); ++i) {
+      const int x = i * 32 + lane, row = x / kQChunks, c = x % kQChunks;
       const bool have = row < qs.count && c * 16 < row_bytes;
-      if (ROWS * Z::kChunks % 32 == 0 || row < ROWS)
-        cp_async16_or_zero(to + row * Z::kRow + (c ^ (row & 7)) * 16, q + (have ? row * row_bytes + c * 16 : 0),
+      if (ROWS * kQChunks % 32 == 0 || row < ROWS)
+        cp_async16_or_zero(to + row * Z::kQRow + (c ^ (row & 7)) * 16, q + (have ? row * row_bytes + c * 16 : 0),
                            have ? 16 : 0);
     }
   }
@@ -326,12 +321,32 @@ struct Loader {
     }
     __syncwarp();
   }
+};
+
+// Copies of bf16 and fp32 rows.
+template <class Z, int ROWS, int QS>
+struct Loader : LoaderBase<Z, ROWS, QS> {
+  using Base = LoaderBase<Z, ROWS, QS>;
+  using Base::el, Base::g, Base::lane, Base::ring, Base::wh;
+  const char *kc, *vc;    // with this lane's chunk
+  uint32_t even, odd;        // where this lane's chunk of rows 4 i + sub lies in a stage, i even or odd
+  int have;               // chunks of a row from this lane's first on
+
+  __device__ __forceinline__ Loader(const Args& g, const uint8_t* raw, const void* q, int warp, int lane, int wh, int wt)
+      : Base(g, raw, q, warp, lane, wh, wt) {
+    const int sub = lane >> 3, c = lane & 7;
+    kc = static_cast<const char*>(g.a.kc) + c * 16;
+    vc = static_cast<const char*>(g.a.vc) + c * 16;
+    even = sub * Z::kRow + (c ^ sub) * 16;
+    odd = sub * Z::kRow + (c ^ (sub + 4)) * 16;
+    have = g.a.v.d * el / 16 - c;
+  }
 
   // Starts the copies of a stage; true if a page lies outside the pool (its tokens read as
   // zeros).  Eight lanes copy 128 bytes of a row, a warp four rows at a time.
   __device__ __forceinline__ bool issue(const Pages& r, int stage) const {
     const PagedView& v = g.a.v;
-    if (QS > 1 && r.b >= 0 && g.p.q_copied) copy_queries(r, stage);
+    if (QS > 1 && r.b >= 0 && g.p.q_copied) this->copy_queries(r, stage);
     const uint32_t head = g.p.by_chunks.div(r.group * g.p.wh + wh);
     const bool inside = (uint32_t)r.page < (uint32_t)v.n_pages, ok = inside && r.off >= 0;
     const uint32_t page = inside ? r.page : 0, off = max(r.off, 0);
@@ -358,6 +373,12 @@ struct Loader {
     }
     return __any_sync(~0u, !inside);
   }
+};
+
+// The loader of a variant.
+template <class Z, int ROWS, int QS>
+struct LoaderOf {
+  using type = Loader<Z, ROWS, QS>;
 };
 
 // tanh to 3e-7 of its value: below 1/2 an odd polynomial (least squares in x^2 on
@@ -814,10 +835,10 @@ template <class Z, class Tile, bool CLUSTER>
 struct Shared {  // after the rings
   // places for queries: as many segments as tiles are copied ahead
   static constexpr int kPlaces = CLUSTER ? 1 : Z::S;
-  alignas(16) uint8_t q[Z::NW * kPlaces * Tile::kRows * Z::kRow];
+  alignas(16) uint8_t q[Z::NW * kPlaces * Tile::kRows * Z::kQRow];
   float4 part[CLUSTER ? Tile::kRows * Z::DP / 4 : 1];  // of the cluster's CTAs, this one's share of the elements
   float2 cluster_ml[CLUSTER ? kMaxCluster : 1][Tile::kRows];
-  alignas(16) float mine[std::is_same<typename Z::T, float>::value ? Z::NW * 8 * Tile::kRows : 4];  // fp32: a warp's weights
+  alignas(16) float mine[std::is_same<typename Z::T, float>::value && !Z::kQuant ? Z::NW * 8 * Tile::kRows : 4];  // fp32: a warp's weights
   alignas(16) float2 ml[Z::NW][Tile::kRows];  // sum -1: a page outside the pool
 };
 
@@ -882,7 +903,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   Walk ahead;
   bool begins = true;  // the first (head group, sequence) is this CTA's from its first tile on
   uint32_t rank = 0;
-  const Loader<Z, Tile::kRows, Shm::kPlaces> load(g, raw, sh.q, warp, lane, wh, wt);
+  const typename LoaderOf<Z, Tile::kRows, Shm::kPlaces>::type load(g, raw, sh.q, warp, lane, wh, wt);
   load.clear(raw);
   if (CLUSTER) {
     cluster_arrive();  // remote stores must find the other CTAs running: waited for before the first

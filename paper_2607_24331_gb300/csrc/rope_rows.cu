@@ -1,7 +1,12 @@
 // Rotary positions (dck_rope) and the rotated append to a paged cache
-// (dck_paged_append).  A pair (x, y) of a head's elements at position t becomes
+// (dck_paged_append, dck_quant_append).  A pair (x, y) of a head's elements at position t becomes
 //   m (x cos a - y sin a, x sin a + y cos a),  a = t w_i  (sin negated: the transpose).
+// For an 8-bit cache a head's row, rounded to its type, is then divided by the least power of two
+// that leaves no magnitude above 448 and rounded to e4m3: the threads that hold it share the largest
+// magnitude by shuffles, so that this too reads and writes every element once.
 // Bound by memory: each element is read and written once.
+#include <math_constants.h>
+
 #include <algorithm>
 
 #include "paged.cuh"
@@ -38,8 +43,29 @@ __device__ __forceinline__ CacheRow cache_row(const RopeLaunch& a, int64_t i, bo
   return r;
 }
 
+// 8-bit rows.  Magnitudes are compared as the integers of their bits; infinities and NaN count as 0
+// there and are stored as NaN.
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+  return u < 0x7f800000u ? u : 0u;
+}
+// The exponent e >= -126 of the scale 2^e of a row with largest magnitude `top`: the least with
+// top <= 448 2^e.  448 = 1.75 2^8: mantissas above 1.75 carry into the exponent.
+__device__ __forceinline__ int scale_exponent(uint32_t top) { return max((int)((top + 0x1fffffu) >> 23) - 135, -126); }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 .. 127
+// Two codes (x the lower) of elements divided by 2^e, `inverse` 2^-e.
+__device__ __forceinline__ uint32_t codes2(float x, float y, float inverse) {
+  const float a = fabsf(x) < CUDART_INF_F ? x * inverse : CUDART_NAN_F, b = fabsf(y) < CUDART_INF_F ? y * inverse : CUDART_NAN_F;
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ float rounded(float x) { return to_f32(from_f32<T>(x)); }
+
 // Any rotary dimension, stride and alignment: a block per token, a thread per pair of
-// elements (or single element past the rotary dimension).
+// elements (or single element past the rotary dimension), a warp per head of an 8-bit cache.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rope_any_kernel(const __grid_constant__ RopeLaunch a) {
   pdl_launch_dependents();
@@ -50,6 +76,44 @@ __global__ void __launch_bounds__(kThreads) rope_any_kernel(const __grid_constan
   for (int r = 0; r < a.n_rows; ++r) {
     const RopeRows& rows = a.rows[r];
     if (rows.cached && !to.have) continue;
+    if (rows.scale) {
+      constexpr int kMost = kMaxPagedHeadDim / 32;  // elements per lane
+      const int lane = threadIdx.x & 31, half = rows.rotate ? a.rope.rot / 2 : 0;
+      const bool halves = a.rope.layout == DCK_ROPE_HALF;
+      for (int h = threadIdx.x >> 5; h < rows.heads; h += kThreads / 32) {
+        const T* sp = static_cast<const T*>(rows.src) + i * rows.src_tok + h * rows.src_head;
+        float x[kMost];
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < kMost; ++k) {
+          const int e = lane + 32 * k;
+          x[k] = 0.f;
+          if (e < 2 * half) {  // one of pair j's elements
+            const int j = halves ? (e < half ? e : e - half) : e / 2;
+            const bool second = halves ? e >= half : e & 1;
+            float sn, cs;
+            signed_sincos(a.rope.f[j], pos, sn, cs);
+            sn *= a.rope.sign * a.rope.magnitude;
+            cs *= a.rope.magnitude;
+            const float u = to_f32(sp[halves ? j : 2 * j]), w = to_f32(sp[halves ? j + half : 2 * j + 1]);
+            x[k] = rounded<T>(second ? u * sn + w * cs : u * cs - w * sn);
+          } else if (e < a.d) {
+            x[k] = to_f32(sp[e]);
+          }
+          top = max(top, finite_bits(x[k]));
+        }
+        top = __reduce_max_sync(~0u, top);
+        const int s = scale_exponent(top);
+        const float inverse = power_of_two(-s);
+        uint8_t* dp = static_cast<uint8_t*>(rows.dst) + to.page * rows.dst_page + to.off * rows.dst_tok + h * rows.dst_head;
+#pragma unroll
+        for (int k = 0; k < kMost; ++k)
+          if (lane + 32 * k < a.d) dp[lane + 32 * k] = (uint8_t)codes2(x[k], 0.f, inverse);
+        if (lane == 0)
+          rows.scale[to.page * rows.scale_page + to.off * rows.scale_tok + h * rows.scale_head] = power_of_two(s);
+      }
+      continue;
+    }
     const T* src = static_cast<const T*>(rows.src) + i * rows.src_tok;
     T* dst = static_cast<T*>(rows.dst) + (rows.cached ? to.page * rows.dst_page + to.off * rows.dst_tok : i * rows.dst_tok);
     const int half = rows.rotate ? a.rope.rot / 2 : 0;
@@ -117,28 +181,30 @@ struct Vec<__nv_bfloat16> {
 struct VecLaunch {
   int turned;   // units of pairs per head
   int units;    // units per head
+  int lanes;    // threads per head: as many, or for 8-bit caches the next power of two
   int across;   // heads that a block's threads cover at a time
   int tokens;   // tokens per block
   int heads;    // heads of all row sets
-  Divider by_units, by_heads, by_turned;
+  Divider by_lanes, by_heads, by_turned;
 };
 constexpr int kRounds = 2;  // units per thread that a block's tokens are chosen for (1, 4 or 8: 43, 44, 48 us there)
 
-template <typename T, bool HALF>
-__global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_constant__ RopeLaunch a,
+template <typename T, bool HALF, bool QUANT>
+__global__ void __launch_bounds__(kThreads, QUANT ? 5 : 6) rope_vec_kernel(const __grid_constant__ RopeLaunch a,
                                                                const __grid_constant__ VecLaunch v) {
   constexpr int N = Vec<T>::N;
   // [tokens][N][turned] (cos, sin) of pair j N + k at k turned + j; then the tokens' cache rows
   extern __shared__ float2 turn[];
   const int pairs = a.rope.rot / 2;
   CacheRow* rows_to = reinterpret_cast<CacheRow*>(turn + v.tokens * pairs);
-  const int tid = threadIdx.x, h0 = v.by_units.div(tid), j = tid - h0 * v.units;
+  const int tid = threadIdx.x, h0 = v.by_lanes.div(tid), j = tid - h0 * v.lanes;
   const int64_t first = (int64_t)blockIdx.x * v.tokens;
   const int n_here = (int)min((int64_t)v.tokens, a.n_tok - first), n_heads = n_here * v.heads;
   // the unit's two vectors: pairs (x, y) side by side or half the rotary dimension apart
   const int past = 2 * v.turned + 2 * (j - v.turned);
   const int va = (j >= v.turned ? past : HALF ? j : 2 * j) * N, vb = (j >= v.turned ? past + 1 : HALF ? j + v.turned : 2 * j + 1) * N;
-  const bool two = vb < a.d;
+  const bool one = !QUANT || va < a.d, two = vb < a.d;
+  const uint32_t sharers = QUANT ? (v.lanes < 32 ? ((1u << v.lanes) - 1) << (tid & 31 & -v.lanes) : ~0u) : 0;
 
   int next = h0 < v.across ? h0 : n_heads, t, head, set;
   uint4 x, y;
@@ -149,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_cons
     set = 0;
     while (set + 1 < a.n_rows && head >= a.rows[set].heads) head -= a.rows[set++].heads;
     const T* src = static_cast<const T*>(a.rows[set].src) + (first + t) * a.rows[set].src_tok + head * a.rows[set].src_head;
-    x = *reinterpret_cast<const uint4*>(src + va);
+    if (one) x = *reinterpret_cast<const uint4*>(src + va);
     if (two) y = *reinterpret_cast<const uint4*>(src + vb);
   };
   pdl_launch_dependents();
@@ -172,10 +238,9 @@ __global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_cons
       if (!to.have) continue;
       at = to.page * rows.dst_page + to.off * rows.dst_tok;
     }
-    T* dst = static_cast<T*>(rows.dst) + at + head * rows.dst_head;
+    float p[N], q[N];
     if (rows.rotate && j < v.turned) {
       const float2* cs = turn + t * pairs + j;
-      float p[N], q[N];
       Vec<T>::open(x, p);
       Vec<T>::open(y, q);
 #pragma unroll
@@ -190,6 +255,37 @@ __global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_cons
       x = Vec<T>::close(p);
       y = Vec<T>::close(q);
     }
+    if (QUANT && rows.scale) {
+      Vec<T>::open(one ? x : make_uint4(0, 0, 0, 0), p);  // what was rounded to T
+      Vec<T>::open(two ? y : make_uint4(0, 0, 0, 0), q);
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < N; ++k) top = max(top, max(finite_bits(p[k]), finite_bits(q[k])));
+      for (int o = v.lanes / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(sharers, top, o));
+      const int e = scale_exponent(top);
+      const float inverse = power_of_two(-e);
+      uint8_t* dst = static_cast<uint8_t*>(rows.dst) + at + head * rows.dst_head;
+      uint32_t c[N / 2];
+#pragma unroll
+      for (int k = 0; k < N / 4; ++k) {
+        c[k] = codes2(p[4 * k], p[4 * k + 1], inverse) | codes2(p[4 * k + 2], p[4 * k + 3], inverse) << 16;
+        c[N / 4 + k] = codes2(q[4 * k], q[4 * k + 1], inverse) | codes2(q[4 * k + 2], q[4 * k + 3], inverse) << 16;
+      }
+      if (N == 8) {
+        if (one) *reinterpret_cast<uint2*>(dst + va) = make_uint2(c[0], c[1]);
+        if (two) *reinterpret_cast<uint2*>(dst + vb) = make_uint2(c[N / 4], c[N / 4 + 1 < N / 2 ? N / 4 + 1 : 0]);
+      } else {
+        if (one) *reinterpret_cast<uint32_t*>(dst + va) = c[0];
+        if (two) *reinterpret_cast<uint32_t*>(dst + vb) = c[N / 4];
+      }
+      if (j == 0) {
+        const CacheRow to = rows_to[t];
+        rows.scale[to.page * rows.scale_page + to.off * rows.scale_tok + head * rows.scale_head] = power_of_two(e);
+      }
+      continue;
+    }
+    T* dst = static_cast<T*>(rows.dst) + at + head * rows.dst_head;
+    if (!one) continue;
     *reinterpret_cast<uint4*>(dst + va) = x;
     if (two) *reinterpret_cast<uint4*>(dst + vb) = y;
   }
@@ -200,21 +296,26 @@ bool vec_plan(const RopeLaunch& a, int sms, VecLaunch* v) {
   constexpr int N = Vec<T>::N;
   if (a.d % N || a.rope.rot % (2 * N)) return false;
   v->heads = 0;
+  bool quant = false;
   for (int r = 0; r < a.n_rows; ++r) {
     const RopeRows& w = a.rows[r];
     if (reinterpret_cast<uintptr_t>(w.src) % 16 || reinterpret_cast<uintptr_t>(w.dst) % 16) return false;
-    for (int64_t st : {w.src_tok, w.src_head, w.dst_tok, w.dst_head, w.dst_page})
+    for (int64_t st : {w.src_tok, w.src_head, w.dst_tok, w.dst_head, w.dst_page})  // (8-bit caches: multiples of 16)
       if (st % N) return false;
+    quant |= w.scale != nullptr;
     v->heads += w.heads;
   }
   v->turned = a.rope.rot / (2 * N);
   v->units = v->turned + ((a.d - a.rope.rot) / N + 1) / 2;
-  if (v->units > kThreads) return false;
-  v->across = kThreads / v->units;
+  if (v->units > (quant ? 32 : kThreads)) return false;
+  v->lanes = v->units;
+  if (quant)
+    for (v->lanes = 1; v->lanes < v->units;) v->lanes *= 2;
+  v->across = kThreads / v->lanes;
   // as many tokens as give every thread a few units, if eight blocks per SM remain
   const int64_t full = (kRounds * v->across + v->heads - 1) / v->heads, one = (v->across + v->heads - 1) / v->heads;
   v->tokens = (int)std::min<int64_t>(std::max<int64_t>(std::min(full, (int64_t)a.n_tok / (8 * sms)), one), a.n_tok);
-  v->by_units = divider(v->units);
+  v->by_lanes = divider(v->lanes);
   v->by_heads = divider(v->heads);
   v->by_turned = divider(std::max(1, v->turned));
   return true;
@@ -228,8 +329,10 @@ cudaError_t launch(const RopeLaunch& a, int sms, cudaStream_t s) {
   }
   const int64_t grid = ((int64_t)a.n_tok + v.tokens - 1) / v.tokens;
   const size_t smem = (size_t)v.tokens * (a.rope.rot / 2 * sizeof(float2) + sizeof(CacheRow));
-  return launch_pdl(a.rope.layout == DCK_ROPE_HALF ? rope_vec_kernel<T, true> : rope_vec_kernel<T, false>, (unsigned)grid, kThreads,
-                    smem, s, a, v);
+  const bool half = a.rope.layout == DCK_ROPE_HALF;
+  const auto k = a.rows[0].scale ? (half ? rope_vec_kernel<T, true, true> : rope_vec_kernel<T, false, true>)
+                                 : (half ? rope_vec_kernel<T, true, false> : rope_vec_kernel<T, false, false>);
+  return launch_pdl(k, (unsigned)grid, kThreads, smem, s, a, v);
 }
 
 }  // namespace

@@ -31,6 +31,9 @@ EXPORTED = (
     "dck_selftest_bounded_wait", "dck_selftest_append_timeout", "dck_decode_step", "dck_decode_step_workspace_size",
     "dck_prefill_workspace_size", "dck_prefill_attention", "dck_validate_paged_desc", "dck_page_update",
     "dck_rope_init", "dck_rope", "dck_paged_append", "dck_paged_decode_workspace_size", "dck_paged_decode_attention",
+    "dck_validate_quant_desc", "dck_quant_append", "dck_quant_read", "dck_quant_decode_workspace_size",
+    "dck_quant_decode_attention", "dck_paged_shared_workspace_size", "dck_paged_shared_attention",
+    "dck_quant_shared_workspace_size", "dck_quant_shared_attention",
 )
 
 
@@ -59,6 +62,11 @@ class PagedDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "dtype")] + [
         (n, ctypes.c_int64) for n in ("k_page_stride", "k_token_stride", "k_head_stride", "v_page_stride",
                                       "v_token_stride", "v_head_stride")]
+
+
+class QuantDesc(ctypes.Structure):
+    _fields_ = [("cache", PagedDesc)] + [(f"{c}_scale_{n}_stride", ctypes.c_int64) for c in "kv"
+                                         for n in ("page", "token", "head")]
 
 
 class RopeTable(ctypes.Structure):
@@ -131,6 +139,27 @@ def lib() -> ctypes.CDLL:
     L.dck_paged_decode_workspace_size.argtypes = [G, I32, I32]
     L.dck_paged_decode_attention.restype = I32
     L.dck_paged_decode_attention.argtypes = [G, P, I64, P, P, P, I64, P, I32, I32, F32, I32, F32, P, P, P, SZ, P]
+    Q8 = ctypes.POINTER(QuantDesc)
+    L.dck_validate_quant_desc.restype = I32
+    L.dck_validate_quant_desc.argtypes = [Q8]
+    L.dck_quant_append.restype = I32
+    L.dck_quant_append.argtypes = [Q8, R, P, I64, P, I64, P, I64, I32, P, P, P, P, P, P, P, P]
+    L.dck_quant_read.restype = I32
+    L.dck_quant_read.argtypes = [Q8, I32, P, P, P, P, P, P, I64, P, I64, P]
+    L.dck_quant_decode_workspace_size.restype = SZ
+    L.dck_quant_decode_workspace_size.argtypes = [Q8, I32, I32]
+    L.dck_quant_decode_attention.restype = I32
+    L.dck_quant_decode_attention.argtypes = [Q8, P, I64, P, P, P, P, P, I64, P, I32, I32, F32, I32, F32, P, P, P, SZ, P]
+    L.dck_paged_shared_workspace_size.restype = SZ
+    L.dck_paged_shared_workspace_size.argtypes = [G, I32, I32, I32]
+    L.dck_paged_shared_attention.restype = I32
+    L.dck_paged_shared_attention.argtypes = [G, P, I64, P, P, P, I64, P, I32, I32, I32, I32, P, P, F32, I32, F32, P, P, P, SZ,
+                                             P]
+    L.dck_quant_shared_workspace_size.restype = SZ
+    L.dck_quant_shared_workspace_size.argtypes = [Q8, I32, I32, I32]
+    L.dck_quant_shared_attention.restype = I32
+    L.dck_quant_shared_attention.argtypes = [Q8, P, I64, P, P, P, P, P, I64, P, I32, I32, I32, I32, P, P, F32, I32, F32, P, P,
+                                             P, SZ, P]
     _lib = L
     return L
 
@@ -197,6 +226,39 @@ class PagedCache:
             raise ValueError("the elements of a head must be consecutive")
         n_pages, page_size, n_kv_heads, head_dim = kcache.shape
         return cls(n_q_heads, n_kv_heads, head_dim, page_size, n_pages, name, kcache.stride()[:3], vcache.stride()[:3])
+
+
+class QuantCache:
+    """A dck_quant_desc: an 8-bit key-value cache in pages, e4m3 codes and a scale for each token and head.
+
+    ``dtype`` is the type of queries, new keys and values, outputs and what is read back.  Strides of codes as in
+    PagedCache (in bytes); those of scales by default of dense [n_pages, page_size, n_kv_heads] arrays.
+    """
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, dtype: str,
+                 k_strides: Optional[Sequence[int]] = None, v_strides: Optional[Sequence[int]] = None,
+                 k_scale_strides: Optional[Sequence[int]] = None, v_scale_strides: Optional[Sequence[int]] = None):
+        cache = PagedCache(n_q_heads, n_kv_heads, head_dim, page_size, n_pages, dtype, k_strides, v_strides)
+        dense = (page_size * n_kv_heads, n_kv_heads, 1)
+        self.desc = QuantDesc(cache.desc, *(k_scale_strides or dense), *(v_scale_strides or dense))
+        self.ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def from_tensors(cls, kcache, k_scale, vcache, v_scale, n_q_heads: int, dtype: str) -> "QuantCache":
+        """The descriptor of torch caches (or views) [n_pages, page_size, n_kv_heads, head_dim], uint8 or float8_e4m3fn,
+        whose head elements are consecutive, and scales [n_pages, page_size, n_kv_heads], float32."""
+        names = ("torch.uint8", "torch.float8_e4m3fn")
+        if (kcache.shape != vcache.shape or kcache.dim() != 4 or str(kcache.dtype) not in names or
+                str(vcache.dtype) not in names):
+            raise ValueError("kcache and vcache: [n_pages, page_size, n_kv_heads, head_dim], uint8 or float8_e4m3fn")
+        if (tuple(k_scale.shape) != tuple(kcache.shape[:3]) or tuple(v_scale.shape) != tuple(kcache.shape[:3]) or
+                str(k_scale.dtype) != "torch.float32" or str(v_scale.dtype) != "torch.float32"):
+            raise ValueError("k_scale and v_scale: [n_pages, page_size, n_kv_heads], float32")
+        if kcache.stride(3) != 1 or vcache.stride(3) != 1:
+            raise ValueError("the elements of a head must be consecutive")
+        n_pages, page_size, n_kv_heads, head_dim = kcache.shape
+        return cls(n_q_heads, n_kv_heads, head_dim, page_size, n_pages, dtype, kcache.stride()[:3], vcache.stride()[:3],
+                   k_scale.stride(), v_scale.stride())
 
 
 class Rope:
@@ -340,6 +402,70 @@ def dck_paged_decode_attention(cache: PagedCache, q, q_stride: int, kcache, vcac
                                             _ptr(block_table), table_stride, _ptr(seq_len), batch,
                                             max_seq_len, scale, window, softcap, _ptr(out),
                                             _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream))
+
+
+def dck_validate_quant_desc(cache: QuantCache) -> int:
+    return lib().dck_validate_quant_desc(cache.ref)
+
+
+def dck_quant_append(cache: QuantCache, rope: Optional[Rope], q, q_stride: int, k, k_stride: int, v, v_stride: int,
+                     n_tok: int, positions, slots, q_out, kcache, k_scale, vcache, v_scale, stream=None) -> int:
+    """New tokens' queries rotated to q_out, their keys (rotated) and values as 8-bit codes and scales to the slots' rows."""
+    return lib().dck_quant_append(cache.ref, rope.ref if rope is not None else None, _ptr(q), q_stride, _ptr(k),
+                                  k_stride, _ptr(v), v_stride, n_tok, _ptr(positions), _ptr(slots), _ptr(q_out),
+                                  _ptr(kcache), _ptr(k_scale), _ptr(vcache), _ptr(v_scale), _stream(stream))
+
+
+def dck_quant_read(cache: QuantCache, n_tok: int, slots, kcache, k_scale, vcache, v_scale, k, k_stride: int, v,
+                   v_stride: int, stream=None) -> int:
+    """The slots' rows of an 8-bit cache in full width."""
+    return lib().dck_quant_read(cache.ref, n_tok, _ptr(slots), _ptr(kcache), _ptr(k_scale), _ptr(vcache), _ptr(v_scale),
+                                _ptr(k), k_stride, _ptr(v), v_stride, _stream(stream))
+
+
+def dck_quant_decode_workspace_size(cache: QuantCache, batch: int, max_seq_len: int) -> int:
+    return lib().dck_quant_decode_workspace_size(cache.ref, batch, max_seq_len)
+
+
+def dck_quant_decode_attention(cache: QuantCache, q, q_stride: int, kcache, k_scale, vcache, v_scale, block_table,
+                               table_stride: int, seq_len, batch: int, max_seq_len: int, scale: float, window: int,
+                               softcap: float, out, lse, workspace, ws_bytes: int, stream=None) -> int:
+    """One query per sequence over its 8-bit pages; lse (optional): the log of the softmax's sum."""
+    return lib().dck_quant_decode_attention(cache.ref, _ptr(q), q_stride, _ptr(kcache), _ptr(k_scale), _ptr(vcache),
+                                            _ptr(v_scale), _ptr(block_table), table_stride, _ptr(seq_len), batch,
+                                            max_seq_len, scale, window, softcap, _ptr(out), _ptr(lse), _ptr(workspace),
+                                            ws_bytes, _stream(stream))
+
+
+def dck_paged_shared_workspace_size(cache: PagedCache, batch: int, max_seq_len: int, max_own: int) -> int:
+    return lib().dck_paged_shared_workspace_size(cache.ref, batch, max_seq_len, max_own)
+
+
+def dck_paged_shared_attention(cache: PagedCache, q, q_stride: int, kcache, vcache, block_table, table_stride: int,
+                               seq_len, batch: int, max_seq_len: int, max_own: int, n_groups: int, group_start,
+                               shared_len, scale: float, window: int, softcap: float, out, lse, workspace,
+                               ws_bytes: int, stream=None) -> int:
+    """dck_paged_decode_attention where the rows of a group begin with the same tokens, read once for all of them."""
+    return lib().dck_paged_shared_attention(cache.ref, _ptr(q), q_stride, _ptr(kcache), _ptr(vcache), _ptr(block_table),
+                                            table_stride, _ptr(seq_len), batch, max_seq_len, max_own, n_groups,
+                                            _ptr(group_start), _ptr(shared_len), scale, window, softcap, _ptr(out),
+                                            _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream))
+
+
+def dck_quant_shared_workspace_size(cache: QuantCache, batch: int, max_seq_len: int, max_own: int) -> int:
+    return lib().dck_quant_shared_workspace_size(cache.ref, batch, max_seq_len, max_own)
+
+
+def dck_quant_shared_attention(cache: QuantCache, q, q_stride: int, kcache, k_scale, vcache, v_scale, block_table,
+                               table_stride: int, seq_len, batch: int, max_seq_len: int, max_own: int, n_groups: int,
+                               group_start, shared_len, scale: float, window: int, softcap: float, out, lse, workspace,
+                               ws_bytes: int, stream=None) -> int:
+    """dck_quant_decode_attention where the rows of a group begin with the same tokens, read once for all of them."""
+    return lib().dck_quant_shared_attention(cache.ref, _ptr(q), q_stride, _ptr(kcache), _ptr(k_scale), _ptr(vcache),
+                                            _ptr(v_scale), _ptr(block_table), table_stride, _ptr(seq_len), batch,
+                                            max_seq_len, max_own, n_groups, _ptr(group_start), _ptr(shared_len), scale,
+                                            window, softcap, _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes,
+                                            _stream(stream))
 
 
 def dck_last_device_error(stream=None) -> int:
