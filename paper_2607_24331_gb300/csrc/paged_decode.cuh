@@ -69,10 +69,49 @@ struct ScoreScale {
   }
 };
 
+// Calls over shared prefixes (paged_shared.cu): what the rows of group g see together, tokens [first, end), is attended
+// to for all of them at once, in items of a block of their queries and a head group, each cut into tiles; the items'
+// tiles form one list, dealt to CTAs in equal ranges.
+struct GroupPlan {
+  int start, rows;   // its rows
+  int first, end;    // the tokens; none: end = first
+  int table;         // the row whose block table they are read by
+  int tiles, blocks; // of an item; items per head group
+  int units;         // tiles of all groups before
+  int queries;       // queries of a KV head in all groups before
+  int bad;           // a page outside the pool
+  int pad[2];
+  // Whether a row that sees tokens up to `eff`, its own ones aside, and from `from` on takes part.
+  __device__ __forceinline__ bool sees(int from, int eff) const { return end > first && eff >= end && from <= first; }
+};
+struct Shared0 {  // of a whole call
+  int units;  // tiles of all items
+  int bad;    // d_group_start is not as it must be
+};
+struct Prefix {
+  Shared0* all;
+  GroupPlan* groups;
+  int* group_of;   // [B]
+  float* part_u;   // partial sums, as in Args; row of an item's query: see row_of
+  float* part_ml;
+  int n_groups, n_items;  // groups; CTAs that tiles are dealt to
+  int rows, wh, tile;     // queries of a block, heads of a head group, tokens of a tile
+  Divider by_qpg;
+
+  // Where query `r` of the block `block` of head `w` of head group `hg` has the partial sum that CTA c leaves: items
+  // in order, CTAs that share one behind one another.  The next item of a CTA or the next CTA of an item is further on
+  // by all the rows that one of them can fill.
+  __device__ __forceinline__ int64_t row_of(const GroupPlan& p, int Hkv, int qpg, int hg, int block, int c, int w, int r) const {
+    const int queries = p.rows * qpg, here = min(rows, queries - block * rows);
+    return (int64_t)p.queries * Hkv + (int64_t)wh * ((int64_t)hg * queries + block * rows + (int64_t)c * rows) + w * here + r;
+  }
+};
+
 struct Args {
   PagedDecodeArgs a;
   Plan p;
   ScoreScale score;
+  Prefix x;  // calls over shared prefixes
   int DP;          // head dim, rounded up to the variant's
   float* part_u;   // [2 n_items][wh][rows][DP]
   float* part_ml;  // [2 n_items][wh][rows][2]: maximum (log2 units), sum (-1: a page outside the pool)
@@ -82,6 +121,15 @@ struct Args {
 cudaError_t launch_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_f32(const Args& g, cudaStream_t s);
 cudaError_t launch_q8(const Args& g, int dtype, cudaStream_t s);
+// Of calls over shared prefixes, what groups share (x) and what rows have of their own (p).
+cudaError_t launch_prefix_bf16(const Args& g, cudaStream_t s);
+cudaError_t launch_prefix_f32(const Args& g, cudaStream_t s);
+cudaError_t launch_prefix_q8(const Args& g, int dtype, cudaStream_t s);
+cudaError_t launch_own_bf16(const Args& g, cudaStream_t s);
+cudaError_t launch_own_f32(const Args& g, cudaStream_t s);
+cudaError_t launch_own_q8(const Args& g, int dtype, cudaStream_t s);
+// (paged_decode.cu) the plan of the queries of `rows` rows over their own tokens, by clusters or whole
+Plan own_plan(const PagedView& v, DecodeKind kind, int B, int max_own, int window, int sms);
 
 inline int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // Warps of a CTA: two CTAs per SM fill its shared memory with rings, or one of twice the warps.
@@ -184,6 +232,8 @@ constexpr int kKeptLens = 1024;
 struct Walk {
   int token, left;  // the tile's first token, and the tiles from it to the end of its (head group, sequence)
   int b, group, len;
+  // calls over shared prefixes: tokens are counted without `skip` of them from token skip_at on
+  int skip_at, skip;
 
   // Sets len, and token to the first visible one.
   __device__ __forceinline__ void see(const PagedDecodeArgs& a, const Batch& q) {
@@ -281,12 +331,14 @@ struct LoaderBase {
     for (int i = lane; i < Z::kStage / 16; i += 32) reinterpret_cast<uint4*>(stage)[i] = make_uint4(0, 0, 0, 0);
   }
 
+  template <bool SKIP = false>
   __device__ __forceinline__ Pages fetch(const Walk& w, bool first) const {
     Pages r;
     r.b = first ? w.b : -1;
     r.group = w.group;
-    const int t = w.token + run + lane;
+    int t = w.token + run + lane;
     const bool have_it = lane < Z::TOK && t < w.len;
+    if (SKIP && t >= w.skip_at) t += w.skip;
     const uint32_t col = g.a.v.by_page.div(have_it ? t : 0);
     r.off = have_it ? t - (int)col * g.a.v.page : -1;
     r.page = have_it ? g.a.table[w.b * g.a.table_stride + col] : 0;
@@ -307,6 +359,30 @@ struct LoaderBase {
         cp_async16_or_zero(to + row * Z::kQRow + (c ^ (row & 7)) * 16, q + (have ? row * row_bytes + c * 16 : 0),
                            have ? 16 : 0);
     }
+  }
+  // The same of `count` queries from query q0 of a group's on, for KV head h.
+  __device__ __forceinline__ const char* query_of(const GroupPlan& p, int h, int q0, int row) const {
+    const int x = q0 + row, b = g.x.by_qpg.div(x), j = h * g.a.v.qpg + x - b * g.a.v.qpg;
+    return static_cast<const char*>(g.a.q) + ((int64_t)(p.start + b) * g.a.q_stride + (int64_t)j * g.a.v.d) * el;
+  }
+  __device__ __forceinline__ void copy_block(const GroupPlan& p, int h, int q0, int count, int at) const {
+    const uint32_t to = places + at * kPlace;
+    for (int x = lane; x < ROWS * kQChunks; x += 32) {
+      const int row = x / kQChunks, c = x % kQChunks;
+      const bool have = row < count && c * 16 < g.a.v.d * el;
+      cp_async16_or_zero(to + row * Z::kQRow + (c ^ (row & 7)) * 16, have ? query_of(p, h, q0, row) + c * 16 : g.a.q, have ? 16 : 0);
+    }
+  }
+  __device__ __forceinline__ void read_block(const GroupPlan& p, int h, int q0, int count, uint8_t* q_all, int warp, int at) const {
+    using T = typename Z::T;
+    T* to = reinterpret_cast<T*>(q_all + (warp * QS + at) * kPlace);
+    constexpr int per = 16 / el;
+    for (int x = lane; x < ROWS * Z::DP; x += 32) {
+      const int row = x / Z::DP, e = x % Z::DP;
+      to[row * Z::DP + ((e / per) ^ (row & 7)) * per + e % per] =
+          row < count && e < g.a.v.d ? reinterpret_cast<const T*>(query_of(p, h, q0, row))[e] : from_f32<T>(0.f);
+    }
+    __syncwarp();
   }
   // The same by single elements, for queries off 16-byte boundaries.
   __device__ __forceinline__ void read_queries(const Queries& qs, int b, uint8_t* q_all, int warp, int at) const {
@@ -876,9 +952,49 @@ __device__ __forceinline__ Joined join_rows(int n, float (&weight)[MOST], F ml_o
   return r;
 }
 
-template <class Z, class Tile, bool CLUSTER>
+// Adds what the CTAs of the shared part left of query `row` of a group, KV head h, elements e to e + 3, to a sum
+// over the row's own tokens.
+__device__ __forceinline__ void join_shared(const Args& g, const GroupPlan& p, int h, int row, int e, float4& sum, Joined& j) {
+  const Prefix& x = g.x;
+  constexpr int kBatch = 4;
+  const int qpg = g.a.v.qpg, hg = h / x.wh, w = h - hg * x.wh, block = row / x.rows, units = x.all->units;
+  const Ranges ranges(units, min(x.n_items, units));
+  const int u = p.units + (hg * p.blocks + block) * p.tiles;
+  const int c0 = ranges.item_of(u), n = ranges.item_of(u + p.tiles - 1) - c0 + 1;
+  const int64_t at0 = x.row_of(p, g.a.v.Hkv, qpg, hg, block, c0, w, row - block * x.rows), step = (int64_t)x.wh * x.rows;
+  for (int i = 0; i < n; i += kBatch) {
+    float2 ml[kBatch];
+    float4 v[kBatch];
+    float top = j.m;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const bool have = i + k < n;
+      const int64_t at = at0 + (have ? i + k : i) * step;
+      ml[k] = __ldcg(reinterpret_cast<const float2*>(x.part_ml + 2 * at));
+      v[k] = __ldcg(reinterpret_cast<const float4*>(x.part_u + at * g.DP + e));
+      if (!have) ml[k] = make_float2(-CUDART_INF_F, 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, ml[k].x);
+    const float base = top == -CUDART_INF_F ? 0.f : top, before = exp2_approx(j.m - base);
+    j.m = top;
+    j.l *= before;
+    sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const float f = exp2_approx(ml[k].x - base);
+      j.l += ml[k].y * f;
+      if (f == 0.f) continue;
+      sum.x += v[k].x * f, sum.y += v[k].y * f, sum.z += v[k].z * f, sum.w += v[k].w * f;
+    }
+  }
+}
+
+// OWN: of a call over shared prefixes, the rows' own tokens (CLUSTER), joined with what the groups share.
+template <class Z, class Tile, bool CLUSTER, bool OWN>
 __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1 : kPerSm)
     paged_decode_kernel(const __grid_constant__ Args g) {
+  static_assert(CLUSTER || !OWN, "own tokens by clusters or whole");
   using T = typename Z::T;
   extern __shared__ __align__(128) uint8_t raw[];
   using Shm = Shared<Z, Tile, CLUSTER>;
@@ -895,9 +1011,11 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   T* out = static_cast<T*>(a.out);
   const bool even = (reinterpret_cast<uintptr_t>(out) & 3) == 0;
   pdl_launch_dependents();
-  pdl_wait();
+  if (!OWN) pdl_wait();  // (the shared part lets this launch begin once the ones before it are complete)
 
   int n_tiles = 0;
+  GroupPlan group;
+  bool takes_part = false, refused = false;  // OWN: in what its group shares; the row is not one to attend to
   Ranges ranges(0, 0);
   int u0, u1;
   Walk ahead;
@@ -912,7 +1030,24 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     ahead.group = pair / a.B;
     ahead.b = pair - ahead.group * a.B;
     bool bad;
-    const int span = visible(a, ahead.b, ahead.token, bad), tiles = (span + g.p.tile - 1) / g.p.tile;
+    int span = visible(a, ahead.b, ahead.token, bad);
+    if (OWN) {
+      if (g.x.all->bad) {
+        span = 0;
+        refused = true;
+      } else {
+        group = g.x.groups[g.x.group_of[ahead.b]];
+        const int len = span + ahead.token, eff = group.rows > 1 ? min(len, max(0, a.shared_len[g.x.group_of[ahead.b]])) : 0;
+        bad |= len - eff > a.max_own;
+        if (bad) span = 0;
+        refused = bad;
+        takes_part = !bad && group.sees(ahead.token, eff);
+        ahead.skip_at = takes_part ? group.first : 0;
+        ahead.skip = takes_part ? group.end - group.first : 0;
+        span -= ahead.skip;
+      }
+    }
+    const int tiles = (span + g.p.tile - 1) / g.p.tile;
     if (bad && ahead.group == 0 && rank == 0 && threadIdx.x == 0) atomicOr(a.err, kErrBadSeq);
     ahead.len = span + ahead.token;
     u0 = (int)rank * tiles / g.p.cluster;
@@ -945,7 +1080,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   Pages pages = {0, -1, 0, -1}, pages2 = {0, -1, 0, -1};
   bool first = true;  // of its (head group, sequence), for this CTA
   const auto fetch_next = [&]() {
-    const Pages p = load.fetch(ahead, first);
+    const Pages p = load.template fetch<OWN>(ahead, first);
     first = false;
     ahead.token += g.p.tile;
     if (--to_fetch > 0 && --ahead.left == 0 && !CLUSTER) {
@@ -1011,6 +1146,8 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     // the end of a (head group, sequence), or of this CTA's part of it
     const bool whole = CLUSTER ? g.p.cluster == 1 : begins && ends;
     if (bad && lane == 0) atomicOr(a.err, kErrBadSeq);
+    if (OWN) bad |= refused;
+    if (OWN && whole) pdl_wait();  // the shared part's sums
     tile.finish();
     const int64_t out_row = (int64_t)at.b * a.v.Hq + qs.first;
     const int64_t part_row = CLUSTER ? 0 : (int64_t)((2 * blockIdx.x + (nth > 0)) * n_heads + wh) * g.p.rows;
@@ -1055,7 +1192,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
         const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
         if (e >= d) continue;
         float w[Z::NW];
-        const Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
+        Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < Z::NW; ++k)
@@ -1071,6 +1208,11 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
             for (int c = 0; c < g.p.cluster; ++c)
               store_remote(remote(&sh.cluster_ml[rank][r], c), make_float2(j.m, j.bad ? -1.f : j.l));
         } else if (whole) {
+          if (OWN && takes_part) {
+            const int h = g.p.by_chunks.div(at.group * g.p.wh + wh);
+            j.bad |= __ldcg(&g.x.groups[g.x.group_of[at.b]].bad) != 0;
+            join_shared(g, group, h, (at.b - group.start) * a.v.qpg + qs.first - h * a.v.qpg + r, e, sum, j);
+          }
           const float f = j.bad || j.l == 0.f ? 0.f : 1.f / j.l;
           put4(out + (out_row + r) * d + e,
                f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f), even);
@@ -1101,6 +1243,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     cluster_wait();
     return;
   }
+  if (OWN) pdl_wait();
   // Every CTA of the cluster has sent its sums: each joins its share of the elements.
   cluster_arrive();
   cluster_wait();
@@ -1109,7 +1252,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
     if (e >= d) continue;
     float w[kMaxCluster];
-    const Joined j = join_rows<kMaxCluster>(g.p.cluster, w, [&](int k) { return sh.cluster_ml[k][r]; });
+    Joined j = join_rows<kMaxCluster>(g.p.cluster, w, [&](int k) { return sh.cluster_ml[k][r]; });
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < kMaxCluster; ++k)
@@ -1118,6 +1261,11 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
         sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
       }
     const int64_t row = (int64_t)at.b * a.v.Hq + qs.first + r;
+    if (OWN && takes_part) {
+      const int h = g.p.by_chunks.div(at.group);
+      j.bad |= __ldcg(&g.x.groups[g.x.group_of[at.b]].bad) != 0;
+      join_shared(g, group, h, (at.b - group.start) * a.v.qpg + qs.first - h * a.v.qpg + r, e, sum, j);
+    }
     const float f = j.bad || j.l == 0.f ? 0.f : 1.f / j.l;
     put4(out + row * d + e,
          f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f), even);
@@ -1129,9 +1277,9 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
 // launch
 // ---------------------------------------------------------------------------
 
-template <class Z, class Tile, bool CLUSTER>
+template <class Z, class Tile, bool CLUSTER, bool OWN = false>
 cudaError_t launch_kernel(const Args& g, cudaStream_t s) {
-  const auto k = paged_decode_kernel<Z, Tile, CLUSTER>;
+  const auto k = paged_decode_kernel<Z, Tile, CLUSTER, OWN>;
   static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

@@ -1,0 +1,216 @@
+// Calls over shared prefixes: what the rows of a group see together, by per-warp rings as in
+// paged_decode.cuh (a tile of up to 16 or 8 queries per warp, of any rows of the group).
+#pragma once
+
+#include "paged_decode.cuh"
+
+namespace dck {
+namespace paged {
+
+// A position in the list of the items' tiles.
+struct ItemWalk {
+  GroupPlan p;
+  int g, hg, block;
+  int token, left;  // the tile's first token, and the tiles from it to the end of the item
+
+  __device__ __forceinline__ void see(const Prefix& x, int at) {
+    g = at;
+    const int4* from = reinterpret_cast<const int4*>(x.groups + at);
+    int4* to = reinterpret_cast<int4*>(&p);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(GroupPlan) / 16); ++i) to[i] = from[i];
+  }
+  // Enters at tile u of the list (called by whole warps).
+  __device__ __forceinline__ void enter(const Prefix& x, int u) {
+    int lo = 0, n = x.n_groups;  // the last group of those with fewer or as many tiles before
+    while (n > 1) {
+      const int step = (n + 31) / 32, i = (threadIdx.x & 31) * step;
+      const uint32_t ok = __ballot_sync(~0u, i < n && x.groups[lo + (i < n ? i : 0)].units <= u);
+      const int k = (31 - __clz(ok)) * step;
+      lo += k;
+      n = min(step, n - k);
+    }
+    see(x, lo);
+    const int at = u - p.units, item = at / p.tiles, tile = at - item * p.tiles;
+    hg = item / p.blocks;
+    block = item - hg * p.blocks;
+    token = p.first + tile * x.tile;
+    left = p.tiles - tile;
+  }
+  // The next item.
+  __device__ __forceinline__ void leave(const Prefix& x, int head_groups) {
+    if (++block == p.blocks) {
+      block = 0;
+      if (++hg == head_groups) {
+        hg = 0;
+        do see(x, g + 1);
+        while (p.tiles == 0);
+      }
+    }
+    token = p.first;
+    left = p.tiles;
+  }
+  __device__ __forceinline__ int count(const Prefix& x, int qpg) const { return min(x.rows, p.rows * qpg - block * x.rows); }
+};
+
+template <class Z, class Tile>
+__global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid_constant__ Args g) {
+  extern __shared__ __align__(128) uint8_t raw[];
+  using Shm = Shared<Z, Tile, false>;
+  Shm& sh = *reinterpret_cast<Shm*>(raw + Z::kRing);
+  const PagedDecodeArgs& a = g.a;
+  const Prefix& x = g.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_heads = x.wh, n_runs = Z::NW / n_heads, wh = warp & (n_heads - 1), wt = warp / n_heads;
+  const int d = a.v.d, qpg = a.v.qpg, head_groups = a.v.Hkv / n_heads;
+  pdl_wait();
+  pdl_launch_dependents();  // the plan, and with it all that the own tokens' launch reads, is there
+  const int units = x.all->units;
+  const Ranges ranges(units, min(x.n_items, units));
+  if ((int)blockIdx.x >= ranges.n) return;
+  const typename LoaderOf<Z, Tile::kRows, Shm::kPlaces>::type load(g, raw, sh.q, warp, lane, wh, wt);
+  load.clear(raw);
+  ItemWalk ahead;
+  ahead.enter(x, ranges.begin(blockIdx.x));
+  ItemWalk at = ahead;
+  int to_compute = ranges.begin(blockIdx.x + 1) - ranges.begin(blockIdx.x), to_copy = to_compute, to_fetch = to_compute;
+
+  // page numbers are read two tiles ahead of the copies
+  struct Next {
+    Pages pages;
+    GroupPlan p;
+    int block;  // of queries that come with the tile, or -1
+  };
+  Next next, next2;
+  bool first = true;
+  const auto fetch_next = [&](Next& n) {
+    Walk w;
+    w.token = ahead.token;
+    w.len = ahead.p.end;
+    w.b = ahead.p.table;
+    w.group = ahead.hg;
+    n.pages = load.fetch(w, false);
+    n.block = first ? ahead.block : -1;
+    if (first) n.p = ahead.p;
+    first = false;
+    ahead.token += x.tile;
+    if (--to_fetch > 0 && --ahead.left == 0) {
+      ahead.leave(x, head_groups);
+      first = true;
+    }
+  };
+  if (to_fetch > 0) fetch_next(next);
+  if (to_fetch > 0) fetch_next(next2);
+  uint32_t outside = 0;
+  int put = 0;
+  const auto copy_next = [&]() {
+    if (to_copy > 0) {
+      --to_copy;
+      if (next.block >= 0 && g.p.q_copied)
+        load.copy_block(next.p, next.pages.group * n_heads + wh, next.block * x.rows,
+                        min(x.rows, next.p.rows * qpg - next.block * x.rows), put);
+      const bool bad = load.issue(next.pages, put);
+      outside = (outside & ~(1u << put)) | (uint32_t)bad << put;
+      next = next2;
+      if (to_fetch > 0) fetch_next(next2);
+      put = put + 1 == Z::S ? 0 : put + 1;
+    }
+    cp_async_commit();
+  };
+  float* mine = sh.mine + warp * 8 * Tile::kRows;
+  Tile tile;
+#pragma unroll 1
+  for (int i = 0; i < Z::S - 1; ++i) copy_next();
+  int get = 0, count = 0;
+  bool bad = false, fresh = true;
+  while (true) {
+    __syncwarp();  // the stage that is filled next has been read
+    copy_next();
+    cp_async_wait<Z::S - 1>();
+    __syncwarp();
+    if (fresh) {
+      count = at.count(x, qpg);
+      if (!g.p.q_copied) load.read_block(at.p, at.hg * n_heads + wh, at.block * x.rows, count, sh.q, warp, get);
+      tile.begin(load.places + get * load.kPlace, lane);
+      fresh = false;
+    }
+    bad |= outside >> get & 1;
+    tile.step(load.ring + get * Z::kStage, at.p.end - at.token - load.run, lane, g.score, mine);
+    const int used = get;
+    get = get + 1 == Z::S ? 0 : get + 1;
+    at.token += x.tile;
+    const bool last = --to_compute <= 0;
+    if (--at.left > 0 && !last) continue;
+    // the end of an item, or of this CTA's part of it
+    if (bad && lane == 0) {
+      atomicOr(a.err, kErrBadSeq);
+      atomicOr(&x.groups[at.g].bad, 1);
+    }
+    tile.finish();
+    const int64_t row0 = x.row_of(at.p, a.v.Hkv, qpg, at.hg, at.block, blockIdx.x, wh, 0);
+    if (n_runs == 1) {
+#pragma unroll
+      for (int y = 0; y < Tile::kMine; ++y) {
+        const int r = Tile::row(y, lane);
+        if (r >= count) continue;
+        if (Tile::speaks(lane)) *reinterpret_cast<float2*>(x.part_ml + 2 * (row0 + r)) = make_float2(tile.m[y], tile.l[y]);
+        float* p = x.part_u + (row0 + r) * Z::DP;
+        tile.each(y, lane, d, [&](int e, float u, float v) { *reinterpret_cast<float2*>(p + e) = make_float2(u, v); });
+      }
+    } else {
+      float* left = reinterpret_cast<float*>(raw + (warp * Z::S + used) * Z::kStage);
+#pragma unroll
+      for (int y = 0; y < Tile::kMine; ++y) {
+        const int r = Tile::row(y, lane);
+        if (Tile::speaks(lane)) sh.ml[warp][r] = make_float2(tile.m[y], tile.l[y]);
+        tile.each(y, lane, d, [&](int e, float u, float v) {
+          *reinterpret_cast<float2*>(left + r * Z::DP + (e ^ (r & 7) * 8)) = make_float2(u, v);
+        });
+      }
+      __syncthreads();
+      for (int i = wt * 32 + lane; i < count * (Z::DP / 4); i += n_runs * 32) {
+        const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
+        if (e >= d) continue;
+        float w[Z::NW];
+        const Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < Z::NW; ++k)
+          if (k < n_runs && w[k] != 0.f) {
+            const float* from = reinterpret_cast<const float*>(raw + ((k * n_heads + wh) * Z::S + used) * Z::kStage);
+            const float4 v = *reinterpret_cast<const float4*>(from + r * Z::DP + (e ^ (r & 7) * 8));
+            sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
+          }
+        *reinterpret_cast<float4*>(x.part_u + (row0 + r) * Z::DP + e) = sum;
+        if (e == 0) *reinterpret_cast<float2*>(x.part_ml + 2 * (row0 + r)) = make_float2(j.m, j.l);
+      }
+      __syncthreads();
+      load.clear_stage(reinterpret_cast<uint8_t*>(left));
+    }
+    if (last) break;
+    bad = false;
+    fresh = true;
+    at.leave(x, head_groups);
+  }
+  cp_async_wait<0>();
+}
+
+template <class Z, class Tile>
+cudaError_t launch_prefix(const Args& g, cudaStream_t s) {
+  const auto k = prefix_kernel<Z, Tile>;
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
+  constexpr size_t smem = Z::kRing + sizeof(Shared<Z, Tile, false>);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+  }
+  e = launch_pdl(k, g.x.n_items, Z::NW * 32, smem, s, g);
+  return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
+}
+
+}  // namespace paged
+}  // namespace dck
