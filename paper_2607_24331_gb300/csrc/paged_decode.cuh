@@ -125,6 +125,7 @@ cudaError_t launch_q8(const Args& g, int dtype, cudaStream_t s);
 cudaError_t launch_prefix_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_prefix_f32(const Args& g, cudaStream_t s);
 cudaError_t launch_prefix_q8(const Args& g, int dtype, cudaStream_t s);
+cudaError_t launch_prefix_tc(const Args& g, cudaStream_t s);  // bf16, head dims up to 128: blocks of 128 queries
 cudaError_t launch_own_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_own_f32(const Args& g, cudaStream_t s);
 cudaError_t launch_own_q8(const Args& g, int dtype, cudaStream_t s);

@@ -137,12 +137,20 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 
 // How the shared part of a call is laid out.
 struct Layout {
+  bool tc;  // on tcgen05
   int rows, wh, tile, n_items;
 };
 Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int sms) {
   Layout l;
   const int DP = padded_dim(v.d), warps = warps_of(DP, false);
   const int64_t queries = (int64_t)v.qpg * B / std::max(n_groups, 1);  // of a group, on average
+  l.tc = kind.dtype == DCK_BF16 && !kind.quant && DP <= 128 && queries > 16;
+  if (l.tc) {
+    l.rows = l.tile = 128;
+    l.wh = 1;
+    l.n_items = sms;
+    return l;
+  }
   l.rows = kind.dtype == DCK_BF16 && DP <= 128 && queries > 8 ? 16 : 8;
   l.wh = warps;
   while (v.Hkv % l.wh) l.wh /= 2;
@@ -150,11 +158,11 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
   l.n_items = std::min(kPerSm * sms, kMaxItems);
   return l;
 }
-int most_rows(const PagedView& v) { return 16 * warps_of(padded_dim(v.d), false); }  // that a CTA leaves of an item
 
 size_t bytes_all(int B) { return 256 + align_up((size_t)B * sizeof(GroupPlan), 256) + align_up((size_t)B * sizeof(int), 256); }
+// (a CTA leaves 128 rows of an item, or each of two on an SM 16 for up to four heads)
 int64_t partial_rows(const PagedView& v, int B, int sms) {
-  return (int64_t)B * v.Hq + (int64_t)std::min(kPerSm * sms, kMaxItems) * most_rows(v);
+  return (int64_t)B * v.Hq + (int64_t)sms * 128;
 }
 
 }  // namespace
@@ -199,7 +207,7 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   h.p.by_chunks = divider(1);
   h.p.wh = l.wh;
   if (e == cudaSuccess)
-    e = kind.quant ? launch_prefix_q8(h, kind.dtype, s) : kind.dtype == DCK_F32 ? launch_prefix_f32(h, s) : launch_prefix_bf16(h, s);
+    e = l.tc ? launch_prefix_tc(h, s) : kind.quant ? launch_prefix_q8(h, kind.dtype, s) : kind.dtype == DCK_F32 ? launch_prefix_f32(h, s) : launch_prefix_bf16(h, s);
   if (e == cudaSuccess)
     e = kind.quant ? launch_own_q8(g, kind.dtype, s) : kind.dtype == DCK_F32 ? launch_own_f32(g, s) : launch_own_bf16(g, s);
   return e;

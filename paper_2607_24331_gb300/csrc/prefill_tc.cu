@@ -123,14 +123,6 @@ __device__ __forceinline__ int prefill_len(const int32_t* seq_len, const int64_t
   return Q <= 0 || Q > L || Q > qmax || L > max_len ? 0 : L;
 }
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ float2 unpack2(uint32_t v) {
-  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
-}
-
 __global__ void __launch_bounds__(kRThreads, 1)
     recon_kernel(const __grid_constant__ RMaps maps, const __grid_constant__ RArgs ra) {
   extern __shared__ uint8_t smem_raw[];
@@ -612,15 +604,6 @@ struct PItems {
     return it.b >= 0;
   }
 };
-
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 r;
-  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 z, x, y;\n"
-      " mov.b64 {%0, %1}, z;\n}\n"
-      : "=f"(r.x), "=f"(r.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
 
 __global__ void __launch_bounds__(kAThreadsP, 1)
     prefill_attn_kernel(const __grid_constant__ AMapsP maps, const __grid_constant__ AArgsP aa) {

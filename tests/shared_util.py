@@ -96,8 +96,7 @@ def bounds(c, d, n, ref, rlse, weight, slack, softcap):
         bo, bl = paged_util.decode_bounds(c["dtype"], d, n, ref, rlse, weight, slack, softcap)
         if c["dtype"] == "bf16":
             bo = bo + weight * 2.0 ** -8
-    # sums in several parts and the lse of rounded weights
-    return bo, bl + (2.0 ** -8 if c["dtype"] == "bf16" and not c["quant"] else 0)
+    return bo, bl
 
 
 def check(c, hq, window=0, softcap=0.0, scale=None, rows=None, **kw):
