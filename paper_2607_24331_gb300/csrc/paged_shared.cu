@@ -146,7 +146,8 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
   const int64_t queries = (int64_t)v.qpg * B / std::max(n_groups, 1);  // of a group, on average
   l.tc = kind.dtype == DCK_BF16 && !kind.quant && DP <= 128 && queries > 16;
   if (l.tc) {
-    l.rows = l.tile = 128;
+    l.rows = 128;
+    l.tile = 64;
     l.wh = 1;
     l.n_items = sms;
     return l;

@@ -9,13 +9,13 @@
 // group, else the softmax and what an SM takes in from L2.
 //
 // Work: one CTA per SM takes an equal range of the items' tiles (paged_shared.cu) and leaves a partial sum per item.
-// Tiles go in turn to two streams, each with scores, output and running maximum of its own, so that the softmax
-// of one runs under the products of the other, whatever the number of queries; the streams join at the item's end.
+// Tiles of 64 tokens go in turn to two streams, each with two buffers of scores, an output and a running maximum of its
+// own, so that the softmax of one runs under the products and the softmax of the other, whatever the number of
+// queries, and scores are ready when a softmax ends; the streams join at the item's end.
 // P overwrites its scores in tensor memory and is the A operand of O += P V from there.  Four warps copy (pages of any size
 // and order: 16-byte asynchronous copies into the swizzled layout), the rows behind a tile's last token as zeros.
-// Registers move from them to the softmax warps, which hold a row's 128 scores.
-#include <cstring>
-
+// (One buffer per stream and tiles of 128 tokens in five slots: keys and values that wait for a softmax filled four of them,
+// 1.6 us a tile of 128.)
 #include "paged_shared.cuh"
 #include "tc_common.cuh"
 
@@ -25,21 +25,21 @@ namespace {
 
 using namespace tc;
 
-// warp 0 MMAs, warps 4-7 and 8-11 softmax of the two streams, warps 12-15 copies
-constexpr int kThreads = 512;
-constexpr int kTok = 128;         // tokens of a tile, queries of an item
+// warps 0-3 and 4-7 softmax of the two streams, warps 8-11 copies, warp 12 MMAs
+constexpr int kThreads = 416;
+constexpr int kRows = 128;        // queries of an item
+constexpr int kTok = 64;          // tokens of a tile
 constexpr int kAtom = 128 * 128;  // 128 rows of 128 bytes
-constexpr int kSlots = 5;         // ring of key and value tiles: K(0), V(0), K(1), V(1), ...
-// registers: 512 threads x 128 at launch = 2 x 128 x 176 (softmax) + 2 x 128 x 80
-constexpr int kRegsSoftmax = 176, kRegsOther = 80;
+constexpr int kHalf = kTok * 128;
 
 template <int DP>
 struct ShmTc {
+  static constexpr int kSlots = DP == 128 ? 11 : 16;  // ring of key and value tiles: K(0), V(0), K(1), V(1), ...
   uint8_t q[DP / 64][kAtom];           // queries [64 elements][row][128 bytes], 128-byte swizzle
-  uint8_t kv[kSlots][DP / 64][kAtom];  // keys or values, rows tokens
-  float2 ml[2][kTok];                  // [stream][row]: maximum and sum
+  uint8_t kv[kSlots][DP / 64][kHalf];  // keys or values, rows tokens
+  float2 ml[2][kRows];                 // [stream][row]: maximum and sum
   uint64_t kv_full[kSlots], kv_empty[kSlots], q_full, q_empty;
-  uint64_t s_full[2], p_full[2][2], o_full[2], ml_full, o_free;  // [stream] (P: [half of its tokens])
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2], o_full[2], ml_full, o_free;  // [stream][buffer]
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -64,42 +64,13 @@ struct Segments {
   }
 };
 
-// Copies in groups that a barrier is told of once they have landed, two groups behind.
-struct Announced {
-  uint64_t* waiting[2];
-  int n;
-  __device__ __forceinline__ void tell(uint64_t* bar, int lane) {
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar);
-  }
-  __device__ __forceinline__ void add(uint64_t* bar, int lane) {
-    cp_async_commit();
-    if (n == 2) {
-      cp_async_wait<2>();
-      tell(waiting[0], lane);
-      waiting[0] = waiting[1];
-      n = 1;
-    }
-    if (n == 0) waiting[0] = bar;
-    else waiting[1] = bar;
-    ++n;
-  }
-  __device__ __forceinline__ void flush(int lane) {
-    cp_async_wait<0>();
-    if (n > 0) tell(waiting[0], lane);
-    if (n > 1) tell(waiting[1], lane);
-    n = 0;
-  }
-  // A wait in which nothing that has landed is held back.
-  __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, int lane, volatile int* abort_flag) {
-    if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
-    flush(lane);
-    return wwait(bar, parity, abort_flag);
-  }
-};
+// Arrives on `bar` once all copies of this thread so far have landed.  (The reader of the barrier orders them before its
+// MMAs: a proxy fence of this thread would wait for the copies behind them too, 2 us a tile.)
+__device__ __forceinline__ void arrive_when_copied(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 
-// Copies of warp w of four: rows 32 w .. 32 w + 31 of each tile.
+// Copies of warp w of four.
 template <int DP>
 struct Copier {
   const Args& g;
@@ -107,30 +78,32 @@ struct Copier {
   uint32_t swizzled[2];  // where this lane's chunk of rows 4 i + lane / 8 lies, i even or odd
   __device__ __forceinline__ Copier(const Args& g, int w, int lane) : g(g), w(w), lane(lane) {
     const int sub = lane >> 3, c = lane & 7;
-    swizzled[0] = (32 * w + sub) * 128 + (c ^ sub) * 16;
-    swizzled[1] = (32 * w + sub) * 128 + (c ^ (sub + 4)) * 16;
+    swizzled[0] = sub * 128 + (c ^ sub) * 16;
+    swizzled[1] = sub * 128 + (c ^ (sub + 4)) * 16;
   }
-  // Rows at `from` + offset of lane r (its row w 32 + r), zeros where it is negative.
-  __device__ __forceinline__ void rows(uint8_t* to, const void* from, int64_t offset) const {
+  // Rows first .. first + N - 1 of a tile with `atom` bytes per 64 elements, at `from` + offset of lane r, zeros where
+  // that is negative.
+  template <int N>
+  __device__ __forceinline__ void rows(uint8_t* to, int atom, int first, const void* from, int64_t offset) const {
     const int c = lane & 7, have = g.a.v.d / 8 - c;
     const char* base = static_cast<const char*>(from) + c * 16;
-    const uint32_t at = smem_u32(to);
+    const uint32_t at = smem_u32(to) + first * 128;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N / 4; ++i) {
       const int64_t o = __shfl_sync(~0u, offset, i * 4 + (lane >> 3));
 #pragma unroll
       for (int j = 0; j < DP / 64; ++j) {
         const bool real = o >= 0 && 8 * j < have;
-        cp_async16_or_zero(at + j * kAtom + swizzled[i & 1] + i * 512, real ? base + o + 128 * j : static_cast<const char*>(from),
+        cp_async16_or_zero(at + j * atom + swizzled[i & 1] + i * 512, real ? base + o + 128 * j : static_cast<const char*>(from),
                            real ? 16 : 0);
       }
     }
   }
-  // Where lane r's query of an item lies, in bytes from g.a.q (-1: none).
+  // Where lane r's query of an item (its row 32 w + r) lies, in bytes from g.a.q (-1: none).
   __device__ __forceinline__ int64_t query(const ItemWalk& at) const {
     const int qpg = g.a.v.qpg, r = 32 * w + lane;
     if (r >= at.count(g.x, qpg)) return -1;
-    const int x = at.block * kTok + r, b = g.x.by_qpg.div(x), j = at.hg * qpg + x - b * qpg;
+    const int x = at.block * kRows + r, b = g.x.by_qpg.div(x), j = at.hg * qpg + x - b * qpg;
     return 2 * ((int64_t)(at.p.start + b) * g.a.q_stride + (int64_t)j * g.a.v.d);
   }
   // The same rows by single elements, for queries off 16-byte boundaries.
@@ -159,6 +132,7 @@ template <int DP>
 __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_constant__ Args g) {
   extern __shared__ uint8_t smem_raw[];
   using Shm = ShmTc<DP>;
+  constexpr int kSlots = Shm::kSlots;
   Shm& sm = *reinterpret_cast<Shm*>(align_1024(smem_raw));
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
@@ -169,134 +143,140 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   const Ranges ranges(units, min(x.n_items, units));
   if ((int)blockIdx.x >= ranges.n) return;
   volatile int* abort_flag = &sm.abort_flag;
-  if (tid == 0) {
-    for (int i = 0; i < kSlots; ++i) {
-      mbar_init(&sm.kv_full[i], 4);
-      mbar_init(&sm.kv_empty[i], 1);
-    }
-    mbar_init(&sm.q_full, 4);
-    mbar_init(&sm.q_empty, 1);
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(&sm.s_full[s], 1);
-      mbar_init(&sm.p_full[s][0], 4);
-      mbar_init(&sm.p_full[s][1], 4);
-      mbar_init(&sm.o_full[s], 1);
-    }
-    mbar_init(&sm.ml_full, 8);
-    mbar_init(&sm.o_free, 8);
-    sm.abort_flag = 0;
-    fence_mbar_init();
-  }
-  if (warp == 0) {
+  if (warp == 12) {
     tmem_alloc(&sm.tmem_base, 512);
     tmem_relinquish();
+    if (lane == 0) {
+      for (int i = 0; i < kSlots; ++i) {
+        mbar_init(&sm.kv_full[i], 128);
+        mbar_init(&sm.kv_empty[i], 1);
+      }
+      mbar_init(&sm.q_full, 128);
+      mbar_init(&sm.q_empty, 1);
+      for (int s = 0; s < 2; ++s) {
+        for (int b = 0; b < 2; ++b) {
+          mbar_init(&sm.s_full[s][b], 1);
+          mbar_init(&sm.p_full[s][b], 4);
+        }
+        mbar_init(&sm.pv_done[s], 1);
+        mbar_init(&sm.o_full[s], 1);
+      }
+      mbar_init(&sm.ml_full, 8);
+      mbar_init(&sm.o_free, 8);
+      sm.abort_flag = 0;
+      fence_mbar_init();
+    }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sm.tmem_base;  // scores and P of stream s at 128 s, its output at 256 + 128 s
+  const uint32_t tmem = sm.tmem_base;  // scores and P of stream s, buffer b at 128 s + 64 b, its output at 256 + 128 s
   Segments sg;
   sg.begin(x, ranges);
 
-  if (warp < 4) {
-    reg_dec<kRegsOther>();
-    if (warp == 0) {
-      // ---- MMAs: the whole warp runs the schedule, one lane issues --------------------
-      const bool el = elect_one();
-      const uint32_t id_s = idesc_bf16(128, 128, false, false);  // S = Q K^T: both K-major
-      const uint32_t id_o = idesc_bf16(128, DP, false, true);    // O += P V: V MN-major
-      const uint64_t dq = sdesc(smem_u32(sm.q[0]), 16, 1024, kSw128);
-      const uint64_t dk = sdesc(smem_u32(sm.kv[0][0]), 16, 1024, kSw128);
-      const uint64_t dv = sdesc(smem_u32(sm.kv[0][0]), kAtom, 1024, kSw128);
-      int seq = 0;                   // tiles of keys and values before this item
-      uint32_t pn[2] = {0, 0};       // P tiles so far
-      bool ok = true;
-      do {
-        const int n = sg.n;
-        const auto ready = [&](int i) { return wwait(&sm.kv_full[i % kSlots], (i / kSlots) & 1, abort_flag); };
-        const auto scores = [&](int k) -> bool {
-          const int i = seq + 2 * k, sl = i % kSlots, s = k & 1;
-          if (!ready(i)) return false;
-          tc_fence_after();
-          if (el) {
-            const uint64_t kb = dk + (uint64_t)(sl * ((DP / 64) * kAtom >> 4));
+  if (warp == 12) {
+    // ---- MMAs: the whole warp runs the schedule, one lane issues ----------------------
+    // A thread's MMAs run in order: scores may go into a buffer right after the P V that reads it.
+    const bool el = elect_one();
+    const uint32_t id_s = idesc_bf16(128, kTok, false, false);  // S = Q K^T: both K-major
+    const uint32_t id_o = idesc_bf16(128, DP, false, true);     // O += P V: V MN-major
+    const uint64_t dq = sdesc(smem_u32(sm.q[0]), 16, 1024, kSw128);
+    const uint64_t dk = sdesc(smem_u32(sm.kv[0][0]), 16, 1024, kSw128);
+    const uint64_t dv = sdesc(smem_u32(sm.kv[0][0]), kHalf, 1024, kSw128);
+    constexpr int kSlotBytes = (DP / 64) * kHalf;
+    // ring positions of the next key tile and the next value tile, with their turns' parities
+    int ks = 0, vs = 1;
+    uint32_t kp = 0, vp = 0, pp[2][2] = {};  // pp: parity of each buffer's next P
+    const auto advance = [&](int& slot, uint32_t& parity) {
+      slot += 2;
+      if (slot >= kSlots) slot -= kSlots, parity ^= 1;
+    };
+    bool ok = true;
+    do {
+      const int n = sg.n;
+      const auto scores = [&](int k) -> bool {
+        if (!wwait(&sm.kv_full[ks], kp, abort_flag)) return false;
+        fence_proxy_async_smem();
+        tc_fence_after();
+        const int s = k & 1, b = k >> 1 & 1;
+        if (el) {
+          const uint64_t kb = dk + (uint64_t)(ks * (kSlotBytes >> 4));
 #pragma unroll
-            for (int j = 0; j < DP / 16; ++j) {
-              const uint64_t o = ((j >> 2) * kAtom + (j & 3) * 32) >> 4;
-              umma_f16(tmem + 128 * s, dq + o, kb + o, id_s, j > 0 ? 1u : 0u);
-            }
-            umma_commit(&sm.s_full[s]);
-            umma_commit(&sm.kv_empty[sl]);
-            if (k + 1 == n) umma_commit(&sm.q_empty);
-          }
-          return true;
-        };
-        if (!(ok = wwait(&sm.q_full, sg.nth & 1, abort_flag))) break;
-        if (!(ok = scores(0))) break;
-        if (n > 1 && !(ok = scores(1))) break;
-        // the last item's output has been read
-        if (sg.nth > 0 && !(ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag))) break;
-        for (int k = 0; k < n; ++k) {
-          const int s = k & 1, i = seq + 2 * k + 1, sl = i % kSlots;
-          if (!(ok = ready(i))) break;
-          const uint64_t vb = dv + (uint64_t)(sl * ((DP / 64) * kAtom >> 4));
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            if (!(ok = wwait(&sm.p_full[s][hf], pn[s] & 1, abort_flag))) break;
-            tc_fence_after();
-            if (el) {
-#pragma unroll
-              for (int j = 4 * hf; j < 4 * hf + 4; ++j)
-                umma_f16_ts(tmem + 256 + 128 * s, tmem + 128 * s + 8 * j, vb + (uint64_t)(j * 2048 >> 4), id_o,
-                            (k > 1 || j > 0) ? 1u : 0u);
-            }
-          }
-          if (!ok) break;
-          ++pn[s];
-          if (el) {
-            umma_commit(&sm.kv_empty[sl]);
-            if (k + 2 >= n) umma_commit(&sm.o_full[s]);
-          }
-          if (k + 2 < n && !(ok = scores(k + 2))) break;
+          for (int j = 0; j < DP / 16; ++j)
+            umma_f16(tmem + 128 * s + 64 * b, dq + (((j >> 2) * kAtom + (j & 3) * 32) >> 4),
+                     kb + (((j >> 2) * kHalf + (j & 3) * 32) >> 4), id_s, j > 0 ? 1u : 0u);
+          umma_commit(&sm.s_full[s][b]);
+          umma_commit(&sm.kv_empty[ks]);
+          if (k + 1 == n) umma_commit(&sm.q_empty);
         }
-        seq += 2 * n;
-      } while (ok && sg.next(x, heads));
-    }
-  } else if (warp < 12) {
-    // ---- softmax of stream s: a thread has row r ------------------------------------
-    reg_inc<kRegsSoftmax>();
-    const int s = (warp - 4) >> 2, r = (warp & 3) * 32 + lane;
+        advance(ks, kp);
+        return true;
+      };
+      if (!(ok = wwait(&sm.q_full, sg.nth & 1, abort_flag))) break;
+      for (int k = 0; k < min(n, 4) && ok; ++k) ok = scores(k);
+      // the last item's output has been read
+      if (ok && sg.nth > 0) ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag);
+      for (int k = 0; k < n && ok; ++k) {
+        const int s = k & 1, b = k >> 1 & 1;
+        if (!(ok = wwait(&sm.kv_full[vs], vp, abort_flag))) break;
+        if (!(ok = wwait(&sm.p_full[s][b], pp[s][b], abort_flag))) break;
+        pp[s][b] ^= 1;
+        fence_proxy_async_smem();
+        tc_fence_after();
+        if (el) {
+          const uint64_t vb = dv + (uint64_t)(vs * (kSlotBytes >> 4));
+#pragma unroll
+          for (int j = 0; j < kTok / 16; ++j)
+            umma_f16_ts(tmem + 256 + 128 * s, tmem + 128 * s + 64 * b + 8 * j, vb + (uint64_t)(j * 2048 >> 4), id_o,
+                        (k > 1 || j > 0) ? 1u : 0u);
+          umma_commit(&sm.pv_done[s]);
+          umma_commit(&sm.kv_empty[vs]);
+          if (k + 2 >= n) umma_commit(&sm.o_full[s]);
+        }
+        advance(vs, vp);
+        if (k + 4 < n) ok = scores(k + 4);
+      }
+    } while (ok && sg.next(x, heads));
+  } else if (warp < 8) {
+    // ---- softmax of stream s: a thread has row r ----------------------------------------
+    const int s = warp >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t lb = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t sb = tmem + lb + 128 * s, ob = tmem + lb + 256 + 128 * s;
+    const uint32_t ob = tmem + lb + 256 + 128 * s;
     const bool plain = g.score.cap2 == 0.f && g.score.scale2 > 0.f;  // scores are s times a positive factor
     const float factor = plain ? g.score.scale2 : 1.f;
-    uint32_t sn = 0, on[2] = {0, 0};
+    uint32_t sp = 0, turn = 0, second = 0;  // sp: bit b the parity of buffer b's next scores; turn: tiles of this
+                                            // stream so far; second: items so far in which stream 1 has any
     bool ok = true;
     do {
       float m = -CUDART_INF_F;
       float2 l = make_float2(0.f, 0.f);
-      for (int k = s; k < sg.n; k += 2) {
-        if (!(ok = wwait(&sm.s_full[s], sn & 1, abort_flag))) break;
-        ++sn;
+      for (int k = s; k < sg.n; k += 2, ++turn) {
+        const int b = k >> 1 & 1;
+        if (!(ok = wwait(&sm.s_full[s][b], sp >> b & 1, abort_flag))) break;
+        sp ^= 1u << b;
         tc_fence_after();
-        float sv[128];
+        const uint32_t sb = tmem + lb + 128 * s + 64 * b;
+        float sv[kTok];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(sb + 32 * c, *reinterpret_cast<float(*)[32]>(&sv[32 * c]));
+        for (int c = 0; c < kTok / 32; ++c) tmem_ld32(sb + 32 * c, *reinterpret_cast<float(*)[32]>(&sv[32 * c]));
         tmem_wait_ld();
         if (!plain) g.score.apply(sv);
         const int live = sg.at.p.end - sg.at.token - kTok * k;
         if (live < kTok) {
 #pragma unroll
-          for (int i = 0; i < 128; ++i) sv[i] = i < live ? sv[i] : -CUDART_INF_F;
+          for (int i = 0; i < kTok; ++i) sv[i] = i < live ? sv[i] : -CUDART_INF_F;
         }
         float mx[4] = {sv[0], sv[1], sv[2], sv[3]};
 #pragma unroll
-        for (int i = 4; i < 128; i += 8)
+        for (int i = 4; i < kTok; i += 8)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) mx[u] = fmaxf(mx[u], i + 4 + u < 128 ? fmaxf(sv[i + u], sv[i + 4 + u]) : sv[i + u]);
+          for (int u = 0; u < 4; ++u) mx[u] = fmaxf(mx[u], i + 4 + u < kTok ? fmaxf(sv[i + u], sv[i + 4 + u]) : sv[i + u]);
         const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * factor;
         const bool raise = mt > m + kHeadroom, rescale = raise && m != -CUDART_INF_F;
         if (__any_sync(~0u, rescale)) {  // (TMEM accesses are the whole warp's: factor 1 for the other rows)
+          // the last product is in O (the one before is: this tile's scores came after it)
+          if (!(ok = wwait(&sm.pv_done[s], (turn - 1) & 1, abort_flag))) break;
+          tc_fence_after();
           const float f = rescale ? exp2_approx(m - mt) : 1.f;
 #pragma unroll 1
           for (int c = 0; c < DP / 16; ++c) {
@@ -312,22 +292,19 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         if (raise) m = mt;
         const float base = m == -CUDART_INF_F ? 0.f : m;
         const float2 f2 = make_float2(factor, factor), nb = make_float2(-base, -base);
+        uint32_t pk[kTok / 2];
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t pk[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float2 d = fma2(make_float2(sv[64 * hf + 2 * i], sv[64 * hf + 2 * i + 1]), f2, nb);
-            const float2 p = make_float2(ex2_approx(d.x), ex2_approx(d.y));
-            pk[i] = pack2(p.x, p.y);
-            l = add2(l, p);
-          }
-          tmem_st32(sb + 32 * hf, pk);
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.p_full[s][hf]);
+        for (int i = 0; i < kTok / 2; ++i) {
+          const float2 d = fma2(make_float2(sv[2 * i], sv[2 * i + 1]), f2, nb);
+          const float2 p = make_float2(ex2_approx(d.x), ex2_approx(d.y));
+          pk[i] = pack2(p.x, p.y);
+          l = add2(l, p);
         }
+        tmem_st32(sb, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.p_full[s][b]);
       }
       if (!ok) break;
       // the streams join: this one writes half of the elements
@@ -336,12 +313,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.ml_full);
       if (!(ok = wwait(&sm.ml_full, sg.nth & 1, abort_flag))) break;
-      if (!(ok = wwait(&sm.o_full[0], on[0] & 1, abort_flag))) break;
-      ++on[0];
       const bool both = sg.n > 1;
+      if (!(ok = wwait(&sm.o_full[0], sg.nth & 1, abort_flag))) break;
       if (both) {
-        if (!(ok = wwait(&sm.o_full[1], on[1] & 1, abort_flag))) break;
-        ++on[1];
+        if (!(ok = wwait(&sm.o_full[1], second & 1, abort_flag))) break;
+        ++second;
       }
       tc_fence_after();
       const float2 u0 = sm.ml[0][r], u1 = sm.ml[1][r];
@@ -370,24 +346,23 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     } while (ok && sg.next(x, heads));
   } else {
     // ---- copies -----------------------------------------------------------------------
-    reg_dec<kRegsOther>();
     const PagedView& v = a.v;
-    const Copier<DP> copy(g, warp - 12, lane);
-    Announced told;
-    told.n = 0;
-    int seq = 0;
+    const int w = warp - 8;
+    const Copier<DP> copy(g, w, lane);
+    int slot = 0;
+    uint32_t parity = 1;  // (a fresh barrier passes a wait for the phase before its first)
     bool ok = true;
     do {
       const int32_t* table = a.table + sg.at.p.table * a.table_stride;
       const auto page_of = [&](int k, int& off) -> int {  // of this lane's token of tile k (off < 0: none)
-        const int t = sg.at.token + kTok * k + 32 * (warp - 12) + lane;
+        const int t = sg.at.token + kTok * k + 16 * w + (lane & 15);
         off = -1;
         if (t >= sg.at.p.end) return 0;
         const uint32_t col = v.by_page.div(t);
         off = t - (int)col * v.page;
         return table[col];
       };
-      int off, page = page_of(0, off);
+      int off, page = page_of(0, off), off2 = -1, page2 = sg.n > 1 ? page_of(1, off2) : 0;
       for (int k = 0; k < sg.n && ok; ++k) {
         const bool inside = (uint32_t)page < (uint32_t)v.n_pages;
         if (off >= 0 && !inside) {
@@ -397,26 +372,30 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         const bool have = off >= 0 && inside;
         const int64_t ko = have ? (int64_t)((uint64_t)page * v.k_page_b + (uint64_t)off * v.k_tok_b + (uint64_t)sg.at.hg * v.k_head_b) : -1;
         const int64_t vo = have ? (int64_t)((uint64_t)page * v.v_page_b + (uint64_t)off * v.v_tok_b + (uint64_t)sg.at.hg * v.v_head_b) : -1;
-        if (k + 1 < sg.n) page = page_of(k + 1, off);  // before its copies need it
+        page = page2, off = off2;
+        if (k + 2 < sg.n) page2 = page_of(k + 2, off2);  // two tiles before its copies need it
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
-          const int i = seq + 2 * k + kind, sl = i % kSlots;
-          if (i >= kSlots && !(ok = told.wait(&sm.kv_empty[sl], ((i / kSlots) - 1) & 1, lane, abort_flag))) break;
-          copy.rows(sm.kv[sl][0], kind ? a.vc : a.kc, kind ? vo : ko);
-          told.add(&sm.kv_full[sl], lane);
+          if (!(ok = wwait(&sm.kv_empty[slot], parity, abort_flag))) break;
+          copy.template rows<16>(sm.kv[slot][0], kHalf, 16 * w, kind ? a.vc : a.kc, kind ? vo : ko);
+          arrive_when_copied(&sm.kv_full[slot]);
+          if (++slot == kSlots) slot = 0, parity ^= 1;
           if (k == 0 && kind == 0) {
             // the last item's scores are all formed: its queries can go
-            if (sg.nth > 0 && !(ok = told.wait(&sm.q_empty, (sg.nth - 1) & 1, lane, abort_flag))) break;
+            if (sg.nth > 0 && !(ok = wwait(&sm.q_empty, (sg.nth - 1) & 1, abort_flag))) break;
             const int64_t qo = copy.query(sg.at);
-            if (g.p.q_copied) copy.rows(sm.q[0], a.q, qo);
-            else copy.elements(sm.q[0], qo);
-            told.add(&sm.q_full, lane);
+            if (g.p.q_copied) {
+              copy.template rows<32>(sm.q[0], kAtom, 32 * w, a.q, qo);
+              arrive_when_copied(&sm.q_full);
+            } else {
+              copy.elements(sm.q[0], qo);
+              mbar_arrive(&sm.q_full);
+            }
           }
         }
       }
-      seq += 2 * sg.n;
     } while (ok && sg.next(x, heads));
-    told.flush(lane);
+    cp_async_wait<0>();
   }
   tc_fence_before();
   __syncthreads();
@@ -425,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     if (tid == 0) atomicOr(a.err, kErrTimeout);
   }
   __syncthreads();
-  if (warp == 0) {
+  if (warp == 12) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
