@@ -527,7 +527,7 @@ dck_status dck_quant_decode_attention(const dck_quant_desc* desc, const void* q,
  * Other arguments as there.  Results differ from those calls' by roundings only.  A row with more than max_own tokens
  * of its own is treated like one with a bad length, a page outside the pool like one for every row that sees it; a
  * shared length below 0 counts as 0 and is recorded; where d_group_start is not as described, every output is zero with
- * lse = -inf, and it is recorded.  At most three launches; results do not depend on the order in which blocks run.
+ * lse = -inf, and it is recorded.  At most four launches; results do not depend on the order in which blocks run.
  */
 size_t dck_paged_shared_workspace_size(const dck_paged_desc* desc, int32_t batch, int32_t max_seq_len, int32_t max_own);
 dck_status dck_paged_shared_attention(const dck_paged_desc* desc, const void* q, int64_t q_stride, const void* kcache,

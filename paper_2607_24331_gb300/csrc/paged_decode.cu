@@ -245,9 +245,8 @@ cudaError_t launch_join(const Args& g, int sms, cudaStream_t s) {
 //   1 x 128   6.9 /  4.6 /  4.4     16 x 512       13.6 /  8.4 / 10.5    64 x 256        21 / - / 15
 //   1 x 1024  9.1 /  6.4 / 14.6     16 x 4096      49.8 / 46.3 / 56      64 x 2048       87 / - / 83
 //   4 x 4096 18.6 / 17.4 / 58       16 x 128..2048 17.3 / 16.1 / 21      64 x 128..2048  37 / - / 44
-// OWN: of the own tokens of a call over shared prefixes, clusters or whole with two runs of tokens at least.
-template <bool OWN = false>
-Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window, int sms) {
+// With `ranges` always by those.
+Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window, int sms, bool ranges = false) {
   Plan p;
   const int DP = padded_dim(v.d), dtype = kind.dtype;
   const int most = dtype == DCK_BF16 && DP <= 128 && v.qpg > 8 ? 16 : 8;
@@ -271,7 +270,7 @@ Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window
   };
   double best = times((dtype == DCK_BF16 ? 7.5 : 12.7) + 0.45 * std::max(0., (double)pairs / wide / slots - 1) -
                           (span <= few / wide * run ? 2.8 : 0), 0);
-  if (OWN) best = INFINITY;
+  if (ranges) best = 0;
   p.cluster = 0;
   p.warps = few;
   p.wh = wide;
@@ -281,7 +280,7 @@ Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window
     if (t < best) best = t, p.cluster = c, p.warps = many, p.wh = 1;
   }
   // a CTA of `few` warps for w heads of a sequence
-  for (int w = 1; w <= wide && !(OWN && w == few); w *= 2) {
+  for (int w = 1; w <= wide; w *= 2) {
     const double waves = std::ceil((double)(pairs / w) / slots);
     const double t = times(4.1 * (1 + 0.43 * (waves - 1)), waves * tiles_of(few / w * run) * step * 0.89);
     if (t < best) best = t, p.cluster = 1, p.warps = few, p.wh = w;
@@ -296,19 +295,16 @@ Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window
   return p;
 }
 
-}  // namespace
-
-Plan own_plan(const PagedView& v, DecodeKind kind, int B, int max_own, int window, int sms) {
-  return plan_of<true>(v, kind, B, max_own, window, sms);
-}
-
-namespace {
-
 size_t bytes_entries(const Plan& p) { return align_up(p.n_items * sizeof(Entry), 256); }
 size_t bytes_ml(const Plan& p) { return align_up((size_t)2 * p.n_items * p.part_rows * 2 * sizeof(float), 256); }
 size_t bytes_u(const Plan& p, int DP) { return align_up((size_t)2 * p.n_items * p.part_rows * DP * sizeof(float), 256); }
 
 }  // namespace
+
+Plan range_plan(const PagedView& v, DecodeKind kind, int B, int max_len, int sms) {
+  return plan_of(v, kind, B, max_len, 0, sms, true);
+}
+
 }  // namespace paged
 
 using namespace paged;

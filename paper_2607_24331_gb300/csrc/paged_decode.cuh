@@ -81,23 +81,31 @@ struct GroupPlan {
   int queries;       // queries of a KV head in all groups before
   int bad;           // a page outside the pool
   int pad[2];
-  // Whether a row that sees tokens up to `eff`, its own ones aside, and from `from` on takes part.
-  __device__ __forceinline__ bool sees(int from, int eff) const { return end > first && eff >= end && from <= first; }
 };
-struct Shared0 {  // of a whole call
-  int units;  // tiles of all items
-  int bad;    // d_group_start is not as it must be
+// What a row attends to by itself: tokens [first, end), counted without `skip` of them from token skip_at on.
+struct RowPlan {
+  int first, end, skip_at, skip;
+  int group;      // its group, -1 if the row takes no part in what that shares
+  int state;      // 0, or kEmpty: zeros whatever the group has
+  int tiles;      // of all rows before (a row has one at least)
+  int pad;
+};
+constexpr int kEmpty = 1;
+struct Whole {  // of a whole call
+  int units;      // tiles of all items
+  int own_tiles;  // of all rows, per head group
 };
 struct Prefix {
-  Shared0* all;
+  Whole* all;
   GroupPlan* groups;
-  int* group_of;   // [B]
-  float* part_u;   // partial sums, as in Args; row of an item's query: see row_of
-  float* part_ml;
+  RowPlan* own;    // [B]
+  float *part_u, *part_ml;  // partial sums, as in Args, of what groups share: rows by row_of
+  float *own_u, *own_ml;    // and of rows' own tokens: rows by own_row
   int n_groups, n_items;  // groups; CTAs that tiles are dealt to
   int rows, wh, tile;     // queries of a block, heads of a head group, tokens of a tile
   Divider by_qpg;
 
+  __device__ __forceinline__ int64_t own_row(const Plan& p, int B, int group, int b, int c, int w) const;
   // Where query `r` of the block `block` of head `w` of head group `hg` has the partial sum that CTA c leaves: items
   // in order, CTAs that share one behind one another.  The next item of a CTA or the next CTA of an item is further on
   // by all the rows that one of them can fill.
@@ -106,6 +114,11 @@ struct Prefix {
     return (int64_t)p.queries * Hkv + (int64_t)wh * ((int64_t)hg * queries + block * rows + (int64_t)c * rows) + w * here + r;
   }
 };
+
+// Where CTA c leaves the sums of row b's own tokens, head w of head group `group`: as row_of, (head group, row) in order.
+__device__ __forceinline__ int64_t Prefix::own_row(const Plan& p, int B, int group, int b, int c, int w) const {
+  return ((int64_t)((int64_t)group * B + b + c) * p.wh + w) * p.rows;
+}
 
 struct Args {
   PagedDecodeArgs a;
@@ -129,8 +142,7 @@ cudaError_t launch_prefix_tc(const Args& g, cudaStream_t s);  // bf16, head dims
 cudaError_t launch_own_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_own_f32(const Args& g, cudaStream_t s);
 cudaError_t launch_own_q8(const Args& g, int dtype, cudaStream_t s);
-// (paged_decode.cu) the plan of the queries of `rows` rows over their own tokens, by clusters or whole
-Plan own_plan(const PagedView& v, DecodeKind kind, int B, int max_own, int window, int sms);
+Plan range_plan(const PagedView& v, DecodeKind kind, int B, int max_len, int sms);  // tiles dealt in ranges
 
 inline int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // Warps of a CTA: two CTAs per SM fill its shared memory with rings, or one of twice the warps.
@@ -953,49 +965,9 @@ __device__ __forceinline__ Joined join_rows(int n, float (&weight)[MOST], F ml_o
   return r;
 }
 
-// Adds what the CTAs of the shared part left of query `row` of a group, KV head h, elements e to e + 3, to a sum
-// over the row's own tokens.
-__device__ __forceinline__ void join_shared(const Args& g, const GroupPlan& p, int h, int row, int e, float4& sum, Joined& j) {
-  const Prefix& x = g.x;
-  constexpr int kBatch = 4;
-  const int qpg = g.a.v.qpg, hg = h / x.wh, w = h - hg * x.wh, block = row / x.rows, units = x.all->units;
-  const Ranges ranges(units, min(x.n_items, units));
-  const int u = p.units + (hg * p.blocks + block) * p.tiles;
-  const int c0 = ranges.item_of(u), n = ranges.item_of(u + p.tiles - 1) - c0 + 1;
-  const int64_t at0 = x.row_of(p, g.a.v.Hkv, qpg, hg, block, c0, w, row - block * x.rows), step = (int64_t)x.wh * x.rows;
-  for (int i = 0; i < n; i += kBatch) {
-    float2 ml[kBatch];
-    float4 v[kBatch];
-    float top = j.m;
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const bool have = i + k < n;
-      const int64_t at = at0 + (have ? i + k : i) * step;
-      ml[k] = __ldcg(reinterpret_cast<const float2*>(x.part_ml + 2 * at));
-      v[k] = __ldcg(reinterpret_cast<const float4*>(x.part_u + at * g.DP + e));
-      if (!have) ml[k] = make_float2(-CUDART_INF_F, 0.f);
-    }
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) top = fmaxf(top, ml[k].x);
-    const float base = top == -CUDART_INF_F ? 0.f : top, before = exp2_approx(j.m - base);
-    j.m = top;
-    j.l *= before;
-    sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const float f = exp2_approx(ml[k].x - base);
-      j.l += ml[k].y * f;
-      if (f == 0.f) continue;
-      sum.x += v[k].x * f, sum.y += v[k].y * f, sum.z += v[k].z * f, sum.w += v[k].w * f;
-    }
-  }
-}
-
-// OWN: of a call over shared prefixes, the rows' own tokens (CLUSTER), joined with what the groups share.
-template <class Z, class Tile, bool CLUSTER, bool OWN>
+template <class Z, class Tile, bool CLUSTER>
 __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1 : kPerSm)
     paged_decode_kernel(const __grid_constant__ Args g) {
-  static_assert(CLUSTER || !OWN, "own tokens by clusters or whole");
   using T = typename Z::T;
   extern __shared__ __align__(128) uint8_t raw[];
   using Shm = Shared<Z, Tile, CLUSTER>;
@@ -1012,11 +984,9 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   T* out = static_cast<T*>(a.out);
   const bool even = (reinterpret_cast<uintptr_t>(out) & 3) == 0;
   pdl_launch_dependents();
-  if (!OWN) pdl_wait();  // (the shared part lets this launch begin once the ones before it are complete)
+  pdl_wait();
 
   int n_tiles = 0;
-  GroupPlan group;
-  bool takes_part = false, refused = false;  // OWN: in what its group shares; the row is not one to attend to
   Ranges ranges(0, 0);
   int u0, u1;
   Walk ahead;
@@ -1031,24 +1001,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     ahead.group = pair / a.B;
     ahead.b = pair - ahead.group * a.B;
     bool bad;
-    int span = visible(a, ahead.b, ahead.token, bad);
-    if (OWN) {
-      if (g.x.all->bad) {
-        span = 0;
-        refused = true;
-      } else {
-        group = g.x.groups[g.x.group_of[ahead.b]];
-        const int len = span + ahead.token, eff = group.rows > 1 ? min(len, max(0, a.shared_len[g.x.group_of[ahead.b]])) : 0;
-        bad |= len - eff > a.max_own;
-        if (bad) span = 0;
-        refused = bad;
-        takes_part = !bad && group.sees(ahead.token, eff);
-        ahead.skip_at = takes_part ? group.first : 0;
-        ahead.skip = takes_part ? group.end - group.first : 0;
-        span -= ahead.skip;
-      }
-    }
-    const int tiles = (span + g.p.tile - 1) / g.p.tile;
+    const int span = visible(a, ahead.b, ahead.token, bad), tiles = (span + g.p.tile - 1) / g.p.tile;
     if (bad && ahead.group == 0 && rank == 0 && threadIdx.x == 0) atomicOr(a.err, kErrBadSeq);
     ahead.len = span + ahead.token;
     u0 = (int)rank * tiles / g.p.cluster;
@@ -1081,7 +1034,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
   Pages pages = {0, -1, 0, -1}, pages2 = {0, -1, 0, -1};
   bool first = true;  // of its (head group, sequence), for this CTA
   const auto fetch_next = [&]() {
-    const Pages p = load.template fetch<OWN>(ahead, first);
+    const Pages p = load.fetch(ahead, first);
     first = false;
     ahead.token += g.p.tile;
     if (--to_fetch > 0 && --ahead.left == 0 && !CLUSTER) {
@@ -1147,8 +1100,6 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     // the end of a (head group, sequence), or of this CTA's part of it
     const bool whole = CLUSTER ? g.p.cluster == 1 : begins && ends;
     if (bad && lane == 0) atomicOr(a.err, kErrBadSeq);
-    if (OWN) bad |= refused;
-    if (OWN && whole) pdl_wait();  // the shared part's sums
     tile.finish();
     const int64_t out_row = (int64_t)at.b * a.v.Hq + qs.first;
     const int64_t part_row = CLUSTER ? 0 : (int64_t)((2 * blockIdx.x + (nth > 0)) * n_heads + wh) * g.p.rows;
@@ -1193,7 +1144,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
         const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
         if (e >= d) continue;
         float w[Z::NW];
-        Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
+        const Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < Z::NW; ++k)
@@ -1209,11 +1160,6 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
             for (int c = 0; c < g.p.cluster; ++c)
               store_remote(remote(&sh.cluster_ml[rank][r], c), make_float2(j.m, j.bad ? -1.f : j.l));
         } else if (whole) {
-          if (OWN && takes_part) {
-            const int h = g.p.by_chunks.div(at.group * g.p.wh + wh);
-            j.bad |= __ldcg(&g.x.groups[g.x.group_of[at.b]].bad) != 0;
-            join_shared(g, group, h, (at.b - group.start) * a.v.qpg + qs.first - h * a.v.qpg + r, e, sum, j);
-          }
           const float f = j.bad || j.l == 0.f ? 0.f : 1.f / j.l;
           put4(out + (out_row + r) * d + e,
                f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f), even);
@@ -1244,7 +1190,6 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     cluster_wait();
     return;
   }
-  if (OWN) pdl_wait();
   // Every CTA of the cluster has sent its sums: each joins its share of the elements.
   cluster_arrive();
   cluster_wait();
@@ -1253,7 +1198,7 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
     const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
     if (e >= d) continue;
     float w[kMaxCluster];
-    Joined j = join_rows<kMaxCluster>(g.p.cluster, w, [&](int k) { return sh.cluster_ml[k][r]; });
+    const Joined j = join_rows<kMaxCluster>(g.p.cluster, w, [&](int k) { return sh.cluster_ml[k][r]; });
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < kMaxCluster; ++k)
@@ -1262,11 +1207,6 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
         sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
       }
     const int64_t row = (int64_t)at.b * a.v.Hq + qs.first + r;
-    if (OWN && takes_part) {
-      const int h = g.p.by_chunks.div(at.group);
-      j.bad |= __ldcg(&g.x.groups[g.x.group_of[at.b]].bad) != 0;
-      join_shared(g, group, h, (at.b - group.start) * a.v.qpg + qs.first - h * a.v.qpg + r, e, sum, j);
-    }
     const float f = j.bad || j.l == 0.f ? 0.f : 1.f / j.l;
     put4(out + row * d + e,
          f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f), even);
@@ -1278,9 +1218,9 @@ __global__ void __launch_bounds__(Z::NW * 32, Z::NW == warps_of(Z::DP, true) ? 1
 // launch
 // ---------------------------------------------------------------------------
 
-template <class Z, class Tile, bool CLUSTER, bool OWN = false>
+template <class Z, class Tile, bool CLUSTER>
 cudaError_t launch_kernel(const Args& g, cudaStream_t s) {
-  const auto k = paged_decode_kernel<Z, Tile, CLUSTER, OWN>;
+  const auto k = paged_decode_kernel<Z, Tile, CLUSTER>;
   static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

@@ -11,7 +11,7 @@
 // shared tokens as the longest does, at most 256 and the number of rows fewer: a chunk's tokens all do,
 // and attend one by one to those at its end, while a row far behind does by itself what it sees.
 //
-// Three launches: the plan (one block), the shared part, the own tokens.  The last starts while the second runs.
+// Four launches: the plan (one block), the shared part, the own tokens (which start as the shared part's CTAs end), the join.
 #include <cmath>
 
 #include "paged_decode.cuh"
@@ -25,13 +25,13 @@ constexpr int kPlanThreads = 512;
 // A row's first visible token, those it sees of the shared ones (0: none, or a bad length), and its length.
 struct RowView {
   int first, eff, len;
+  bool bad;
 };
 __device__ __forceinline__ RowView row_view(const PagedDecodeArgs& a, int b, int shared) {
   RowView r;
-  bool bad;
-  const int span = visible(a, b, r.first, bad);
-  r.len = bad ? 0 : span + r.first;
-  r.eff = min(r.len, shared);
+  const int span = visible(a, b, r.first, r.bad);
+  r.len = r.bad ? r.first : span + r.first;
+  r.eff = r.bad ? 0 : min(r.len, shared);
   return r;
 }
 
@@ -49,7 +49,6 @@ __device__ __forceinline__ void plan_group(const Args& g, int at, bool there) {
   for (int b = start + lane; b < end; b += LANES) {
     const RowView r = row_view(a, b, shared);
     if (r.len > longest) longest = r.len, row = b;
-    x.group_of[b] = at;
   }
 #pragma unroll
   for (int o = LANES / 2; o; o >>= 1) {
@@ -67,7 +66,23 @@ __device__ __forceinline__ void plan_group(const Args& g, int at, bool there) {
     last = min(last, __shfl_xor_sync(~0u, last, o));
     first = max(first, __shfl_xor_sync(~0u, first, o));
   }
-  if (rows < 2 || last <= first) last = first = 0;
+  if (last <= first) last = first = 0;
+  if (rows < 2) last = first = 0;
+  // what each row has of its own; the counts of tiles are summed up later
+  for (int b = start + lane; b < end; b += LANES) {
+    const RowView r = row_view(a, b, rows > 1 ? shared : 0);
+    RowPlan own;
+    const bool takes_part = last > first && r.eff >= last && r.first <= first, bad = r.bad || r.len - r.eff > a.max_own;
+    if (bad) atomicOr(a.err, kErrBadSeq);
+    own.state = bad ? kEmpty : 0;
+    own.group = takes_part && !bad ? at : -1;
+    own.skip_at = takes_part ? first : 0;
+    own.skip = takes_part ? last - first : 0;
+    own.first = r.first;
+    own.end = bad ? r.first : r.len - own.skip;
+    own.tiles = own.pad = 0;
+    x.own[b] = own;
+  }
   if (!there || lane) return;
   GroupPlan p;
   p.start = start;
@@ -126,12 +141,144 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       }
       __syncthreads();
     }
-    if (units > kUnitLimit) wrong = 1;
+  }
+  if (units > kUnitLimit) wrong = 1;
+  // the rows' own tiles
+  int64_t tiles = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    RowPlan own = {0, 0, 0, 0, -1, kEmpty, 0, 0};
+    if (b < a.B && !wrong) own = x.own[b];
+    const int64_t mine = b < a.B ? max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile) : 0;
+    int64_t t = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(~0u, t, o);
+      if (lane >= o) t += y;
+    }
+    if (lane == 31) sums[0][warp] = t;
+    __syncthreads();
+    int64_t before = tiles;
+    for (int w = 0; w < kPlanThreads / 32; ++w) {
+      if (w < warp) before += sums[0][w];
+      tiles += sums[0][w];
+    }
+    if (b < a.B) {
+      own.tiles = (int)min(before + t - mine, (int64_t)kUnitLimit);
+      x.own[b] = own;
+    }
+    __syncthreads();
+    if (b0 + kPlanThreads >= a.B && tiles * g.p.groups > kUnitLimit) {  // too many: once more, with none
+      wrong = 1;
+      tiles = 0;
+      b0 = -kPlanThreads;
+    }
   }
   if (tid == 0) {
     if (wrong) atomicOr(a.err, kErrBadSeq);
     x.all->units = wrong ? 0 : (int)units;
-    x.all->bad = wrong;
+    x.all->own_tiles = (int)tiles;
+  }
+}
+
+// Joins a row's partial sums, those of its own tokens and of what it shares: a warp per row and query head.
+constexpr int kJoinThreads = 128;
+
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args g, const Divider by_heads,
+                                                            const Divider by_rows) {
+  constexpr int kBatch = 4;
+  const PagedDecodeArgs& a = g.a;
+  const Prefix& x = g.x;
+  const int lane = threadIdx.x & 31, d = a.v.d, qpg = a.v.qpg;
+  const int64_t nth = (int64_t)blockIdx.x * (kJoinThreads / 32) + threadIdx.x / 32;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (nth >= (int64_t)a.B * a.v.Hq) return;
+  const int b = by_heads.div((uint32_t)nth), j = (int)(nth - (int64_t)b * a.v.Hq);
+  const RowPlan own = x.own[b];
+  const int h = x.by_qpg.div(j), q = j - h * qpg, chunk = by_rows.div(q), r = q - chunk * g.p.rows, vh = h * g.p.chunks + chunk;
+  const int group = vh / g.p.wh, w = vh - group * g.p.wh;
+  // the CTAs that have left sums of its own tokens
+  const int own_tiles = x.all->own_tiles, units = g.p.groups * own_tiles;
+  const Ranges ranges(units, min(g.p.n_items, units));
+  const int u = group * own_tiles + own.tiles, tiles = max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile);
+  const int c0 = ranges.item_of(u), n_own = own.end > own.first ? ranges.item_of(u + tiles - 1) - c0 + 1 : 0;
+  const int64_t own0 = x.own_row(g.p, a.B, group, b, c0, w) + r, own_step = (int64_t)g.p.wh * g.p.rows;
+  bool bad = own.state == kEmpty;
+  // and of what its group shares
+  int n = n_own;
+  int64_t part0 = 0;
+  const int64_t part_step = (int64_t)x.wh * x.rows;
+  if (own.group >= 0) {
+    const GroupPlan p = x.groups[own.group];
+    bad |= p.bad != 0;
+    const int row = (b - p.start) * qpg + q, hg = h / x.wh, block = row / x.rows;
+    const Ranges items(x.all->units, min(x.n_items, x.all->units));
+    const int v = p.units + (hg * p.blocks + block) * p.tiles, i0 = items.item_of(v);
+    n += items.item_of(v + p.tiles - 1) - i0 + 1;
+    part0 = x.row_of(p, a.v.Hkv, qpg, hg, block, i0, h - hg * x.wh, row - block * x.rows);
+  }
+  if (bad) n = 0;
+  const auto sums_of = [&](int i) {
+    return i < n_own ? x.own_u + (own0 + i * own_step) * g.DP : x.part_u + (part0 + (i - n_own) * part_step) * g.DP;
+  };
+  const auto ml_of = [&](int i) {
+    return *reinterpret_cast<const float2*>(i < n_own ? x.own_ml + 2 * (own0 + i * own_step)
+                                                      : x.part_ml + 2 * (part0 + (i - n_own) * part_step));
+  };
+  T* out = static_cast<T*>(a.out);
+  const int quads = min(g.DP / 4, 32), lanes = 32 / quads, turn = lane / quads;
+  for (int q0 = 0; q0 < g.DP / 4; q0 += quads) {  // once, but twice for heads above 128
+    const int el = 4 * (q0 + lane % quads);
+    float M = -CUDART_INF_F, total = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      const int count = min(32, n - i0);
+      float4 v[kBatch];
+      const auto fetch = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+          if (i + k * lanes < count && el < d) v[k] = *reinterpret_cast<const float4*>(sums_of(i0 + i + k * lanes) + el);
+      };
+      float2 ml = make_float2(-CUDART_INF_F, 0.f);
+      if (lane < count) ml = ml_of(i0 + lane);
+      fetch(turn);
+      float top = fmaxf(M, ml.x);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+      const float base = top == -CUDART_INF_F ? 0.f : top, f = exp2_approx(ml.x - base), before = exp2_approx(M - base);
+      float l = ml.y * f;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+      bad |= __any_sync(~0u, ml.y < 0.f) != 0;
+      total = total * before + l;
+      sum.x *= before, sum.y *= before, sum.z *= before, sum.w *= before;
+      M = top;
+      for (int i = 0; i < count; i += kBatch * lanes) {
+        if (i) fetch(i + turn);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          const int p = i + turn + k * lanes;
+          const float c = __shfl_sync(~0u, f, p & 31);
+          if (p < count && el < d && c != 0.f)
+            sum.x += v[k].x * c, sum.y += v[k].y * c, sum.z += v[k].z * c, sum.w += v[k].w * c;
+        }
+      }
+    }
+    for (int k = quads; k < 32; k <<= 1) {  // the lanes that share a quad of elements
+      sum.x += __shfl_xor_sync(~0u, sum.x, k);
+      sum.y += __shfl_xor_sync(~0u, sum.y, k);
+      sum.z += __shfl_xor_sync(~0u, sum.z, k);
+      sum.w += __shfl_xor_sync(~0u, sum.w, k);
+    }
+    if (turn == 0 && el < d) {
+      const bool none = bad || total == 0.f;
+      const float f = 1.f / total;
+      put4(out + nth * d + el, none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f),
+           (reinterpret_cast<uintptr_t>(out) & 3) == 0);
+      if (a.lse && el == 0) a.lse[nth] = none ? -CUDART_INF_F : (M + log2f(total)) * 0.693147180559945f;
+    }
   }
 }
 
@@ -160,11 +307,22 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
   return l;
 }
 
-size_t bytes_all(int B) { return 256 + align_up((size_t)B * sizeof(GroupPlan), 256) + align_up((size_t)B * sizeof(int), 256); }
-// (a CTA leaves 128 rows of an item, or each of two on an SM 16 for up to four heads)
-int64_t partial_rows(const PagedView& v, int B, int sms) {
-  return (int64_t)B * v.Hq + (int64_t)sms * 128;
-}
+// The parts of the workspace.
+struct Parts {
+  size_t groups, own, part_ml, part_u, own_ml, own_u, all;
+  Parts(const PagedView& v, const Plan& p, int B, int sms) {
+    // (a CTA leaves 128 rows of an item, or each of two on an SM 16 for up to four heads)
+    const size_t rows = (size_t)B * v.Hq + (size_t)sms * 128, DP = padded_dim(v.d);
+    const size_t own_rows = ((size_t)p.groups * B + p.n_items) * p.wh * p.rows;
+    groups = 256;
+    own = groups + align_up((size_t)B * sizeof(GroupPlan), 256);
+    part_ml = own + align_up((size_t)B * sizeof(RowPlan), 256);
+    part_u = part_ml + align_up(rows * 2 * sizeof(float), 256);
+    own_ml = part_u + align_up(rows * DP * sizeof(float), 256);
+    own_u = own_ml + align_up(own_rows * 2 * sizeof(float), 256);
+    all = own_u + align_up(own_rows * DP * sizeof(float), 256);
+  }
+};
 
 }  // namespace
 }  // namespace paged
@@ -172,28 +330,28 @@ int64_t partial_rows(const PagedView& v, int B, int sms) {
 using namespace paged;
 
 size_t paged_shared_workspace(const PagedView& v, DecodeKind kind, int B, int max_len, int max_own, int sms) {
-  const int64_t rows = partial_rows(v, std::max(B, 1), sms);
-  return std::max(paged_decode_workspace(v, kind, B, max_len, sms),
-                  bytes_all(std::max(B, 1)) + align_up((size_t)rows * 2 * sizeof(float), 256) +
-                      align_up((size_t)rows * padded_dim(v.d) * sizeof(float), 256));
+  const Plan p = range_plan(v, kind, std::max(B, 1), std::min(max_own, max_len), sms);
+  return std::max(paged_decode_workspace(v, kind, B, max_len, sms), Parts(v, p, std::max(B, 1), sms).all);
 }
 
 cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int sms, cudaStream_t s) {
   Args g = {};
   g.a = a;
-  g.p = own_plan(a.v, kind, a.B, std::min(a.max_own, a.max_len), a.window, sms);
+  g.p = range_plan(a.v, kind, a.B, std::min(a.max_own, a.max_len), sms);
   g.DP = padded_dim(a.v.d);
   g.score.set(a.scale, a.softcap);
   const int el = kind.dtype == DCK_F32 ? 4 : 2;
   g.p.q_copied = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride * el % 16 == 0;
   const Layout l = layout_of(a.v, kind, a.B, a.n_groups, sms);
+  const Parts parts(a.v, g.p, a.B, sms);
   char* ws = static_cast<char*>(a.ws);
-  g.x.all = reinterpret_cast<Shared0*>(ws);
-  g.x.groups = reinterpret_cast<GroupPlan*>(ws + 256);
-  g.x.group_of = reinterpret_cast<int*>(ws + 256 + align_up((size_t)a.B * sizeof(GroupPlan), 256));
-  ws += bytes_all(a.B);
-  g.x.part_ml = reinterpret_cast<float*>(ws);
-  g.x.part_u = reinterpret_cast<float*>(ws + align_up((size_t)partial_rows(a.v, a.B, sms) * 2 * sizeof(float), 256));
+  g.x.all = reinterpret_cast<Whole*>(ws);
+  g.x.groups = reinterpret_cast<GroupPlan*>(ws + parts.groups);
+  g.x.own = reinterpret_cast<RowPlan*>(ws + parts.own);
+  g.x.part_ml = reinterpret_cast<float*>(ws + parts.part_ml);
+  g.x.part_u = reinterpret_cast<float*>(ws + parts.part_u);
+  g.x.own_ml = reinterpret_cast<float*>(ws + parts.own_ml);
+  g.x.own_u = reinterpret_cast<float*>(ws + parts.own_u);
   g.x.n_groups = a.n_groups;
   g.x.n_items = l.n_items;
   g.x.rows = l.rows;
@@ -211,7 +369,11 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
     e = l.tc ? launch_prefix_tc(h, s) : kind.quant ? launch_prefix_q8(h, kind.dtype, s) : kind.dtype == DCK_F32 ? launch_prefix_f32(h, s) : launch_prefix_bf16(h, s);
   if (e == cudaSuccess)
     e = kind.quant ? launch_own_q8(g, kind.dtype, s) : kind.dtype == DCK_F32 ? launch_own_f32(g, s) : launch_own_bf16(g, s);
-  return e;
+  if (e != cudaSuccess) return e;
+  const int64_t warps = (int64_t)a.B * a.v.Hq, blocks = (warps * 32 + kJoinThreads - 1) / kJoinThreads;
+  const auto join = kind.dtype == DCK_F32 ? join_kernel<float> : join_kernel<__nv_bfloat16>;
+  e = launch_pdl(join, (unsigned)blocks, kJoinThreads, 0, s, g, divider((uint32_t)a.v.Hq), divider((uint32_t)g.p.rows));
+  return e == cudaSuccess ? hook_launched(a.hook, s) : e;
 }
 
 }  // namespace dck

@@ -53,6 +53,53 @@ struct ItemWalk {
   __device__ __forceinline__ int count(const Prefix& x, int qpg) const { return min(x.rows, p.rows * qpg - block * x.rows); }
 };
 
+// Stores the sums of a CTA's tiles of queries: `count` of them per head, from partial row row0 on (of this warp's head).
+// A head's runs of tokens add up first: each warp leaves its sums in stage `used`, which it has just read.
+// Sum -1: a page outside the pool.
+template <class Z, class Tile, class Shm>
+__device__ __forceinline__ void leave_sums(uint8_t* raw, Shm& sh, const Tile& tile, int warp, int lane, int n_heads, int n_runs,
+                                           int used, int count, int d, bool bad, float* part_u, float* part_ml, int64_t row0) {
+  const int wh = warp & (n_heads - 1), wt = warp / n_heads;
+  if (n_runs == 1) {
+#pragma unroll
+    for (int y = 0; y < Tile::kMine; ++y) {
+      const int r = Tile::row(y, lane);
+      if (r >= count) continue;
+      if (Tile::speaks(lane)) *reinterpret_cast<float2*>(part_ml + 2 * (row0 + r)) = make_float2(tile.m[y], bad ? -1.f : tile.l[y]);
+      float* p = part_u + (row0 + r) * Z::DP;
+      tile.each(y, lane, d, [&](int e, float u, float v) { *reinterpret_cast<float2*>(p + e) = make_float2(u, v); });
+    }
+    return;
+  }
+  float* left = reinterpret_cast<float*>(raw + (warp * Z::S + used) * Z::kStage);
+#pragma unroll
+  for (int y = 0; y < Tile::kMine; ++y) {
+    const int r = Tile::row(y, lane);
+    if (Tile::speaks(lane)) sh.ml[warp][r] = make_float2(tile.m[y], bad ? -1.f : tile.l[y]);
+    tile.each(y, lane, d, [&](int e, float u, float v) {
+      *reinterpret_cast<float2*>(left + r * Z::DP + (e ^ (r & 7) * 8)) = make_float2(u, v);
+    });
+  }
+  __syncthreads();
+  for (int i = wt * 32 + lane; i < count * (Z::DP / 4); i += n_runs * 32) {
+    const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
+    if (e >= d) continue;
+    float w[Z::NW];
+    const Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < Z::NW; ++k)
+      if (k < n_runs && w[k] != 0.f) {
+        const float* from = reinterpret_cast<const float*>(raw + ((k * n_heads + wh) * Z::S + used) * Z::kStage);
+        const float4 v = *reinterpret_cast<const float4*>(from + r * Z::DP + (e ^ (r & 7) * 8));
+        sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
+      }
+    *reinterpret_cast<float4*>(part_u + (row0 + r) * Z::DP + e) = sum;
+    if (e == 0) *reinterpret_cast<float2*>(part_ml + 2 * (row0 + r)) = make_float2(j.m, j.bad ? -1.f : j.l);
+  }
+  __syncthreads();
+}
+
 template <class Z, class Tile>
 __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid_constant__ Args g) {
   extern __shared__ __align__(128) uint8_t raw[];
@@ -147,46 +194,9 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
       atomicOr(&x.groups[at.g].bad, 1);
     }
     tile.finish();
-    const int64_t row0 = x.row_of(at.p, a.v.Hkv, qpg, at.hg, at.block, blockIdx.x, wh, 0);
-    if (n_runs == 1) {
-#pragma unroll
-      for (int y = 0; y < Tile::kMine; ++y) {
-        const int r = Tile::row(y, lane);
-        if (r >= count) continue;
-        if (Tile::speaks(lane)) *reinterpret_cast<float2*>(x.part_ml + 2 * (row0 + r)) = make_float2(tile.m[y], tile.l[y]);
-        float* p = x.part_u + (row0 + r) * Z::DP;
-        tile.each(y, lane, d, [&](int e, float u, float v) { *reinterpret_cast<float2*>(p + e) = make_float2(u, v); });
-      }
-    } else {
-      float* left = reinterpret_cast<float*>(raw + (warp * Z::S + used) * Z::kStage);
-#pragma unroll
-      for (int y = 0; y < Tile::kMine; ++y) {
-        const int r = Tile::row(y, lane);
-        if (Tile::speaks(lane)) sh.ml[warp][r] = make_float2(tile.m[y], tile.l[y]);
-        tile.each(y, lane, d, [&](int e, float u, float v) {
-          *reinterpret_cast<float2*>(left + r * Z::DP + (e ^ (r & 7) * 8)) = make_float2(u, v);
-        });
-      }
-      __syncthreads();
-      for (int i = wt * 32 + lane; i < count * (Z::DP / 4); i += n_runs * 32) {
-        const int r = i / (Z::DP / 4), e = i % (Z::DP / 4) * 4;
-        if (e >= d) continue;
-        float w[Z::NW];
-        const Joined j = join_rows<Z::NW>(n_runs, w, [&](int k) { return sh.ml[k * n_heads + wh][r]; });
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < Z::NW; ++k)
-          if (k < n_runs && w[k] != 0.f) {
-            const float* from = reinterpret_cast<const float*>(raw + ((k * n_heads + wh) * Z::S + used) * Z::kStage);
-            const float4 v = *reinterpret_cast<const float4*>(from + r * Z::DP + (e ^ (r & 7) * 8));
-            sum.x += v.x * w[k], sum.y += v.y * w[k], sum.z += v.z * w[k], sum.w += v.w * w[k];
-          }
-        *reinterpret_cast<float4*>(x.part_u + (row0 + r) * Z::DP + e) = sum;
-        if (e == 0) *reinterpret_cast<float2*>(x.part_ml + 2 * (row0 + r)) = make_float2(j.m, j.l);
-      }
-      __syncthreads();
-      load.clear_stage(reinterpret_cast<uint8_t*>(left));
-    }
+    leave_sums<Z>(raw, sh, tile, warp, lane, n_heads, n_runs, used, count, d, false, x.part_u, x.part_ml,
+                  x.row_of(at.p, a.v.Hkv, qpg, at.hg, at.block, blockIdx.x, wh, 0));
+    if (n_runs > 1) load.clear_stage(raw + (warp * Z::S + used) * Z::kStage);
     if (last) break;
     bad = false;
     fresh = true;
@@ -195,21 +205,170 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
   cp_async_wait<0>();
 }
 
+// A position in the list of the rows' own tiles (head groups outermost).
+struct OwnWalk : Walk {
+  RowPlan p, next;
+
+  static __device__ __forceinline__ RowPlan row(const Prefix& x, int b) {
+    RowPlan r;
+    const int4* from = reinterpret_cast<const int4*>(x.own + b);
+    int4* to = reinterpret_cast<int4*>(&r);
+    to[0] = from[0], to[1] = from[1];
+    return r;
+  }
+  __device__ __forceinline__ void take(int tile) {
+    token = p.first;
+    len = p.end;
+    skip_at = p.skip_at;
+    skip = p.skip;
+    left = max(1, (p.end - p.first + tile - 1) / tile);
+  }
+  // Enters at tile u (called by whole warps).
+  __device__ __forceinline__ void enter(const Args& g, int u) {
+    const Prefix& x = g.x;
+    group = u / x.all->own_tiles;
+    const int at = u - group * x.all->own_tiles;
+    int lo = 0, n = g.a.B;  // the last row with as many tiles before or fewer
+    while (n > 1) {
+      const int step = (n + 31) / 32, i = (threadIdx.x & 31) * step;
+      const uint32_t ok = __ballot_sync(~0u, i < n && x.own[lo + (i < n ? i : 0)].tiles <= at);
+      const int k = (31 - __clz(ok)) * step;
+      lo += k;
+      n = min(step, n - k);
+    }
+    b = lo;
+    p = row(x, b);
+    next = row(x, b + 1 < g.a.B ? b + 1 : 0);
+    take(g.p.tile);
+    const int tile = at - p.tiles;
+    token += tile * g.p.tile;
+    left -= tile;
+  }
+  // The next (head group, row); the plan of the one after it is read ahead.
+  __device__ __forceinline__ void leave(const Args& g) {
+    if (++b == g.a.B) b = 0, ++group;
+    p = next;
+    next = row(g.x, b + 1 < g.a.B ? b + 1 : 0);
+    take(g.p.tile);
+  }
+};
+
+// What the rows have of their own: tiles dealt in ranges as in paged_decode_kernel, a partial sum left of each (head group,
+// row) by each CTA that has tiles of it.
 template <class Z, class Tile>
-cudaError_t launch_prefix(const Args& g, cudaStream_t s) {
-  const auto k = prefix_kernel<Z, Tile>;
-  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
-  constexpr size_t smem = Z::kRing + sizeof(Shared<Z, Tile, false>);
+__global__ void __launch_bounds__(Z::NW * 32, kPerSm) own_kernel(const __grid_constant__ Args g) {
+  extern __shared__ __align__(128) uint8_t raw[];
+  using Shm = Shared<Z, Tile, false>;
+  Shm& sh = *reinterpret_cast<Shm*>(raw + Z::kRing);
+  const PagedDecodeArgs& a = g.a;
+  const Prefix& x = g.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_heads = g.p.wh, n_runs = g.p.wt, wh = warp & (n_heads - 1), wt = warp / n_heads;
+  const int d = a.v.d, n_tiles = x.all->own_tiles, units = g.p.groups * n_tiles;
+  pdl_launch_dependents();  // (the shared part let this launch begin: the plan and all before it are complete)
+  const Ranges ranges(units, min(g.p.n_items, units));
+  if ((int)blockIdx.x >= ranges.n) {
+    pdl_wait();  // what waits for this launch waits for the shared part too
+    return;
+  }
+  const typename LoaderOf<Z, Tile::kRows, Shm::kPlaces>::type load(g, raw, sh.q, warp, lane, wh, wt);
+  load.clear(raw);
+  const int u0 = ranges.begin(blockIdx.x), u1 = ranges.begin(blockIdx.x + 1);
+  OwnWalk ahead;
+  ahead.enter(g, u0);
+  OwnWalk at = ahead;
+  int to_compute = u1 - u0, to_copy = to_compute, to_fetch = to_compute;
+  Pages pages = {0, -1, 0, -1}, pages2 = {0, -1, 0, -1};
+  bool first = true;
+  const auto fetch_next = [&]() {
+    const Pages p = load.template fetch<true>(ahead, first);
+    first = false;
+    ahead.token += g.p.tile;
+    if (--to_fetch > 0 && --ahead.left == 0) {
+      ahead.leave(g);
+      first = true;
+    }
+    return p;
+  };
+  if (to_fetch > 0) pages = fetch_next();
+  if (to_fetch > 0) pages2 = fetch_next();
+  uint32_t outside = 0;
+  int put = 0;
+  const auto copy_next = [&]() {
+    if (to_copy > 0) {
+      --to_copy;
+      const bool bad = load.issue(pages, put);
+      outside = (outside & ~(1u << put)) | (uint32_t)bad << put;
+      pages = pages2;
+      if (to_fetch > 0) pages2 = fetch_next();
+      put = put + 1 == Z::S ? 0 : put + 1;
+    }
+    cp_async_commit();
+  };
+  float* mine = sh.mine + warp * 8 * Tile::kRows;
+  Tile tile;
+  Queries qs;
+#pragma unroll 1
+  for (int i = 0; i < Z::S - 1; ++i) copy_next();
+  int get = 0;
+  bool bad = false, fresh = true;
+  while (true) {
+    __syncwarp();  // the stage that is filled next has been read
+    copy_next();
+    cp_async_wait<Z::S - 1>();
+    __syncwarp();
+    if (fresh) {
+      qs = queries_of(g, at.group, wh);
+      if (!g.p.q_copied) load.read_queries(qs, at.b, sh.q, warp, get);
+      tile.begin(load.places + get * load.kPlace, lane);
+      fresh = false;
+    }
+    bad |= outside >> get & 1;
+    tile.step(load.ring + get * Z::kStage, at.len - at.token - load.run, lane, g.score, mine);
+    const int used = get;
+    get = get + 1 == Z::S ? 0 : get + 1;
+    at.token += g.p.tile;
+    const bool last = --to_compute <= 0;
+    if (--at.left > 0 && !last) continue;
+    // the end of a (head group, row), or of this CTA's part of it
+    if (bad && lane == 0) atomicOr(a.err, kErrBadSeq);
+    tile.finish();
+    leave_sums<Z>(raw, sh, tile, warp, lane, n_heads, n_runs, used, qs.count, d, bad, x.own_u, x.own_ml,
+                  x.own_row(g.p, a.B, at.group, at.b, blockIdx.x, wh));
+    if (last) break;
+    if (n_runs > 1) load.clear_stage(raw + (warp * Z::S + used) * Z::kStage);
+    bad = false;
+    fresh = true;
+    at.leave(g);
+  }
+  cp_async_wait<0>();
+  pdl_wait();
+}
+
+template <class K>
+cudaError_t launch_part(K kernel, std::atomic<uint64_t>& ready, int grid, int threads, size_t smem, const Args& g, cudaStream_t s) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {  // devices on which it may use its shared memory
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     if (dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
   }
-  e = launch_pdl(k, g.x.n_items, Z::NW * 32, smem, s, g);
+  e = launch_pdl(kernel, grid, threads, smem, s, g);
   return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
+}
+
+template <class Z, class Tile>
+cudaError_t launch_own(const Args& g, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  return launch_part(own_kernel<Z, Tile>, ready, g.p.n_items, Z::NW * 32, Z::kRing + sizeof(Shared<Z, Tile, false>), g, s);
+}
+
+template <class Z, class Tile>
+cudaError_t launch_prefix(const Args& g, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  return launch_part(prefix_kernel<Z, Tile>, ready, g.x.n_items, Z::NW * 32, Z::kRing + sizeof(Shared<Z, Tile, false>), g, s);
 }
 
 }  // namespace paged

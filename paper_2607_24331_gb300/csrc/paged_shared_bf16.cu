@@ -5,14 +5,10 @@ namespace dck {
 namespace paged {
 namespace {
 
-template <int DP, int S, int S_ALONE, bool PACK>
+template <int DP, int S, bool PACK>
 cudaError_t own(const Args& g, cudaStream_t s) {
-  if (g.p.warps == warps_of(DP, true)) {
-    using Z = Sizes<__nv_bfloat16, DP, warps_of(DP, true), S_ALONE, 16>;
-    return launch_kernel<Z, TensorTile<Z, PACK>, true, true>(g, s);
-  }
   using Z = Sizes<__nv_bfloat16, DP, warps_of(DP, false), S, 16>;
-  return launch_kernel<Z, TensorTile<Z, PACK>, true, true>(g, s);
+  return launch_own<Z, TensorTile<Z, PACK>>(g, s);
 }
 
 template <int DP, int S, bool PACK>
@@ -24,9 +20,9 @@ cudaError_t prefix(const Args& g, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_own_bf16(const Args& g, cudaStream_t s) {
-  if (g.DP == 256) return own<256, 2, 2, true>(g, s);
-  if (g.DP == 128) return g.p.rows > 8 ? own<128, 2, 2, false>(g, s) : own<128, 2, 3, true>(g, s);
-  return g.p.rows > 8 ? own<64, 4, 4, false>(g, s) : own<64, 4, 4, true>(g, s);
+  if (g.DP == 256) return own<256, 2, true>(g, s);
+  if (g.DP == 128) return g.p.rows > 8 ? own<128, 2, false>(g, s) : own<128, 2, true>(g, s);
+  return g.p.rows > 8 ? own<64, 4, false>(g, s) : own<64, 4, true>(g, s);
 }
 
 cudaError_t launch_prefix_bf16(const Args& g, cudaStream_t s) {

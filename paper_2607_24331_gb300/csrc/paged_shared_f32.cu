@@ -5,21 +5,11 @@ namespace dck {
 namespace paged {
 namespace {
 
-template <int DP, int S, int ROWS>
-cudaError_t own_rows(const Args& g, cudaStream_t s) {
-  if (g.p.warps == warps_of(DP, true)) {
-    using Z = Sizes<float, DP, warps_of(DP, true), S, 8>;
-    return launch_kernel<Z, SimtTile<Z, ROWS>, true, true>(g, s);
-  }
-  using Z = Sizes<float, DP, warps_of(DP, false), S, 8>;
-  return launch_kernel<Z, SimtTile<Z, ROWS>, true, true>(g, s);
-}
-
 template <int DP, int S>
 cudaError_t own(const Args& g, cudaStream_t s) {
-  if (g.p.rows == 1) return own_rows<DP, S, 1>(g, s);
-  if (g.p.rows <= 4) return own_rows<DP, S, 4>(g, s);
-  return own_rows<DP, S, 8>(g, s);
+  using Z = Sizes<float, DP, warps_of(DP, false), S, 8>;
+  if (g.p.rows == 1) return launch_own<Z, SimtTile<Z, 1>>(g, s);
+  return g.p.rows <= 4 ? launch_own<Z, SimtTile<Z, 4>>(g, s) : launch_own<Z, SimtTile<Z, 8>>(g, s);
 }
 
 template <int DP, int S>

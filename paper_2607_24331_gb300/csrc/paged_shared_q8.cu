@@ -6,14 +6,10 @@ namespace dck {
 namespace paged {
 namespace {
 
-template <typename T, int DP, int S, int S_ALONE, bool PACK>
+template <typename T, int DP, int S, bool PACK>
 cudaError_t own(const Args& g, cudaStream_t s) {
-  if (g.p.warps == warps_of(DP, true)) {
-    using Z = QuantSizes<T, DP, warps_of(DP, true), S_ALONE>;
-    return launch_kernel<Z, QuantTile<Z, PACK>, true, true>(g, s);
-  }
   using Z = QuantSizes<T, DP, warps_of(DP, false), S>;
-  return launch_kernel<Z, QuantTile<Z, PACK>, true, true>(g, s);
+  return launch_own<Z, QuantTile<Z, PACK>>(g, s);
 }
 
 template <typename T, int DP, int S, bool PACK>
@@ -26,13 +22,13 @@ cudaError_t prefix(const Args& g, cudaStream_t s) {
 
 cudaError_t launch_own_q8(const Args& g, int dtype, cudaStream_t s) {
   if (dtype == DCK_F32) {
-    if (g.DP == 256) return own<float, 256, 2, 2, true>(g, s);
-    return g.DP == 128 ? own<float, 128, 2, 2, true>(g, s) : own<float, 64, 4, 4, true>(g, s);
+    if (g.DP == 256) return own<float, 256, 2, true>(g, s);
+    return g.DP == 128 ? own<float, 128, 2, true>(g, s) : own<float, 64, 4, true>(g, s);
   }
   using T = __nv_bfloat16;
-  if (g.DP == 256) return own<T, 256, 2, 2, true>(g, s);
-  if (g.DP == 128) return g.p.rows > 8 ? own<T, 128, 2, 2, false>(g, s) : own<T, 128, 2, 3, true>(g, s);
-  return g.p.rows > 8 ? own<T, 64, 4, 4, false>(g, s) : own<T, 64, 4, 4, true>(g, s);
+  if (g.DP == 256) return own<T, 256, 2, true>(g, s);
+  if (g.DP == 128) return g.p.rows > 8 ? own<T, 128, 2, false>(g, s) : own<T, 128, 2, true>(g, s);
+  return g.p.rows > 8 ? own<T, 64, 4, false>(g, s) : own<T, 64, 4, true>(g, s);
 }
 
 cudaError_t launch_prefix_q8(const Args& g, int dtype, cudaStream_t s) {

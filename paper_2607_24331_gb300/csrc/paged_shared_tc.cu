@@ -412,20 +412,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
 
 template <int DP>
 cudaError_t launch(const Args& g, cudaStream_t s) {
-  const auto k = prefix_tc_kernel<DP>;
-  static std::atomic<uint64_t> ready{0};  // devices on which the kernel may use its shared memory
+  static std::atomic<uint64_t> ready{0};
   constexpr size_t smem = sizeof(ShmTc<DP>) + 1024;
   static_assert(smem <= 232448, "shared memory of a CTA");
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
-  }
-  e = launch_pdl(k, g.x.n_items, kThreads, smem, s, g);
-  return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
+  return launch_part(prefix_tc_kernel<DP>, ready, g.x.n_items, kThreads, smem, g, s);
 }
 
 }  // namespace
