@@ -96,7 +96,7 @@ struct QuantReadArgs {
   int64_t k_stride, v_stride;
   int* err;
 };
-cudaError_t launch_quant_read(const QuantReadArgs& a, int dtype, int sms, cudaStream_t s);
+cudaError_t launch_quant_read(const QuantReadArgs& a, int dtype, cudaStream_t s);
 
 struct PagedDecodeArgs {
   PagedView v;

@@ -414,8 +414,7 @@ dck_status dck_quant_read(const dck_quant_desc* desc, int32_t n_tok, const int64
   if (k_stride > most || v_stride > most || k_stride < 0 || v_stride < 0 || (n_tok > 1 && (k_stride < row || v_stride < row)))
     return DCK_ERR_INVALID;
   QuantReadArgs a;
-  int sms = 0;
-  if (!device_state(&a.err, &sms)) return DCK_ERR_CUDA;
+  if (!device_state(&a.err, nullptr)) return DCK_ERR_CUDA;
   a.v = make_view(desc);
   a.n_tok = n_tok;
   a.slots = d_slots;
@@ -427,7 +426,7 @@ dck_status dck_quant_read(const dck_quant_desc* desc, int32_t n_tok, const int64
   a.v_out = v;
   a.k_stride = k_stride;
   a.v_stride = v_stride;
-  if (launch_quant_read(a, desc->cache.dtype, sms, static_cast<cudaStream_t>(stream)) != cudaSuccess) return DCK_ERR_CUDA;
+  if (launch_quant_read(a, desc->cache.dtype, static_cast<cudaStream_t>(stream)) != cudaSuccess) return DCK_ERR_CUDA;
   set_last_launches(1);
   return DCK_OK;
 }

@@ -262,7 +262,8 @@ Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window
   while (heads % wide) wide /= 2;
 
   const int row = DP * el, slots = kPerSm * sms;
-  const double step = row <= 128 ? 0.45 : row == 256 ? 0.65 : row == 512 ? 0.95 : 1.37;  // a warp's run of tokens
+  const double step = kind.quant ? (DP == 64 ? 1.2 : DP == 128 ? 1.85 : 3.4)
+                                 : row <= 128 ? 0.45 : row == 256 ? 0.65 : row == 512 ? 0.95 : 1.37;  // a warp's run of tokens
   const double bytes = 1.07 * 2. * B * span * v.Hkv * (v.d * el + (kind.quant ? 4 : 0)) / 6.8e6;
   // (product of the two times) of a way with a fixed part and the longest CTA's part
   const auto times = [&](double fixed, double longest) {

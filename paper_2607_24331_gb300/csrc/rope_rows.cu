@@ -190,7 +190,7 @@ struct VecLaunch {
 constexpr int kRounds = 2;  // units per thread that a block's tokens are chosen for (1, 4 or 8: 43, 44, 48 us there)
 
 template <typename T, bool HALF, bool QUANT>
-__global__ void __launch_bounds__(kThreads, QUANT ? 5 : 6) rope_vec_kernel(const __grid_constant__ RopeLaunch a,
+__global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_constant__ RopeLaunch a,
                                                                const __grid_constant__ VecLaunch v) {
   constexpr int N = Vec<T>::N;
   // [tokens][N][turned] (cos, sin) of pair j N + k at k turned + j; then the tokens' cache rows
