@@ -43,21 +43,18 @@ __device__ __forceinline__ CacheRow cache_row(const RopeLaunch& a, int64_t i, bo
   return r;
 }
 
-// 8-bit rows.  Magnitudes are compared as the integers of their bits; infinities and NaN count as 0
-// there and are stored as NaN.
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
-}
-// The exponent e >= -126 of the scale 2^e of a row with largest magnitude `top`: the least with
+// 8-bit rows.  The exponent e >= -126 of the scale 2^e of a row with largest magnitude `top`: the least with
 // top <= 448 2^e.  448 = 1.75 2^8: mantissas above 1.75 carry into the exponent.
-__device__ __forceinline__ int scale_exponent(uint32_t top) { return max((int)((top + 0x1fffffu) >> 23) - 135, -126); }
+__device__ __forceinline__ int scale_exponent(float top) { return max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 135, -126); }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 .. 127
-// Two codes (x the lower) of elements divided by 2^e, `inverse` 2^-e.
-__device__ __forceinline__ uint32_t codes2(float x, float y, float inverse) {
-  const float a = fabsf(x) < CUDART_INF_F ? x * inverse : CUDART_NAN_F, b = fabsf(y) < CUDART_INF_F ? y * inverse : CUDART_NAN_F;
+// The larger magnitude (of a number and NaN: the number).
+__device__ __forceinline__ float larger(float x, float y) { return fmaxf(fabsf(x), fabsf(y)); }
+// Infinities count as 0 for the scale and are stored as NaN: so they are made NaN, in rows that have any.
+__device__ __forceinline__ float without_infinity(float x) { return fabsf(x) < CUDART_INF_F ? x : CUDART_NAN_F; }
+// Two codes (x the lower).
+__device__ __forceinline__ uint32_t codes2(float x, float y) {
   uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y), "f"(x));
   return r;
 }
 
@@ -83,7 +80,7 @@ __global__ void __launch_bounds__(kThreads) rope_any_kernel(const __grid_constan
       for (int h = threadIdx.x >> 5; h < rows.heads; h += kThreads / 32) {
         const T* sp = static_cast<const T*>(rows.src) + i * rows.src_tok + h * rows.src_head;
         float x[kMost];
-        uint32_t top = 0;
+        float top = 0.f;
 #pragma unroll
         for (int k = 0; k < kMost; ++k) {
           const int e = lane + 32 * k;
@@ -100,15 +97,17 @@ __global__ void __launch_bounds__(kThreads) rope_any_kernel(const __grid_constan
           } else if (e < a.d) {
             x[k] = to_f32(sp[e]);
           }
-          top = max(top, finite_bits(x[k]));
+          x[k] = without_infinity(x[k]);
+          top = larger(top, x[k]);
         }
-        top = __reduce_max_sync(~0u, top);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
         const int s = scale_exponent(top);
         const float inverse = power_of_two(-s);
         uint8_t* dp = static_cast<uint8_t*>(rows.dst) + to.page * rows.dst_page + to.off * rows.dst_tok + h * rows.dst_head;
 #pragma unroll
         for (int k = 0; k < kMost; ++k)
-          if (lane + 32 * k < a.d) dp[lane + 32 * k] = (uint8_t)codes2(x[k], 0.f, inverse);
+          if (lane + 32 * k < a.d) dp[lane + 32 * k] = (uint8_t)codes2(x[k] * inverse, 0.f);
         if (lane == 0)
           rows.scale[to.page * rows.scale_page + to.off * rows.scale_tok + h * rows.scale_head] = power_of_two(s);
       }
@@ -258,18 +257,27 @@ __global__ void __launch_bounds__(kThreads, 6) rope_vec_kernel(const __grid_cons
     if (QUANT && rows.scale) {
       Vec<T>::open(one ? x : make_uint4(0, 0, 0, 0), p);  // what was rounded to T
       Vec<T>::open(two ? y : make_uint4(0, 0, 0, 0), q);
-      uint32_t top = 0;
+      const auto largest = [&]() {
+        float top = 0.f;
 #pragma unroll
-      for (int k = 0; k < N; ++k) top = max(top, max(finite_bits(p[k]), finite_bits(q[k])));
-      for (int o = v.lanes / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(sharers, top, o));
+        for (int k = 0; k < N; ++k) top = larger(top, p[k]), top = larger(top, q[k]);
+        for (int o = v.lanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(sharers, top, o));
+        return top;
+      };
+      float top = largest();
+      if (top == CUDART_INF_F) {  // (alike in all threads of the row)
+#pragma unroll
+        for (int k = 0; k < N; ++k) p[k] = without_infinity(p[k]), q[k] = without_infinity(q[k]);
+        top = largest();
+      }
       const int e = scale_exponent(top);
       const float inverse = power_of_two(-e);
       uint8_t* dst = static_cast<uint8_t*>(rows.dst) + at + head * rows.dst_head;
       uint32_t c[N / 2];
 #pragma unroll
       for (int k = 0; k < N / 4; ++k) {
-        c[k] = codes2(p[4 * k], p[4 * k + 1], inverse) | codes2(p[4 * k + 2], p[4 * k + 3], inverse) << 16;
-        c[N / 4 + k] = codes2(q[4 * k], q[4 * k + 1], inverse) | codes2(q[4 * k + 2], q[4 * k + 3], inverse) << 16;
+        c[k] = codes2(p[4 * k] * inverse, p[4 * k + 1] * inverse) | codes2(p[4 * k + 2] * inverse, p[4 * k + 3] * inverse) << 16;
+        c[N / 4 + k] = codes2(q[4 * k] * inverse, q[4 * k + 1] * inverse) | codes2(q[4 * k + 2] * inverse, q[4 * k + 3] * inverse) << 16;
       }
       if (N == 8) {
         if (one) *reinterpret_cast<uint2*>(dst + va) = make_uint2(c[0], c[1]);
