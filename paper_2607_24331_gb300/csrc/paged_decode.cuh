@@ -95,10 +95,29 @@ struct Whole {  // of a whole call
   int units;      // tiles of all items
   int own_tiles;  // of all rows, per head group
 };
+// Where a CTA begins: its first item, or (head group, row), the tile's first token and the tiles from it to the end
+// of that, and how many it has in all.
+struct ItemStart {
+  GroupPlan p;
+  int g, hg, block, token, left, n, pad[2];
+};
+struct OwnStart {
+  RowPlan p;
+  int b, hg, token, left, n, pad[3];
+};
+template <class S>
+__device__ __forceinline__ S load_record(const S* from) {
+  S r;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(S) / 16); ++i) reinterpret_cast<int4*>(&r)[i] = reinterpret_cast<const int4*>(from)[i];
+  return r;
+}
 struct Prefix {
   Whole* all;
   GroupPlan* groups;
   RowPlan* own;    // [B]
+  ItemStart* item_start;  // [n_items]
+  OwnStart* own_start;    // [p.n_items]
   float *part_u, *part_ml;  // partial sums, as in Args, of what groups share: rows by row_of
   float *own_u, *own_ml;    // and of rows' own tokens: rows by own_row
   int n_groups, n_items;  // groups; CTAs that tiles are dealt to
@@ -232,6 +251,13 @@ struct Ranges {
       : units(units), n(n), each(n ? units / n : 0), rest(units - each * n) {}
   __device__ __forceinline__ int begin(int c) const { return c * each + c * rest / n; }
   __device__ __forceinline__ int item_of(int u) const { return (int)(((int64_t)(u + 1) * n + units - 1) / units) - 1; }
+  // The same without the long division: a quotient in fp32 is off by one or two at most.
+  __device__ __forceinline__ int near_item_of(int u) const {
+    int c = min(n - 1, (int)(__fdividef((float)u, (float)units) * n));
+    while (begin(c + 1) <= u) ++c;
+    while (begin(c) > u) --c;
+    return c;
+  }
 };
 
 // What the plan keeps of the sequences in shared memory.

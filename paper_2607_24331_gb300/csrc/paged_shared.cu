@@ -14,7 +14,7 @@
 // Four launches: the plan (one block), the shared part, the own tokens (which start as the shared part's CTAs end), the join.
 #include <cmath>
 
-#include "paged_decode.cuh"
+#include "paged_shared.cuh"
 
 namespace dck {
 namespace paged {
@@ -35,14 +35,25 @@ __device__ __forceinline__ RowView row_view(const PagedDecodeArgs& a, int b, int
   return r;
 }
 
-// A subgroup of LANES threads per group of rows at a time.
+// What the plan keeps in shared memory: per group its tiles of all items of a head group and then those of all
+// groups before (in 64 bits); per row its own tiles, then those of all rows before.
+struct PlanSums {
+  int64_t* units;  // [n_groups + 1]
+  int* tiles;      // [B + 1]
+};
+
+// A subgroup of LANES threads per group of rows at a time; true if d_group_start is not as it must be.
 template <int LANES>
-__device__ __forceinline__ void plan_group(const Args& g, int at, bool there) {
+__device__ __forceinline__ bool plan_group(const Args& g, const PlanSums& sums, int at, bool there) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int lane = threadIdx.x % LANES;
-  const int start = there ? a.group_start[at] : 0, end = there ? a.group_start[at + 1] : 0;
-  const int said = there ? a.shared_len[at] : 0, shared = max(said, 0), rows = end - start;
+  int start = 0, end = 0, said = 0;
+  if (there) start = a.group_start[at], end = a.group_start[at + 1], said = a.shared_len[at];
+  const bool wrong = there && (start < 0 || end < start || end > a.B || (at == 0 && start != 0) ||
+                               (at == x.n_groups - 1 && end != a.B));
+  if (wrong) end = start;
+  const int shared = max(said, 0), rows = end - start;
   if (said < 0 && lane == 0) atomicOr(a.err, kErrBadSeq);
   // the longest row, the first of them
   int longest = 0, row = start;
@@ -66,9 +77,8 @@ __device__ __forceinline__ void plan_group(const Args& g, int at, bool there) {
     last = min(last, __shfl_xor_sync(~0u, last, o));
     first = max(first, __shfl_xor_sync(~0u, first, o));
   }
-  if (last <= first) last = first = 0;
-  if (rows < 2) last = first = 0;
-  // what each row has of its own; the counts of tiles are summed up later
+  if (rows < 2 || last <= first) last = first = 0;
+  // what each row has of its own
   for (int b = start + lane; b < end; b += LANES) {
     const RowView r = row_view(a, b, rows > 1 ? shared : 0);
     RowPlan own;
@@ -82,8 +92,9 @@ __device__ __forceinline__ void plan_group(const Args& g, int at, bool there) {
     own.end = bad ? r.first : r.len - own.skip;
     own.tiles = own.pad = 0;
     x.own[b] = own;
+    sums.tiles[b] = max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile);
   }
-  if (!there || lane) return;
+  if (!there || lane) return wrong;
   GroupPlan p;
   p.start = start;
   p.rows = rows;
@@ -92,92 +103,123 @@ __device__ __forceinline__ void plan_group(const Args& g, int at, bool there) {
   p.table = row;
   p.tiles = (last - first + x.tile - 1) / x.tile;
   p.blocks = (int)(((int64_t)rows * a.v.qpg + x.rows - 1) / x.rows);
-  p.units = p.queries = p.bad = p.pad[0] = p.pad[1] = 0;
+  p.units = p.bad = p.pad[0] = p.pad[1] = 0;
+  p.queries = start * a.v.qpg;
   x.groups[at] = p;
+  sums.units[at] = (int64_t)p.tiles * p.blocks * (a.v.Hkv / x.wh);
+  return wrong;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Args g) {
-  const PagedDecodeArgs& a = g.a;
-  const Prefix& x = g.x;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = x.n_groups;
-  __shared__ int64_t sums[2][kPlanThreads / 32];
-  pdl_launch_dependents();
-  pdl_wait();
-  int wrong = 0;
-  for (int i = tid; i < n; i += kPlanThreads) {
-    const int s = a.group_start[i], e = a.group_start[i + 1];
-    wrong |= s < 0 || e < s || e > a.B || (i == 0 && s != 0) || (i == n - 1 && e != a.B);
-  }
-  wrong = __syncthreads_or(wrong);
-  int64_t units = 0, queries = 0;
-  if (!wrong) {
-    if (n <= 2 * kPlanThreads / 32) {
-      for (int i = warp; i < n; i += kPlanThreads / 32) plan_group<32>(g, i, true);
-    } else {
-      for (int i = 0; i < n; i += kPlanThreads / 8) plan_group<8>(g, i + tid / 8, i + tid / 8 < n);
-    }
-    __syncthreads();
-    const int head_groups = a.v.Hkv / x.wh;
-    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
-      const int i = i0 + tid;
-      const int64_t mine = i < n ? (int64_t)x.groups[i].tiles * x.groups[i].blocks * head_groups : 0;
-      const int64_t q = i < n ? (int64_t)x.groups[i].rows * a.v.qpg : 0;
-      int64_t u = mine, v = q;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(~0u, u, o), z = __shfl_up_sync(~0u, v, o);
-        if (lane >= o) u += y, v += z;
-      }
-      if (lane == 31) sums[0][warp] = u, sums[1][warp] = v;
-      __syncthreads();
-      int64_t before = units, ahead = queries;
-      for (int w = 0; w < kPlanThreads / 32; ++w) {
-        if (w < warp) before += sums[0][w], ahead += sums[1][w];
-        units += sums[0][w], queries += sums[1][w];
-      }
-      if (i < n) {
-        x.groups[i].units = (int)min(before + u - mine, (int64_t)kUnitLimit);
-        x.groups[i].queries = (int)(ahead + v - q);
-      }
-      __syncthreads();
-    }
-  }
-  if (units > kUnitLimit) wrong = 1;
-  // the rows' own tiles
-  int64_t tiles = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
-    const int b = b0 + tid;
-    RowPlan own = {0, 0, 0, 0, -1, kEmpty, 0, 0};
-    if (b < a.B && !wrong) own = x.own[b];
-    const int64_t mine = b < a.B ? max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile) : 0;
+// Sums of all before each of v[0 .. n - 1], in place, and of all in v[n].  Called by the whole block.
+template <typename V>
+__device__ __forceinline__ void sum_before(V* v, int n, int64_t* scratch) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int64_t base = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    const int64_t mine = i < n ? v[i] : 0;
     int64_t t = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t y = __shfl_up_sync(~0u, t, o);
       if (lane >= o) t += y;
     }
-    if (lane == 31) sums[0][warp] = t;
+    if (lane == 31) scratch[warp] = t;
     __syncthreads();
-    int64_t before = tiles;
+    int64_t before = base;
+#pragma unroll
     for (int w = 0; w < kPlanThreads / 32; ++w) {
-      if (w < warp) before += sums[0][w];
-      tiles += sums[0][w];
+      if (w < warp) before += scratch[w];
+      base += scratch[w];
     }
-    if (b < a.B) {
-      own.tiles = (int)min(before + t - mine, (int64_t)kUnitLimit);
-      x.own[b] = own;
+    if (i < n) v[i] = (V)min(before + t - mine, (int64_t)kUnitLimit);
+    __syncthreads();
+  }
+  if (tid == 0) v[n] = (V)min(base, (int64_t)kUnitLimit + 1);  // too many: above the limit
+  __syncthreads();
+}
+// The last i of 0 .. n - 1 with v[i] <= u.
+template <typename V>
+__device__ __forceinline__ int last_of(const V* v, int n, int u) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (v[mid] <= u) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Args g) {
+  const PagedDecodeArgs& a = g.a;
+  const Prefix& x = g.x;
+  const int tid = threadIdx.x, n = x.n_groups;
+  extern __shared__ int64_t plan_memory[];
+  __shared__ int64_t scratch[kPlanThreads / 32];
+  const PlanSums sums = {plan_memory, reinterpret_cast<int*>(plan_memory + n + 1)};
+  pdl_launch_dependents();
+  pdl_wait();
+  int wrong = 0;
+  if (n <= 2 * kPlanThreads / 32) {
+    for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, sums, i, true);
+  } else {
+    for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, sums, i + tid / 8, i + tid / 8 < n);
+  }
+  wrong = __syncthreads_or(wrong);
+  sum_before(sums.units, n, scratch);
+  if (!wrong) sum_before(sums.tiles, a.B, scratch);
+  if (sums.units[n] > kUnitLimit || (!wrong && (int64_t)sums.tiles[a.B] * g.p.groups > kUnitLimit)) wrong = 1;
+  __syncthreads();
+  if (wrong) {  // every row is empty, of one tile
+    for (int b = tid; b < a.B; b += kPlanThreads) {
+      x.own[b] = {0, 0, 0, 0, -1, kEmpty, 0, 0};
+      sums.tiles[b] = b;
+    }
+    if (tid == 0) {
+      atomicOr(a.err, kErrBadSeq);
+      sums.tiles[a.B] = a.B;
+      sums.units[n] = 0;
     }
     __syncthreads();
-    if (b0 + kPlanThreads >= a.B && tiles * g.p.groups > kUnitLimit) {  // too many: once more, with none
-      wrong = 1;
-      tiles = 0;
-      b0 = -kPlanThreads;
-    }
   }
-  if (tid == 0) {
-    if (wrong) atomicOr(a.err, kErrBadSeq);
-    x.all->units = wrong ? 0 : (int)units;
-    x.all->own_tiles = (int)tiles;
+  for (int i = tid; i < n; i += kPlanThreads) x.groups[i].units = (int)sums.units[i];
+  for (int b = tid; b < a.B; b += kPlanThreads) x.own[b].tiles = sums.tiles[b];
+  const int units = (int)sums.units[n], own_tiles = sums.tiles[a.B];
+  if (tid == 0) *x.all = {units, own_tiles};
+  __syncthreads();
+  // where each CTA begins
+  const Ranges items(units, min(x.n_items, units));
+  for (int c = tid; c < x.n_items; c += kPlanThreads) {
+    ItemStart s;
+    s.n = c < items.n ? items.begin(c + 1) - items.begin(c) : 0;
+    if (s.n) {
+      const int u = items.begin(c);
+      s.g = last_of(sums.units, n, u);
+      s.p = load_record(x.groups + s.g);
+      const int at = u - s.p.units, item = at / s.p.tiles, tile = at - item * s.p.tiles;
+      s.hg = item / s.p.blocks;
+      s.block = item - s.hg * s.p.blocks;
+      s.token = s.p.first + tile * x.tile;
+      s.left = s.p.tiles - tile;
+    }
+    x.item_start[c] = s;
+  }
+  const int own_units = own_tiles * g.p.groups;
+  const Ranges rows(own_units, min(g.p.n_items, own_units));
+  for (int c = tid; c < g.p.n_items; c += kPlanThreads) {
+    OwnStart s;
+    s.n = c < rows.n ? rows.begin(c + 1) - rows.begin(c) : 0;
+    s.b = s.hg = 0;
+    if (s.n) {
+      const int u = rows.begin(c);
+      s.hg = u / own_tiles;
+      const int at = u - s.hg * own_tiles;
+      s.b = last_of(sums.tiles, a.B, at);
+      s.p = load_record(x.own + s.b);
+      s.token = s.p.first + (at - sums.tiles[s.b]) * g.p.tile;
+      s.left = sums.tiles[s.b + 1] - at;
+    }
+    x.own_start[c] = s;
   }
 }
 
@@ -203,7 +245,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   const int own_tiles = x.all->own_tiles, units = g.p.groups * own_tiles;
   const Ranges ranges(units, min(g.p.n_items, units));
   const int u = group * own_tiles + own.tiles, tiles = max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile);
-  const int c0 = ranges.item_of(u), n_own = own.end > own.first ? ranges.item_of(u + tiles - 1) - c0 + 1 : 0;
+  const int c0 = ranges.near_item_of(u), n_own = own.end > own.first ? ranges.near_item_of(u + tiles - 1) - c0 + 1 : 0;
   const int64_t own0 = x.own_row(g.p, a.B, group, b, c0, w) + r, own_step = (int64_t)g.p.wh * g.p.rows;
   bool bad = own.state == kEmpty;
   // and of what its group shares
@@ -215,8 +257,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     bad |= p.bad != 0;
     const int row = (b - p.start) * qpg + q, hg = h / x.wh, block = row / x.rows;
     const Ranges items(x.all->units, min(x.n_items, x.all->units));
-    const int v = p.units + (hg * p.blocks + block) * p.tiles, i0 = items.item_of(v);
-    n += items.item_of(v + p.tiles - 1) - i0 + 1;
+    const int v = p.units + (hg * p.blocks + block) * p.tiles, i0 = items.near_item_of(v);
+    n += items.near_item_of(v + p.tiles - 1) - i0 + 1;
     part0 = x.row_of(p, a.v.Hkv, qpg, hg, block, i0, h - hg * x.wh, row - block * x.rows);
   }
   if (bad) n = 0;
@@ -293,7 +335,7 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
   const int64_t queries = (int64_t)v.qpg * B / std::max(n_groups, 1);  // of a group, on average
   l.tc = kind.dtype == DCK_BF16 && !kind.quant && DP <= 128 && queries > 16;
   if (l.tc) {
-    l.rows = 128;
+    l.rows = 256;
     l.tile = 64;
     l.wh = 1;
     l.n_items = sms;
@@ -309,14 +351,16 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
 
 // The parts of the workspace.
 struct Parts {
-  size_t groups, own, part_ml, part_u, own_ml, own_u, all;
+  size_t groups, own, item_start, own_start, part_ml, part_u, own_ml, own_u, all;
   Parts(const PagedView& v, const Plan& p, int B, int sms) {
-    // (a CTA leaves 128 rows of an item, or each of two on an SM 16 for up to four heads)
-    const size_t rows = (size_t)B * v.Hq + (size_t)sms * 128, DP = padded_dim(v.d);
+    // (a CTA leaves 256 rows of an item, or each of two on an SM 16 for up to four heads)
+    const size_t rows = (size_t)B * v.Hq + (size_t)sms * 256, DP = padded_dim(v.d);
     const size_t own_rows = ((size_t)p.groups * B + p.n_items) * p.wh * p.rows;
     groups = 256;
     own = groups + align_up((size_t)B * sizeof(GroupPlan), 256);
-    part_ml = own + align_up((size_t)B * sizeof(RowPlan), 256);
+    item_start = own + align_up((size_t)B * sizeof(RowPlan), 256);
+    own_start = item_start + align_up(kMaxItems * sizeof(ItemStart), 256);
+    part_ml = own_start + align_up(kMaxItems * sizeof(OwnStart), 256);
     part_u = part_ml + align_up(rows * 2 * sizeof(float), 256);
     own_ml = part_u + align_up(rows * DP * sizeof(float), 256);
     own_u = own_ml + align_up(own_rows * 2 * sizeof(float), 256);
@@ -348,6 +392,8 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   g.x.all = reinterpret_cast<Whole*>(ws);
   g.x.groups = reinterpret_cast<GroupPlan*>(ws + parts.groups);
   g.x.own = reinterpret_cast<RowPlan*>(ws + parts.own);
+  g.x.item_start = reinterpret_cast<ItemStart*>(ws + parts.item_start);
+  g.x.own_start = reinterpret_cast<OwnStart*>(ws + parts.own_start);
   g.x.part_ml = reinterpret_cast<float*>(ws + parts.part_ml);
   g.x.part_u = reinterpret_cast<float*>(ws + parts.part_u);
   g.x.own_ml = reinterpret_cast<float*>(ws + parts.own_ml);
@@ -358,7 +404,10 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   g.x.wh = l.wh;
   g.x.tile = l.tile;
   g.x.by_qpg = divider((uint32_t)a.v.qpg);
-  cudaError_t e = launch_pdl(plan_kernel, 1, kPlanThreads, 0, s, g);
+  static std::atomic<uint64_t> ready{0};
+  const auto plan_bytes = [](int groups, int rows) { return sizeof(int64_t) * (groups + 1) + sizeof(int) * (rows + 1); };
+  cudaError_t e = allow_shared(plan_kernel, ready, plan_bytes(kMaxBatch, kMaxBatch));
+  if (e == cudaSuccess) e = launch_pdl(plan_kernel, 1, kPlanThreads, plan_bytes(a.n_groups, a.B), s, g);
   if (e == cudaSuccess) e = hook_launched(a.hook, s);
   // heads of the shared part are KV heads themselves
   Args h = g;

@@ -15,27 +15,14 @@ struct ItemWalk {
 
   __device__ __forceinline__ void see(const Prefix& x, int at) {
     g = at;
-    const int4* from = reinterpret_cast<const int4*>(x.groups + at);
-    int4* to = reinterpret_cast<int4*>(&p);
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(GroupPlan) / 16); ++i) to[i] = from[i];
+    p = load_record(x.groups + at);
   }
-  // Enters at tile u of the list (called by whole warps).
-  __device__ __forceinline__ void enter(const Prefix& x, int u) {
-    int lo = 0, n = x.n_groups;  // the last group of those with fewer or as many tiles before
-    while (n > 1) {
-      const int step = (n + 31) / 32, i = (threadIdx.x & 31) * step;
-      const uint32_t ok = __ballot_sync(~0u, i < n && x.groups[lo + (i < n ? i : 0)].units <= u);
-      const int k = (31 - __clz(ok)) * step;
-      lo += k;
-      n = min(step, n - k);
-    }
-    see(x, lo);
-    const int at = u - p.units, item = at / p.tiles, tile = at - item * p.tiles;
-    hg = item / p.blocks;
-    block = item - hg * p.blocks;
-    token = p.first + tile * x.tile;
-    left = p.tiles - tile;
+  // Enters where CTA c begins; its number of tiles.
+  __device__ __forceinline__ int enter(const Prefix& x, int c) {
+    const ItemStart s = load_record(x.item_start + c);
+    p = s.p;
+    g = s.g, hg = s.hg, block = s.block, token = s.token, left = s.left;
+    return s.n;
   }
   // The next item.
   __device__ __forceinline__ void leave(const Prefix& x, int head_groups) {
@@ -112,15 +99,13 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
   const int d = a.v.d, qpg = a.v.qpg, head_groups = a.v.Hkv / n_heads;
   pdl_wait();
   pdl_launch_dependents();  // the plan, and with it all that the own tokens' launch reads, is there
-  const int units = x.all->units;
-  const Ranges ranges(units, min(x.n_items, units));
-  if ((int)blockIdx.x >= ranges.n) return;
+  ItemWalk ahead;
+  int to_compute = ahead.enter(x, blockIdx.x);
+  if (to_compute == 0) return;
   const typename LoaderOf<Z, Tile::kRows, Shm::kPlaces>::type load(g, raw, sh.q, warp, lane, wh, wt);
   load.clear(raw);
-  ItemWalk ahead;
-  ahead.enter(x, ranges.begin(blockIdx.x));
   ItemWalk at = ahead;
-  int to_compute = ranges.begin(blockIdx.x + 1) - ranges.begin(blockIdx.x), to_copy = to_compute, to_fetch = to_compute;
+  int to_copy = to_compute, to_fetch = to_compute;
 
   // page numbers are read two tiles ahead of the copies
   struct Next {
@@ -209,13 +194,6 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
 struct OwnWalk : Walk {
   RowPlan p, next;
 
-  static __device__ __forceinline__ RowPlan row(const Prefix& x, int b) {
-    RowPlan r;
-    const int4* from = reinterpret_cast<const int4*>(x.own + b);
-    int4* to = reinterpret_cast<int4*>(&r);
-    to[0] = from[0], to[1] = from[1];
-    return r;
-  }
   __device__ __forceinline__ void take(int tile) {
     token = p.first;
     len = p.end;
@@ -223,32 +201,24 @@ struct OwnWalk : Walk {
     skip = p.skip;
     left = max(1, (p.end - p.first + tile - 1) / tile);
   }
-  // Enters at tile u (called by whole warps).
-  __device__ __forceinline__ void enter(const Args& g, int u) {
-    const Prefix& x = g.x;
-    group = u / x.all->own_tiles;
-    const int at = u - group * x.all->own_tiles;
-    int lo = 0, n = g.a.B;  // the last row with as many tiles before or fewer
-    while (n > 1) {
-      const int step = (n + 31) / 32, i = (threadIdx.x & 31) * step;
-      const uint32_t ok = __ballot_sync(~0u, i < n && x.own[lo + (i < n ? i : 0)].tiles <= at);
-      const int k = (31 - __clz(ok)) * step;
-      lo += k;
-      n = min(step, n - k);
-    }
-    b = lo;
-    p = row(x, b);
-    next = row(x, b + 1 < g.a.B ? b + 1 : 0);
+  // Enters where CTA c begins; its number of tiles.
+  __device__ __forceinline__ int enter(const Args& g, int c) {
+    const OwnStart s = load_record(g.x.own_start + c);
+    p = s.p;
+    b = s.b;
+    group = s.hg;
+    if (s.n == 0) return 0;
+    next = load_record(g.x.own + (b + 1 < g.a.B ? b + 1 : 0));
     take(g.p.tile);
-    const int tile = at - p.tiles;
-    token += tile * g.p.tile;
-    left -= tile;
+    token = s.token;
+    left = s.left;
+    return s.n;
   }
   // The next (head group, row); the plan of the one after it is read ahead.
   __device__ __forceinline__ void leave(const Args& g) {
     if (++b == g.a.B) b = 0, ++group;
     p = next;
-    next = row(g.x, b + 1 < g.a.B ? b + 1 : 0);
+    next = load_record(g.x.own + (b + 1 < g.a.B ? b + 1 : 0));
     take(g.p.tile);
   }
 };
@@ -264,20 +234,18 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) own_kernel(const __grid_co
   const Prefix& x = g.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n_heads = g.p.wh, n_runs = g.p.wt, wh = warp & (n_heads - 1), wt = warp / n_heads;
-  const int d = a.v.d, n_tiles = x.all->own_tiles, units = g.p.groups * n_tiles;
+  const int d = a.v.d;
   pdl_launch_dependents();  // (the shared part let this launch begin: the plan and all before it are complete)
-  const Ranges ranges(units, min(g.p.n_items, units));
-  if ((int)blockIdx.x >= ranges.n) {
+  OwnWalk ahead;
+  int to_compute = ahead.enter(g, blockIdx.x);
+  if (to_compute == 0) {
     pdl_wait();  // what waits for this launch waits for the shared part too
     return;
   }
   const typename LoaderOf<Z, Tile::kRows, Shm::kPlaces>::type load(g, raw, sh.q, warp, lane, wh, wt);
   load.clear(raw);
-  const int u0 = ranges.begin(blockIdx.x), u1 = ranges.begin(blockIdx.x + 1);
-  OwnWalk ahead;
-  ahead.enter(g, u0);
   OwnWalk at = ahead;
-  int to_compute = u1 - u0, to_copy = to_compute, to_fetch = to_compute;
+  int to_copy = to_compute, to_fetch = to_compute;
   Pages pages = {0, -1, 0, -1}, pages2 = {0, -1, 0, -1};
   bool first = true;
   const auto fetch_next = [&]() {
@@ -345,17 +313,20 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) own_kernel(const __grid_co
   pdl_wait();
 }
 
+// Lets `kernel` use `bytes` of shared memory, once per device.
 template <class K>
-cudaError_t launch_part(K kernel, std::atomic<uint64_t>& ready, int grid, int threads, size_t smem, const Args& g, cudaStream_t s) {
+cudaError_t allow_shared(K kernel, std::atomic<uint64_t>& ready, size_t bytes) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev > 63 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {  // devices on which it may use its shared memory
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
-  }
-  e = launch_pdl(kernel, grid, threads, smem, s, g);
+  if (e != cudaSuccess || (dev < 64 && ready.load(std::memory_order_relaxed) >> dev & 1)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess && dev < 64) ready.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+  return e;
+}
+template <class K>
+cudaError_t launch_part(K kernel, std::atomic<uint64_t>& ready, int grid, int threads, size_t smem, const Args& g, cudaStream_t s) {
+  cudaError_t e = allow_shared(kernel, ready, smem);
+  if (e == cudaSuccess) e = launch_pdl(kernel, grid, threads, smem, s, g);
   return e == cudaSuccess ? hook_launched(g.a.hook, s) : e;
 }
 

@@ -1,21 +1,20 @@
 // Attention over shared prefixes on bf16 caches, many queries to a KV head: what the rows of a group see together,
 // on tcgen05.
 //
-// Mathematics: an item's up to 128 queries (of one KV head, of any rows of the group) are the rows of S = Q K^T and
-// O += P V, M = 128, over tiles of 128 tokens; P = 2^(s - m) in bf16 (a weight is off by 2^-8 of itself at
+// Mathematics: an item's up to 256 queries (of one KV head, of any rows of the group) are the rows of S = Q K^T and
+// O += P V, M = 128 twice, over tiles of 64 tokens; P = 2^(s - m) in bf16 (a weight is off by 2^-8 of itself at
 // most, as the output by its own rounding, and errors of many weights cancel; a second term would make the products half as
 // long again), m a reference within 2^8 of the running maximum, all sums fp32, those of the weights before they are rounded.
-// Bound: a tile is 4 d bytes a token, read once per 128 queries, against 8.4 MFLOP (d = 128): HBM for few blocks of queries per
-// group, else the softmax and what an SM takes in from L2.
+// Bound: a tile is 4 d bytes a token, read once per 256 queries, against 8.4 MFLOP per 128 of them (d = 128): HBM for few
+// blocks of queries per group, else the softmax and what an SM takes in from L2.
 //
 // Work: one CTA per SM takes an equal range of the items' tiles (paged_shared.cu) and leaves a partial sum per item.
-// Tiles of 64 tokens go in turn to two streams, each with two buffers of scores, an output and a running maximum of its
-// own, so that the softmax of one runs under the products and the softmax of the other, whatever the number of
-// queries, and scores are ready when a softmax ends; the streams join at the item's end.
+// Two streams, each with two buffers of scores, an output and a running maximum of its own: of an item of more than 128
+// queries a stream has half of them and all tiles, of others all queries and every other tile (the streams join at the
+// item's end). So the softmax of one runs under the products and the softmax of the other, and scores are ready when a
+// softmax ends.
 // P overwrites its scores in tensor memory and is the A operand of O += P V from there.  Four warps copy (pages of any size
 // and order: 16-byte asynchronous copies into the swizzled layout), the rows behind a tile's last token as zeros.
-// (One buffer per stream and tiles of 128 tokens in five slots: keys and values that wait for a softmax filled four of them,
-// 1.6 us a tile of 128.)
 #include "paged_shared.cuh"
 #include "tc_common.cuh"
 
@@ -25,17 +24,19 @@ namespace {
 
 using namespace tc;
 
-// warps 0-3 and 4-7 softmax of the two streams, warps 8-11 copies, warp 12 MMAs
-constexpr int kThreads = 416;
-constexpr int kRows = 128;        // queries of an item
+// warps 0-3 and 4-7 softmax of the two streams, warps 8-11 copies, warps 12 and 13 their MMAs
+constexpr int kThreads = 512;
+// registers: 512 threads x 128 at launch = 2 x 128 x 168 (softmax) + 2 x 128 x 88
+constexpr int kRegsSoftmax = 168, kRegsOther = 88;
+constexpr int kRows = 128;        // queries of a stream
 constexpr int kTok = 64;          // tokens of a tile
 constexpr int kAtom = 128 * 128;  // 128 rows of 128 bytes
 constexpr int kHalf = kTok * 128;
 
 template <int DP>
 struct ShmTc {
-  static constexpr int kSlots = DP == 128 ? 11 : 16;  // ring of key and value tiles: K(0), V(0), K(1), V(1), ...
-  uint8_t q[DP / 64][kAtom];           // queries [64 elements][row][128 bytes], 128-byte swizzle
+  static constexpr int kSlots = DP == 128 ? 9 : 16;  // ring of key and value tiles: K(0), V(0), K(1), V(1), ...
+  uint8_t q[2][DP / 64][kAtom];        // queries [128 of them][64 elements][row][128 bytes], 128-byte swizzle
   uint8_t kv[kSlots][DP / 64][kHalf];  // keys or values, rows tokens
   float2 ml[2][kRows];                 // [stream][row]: maximum and sum
   uint64_t kv_full[kSlots], kv_empty[kSlots], q_full, q_empty;
@@ -44,25 +45,34 @@ struct ShmTc {
   int abort_flag;
 };
 
-// This CTA's items one after the other; n: tiles of the item that it has.
+// This CTA's items one after the other; n: tiles of the item that it has; pair: more than 128 queries.
 struct Segments {
   ItemWalk at;
   int left, n, nth;
-  __device__ __forceinline__ void begin(const Prefix& x, const Ranges& r) {
-    at.enter(x, r.begin(blockIdx.x));
-    left = r.begin(blockIdx.x + 1) - r.begin(blockIdx.x);
+  bool pair;
+  __device__ __forceinline__ void see(const Prefix& x, int qpg) {
     n = min(at.left, left);
-    nth = 0;
+    pair = at.count(x, qpg) > kRows;
   }
-  __device__ __forceinline__ bool next(const Prefix& x, int heads) {
+  __device__ __forceinline__ bool next(const Prefix& x, int heads, int qpg) {
     left -= n;
     if (left <= 0) return false;
     at.leave(x, heads);
-    n = min(at.left, left);
+    see(x, qpg);
     ++nth;
     return true;
   }
+  // Stream s has the tiles from `first(s)` on, every `step()`th.
+  __device__ __forceinline__ int first(int s) const { return pair ? 0 : s; }
+  __device__ __forceinline__ int step() const { return pair ? 1 : 2; }
 };
+
+// 32 bytes, a whole sector, at once.
+__device__ __forceinline__ void store8(float* p, const float* v) {
+  asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+               "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
 
 // Arrives on `bar` once all copies of this thread so far have landed.  (The reader of the barrier orders them before its
 // MMAs: a proxy fence of this thread would wait for the copies behind them too, 2 us a tile.)
@@ -99,11 +109,11 @@ struct Copier {
       }
     }
   }
-  // Where lane r's query of an item (its row 32 w + r) lies, in bytes from g.a.q (-1: none).
-  __device__ __forceinline__ int64_t query(const ItemWalk& at) const {
-    const int qpg = g.a.v.qpg, r = 32 * w + lane;
+  // Where lane r's query of a stream (row 32 w + r from row `from` of the item on) lies, in bytes from g.a.q (-1: none).
+  __device__ __forceinline__ int64_t query(const ItemWalk& at, int from) const {
+    const int qpg = g.a.v.qpg, r = from + 32 * w + lane;
     if (r >= at.count(g.x, qpg)) return -1;
-    const int x = at.block * kRows + r, b = g.x.by_qpg.div(x), j = at.hg * qpg + x - b * qpg;
+    const int x = at.block * g.x.rows + r, b = g.x.by_qpg.div(x), j = at.hg * qpg + x - b * qpg;
     return 2 * ((int64_t)(at.p.start + b) * g.a.q_stride + (int64_t)j * g.a.v.d);
   }
   // The same rows by single elements, for queries off 16-byte boundaries.
@@ -139,9 +149,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, heads = a.v.Hkv;
   pdl_wait();
   pdl_launch_dependents();  // the plan, and with it all that the own tokens' launch reads, is there
-  const int units = x.all->units;
-  const Ranges ranges(units, min(x.n_items, units));
-  if ((int)blockIdx.x >= ranges.n) return;
+  Segments sg;
+  sg.left = sg.at.enter(x, blockIdx.x);
+  if (sg.left == 0) return;
+  sg.nth = 0;
+  sg.see(x, a.v.qpg);
   volatile int* abort_flag = &sm.abort_flag;
   if (warp == 12) {
     tmem_alloc(&sm.tmem_base, 512);
@@ -149,10 +161,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     if (lane == 0) {
       for (int i = 0; i < kSlots; ++i) {
         mbar_init(&sm.kv_full[i], 128);
-        mbar_init(&sm.kv_empty[i], 1);
+        mbar_init(&sm.kv_empty[i], 2);
       }
       mbar_init(&sm.q_full, 128);
-      mbar_init(&sm.q_empty, 1);
+      mbar_init(&sm.q_empty, 2);
       for (int s = 0; s < 2; ++s) {
         for (int b = 0; b < 2; ++b) {
           mbar_init(&sm.s_full[s][b], 1);
@@ -171,87 +183,114 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;  // scores and P of stream s, buffer b at 128 s + 64 b, its output at 256 + 128 s
-  Segments sg;
-  sg.begin(x, ranges);
 
-  if (warp == 12) {
-    // ---- MMAs: the whole warp runs the schedule, one lane issues ----------------------
-    // A thread's MMAs run in order: scores may go into a buffer right after the P V that reads it.
-    const bool el = elect_one();
-    const uint32_t id_s = idesc_bf16(128, kTok, false, false);  // S = Q K^T: both K-major
-    const uint32_t id_o = idesc_bf16(128, DP, false, true);     // O += P V: V MN-major
-    const uint64_t dq = sdesc(smem_u32(sm.q[0]), 16, 1024, kSw128);
-    const uint64_t dk = sdesc(smem_u32(sm.kv[0][0]), 16, 1024, kSw128);
-    const uint64_t dv = sdesc(smem_u32(sm.kv[0][0]), kHalf, 1024, kSw128);
-    constexpr int kSlotBytes = (DP / 64) * kHalf;
-    // ring positions of the next key tile and the next value tile, with their turns' parities
-    int ks = 0, vs = 1;
-    uint32_t kp = 0, vp = 0, pp[2][2] = {};  // pp: parity of each buffer's next P
-    const auto advance = [&](int& slot, uint32_t& parity) {
-      slot += 2;
-      if (slot >= kSlots) slot -= kSlots, parity ^= 1;
-    };
-    bool ok = true;
-    do {
-      const int n = sg.n;
-      const auto scores = [&](int k) -> bool {
-        if (!wwait(&sm.kv_full[ks], kp, abort_flag)) return false;
-        fence_proxy_async_smem();
-        tc_fence_after();
-        const int s = k & 1, b = k >> 1 & 1;
-        if (el) {
-          const uint64_t kb = dk + (uint64_t)(ks * (kSlotBytes >> 4));
+  if (warp >= 12) {
+    reg_dec<kRegsOther>();
+    if (warp < 14) {
+      // ---- MMAs of stream s: the whole warp runs the schedule, one lane issues -----------
+      // A warp per stream: a step's waits and MMAs take a warp as long as the MMAs of both streams do (one warp for both:
+      // 1.3 us a tile of 2 x 128 queries). A thread's MMAs run in order: scores may go into a buffer right
+      // after the P V that reads it.
+      const bool el = elect_one();
+      const int s = warp - 12;
+      const uint32_t id_s = idesc_bf16(128, kTok, false, false);  // S = Q K^T: both K-major
+      const uint32_t id_o = idesc_bf16(128, DP, false, true);     // O += P V: V MN-major
+      const uint64_t dq = sdesc(smem_u32(sm.q[0][0]), 16, 1024, kSw128);
+      const uint64_t dk = sdesc(smem_u32(sm.kv[0][0]), 16, 1024, kSw128);
+      const uint64_t dv = sdesc(smem_u32(sm.kv[0][0]), kHalf, 1024, kSw128);
+      constexpr int kSlotBytes = (DP / 64) * kHalf;
+      const uint32_t ts = tmem + 128 * s, to = tmem + 256 + 128 * s;
+      int base = 0;         // ring position of the item's first keys
+      uint32_t turn[2] = {0, 0};  // P tiles so far, of each buffer
+      bool ok = true;
+      do {
+        const int n = sg.n, first = sg.first(s), step = sg.step(), tiles = (n - first + step - 1) / step;
+        const uint64_t qb = dq + (uint64_t)((sg.pair ? s : 0) * ((DP / 64) * kAtom >> 4));
+        // (barriers of the ring expect both streams; the one that has a tile alone arrives twice)
+        const auto done = [&](uint64_t* bar) {
+          umma_commit(bar);
+          if (!sg.pair) umma_commit(bar);
+        };
+        if (!(ok = wwait(&sm.q_full, sg.nth & 1, abort_flag))) break;
+        if (tiles == 0 && el) umma_commit(&sm.q_empty);
+        int si = 0, vi = 0;  // the next scores and the next products with values
+        long long since = 0;
+        while (vi < tiles) {
+          bool idle = true;
+          if (si < tiles && si < vi + 2) {
+            const int at = base + 2 * (first + si * step), slot = at % kSlots;
+            if (__all_sync(~0u, mbar_test(&sm.kv_full[slot], at / kSlots & 1))) {
+              idle = false;
+              fence_proxy_async_smem();
+              tc_fence_after();
+              if (el) {
+                const uint64_t kb = dk + (uint64_t)(slot * (kSlotBytes >> 4));
 #pragma unroll
-          for (int j = 0; j < DP / 16; ++j)
-            umma_f16(tmem + 128 * s + 64 * b, dq + (((j >> 2) * kAtom + (j & 3) * 32) >> 4),
-                     kb + (((j >> 2) * kHalf + (j & 3) * 32) >> 4), id_s, j > 0 ? 1u : 0u);
-          umma_commit(&sm.s_full[s][b]);
-          umma_commit(&sm.kv_empty[ks]);
-          if (k + 1 == n) umma_commit(&sm.q_empty);
-        }
-        advance(ks, kp);
-        return true;
-      };
-      if (!(ok = wwait(&sm.q_full, sg.nth & 1, abort_flag))) break;
-      for (int k = 0; k < min(n, 4) && ok; ++k) ok = scores(k);
-      // the last item's output has been read
-      if (ok && sg.nth > 0) ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag);
-      for (int k = 0; k < n && ok; ++k) {
-        const int s = k & 1, b = k >> 1 & 1;
-        if (!(ok = wwait(&sm.kv_full[vs], vp, abort_flag))) break;
-        if (!(ok = wwait(&sm.p_full[s][b], pp[s][b], abort_flag))) break;
-        pp[s][b] ^= 1;
-        fence_proxy_async_smem();
-        tc_fence_after();
-        if (el) {
-          const uint64_t vb = dv + (uint64_t)(vs * (kSlotBytes >> 4));
+                for (int j = 0; j < DP / 16; ++j)
+                  umma_f16(ts + 64 * (si & 1), qb + (((j >> 2) * kAtom + (j & 3) * 32) >> 4),
+                           kb + (((j >> 2) * kHalf + (j & 3) * 32) >> 4), id_s, j > 0 ? 1u : 0u);
+                umma_commit(&sm.s_full[s][si & 1]);
+                done(&sm.kv_empty[slot]);
+                if (si + 1 == tiles) umma_commit(&sm.q_empty);
+              }
+              ++si;
+            }
+          }
+          const int b = vi & 1;
+          if (vi < si && __all_sync(~0u, mbar_test(&sm.p_full[s][b], turn[b] & 1))) {
+            const int at = base + 2 * (first + vi * step) + 1, slot = at % kSlots;
+            if (__all_sync(~0u, mbar_test(&sm.kv_full[slot], at / kSlots & 1))) {
+              idle = false;
+              // the last item's output has been read
+              if (vi == 0 && sg.nth > 0 && !(ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag))) break;
+              ++turn[b];
+              fence_proxy_async_smem();
+              tc_fence_after();
+              if (el) {
+                const uint64_t vb = dv + (uint64_t)(slot * (kSlotBytes >> 4));
 #pragma unroll
-          for (int j = 0; j < kTok / 16; ++j)
-            umma_f16_ts(tmem + 256 + 128 * s, tmem + 128 * s + 64 * b + 8 * j, vb + (uint64_t)(j * 2048 >> 4), id_o,
-                        (k > 1 || j > 0) ? 1u : 0u);
-          umma_commit(&sm.pv_done[s]);
-          umma_commit(&sm.kv_empty[vs]);
-          if (k + 2 >= n) umma_commit(&sm.o_full[s]);
+                for (int j = 0; j < kTok / 16; ++j)
+                  umma_f16_ts(to, ts + 64 * b + 8 * j, vb + (uint64_t)(j * 2048 >> 4), id_o, (vi > 0 || j > 0) ? 1u : 0u);
+                umma_commit(&sm.pv_done[s]);
+                done(&sm.kv_empty[slot]);
+                if (vi + 1 == tiles) umma_commit(&sm.o_full[s]);
+              }
+              ++vi;
+            }
+          }
+          // a bounded wait, as in mbar_wait
+          if (!idle) {
+            since = 0;
+          } else {
+            const long long now = clock64();
+            if (since == 0) since = now;
+            if (now - since > kWaitCycles) *abort_flag = 1;
+            if (__any_sync(~0u, *abort_flag)) {
+              ok = false;
+              break;
+            }
+          }
         }
-        advance(vs, vp);
-        if (k + 4 < n) ok = scores(k + 4);
-      }
-    } while (ok && sg.next(x, heads));
+        base += 2 * n;
+      } while (ok && sg.next(x, heads, a.v.qpg));
+    }
   } else if (warp < 8) {
     // ---- softmax of stream s: a thread has row r ----------------------------------------
+    reg_inc<kRegsSoftmax>();
     const int s = warp >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t lb = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ob = tmem + lb + 256 + 128 * s;
     const bool plain = g.score.cap2 == 0.f && g.score.scale2 > 0.f;  // scores are s times a positive factor
     const float factor = plain ? g.score.scale2 : 1.f;
-    uint32_t sp = 0, turn = 0, second = 0;  // sp: bit b the parity of buffer b's next scores; turn: tiles of this
-                                            // stream so far; second: items so far in which stream 1 has any
+    // sp: bit b the parity of buffer b's next scores; turn: tiles of this stream so far; joined: items so far whose streams
+    // join; outputs: items so far in which stream s has tiles
+    uint32_t sp = 0, turn = 0, joined = 0, outputs[2] = {0, 0};
     bool ok = true;
     do {
       float m = -CUDART_INF_F;
       float2 l = make_float2(0.f, 0.f);
-      for (int k = s; k < sg.n; k += 2, ++turn) {
-        const int b = k >> 1 & 1;
+      for (int k = sg.first(s), j = 0; k < sg.n; k += sg.step(), ++j, ++turn) {
+        const int b = j & 1;
         if (!(ok = wwait(&sm.s_full[s][b], sp >> b & 1, abort_flag))) break;
         sp ^= 1u << b;
         tc_fence_after();
@@ -307,45 +346,66 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         if (lane == 0) mbar_arrive(&sm.p_full[s][b]);
       }
       if (!ok) break;
-      // the streams join: this one writes half of the elements
-      if (sg.nth > 0 && !(ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag))) break;
-      sm.ml[s][r] = make_float2(m, l.x + l.y);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.ml_full);
-      if (!(ok = wwait(&sm.ml_full, sg.nth & 1, abort_flag))) break;
-      const bool both = sg.n > 1;
-      if (!(ok = wwait(&sm.o_full[0], sg.nth & 1, abort_flag))) break;
-      if (both) {
-        if (!(ok = wwait(&sm.o_full[1], second & 1, abort_flag))) break;
-        ++second;
+      const bool pair = sg.pair, both = pair || sg.n > 1;
+      const int count = sg.at.count(x, a.v.qpg), mine = pair ? s * kRows + r : r;
+      const int64_t row = x.row_of(sg.at.p, heads, a.v.qpg, sg.at.hg, sg.at.block, blockIdx.x, 0, mine);
+      float* to = x.part_u + row * DP;
+      float f0 = 1.f, f1 = 0.f;
+      if (!pair) {
+        // the streams join: this one writes half of the elements
+        if (sg.nth > 0 && !(ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag))) break;
+        sm.ml[s][r] = make_float2(m, l.x + l.y);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.ml_full);
+        if (!(ok = wwait(&sm.ml_full, joined & 1, abort_flag))) break;
+        ++joined;
+        const float2 u0 = sm.ml[0][r], u1 = sm.ml[1][r];
+        const float top = both ? fmaxf(u0.x, u1.x) : u0.x, base = top == -CUDART_INF_F ? 0.f : top;
+        f0 = exp2_approx(u0.x - base), f1 = both ? exp2_approx(u1.x - base) : 0.f;
+        if (s == 0 && mine < count)
+          *reinterpret_cast<float2*>(x.part_ml + 2 * row) = make_float2(top, u0.y * f0 + (both ? u1.y * f1 : 0.f));
+      } else if (mine < count) {
+        *reinterpret_cast<float2*>(x.part_ml + 2 * row) = make_float2(m, l.x + l.y);
       }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {  // both streams' last products where both have any
+        if (t == 1 && !both) continue;
+        if ((!pair || t == s) && !(ok = wwait(&sm.o_full[t], outputs[t] & 1, abort_flag))) break;
+        ++outputs[t];
+      }
+      if (!ok) break;
       tc_fence_after();
-      const float2 u0 = sm.ml[0][r], u1 = sm.ml[1][r];
-      const float top = both ? fmaxf(u0.x, u1.x) : u0.x, base = top == -CUDART_INF_F ? 0.f : top;
-      const float f0 = exp2_approx(u0.x - base), f1 = both ? exp2_approx(u1.x - base) : 0.f;
-      const bool mine = r < sg.at.count(x, a.v.qpg);
-      const int64_t row = x.row_of(sg.at.p, heads, a.v.qpg, sg.at.hg, sg.at.block, blockIdx.x, 0, r);
-      float* to = x.part_u + row * DP + s * (DP / 2);
-      if (s == 0 && mine) *reinterpret_cast<float2*>(x.part_ml + 2 * row) = make_float2(top, u0.y * f0 + (both ? u1.y * f1 : 0.f));
+      if (pair) {
 #pragma unroll 1
-      for (int c = 0; c < DP / 2; c += 16) {
-        float v[16], w[16];
-        tmem_ld16(tmem + lb + 256 + s * (DP / 2) + c, v);
-        if (both) tmem_ld16(tmem + lb + 384 + s * (DP / 2) + c, w);
-        tmem_wait_ld();
+        for (int c = 0; c < DP; c += 32) {
+          float v[32];
+          tmem_ld32(ob + c, v);
+          tmem_wait_ld();
+          if (mine < count)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = both ? (f0 == 0.f ? 0.f : v[i] * f0) + (f1 == 0.f ? 0.f : w[i] * f1) : v[i] * f0;
-        if (mine)
+            for (int i = 0; i < 32; i += 8) store8(to + c + i, v + i);
+        }
+      } else {
+#pragma unroll 1
+        for (int c = s * (DP / 2); c < (s + 1) * (DP / 2); c += 32) {
+          float v[32], w[32];
+          tmem_ld32(tmem + lb + 256 + c, v);
+          if (both) tmem_ld32(tmem + lb + 384 + c, w);
+          tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<float4*>(to + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+          for (int i = 0; i < 32; ++i) v[i] = (f0 == 0.f ? 0.f : v[i] * f0) + (f1 == 0.f ? 0.f : w[i] * f1);
+          if (mine < count)
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) store8(to + c + i, v + i);
+        }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.o_free);
-    } while (ok && sg.next(x, heads));
+    } while (ok && sg.next(x, heads, a.v.qpg));
   } else {
     // ---- copies -----------------------------------------------------------------------
+    reg_dec<kRegsOther>();
     const PagedView& v = a.v;
     const int w = warp - 8;
     const Copier<DP> copy(g, w, lane);
@@ -363,6 +423,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         return table[col];
       };
       int off, page = page_of(0, off), off2 = -1, page2 = sg.n > 1 ? page_of(1, off2) : 0;
+      // the last item's scores are all formed: its queries can go
+      if (sg.nth > 0 && !(ok = wwait(&sm.q_empty, (sg.nth - 1) & 1, abort_flag))) break;
+      for (int t = 0; t < (sg.pair ? 2 : 1); ++t) {
+        const int64_t qo = copy.query(sg.at, t * kRows);
+        if (g.p.q_copied) copy.template rows<32>(sm.q[t][0], kAtom, 32 * w, a.q, qo);
+        else copy.elements(sm.q[t][0], qo);
+      }
+      if (g.p.q_copied) arrive_when_copied(&sm.q_full);
+      else mbar_arrive(&sm.q_full);
       for (int k = 0; k < sg.n && ok; ++k) {
         const bool inside = (uint32_t)page < (uint32_t)v.n_pages;
         if (off >= 0 && !inside) {
@@ -380,21 +449,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
           copy.template rows<16>(sm.kv[slot][0], kHalf, 16 * w, kind ? a.vc : a.kc, kind ? vo : ko);
           arrive_when_copied(&sm.kv_full[slot]);
           if (++slot == kSlots) slot = 0, parity ^= 1;
-          if (k == 0 && kind == 0) {
-            // the last item's scores are all formed: its queries can go
-            if (sg.nth > 0 && !(ok = wwait(&sm.q_empty, (sg.nth - 1) & 1, abort_flag))) break;
-            const int64_t qo = copy.query(sg.at);
-            if (g.p.q_copied) {
-              copy.template rows<32>(sm.q[0], kAtom, 32 * w, a.q, qo);
-              arrive_when_copied(&sm.q_full);
-            } else {
-              copy.elements(sm.q[0], qo);
-              mbar_arrive(&sm.q_full);
-            }
-          }
         }
       }
-    } while (ok && sg.next(x, heads));
+    } while (ok && sg.next(x, heads, a.v.qpg));
     cp_async_wait<0>();
   }
   tc_fence_before();
