@@ -78,9 +78,8 @@ struct GroupPlan {
   int table;         // the row whose block table they are read by
   int tiles, blocks; // of an item; items per head group
   int units;         // tiles of all groups before
-  int queries;       // queries of a KV head in all groups before
   int bad;           // a page outside the pool
-  int pad[2];
+  int pad[3];
 };
 // What a row attends to by itself: tokens [first, end), counted without `skip` of them from token skip_at on.
 struct RowPlan {
@@ -88,13 +87,10 @@ struct RowPlan {
   int group;      // its group, -1 if the row takes no part in what that shares
   int state;      // 0, or kEmpty: zeros whatever the group has
   int tiles;      // of all rows before (a row has one at least)
-  int pad;
+  int start, rows, blocks;  // of its group
+  int pad[2];
 };
 constexpr int kEmpty = 1;
-struct Whole {  // of a whole call
-  int units;      // tiles of all items
-  int own_tiles;  // of all rows, per head group
-};
 // Where a CTA begins: its first item, or (head group, row), the tile's first token and the tiles from it to the end
 // of that, and how many it has in all.
 struct ItemStart {
@@ -105,6 +101,9 @@ struct OwnStart {
   RowPlan p;
   int b, hg, token, left, n, pad[3];
 };
+struct CtaRange {  // of those that have tiles of an item, or of a (head group, row)
+  int first, last;
+};
 template <class S>
 __device__ __forceinline__ S load_record(const S* from) {
   S r;
@@ -113,24 +112,29 @@ __device__ __forceinline__ S load_record(const S* from) {
   return r;
 }
 struct Prefix {
-  Whole* all;
   GroupPlan* groups;
   RowPlan* own;    // [B]
   ItemStart* item_start;  // [n_items]
   OwnStart* own_start;    // [p.n_items]
+  CtaRange* item_ctas;    // [B Hq] by item_id: who leaves sums
+  CtaRange* own_ctas;     // [(head group, row)]
   float *part_u, *part_ml;  // partial sums, as in Args, of what groups share: rows by row_of
   float *own_u, *own_ml;    // and of rows' own tokens: rows by own_row
   int n_groups, n_items;  // groups; CTAs that tiles are dealt to
   int rows, wh, tile;     // queries of a block, heads of a head group, tokens of a tile
-  Divider by_qpg;
+  Divider by_qpg, by_rows;
 
   __device__ __forceinline__ int64_t own_row(const Plan& p, int B, int group, int b, int c, int w) const;
+  // A number below B Hq of an item: every block has a query.
+  __device__ __forceinline__ int64_t item_id(int start, int blocks, int Hq, int hg, int block) const {
+    return (int64_t)start * Hq + (int64_t)hg * blocks + block;
+  }
   // Where query `r` of the block `block` of head `w` of head group `hg` has the partial sum that CTA c leaves: items
   // in order, CTAs that share one behind one another.  The next item of a CTA or the next CTA of an item is further on
-  // by all the rows that one of them can fill.
-  __device__ __forceinline__ int64_t row_of(const GroupPlan& p, int Hkv, int qpg, int hg, int block, int c, int w, int r) const {
-    const int queries = p.rows * qpg, here = min(rows, queries - block * rows);
-    return (int64_t)p.queries * Hkv + (int64_t)wh * ((int64_t)hg * queries + block * rows + (int64_t)c * rows) + w * here + r;
+  // by all the rows that one of them can fill.  The group: rows from `start` on, `queries` on a KV head.
+  __device__ __forceinline__ int64_t row_of(int start, int queries, int Hq, int qpg, int hg, int block, int c, int w, int r) const {
+    const int here = min(rows, queries - block * rows);
+    return (int64_t)start * Hq + (int64_t)wh * ((int64_t)hg * queries + block * rows + (int64_t)c * rows) + w * here + r;
   }
 };
 
@@ -251,13 +255,6 @@ struct Ranges {
       : units(units), n(n), each(n ? units / n : 0), rest(units - each * n) {}
   __device__ __forceinline__ int begin(int c) const { return c * each + c * rest / n; }
   __device__ __forceinline__ int item_of(int u) const { return (int)(((int64_t)(u + 1) * n + units - 1) / units) - 1; }
-  // The same without the long division: a quotient in fp32 is off by one or two at most.
-  __device__ __forceinline__ int near_item_of(int u) const {
-    int c = min(n - 1, (int)(__fdividef((float)u, (float)units) * n));
-    while (begin(c + 1) <= u) ++c;
-    while (begin(c) > u) --c;
-    return c;
-  }
 };
 
 // What the plan keeps of the sequences in shared memory.

@@ -35,16 +35,18 @@ __device__ __forceinline__ RowView row_view(const PagedDecodeArgs& a, int b, int
   return r;
 }
 
-// What the plan keeps in shared memory: per group its tiles of all items of a head group and then those of all
-// groups before (in 64 bits); per row its own tiles, then those of all rows before.
-struct PlanSums {
-  int64_t* units;  // [n_groups + 1]
-  int* tiles;      // [B + 1]
+// What the plan works on: its records, in shared memory where they fit (kFew groups and rows), else where they go; tiles
+// of all groups, and of all rows, before each.
+constexpr int kFew = kPlanThreads;
+struct PlanState {
+  GroupPlan* groups;
+  RowPlan* own;
+  int *units, *tiles;  // [n_groups + 1], [B + 1]
 };
 
 // A subgroup of LANES threads per group of rows at a time; true if d_group_start is not as it must be.
 template <int LANES>
-__device__ __forceinline__ bool plan_group(const Args& g, const PlanSums& sums, int at, bool there) {
+__device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, int at, bool there) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int lane = threadIdx.x % LANES;
@@ -78,6 +80,7 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanSums& sums, 
     first = max(first, __shfl_xor_sync(~0u, first, o));
   }
   if (rows < 2 || last <= first) last = first = 0;
+  const int64_t blocks = ((int64_t)rows * a.v.qpg + x.rows - 1) / x.rows;
   // what each row has of its own
   for (int b = start + lane; b < end; b += LANES) {
     const RowView r = row_view(a, b, rows > 1 ? shared : 0);
@@ -90,9 +93,11 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanSums& sums, 
     own.skip = takes_part ? last - first : 0;
     own.first = r.first;
     own.end = bad ? r.first : r.len - own.skip;
-    own.tiles = own.pad = 0;
-    x.own[b] = own;
-    sums.tiles[b] = max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile);
+    own.start = start;
+    own.rows = rows;
+    own.blocks = (int)blocks;
+    s.own[b] = own;
+    s.tiles[b] = max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile);
   }
   if (!there || lane) return wrong;
   GroupPlan p;
@@ -102,45 +107,52 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanSums& sums, 
   p.end = last;
   p.table = row;
   p.tiles = (last - first + x.tile - 1) / x.tile;
-  p.blocks = (int)(((int64_t)rows * a.v.qpg + x.rows - 1) / x.rows);
-  p.units = p.bad = p.pad[0] = p.pad[1] = 0;
-  p.queries = start * a.v.qpg;
-  x.groups[at] = p;
-  sums.units[at] = (int64_t)p.tiles * p.blocks * (a.v.Hkv / x.wh);
+  p.blocks = (int)blocks;
+  p.bad = 0;
+  s.groups[at] = p;
+  s.units[at] = (int)min((int64_t)p.tiles * blocks * (a.v.Hkv / x.wh), (int64_t)kUnitLimit + 1);
   return wrong;
 }
 
-// Sums of all before each of v[0 .. n - 1], in place, and of all in v[n].  Called by the whole block.
-template <typename V>
-__device__ __forceinline__ void sum_before(V* v, int n, int64_t* scratch) {
+// In place of units[0 .. n - 1] and tiles[0 .. m - 1] the sums of all before each, and of all in units[n] and tiles[m]:
+// kUnitLimit + 1 at most.  Called by the whole block.
+__device__ __forceinline__ void sum_before(const PlanState& s, int n, int m, int64_t (&scratch)[2][kPlanThreads / 32]) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int64_t base = 0;
-  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+  int64_t base[2] = {0, 0};
+  for (int i0 = 0; i0 < max(n, m); i0 += kPlanThreads) {
     const int i = i0 + tid;
-    const int64_t mine = i < n ? v[i] : 0;
-    int64_t t = mine;
+    const int64_t mine[2] = {i < n ? s.units[i] : 0, i < m ? s.tiles[i] : 0};
+    int64_t t[2] = {mine[0], mine[1]};
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(~0u, t, o);
-      if (lane >= o) t += y;
-    }
-    if (lane == 31) scratch[warp] = t;
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t y = __shfl_up_sync(~0u, t[k], o);
+        if (lane >= o) t[k] += y;
+      }
+    if (lane == 31) scratch[0][warp] = t[0], scratch[1][warp] = t[1];
     __syncthreads();
-    int64_t before = base;
+    const int warps = min(kPlanThreads, max(n, m) - i0 + 31) / 32;
+    int64_t before[2] = {base[0], base[1]};
+    for (int w = 0; w < warps; ++w)
 #pragma unroll
-    for (int w = 0; w < kPlanThreads / 32; ++w) {
-      if (w < warp) before += scratch[w];
-      base += scratch[w];
-    }
-    if (i < n) v[i] = (V)min(before + t - mine, (int64_t)kUnitLimit);
+      for (int k = 0; k < 2; ++k) {
+        const int64_t y = scratch[k][w];
+        if (w < warp) before[k] += y;
+        base[k] += y;
+      }
+    if (i < n) s.units[i] = (int)min(before[0] + t[0] - mine[0], (int64_t)kUnitLimit + 1);
+    if (i < m) s.tiles[i] = (int)min(before[1] + t[1] - mine[1], (int64_t)kUnitLimit + 1);
     __syncthreads();
   }
-  if (tid == 0) v[n] = (V)min(base, (int64_t)kUnitLimit + 1);  // too many: above the limit
+  if (tid == 0) {
+    s.units[n] = (int)min(base[0], (int64_t)kUnitLimit + 1);
+    s.tiles[m] = (int)min(base[1], (int64_t)kUnitLimit + 1);
+  }
   __syncthreads();
 }
 // The last i of 0 .. n - 1 with v[i] <= u.
-template <typename V>
-__device__ __forceinline__ int last_of(const V* v, int n, int u) {
+__device__ __forceinline__ int last_of(const int* v, int n, int u) {
   int lo = 0, hi = n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -150,76 +162,93 @@ __device__ __forceinline__ int last_of(const V* v, int n, int u) {
   return lo;
 }
 
+size_t plan_bytes(int groups, int rows) {
+  const bool few = groups <= kFew && rows <= kFew;
+  return (few ? groups * sizeof(GroupPlan) + rows * sizeof(RowPlan) : 0) + sizeof(int) * (groups + 1 + rows + 1);
+}
+
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Args g) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int tid = threadIdx.x, n = x.n_groups;
-  extern __shared__ int64_t plan_memory[];
-  __shared__ int64_t scratch[kPlanThreads / 32];
-  const PlanSums sums = {plan_memory, reinterpret_cast<int*>(plan_memory + n + 1)};
+  const bool few = n <= kFew && a.B <= kFew;
+  extern __shared__ __align__(16) uint8_t plan_memory[];
+  __shared__ int64_t scratch[2][kPlanThreads / 32];
+  PlanState s;
+  uint8_t* at = plan_memory;
+  s.groups = few ? reinterpret_cast<GroupPlan*>(at) : x.groups;
+  if (few) at += n * sizeof(GroupPlan);
+  s.own = few ? reinterpret_cast<RowPlan*>(at) : x.own;
+  if (few) at += a.B * sizeof(RowPlan);
+  s.units = reinterpret_cast<int*>(at);
+  s.tiles = s.units + n + 1;
   pdl_launch_dependents();
   pdl_wait();
   int wrong = 0;
   if (n <= 2 * kPlanThreads / 32) {
-    for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, sums, i, true);
+    for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, s, i, true);
   } else {
-    for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, sums, i + tid / 8, i + tid / 8 < n);
+    for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, s, i + tid / 8, i + tid / 8 < n);
   }
   wrong = __syncthreads_or(wrong);
-  sum_before(sums.units, n, scratch);
-  if (!wrong) sum_before(sums.tiles, a.B, scratch);
-  if (sums.units[n] > kUnitLimit || (!wrong && (int64_t)sums.tiles[a.B] * g.p.groups > kUnitLimit)) wrong = 1;
-  __syncthreads();
-  if (wrong) {  // every row is empty, of one tile
-    for (int b = tid; b < a.B; b += kPlanThreads) {
-      x.own[b] = {0, 0, 0, 0, -1, kEmpty, 0, 0};
-      sums.tiles[b] = b;
-    }
-    if (tid == 0) {
-      atomicOr(a.err, kErrBadSeq);
-      sums.tiles[a.B] = a.B;
-      sums.units[n] = 0;
-    }
+  if (!wrong) {
+    sum_before(s, n, a.B, scratch);
+    wrong = s.units[n] > kUnitLimit || (int64_t)s.tiles[a.B] * g.p.groups > kUnitLimit;
     __syncthreads();
   }
-  for (int i = tid; i < n; i += kPlanThreads) x.groups[i].units = (int)sums.units[i];
-  for (int b = tid; b < a.B; b += kPlanThreads) x.own[b].tiles = sums.tiles[b];
-  const int units = (int)sums.units[n], own_tiles = sums.tiles[a.B];
-  if (tid == 0) *x.all = {units, own_tiles};
+  if (wrong) {  // every row is empty, of one tile
+    for (int b = tid; b <= a.B; b += kPlanThreads) {
+      if (b < a.B) s.own[b] = {0, 0, 0, 0, -1, kEmpty, 0, 0, 0, 0, {0, 0}};
+      s.tiles[b] = b;
+    }
+    for (int i = tid; i <= n; i += kPlanThreads) s.units[i] = 0;
+    if (tid == 0) atomicOr(a.err, kErrBadSeq);
+  }
   __syncthreads();
   // where each CTA begins
+  const int units = s.units[n], own_tiles = s.tiles[a.B];
   const Ranges items(units, min(x.n_items, units));
   for (int c = tid; c < x.n_items; c += kPlanThreads) {
-    ItemStart s;
-    s.n = c < items.n ? items.begin(c + 1) - items.begin(c) : 0;
-    if (s.n) {
+    ItemStart r;
+    r.n = 0;
+    if (c < items.n) {
       const int u = items.begin(c);
-      s.g = last_of(sums.units, n, u);
-      s.p = load_record(x.groups + s.g);
-      const int at = u - s.p.units, item = at / s.p.tiles, tile = at - item * s.p.tiles;
-      s.hg = item / s.p.blocks;
-      s.block = item - s.hg * s.p.blocks;
-      s.token = s.p.first + tile * x.tile;
-      s.left = s.p.tiles - tile;
+      r.n = items.begin(c + 1) - u;
+      r.g = last_of(s.units, n, u);
+      r.p = s.groups[r.g];
+      const int in = u - s.units[r.g], item = in / r.p.tiles, tile = in - item * r.p.tiles;
+      r.hg = item / r.p.blocks;
+      r.block = item - r.hg * r.p.blocks;
+      r.token = r.p.first + tile * x.tile;
+      r.left = r.p.tiles - tile;
     }
-    x.item_start[c] = s;
+    x.item_start[c] = r;
   }
   const int own_units = own_tiles * g.p.groups;
   const Ranges rows(own_units, min(g.p.n_items, own_units));
-  for (int c = tid; c < g.p.n_items; c += kPlanThreads) {
-    OwnStart s;
-    s.n = c < rows.n ? rows.begin(c + 1) - rows.begin(c) : 0;
-    s.b = s.hg = 0;
-    if (s.n) {
+  for (int c = kPlanThreads - 1 - tid; c < g.p.n_items; c += kPlanThreads) {
+    OwnStart r;
+    r.n = r.b = r.hg = 0;
+    if (c < rows.n) {
       const int u = rows.begin(c);
-      s.hg = u / own_tiles;
-      const int at = u - s.hg * own_tiles;
-      s.b = last_of(sums.tiles, a.B, at);
-      s.p = load_record(x.own + s.b);
-      s.token = s.p.first + (at - sums.tiles[s.b]) * g.p.tile;
-      s.left = sums.tiles[s.b + 1] - at;
+      r.n = rows.begin(c + 1) - u;
+      r.hg = u / own_tiles;
+      const int in = u - r.hg * own_tiles;
+      r.b = last_of(s.tiles, a.B, in);
+      r.p = s.own[r.b];
+      r.token = r.p.first + (in - s.tiles[r.b]) * g.p.tile;
+      r.left = s.tiles[r.b + 1] - in;
     }
-    x.own_start[c] = s;
+    x.own_start[c] = r;
+  }
+  // the records themselves
+  for (int i = tid; i < n; i += kPlanThreads) {
+    if (few) x.groups[i] = s.groups[i];
+    x.groups[i].units = s.units[i];
+  }
+  for (int b = tid; b < a.B; b += kPlanThreads) {
+    if (few) x.own[b] = s.own[b];
+    x.own[b].tiles = s.tiles[b];
   }
 }
 
@@ -228,40 +257,35 @@ constexpr int kJoinThreads = 128;
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args g, const Divider by_heads,
-                                                            const Divider by_rows) {
+                                                            const Divider by_rows, const int heads_log2) {
   constexpr int kBatch = 4;
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int lane = threadIdx.x & 31, d = a.v.d, qpg = a.v.qpg;
   const int64_t nth = (int64_t)blockIdx.x * (kJoinThreads / 32) + threadIdx.x / 32;
   pdl_launch_dependents();
-  pdl_wait();
   if (nth >= (int64_t)a.B * a.v.Hq) return;
+  // (the launch before begins once the plan is complete)
   const int b = by_heads.div((uint32_t)nth), j = (int)(nth - (int64_t)b * a.v.Hq);
-  const RowPlan own = x.own[b];
+  const RowPlan own = load_record(x.own + b);
   const int h = x.by_qpg.div(j), q = j - h * qpg, chunk = by_rows.div(q), r = q - chunk * g.p.rows, vh = h * g.p.chunks + chunk;
-  const int group = vh / g.p.wh, w = vh - group * g.p.wh;
-  // the CTAs that have left sums of its own tokens
-  const int own_tiles = x.all->own_tiles, units = g.p.groups * own_tiles;
-  const Ranges ranges(units, min(g.p.n_items, units));
-  const int u = group * own_tiles + own.tiles, tiles = max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile);
-  const int c0 = ranges.near_item_of(u), n_own = own.end > own.first ? ranges.near_item_of(u + tiles - 1) - c0 + 1 : 0;
-  const int64_t own0 = x.own_row(g.p, a.B, group, b, c0, w) + r, own_step = (int64_t)g.p.wh * g.p.rows;
+  const int group = vh >> heads_log2, w = vh & (g.p.wh - 1);
+  const int row = (b - own.start) * qpg + q, block = x.by_rows.div(row), hg = h / x.wh;
+  const bool shares = own.group >= 0;
+  pdl_wait();
   bool bad = own.state == kEmpty;
-  // and of what its group shares
-  int n = n_own;
-  int64_t part0 = 0;
-  const int64_t part_step = (int64_t)x.wh * x.rows;
-  if (own.group >= 0) {
-    const GroupPlan p = x.groups[own.group];
-    bad |= p.bad != 0;
-    const int row = (b - p.start) * qpg + q, hg = h / x.wh, block = row / x.rows;
-    const Ranges items(x.all->units, min(x.n_items, x.all->units));
-    const int v = p.units + (hg * p.blocks + block) * p.tiles, i0 = items.near_item_of(v);
-    n += items.near_item_of(v + p.tiles - 1) - i0 + 1;
-    part0 = x.row_of(p, a.v.Hkv, qpg, hg, block, i0, h - hg * x.wh, row - block * x.rows);
+  // the CTAs that have left sums of its own tokens, and of what its group shares
+  const CtaRange mine = x.own_ctas[(int64_t)group * a.B + b];
+  CtaRange theirs = {0, -1};
+  if (shares) {
+    theirs = x.item_ctas[x.item_id(own.start, own.blocks, a.v.Hq, hg, block)];
+    // (numbers that are none: a CTA gave up waiting)
+    bad |= x.groups[own.group].bad != 0 || theirs.first < 0 || theirs.first > theirs.last || theirs.last >= x.n_items;
   }
-  if (bad) n = 0;
+  const int n_own = own.end > own.first ? mine.last - mine.first + 1 : 0, n = bad ? 0 : n_own + theirs.last - theirs.first + 1;
+  const int64_t own0 = x.own_row(g.p, a.B, group, b, mine.first, w) + r, own_step = (int64_t)g.p.wh * g.p.rows;
+  const int64_t part0 = x.row_of(own.start, own.rows * qpg, a.v.Hq, qpg, hg, block, theirs.first, h - hg * x.wh, row - block * x.rows);
+  const int64_t part_step = (int64_t)x.wh * x.rows;
   const auto sums_of = [&](int i) {
     return i < n_own ? x.own_u + (own0 + i * own_step) * g.DP : x.part_u + (part0 + (i - n_own) * part_step) * g.DP;
   };
@@ -351,20 +375,26 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
 
 // The parts of the workspace.
 struct Parts {
-  size_t groups, own, item_start, own_start, part_ml, part_u, own_ml, own_u, all;
+  size_t groups, own, item_start, own_start, item_ctas, own_ctas, part_ml, part_u, own_ml, own_u, all = 0;
   Parts(const PagedView& v, const Plan& p, int B, int sms) {
     // (a CTA leaves 256 rows of an item, or each of two on an SM 16 for up to four heads)
     const size_t rows = (size_t)B * v.Hq + (size_t)sms * 256, DP = padded_dim(v.d);
     const size_t own_rows = ((size_t)p.groups * B + p.n_items) * p.wh * p.rows;
-    groups = 256;
-    own = groups + align_up((size_t)B * sizeof(GroupPlan), 256);
-    item_start = own + align_up((size_t)B * sizeof(RowPlan), 256);
-    own_start = item_start + align_up(kMaxItems * sizeof(ItemStart), 256);
-    part_ml = own_start + align_up(kMaxItems * sizeof(OwnStart), 256);
-    part_u = part_ml + align_up(rows * 2 * sizeof(float), 256);
-    own_ml = part_u + align_up(rows * DP * sizeof(float), 256);
-    own_u = own_ml + align_up(own_rows * 2 * sizeof(float), 256);
-    all = own_u + align_up(own_rows * DP * sizeof(float), 256);
+    const auto take = [&](size_t bytes) {
+      const size_t at = all;
+      all += align_up(bytes, 256);
+      return at;
+    };
+    groups = take((size_t)B * sizeof(GroupPlan));
+    own = take((size_t)B * sizeof(RowPlan));
+    item_start = take(kMaxItems * sizeof(ItemStart));
+    own_start = take(kMaxItems * sizeof(OwnStart));
+    item_ctas = take((size_t)B * v.Hq * sizeof(CtaRange));
+    own_ctas = take((size_t)B * p.groups * sizeof(CtaRange));
+    part_ml = take(rows * 2 * sizeof(float));
+    part_u = take(rows * DP * sizeof(float));
+    own_ml = take(own_rows * 2 * sizeof(float));
+    own_u = take(own_rows * DP * sizeof(float));
   }
 };
 
@@ -389,7 +419,8 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   const Layout l = layout_of(a.v, kind, a.B, a.n_groups, sms);
   const Parts parts(a.v, g.p, a.B, sms);
   char* ws = static_cast<char*>(a.ws);
-  g.x.all = reinterpret_cast<Whole*>(ws);
+  g.x.item_ctas = reinterpret_cast<CtaRange*>(ws + parts.item_ctas);
+  g.x.own_ctas = reinterpret_cast<CtaRange*>(ws + parts.own_ctas);
   g.x.groups = reinterpret_cast<GroupPlan*>(ws + parts.groups);
   g.x.own = reinterpret_cast<RowPlan*>(ws + parts.own);
   g.x.item_start = reinterpret_cast<ItemStart*>(ws + parts.item_start);
@@ -404,9 +435,9 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   g.x.wh = l.wh;
   g.x.tile = l.tile;
   g.x.by_qpg = divider((uint32_t)a.v.qpg);
+  g.x.by_rows = divider((uint32_t)l.rows);
   static std::atomic<uint64_t> ready{0};
-  const auto plan_bytes = [](int groups, int rows) { return sizeof(int64_t) * (groups + 1) + sizeof(int) * (rows + 1); };
-  cudaError_t e = allow_shared(plan_kernel, ready, plan_bytes(kMaxBatch, kMaxBatch));
+  cudaError_t e = allow_shared(plan_kernel, ready, plan_bytes(kFew, kFew));
   if (e == cudaSuccess) e = launch_pdl(plan_kernel, 1, kPlanThreads, plan_bytes(a.n_groups, a.B), s, g);
   if (e == cudaSuccess) e = hook_launched(a.hook, s);
   // heads of the shared part are KV heads themselves
@@ -420,8 +451,10 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
     e = kind.quant ? launch_own_q8(g, kind.dtype, s) : kind.dtype == DCK_F32 ? launch_own_f32(g, s) : launch_own_bf16(g, s);
   if (e != cudaSuccess) return e;
   const int64_t warps = (int64_t)a.B * a.v.Hq, blocks = (warps * 32 + kJoinThreads - 1) / kJoinThreads;
+  int heads_log2 = 0;
+  while (1 << heads_log2 < g.p.wh) ++heads_log2;
   const auto join = kind.dtype == DCK_F32 ? join_kernel<float> : join_kernel<__nv_bfloat16>;
-  e = launch_pdl(join, (unsigned)blocks, kJoinThreads, 0, s, g, divider((uint32_t)a.v.Hq), divider((uint32_t)g.p.rows));
+  e = launch_pdl(join, (unsigned)blocks, kJoinThreads, 0, s, g, divider((uint32_t)a.v.Hq), divider((uint32_t)g.p.rows), heads_log2);
   return e == cudaSuccess ? hook_launched(a.hook, s) : e;
 }
 

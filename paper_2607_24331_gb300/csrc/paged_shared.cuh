@@ -38,6 +38,18 @@ struct ItemWalk {
     left = p.tiles;
   }
   __device__ __forceinline__ int count(const Prefix& x, int qpg) const { return min(x.rows, p.rows * qpg - block * x.rows); }
+  // Whether the tile is the item's first.
+  __device__ __forceinline__ bool begins() const { return token == p.first; }
+  // Notes that this CTA has a part of the item, its first or last.
+  __device__ __forceinline__ void sign(const Prefix& x, int Hq, bool begun, bool ended) const {
+    CtaRange* r = x.item_ctas + x.item_id(p.start, p.blocks, Hq, hg, block);
+    if (begun) r->first = blockIdx.x;
+    if (ended) r->last = blockIdx.x;
+  }
+  // Where this CTA's sums of query r of head w go.
+  __device__ __forceinline__ int64_t row_of(const Prefix& x, int Hq, int qpg, int w, int r) const {
+    return x.row_of(p.start, p.rows * qpg, Hq, qpg, hg, block, blockIdx.x, w, r);
+  }
 };
 
 // Stores the sums of a CTA's tiles of queries: `count` of them per head, from partial row row0 on (of this warp's head).
@@ -154,7 +166,7 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
 #pragma unroll 1
   for (int i = 0; i < Z::S - 1; ++i) copy_next();
   int get = 0, count = 0;
-  bool bad = false, fresh = true;
+  bool bad = false, fresh = true, begun = at.begins();
   while (true) {
     __syncwarp();  // the stage that is filled next has been read
     copy_next();
@@ -180,7 +192,9 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
     }
     tile.finish();
     leave_sums<Z>(raw, sh, tile, warp, lane, n_heads, n_runs, used, count, d, false, x.part_u, x.part_ml,
-                  x.row_of(at.p, a.v.Hkv, qpg, at.hg, at.block, blockIdx.x, wh, 0));
+                  at.row_of(x, a.v.Hq, qpg, wh, 0));
+    if (threadIdx.x == 0) at.sign(x, a.v.Hq, begun, at.left == 0);
+    begun = true;
     if (n_runs > 1) load.clear_stage(raw + (warp * Z::S + used) * Z::kStage);
     if (last) break;
     bad = false;
@@ -279,7 +293,7 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) own_kernel(const __grid_co
 #pragma unroll 1
   for (int i = 0; i < Z::S - 1; ++i) copy_next();
   int get = 0;
-  bool bad = false, fresh = true;
+  bool bad = false, fresh = true, begun = at.token == at.p.first;
   while (true) {
     __syncwarp();  // the stage that is filled next has been read
     copy_next();
@@ -303,6 +317,12 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) own_kernel(const __grid_co
     tile.finish();
     leave_sums<Z>(raw, sh, tile, warp, lane, n_heads, n_runs, used, qs.count, d, bad, x.own_u, x.own_ml,
                   x.own_row(g.p, a.B, at.group, at.b, blockIdx.x, wh));
+    if (threadIdx.x == 0) {
+      CtaRange* r = x.own_ctas + (int64_t)at.group * a.B + at.b;
+      if (begun) r->first = blockIdx.x;
+      if (at.left == 0) r->last = blockIdx.x;
+    }
+    begun = true;
     if (last) break;
     if (n_runs > 1) load.clear_stage(raw + (warp * Z::S + used) * Z::kStage);
     bad = false;

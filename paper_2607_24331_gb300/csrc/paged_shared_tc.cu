@@ -348,7 +348,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
       if (!ok) break;
       const bool pair = sg.pair, both = pair || sg.n > 1;
       const int count = sg.at.count(x, a.v.qpg), mine = pair ? s * kRows + r : r;
-      const int64_t row = x.row_of(sg.at.p, heads, a.v.qpg, sg.at.hg, sg.at.block, blockIdx.x, 0, mine);
+      const int64_t row = sg.at.row_of(x, a.v.Hq, a.v.qpg, 0, mine);
+      if (tid == 0) sg.at.sign(x, a.v.Hq, sg.at.begins(), sg.n == sg.at.left);
       float* to = x.part_u + row * DP;
       float f0 = 1.f, f1 = 0.f;
       if (!pair) {
