@@ -258,7 +258,7 @@ constexpr int kJoinThreads = 128;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Args g, const Divider by_heads,
                                                             const Divider by_rows, const int heads_log2) {
-  constexpr int kBatch = 4;
+  constexpr int kBatch = 8;
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int lane = threadIdx.x & 31, d = a.v.d, qpg = a.v.qpg;

@@ -240,7 +240,7 @@ struct OwnWalk : Walk {
 // What the rows have of their own: tiles dealt in ranges as in paged_decode_kernel, a partial sum left of each (head group,
 // row) by each CTA that has tiles of it.
 template <class Z, class Tile>
-__global__ void __launch_bounds__(Z::NW * 32, kPerSm) own_kernel(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(Z::NW * 32, 3) own_kernel(const __grid_constant__ Args g) {
   extern __shared__ __align__(128) uint8_t raw[];
   using Shm = Shared<Z, Tile, false>;
   Shm& sh = *reinterpret_cast<Shm*>(raw + Z::kRing);
