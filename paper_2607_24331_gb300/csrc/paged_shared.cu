@@ -362,7 +362,7 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
     l.rows = 256;
     l.tile = 64;
     l.wh = 1;
-    l.n_items = sms;
+    l.n_items = std::max(1, sms - 1);  // the plan's block has the last SM while they get ready
     return l;
   }
   l.rows = kind.dtype == DCK_BF16 && DP <= 128 && queries > 8 ? 16 : 8;

@@ -15,6 +15,10 @@
 // softmax ends.
 // P overwrites its scores in tensor memory and is the A operand of O += P V from there.  Four warps copy (pages of any size
 // and order: 16-byte asynchronous copies into the swizzled layout), the rows behind a tile's last token as zeros.
+//
+// The CTAs are there while the plan is made, and meanwhile go through their code once on an item of nothing: no wait, no
+// copy of anything, no MMA, nothing stored.  Instructions that are not in an SM's caches come at some 16 in 0.1 us; without that pass
+// the first tile's softmax alone took 3 us for 0.5.
 #include "paged_shared.cuh"
 #include "tc_common.cuh"
 
@@ -30,6 +34,7 @@ constexpr int kThreads = 512;
 constexpr int kRegsSoftmax = 168, kRegsOther = 88;
 constexpr int kRows = 128;        // queries of a stream
 constexpr int kTok = 64;          // tokens of a tile
+constexpr int kAhead = 4;         // tiles whose page numbers are read at a time
 constexpr int kAtom = 128 * 128;  // 128 rows of 128 bytes
 constexpr int kHalf = kTok * 128;
 
@@ -54,7 +59,26 @@ struct Segments {
     n = min(at.left, left);
     pair = at.count(x, qpg) > kRows;
   }
+  bool dry;  // the item of nothing
+  __device__ __forceinline__ void begin_dry() {
+    dry = true;
+    pair = false;
+    n = 2;
+    left = nth = 0;
+    at.p.start = at.p.rows = at.p.first = at.p.table = at.token = at.hg = at.block = at.left = 0;
+    at.p.end = 2 * kTok;
+  }
+  // The next item: the first real one once the plan is there.
   __device__ __forceinline__ bool next(const Prefix& x, int heads, int qpg) {
+    if (dry) {
+      dry = false;
+      pdl_wait();
+      pdl_launch_dependents();  // the plan, and with it all that the own tokens' launch reads, is there
+      left = at.enter(x, blockIdx.x);
+      if (left == 0) return false;
+      see(x, qpg);
+      return true;
+    }
     left -= n;
     if (left <= 0) return false;
     at.leave(x, heads);
@@ -147,13 +171,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, heads = a.v.Hkv;
-  pdl_wait();
-  pdl_launch_dependents();  // the plan, and with it all that the own tokens' launch reads, is there
-  Segments sg;
-  sg.left = sg.at.enter(x, blockIdx.x);
-  if (sg.left == 0) return;
-  sg.nth = 0;
-  sg.see(x, a.v.qpg);
   volatile int* abort_flag = &sm.abort_flag;
   if (warp == 12) {
     tmem_alloc(&sm.tmem_base, 512);
@@ -182,6 +199,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  Segments sg;
+  sg.begin_dry();
   const uint32_t tmem = sm.tmem_base;  // scores and P of stream s, buffer b at 128 s + 64 b, its output at 256 + 128 s
 
   if (warp >= 12) {
@@ -211,19 +230,20 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
           umma_commit(bar);
           if (!sg.pair) umma_commit(bar);
         };
-        if (!(ok = wwait(&sm.q_full, sg.nth & 1, abort_flag))) break;
-        if (tiles == 0 && el) umma_commit(&sm.q_empty);
+        const bool dry = sg.dry, issue = el && !dry;
+        if (!dry && !(ok = wwait(&sm.q_full, sg.nth & 1, abort_flag))) break;
+        if (tiles == 0 && issue) umma_commit(&sm.q_empty);
         int si = 0, vi = 0;  // the next scores and the next products with values
         long long since = 0;
         while (vi < tiles) {
           bool idle = true;
           if (si < tiles && si < vi + 2) {
             const int at = base + 2 * (first + si * step), slot = at % kSlots;
-            if (__all_sync(~0u, mbar_test(&sm.kv_full[slot], at / kSlots & 1))) {
+            if (__all_sync(~0u, mbar_test(&sm.kv_full[slot], at / kSlots & 1) || dry)) {
               idle = false;
               fence_proxy_async_smem();
               tc_fence_after();
-              if (el) {
+              if (issue) {
                 const uint64_t kb = dk + (uint64_t)(slot * (kSlotBytes >> 4));
 #pragma unroll
                 for (int j = 0; j < DP / 16; ++j)
@@ -237,16 +257,16 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
             }
           }
           const int b = vi & 1;
-          if (vi < si && __all_sync(~0u, mbar_test(&sm.p_full[s][b], turn[b] & 1))) {
+          if (vi < si && __all_sync(~0u, mbar_test(&sm.p_full[s][b], turn[b] & 1) || dry)) {
             const int at = base + 2 * (first + vi * step) + 1, slot = at % kSlots;
-            if (__all_sync(~0u, mbar_test(&sm.kv_full[slot], at / kSlots & 1))) {
+            if (__all_sync(~0u, mbar_test(&sm.kv_full[slot], at / kSlots & 1) || dry)) {
               idle = false;
               // the last item's output has been read
               if (vi == 0 && sg.nth > 0 && !(ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag))) break;
-              ++turn[b];
+              turn[b] += !dry;
               fence_proxy_async_smem();
               tc_fence_after();
-              if (el) {
+              if (issue) {
                 const uint64_t vb = dv + (uint64_t)(slot * (kSlotBytes >> 4));
 #pragma unroll
                 for (int j = 0; j < kTok / 16; ++j)
@@ -271,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
             }
           }
         }
-        base += 2 * n;
+        if (!dry) base += 2 * n;
       } while (ok && sg.next(x, heads, a.v.qpg));
     }
   } else if (warp < 8) {
@@ -287,12 +307,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     uint32_t sp = 0, turn = 0, joined = 0, outputs[2] = {0, 0};
     bool ok = true;
     do {
+      const bool dry = sg.dry;
       float m = -CUDART_INF_F;
       float2 l = make_float2(0.f, 0.f);
-      for (int k = sg.first(s), j = 0; k < sg.n; k += sg.step(), ++j, ++turn) {
+      for (int k = sg.first(s), j = 0; k < sg.n; k += sg.step(), ++j, turn += !dry) {
         const int b = j & 1;
-        if (!(ok = wwait(&sm.s_full[s][b], sp >> b & 1, abort_flag))) break;
-        sp ^= 1u << b;
+        if (!dry && !(ok = wwait(&sm.s_full[s][b], sp >> b & 1, abort_flag))) break;
+        sp ^= (uint32_t)!dry << b;
         tc_fence_after();
         const uint32_t sb = tmem + lb + 128 * s + 64 * b;
         float sv[kTok];
@@ -343,13 +364,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.p_full[s][b]);
+        if (lane == 0 && !dry) mbar_arrive(&sm.p_full[s][b]);
       }
       if (!ok) break;
       const bool pair = sg.pair, both = pair || sg.n > 1;
-      const int count = sg.at.count(x, a.v.qpg), mine = pair ? s * kRows + r : r;
+      const int count = dry ? 0 : sg.at.count(x, a.v.qpg), mine = pair ? s * kRows + r : r;
       const int64_t row = sg.at.row_of(x, a.v.Hq, a.v.qpg, 0, mine);
-      if (tid == 0) sg.at.sign(x, a.v.Hq, sg.at.begins(), sg.n == sg.at.left);
+      if (tid == 0 && !dry) sg.at.sign(x, a.v.Hq, sg.at.begins(), sg.n == sg.at.left);
       float* to = x.part_u + row * DP;
       float f0 = 1.f, f1 = 0.f;
       if (!pair) {
@@ -357,9 +378,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
         if (sg.nth > 0 && !(ok = wwait(&sm.o_free, (sg.nth - 1) & 1, abort_flag))) break;
         sm.ml[s][r] = make_float2(m, l.x + l.y);
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.ml_full);
-        if (!(ok = wwait(&sm.ml_full, joined & 1, abort_flag))) break;
-        ++joined;
+        if (lane == 0 && !dry) mbar_arrive(&sm.ml_full);
+        if (!dry && !(ok = wwait(&sm.ml_full, joined & 1, abort_flag))) break;
+        joined += !dry;
         const float2 u0 = sm.ml[0][r], u1 = sm.ml[1][r];
         const float top = both ? fmaxf(u0.x, u1.x) : u0.x, base = top == -CUDART_INF_F ? 0.f : top;
         f0 = exp2_approx(u0.x - base), f1 = both ? exp2_approx(u1.x - base) : 0.f;
@@ -371,8 +392,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
 #pragma unroll
       for (int t = 0; t < 2; ++t) {  // both streams' last products where both have any
         if (t == 1 && !both) continue;
-        if ((!pair || t == s) && !(ok = wwait(&sm.o_full[t], outputs[t] & 1, abort_flag))) break;
-        ++outputs[t];
+        if (!dry && (!pair || t == s) && !(ok = wwait(&sm.o_full[t], outputs[t] & 1, abort_flag))) break;
+        outputs[t] += !dry;
       }
       if (!ok) break;
       tc_fence_after();
@@ -402,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.o_free);
+      if (lane == 0 && !dry) mbar_arrive(&sm.o_free);
     } while (ok && sg.next(x, heads, a.v.qpg));
   } else {
     // ---- copies -----------------------------------------------------------------------
@@ -414,44 +435,63 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
     uint32_t parity = 1;  // (a fresh barrier passes a wait for the phase before its first)
     bool ok = true;
     do {
+      const bool dry = sg.dry;
       const int32_t* table = a.table + sg.at.p.table * a.table_stride;
       const auto page_of = [&](int k, int& off) -> int {  // of this lane's token of tile k (off < 0: none)
         const int t = sg.at.token + kTok * k + 16 * w + (lane & 15);
         off = -1;
-        if (t >= sg.at.p.end) return 0;
+        if (dry || k >= sg.n || t >= sg.at.p.end) return 0;
         const uint32_t col = v.by_page.div(t);
         off = t - (int)col * v.page;
         return table[col];
       };
-      int off, page = page_of(0, off), off2 = -1, page2 = sg.n > 1 ? page_of(1, off2) : 0;
+      // page numbers are read four tiles ahead
+      int page[kAhead], off[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) page[i] = page_of(i, off[i]);
       // the last item's scores are all formed: its queries can go
       if (sg.nth > 0 && !(ok = wwait(&sm.q_empty, (sg.nth - 1) & 1, abort_flag))) break;
+#pragma unroll 1
       for (int t = 0; t < (sg.pair ? 2 : 1); ++t) {
-        const int64_t qo = copy.query(sg.at, t * kRows);
+        const int64_t qo = dry ? -1 : copy.query(sg.at, t * kRows);
         if (g.p.q_copied) copy.template rows<32>(sm.q[t][0], kAtom, 32 * w, a.q, qo);
         else copy.elements(sm.q[t][0], qo);
       }
-      if (g.p.q_copied) arrive_when_copied(&sm.q_full);
-      else mbar_arrive(&sm.q_full);
-      for (int k = 0; k < sg.n && ok; ++k) {
-        const bool inside = (uint32_t)page < (uint32_t)v.n_pages;
-        if (off >= 0 && !inside) {
-          atomicOr(a.err, kErrBadSeq);
-          atomicOr(&x.groups[sg.at.g].bad, 1);
-        }
-        const bool have = off >= 0 && inside;
-        const int64_t ko = have ? (int64_t)((uint64_t)page * v.k_page_b + (uint64_t)off * v.k_tok_b + (uint64_t)sg.at.hg * v.k_head_b) : -1;
-        const int64_t vo = have ? (int64_t)((uint64_t)page * v.v_page_b + (uint64_t)off * v.v_tok_b + (uint64_t)sg.at.hg * v.v_head_b) : -1;
-        page = page2, off = off2;
-        if (k + 2 < sg.n) page2 = page_of(k + 2, off2);  // two tiles before its copies need it
+      if (!dry) {
+        if (g.p.q_copied) arrive_when_copied(&sm.q_full);
+        else mbar_arrive(&sm.q_full);
+      }
+#pragma unroll 1
+      for (int k0 = 0; k0 < sg.n && ok; k0 += kAhead) {
+        int64_t at[kAhead][2];  // where this lane's token's keys and values lie, in bytes (-1: none)
 #pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-          if (!(ok = wwait(&sm.kv_empty[slot], parity, abort_flag))) break;
-          copy.template rows<16>(sm.kv[slot][0], kHalf, 16 * w, kind ? a.vc : a.kc, kind ? vo : ko);
-          arrive_when_copied(&sm.kv_full[slot]);
-          if (++slot == kSlots) slot = 0, parity ^= 1;
+        for (int i = 0; i < kAhead; ++i) {
+          const bool inside = (uint32_t)page[i] < (uint32_t)v.n_pages;
+          if (off[i] >= 0 && !inside) {
+            atomicOr(a.err, kErrBadSeq);
+            atomicOr(&x.groups[sg.at.g].bad, 1);
+          }
+          const bool have = off[i] >= 0 && inside;
+          at[i][0] = have ? (int64_t)((uint64_t)page[i] * v.k_page_b + (uint64_t)off[i] * v.k_tok_b + (uint64_t)sg.at.hg * v.k_head_b) : -1;
+          at[i][1] = have ? (int64_t)((uint64_t)page[i] * v.v_page_b + (uint64_t)off[i] * v.v_tok_b + (uint64_t)sg.at.hg * v.v_head_b) : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) page[i] = page_of(k0 + kAhead + i, off[i]);
+        for (int i = 0; i < kAhead && k0 + i < sg.n && ok; ++i) {
+          const int64_t ko = i == 0 ? at[0][0] : i == 1 ? at[1][0] : i == 2 ? at[2][0] : at[3][0];
+          const int64_t vo = i == 0 ? at[0][1] : i == 1 ? at[1][1] : i == 2 ? at[2][1] : at[3][1];
+#pragma unroll 1
+          for (int kind = 0; kind < 2; ++kind) {
+            if (!dry && !(ok = wwait(&sm.kv_empty[slot], parity, abort_flag))) break;
+            copy.template rows<16>(sm.kv[slot][0], kHalf, 16 * w, kind ? a.vc : a.kc, kind ? vo : ko);
+            if (!dry) {
+              arrive_when_copied(&sm.kv_full[slot]);
+              if (++slot == kSlots) slot = 0, parity ^= 1;
+            }
+          }
         }
       }
+      if (dry) cp_async_wait<0>();
     } while (ok && sg.next(x, heads, a.v.qpg));
     cp_async_wait<0>();
   }
