@@ -72,7 +72,7 @@ struct ScoreScale {
 // Calls over shared prefixes (paged_shared.cu): what the rows of group g see together, tokens [first, end), is attended
 // to for all of them at once, in items of a block of their queries and a head group, each cut into tiles; the items'
 // tiles form one list, dealt to CTAs in equal ranges.
-struct GroupPlan {
+struct alignas(16) GroupPlan {
   int start, rows;   // its rows
   int first, end;    // the tokens; none: end = first
   int table;         // the row whose block table they are read by
@@ -82,7 +82,7 @@ struct GroupPlan {
   int pad[3];
 };
 // What a row attends to by itself: tokens [first, end), counted without `skip` of them from token skip_at on.
-struct RowPlan {
+struct alignas(16) RowPlan {
   int first, end, skip_at, skip;
   int group;      // its group, -1 if the row takes no part in what that shares
   int state;      // 0, or kEmpty: zeros whatever the group has
@@ -93,11 +93,11 @@ struct RowPlan {
 constexpr int kEmpty = 1;
 // Where a CTA begins: its first item, or (head group, row), the tile's first token and the tiles from it to the end
 // of that, and how many it has in all.
-struct ItemStart {
+struct alignas(16) ItemStart {
   GroupPlan p;
   int g, hg, block, token, left, n, pad[2];
 };
-struct OwnStart {
+struct alignas(16) OwnStart {
   RowPlan p;
   int b, hg, token, left, n, pad[3];
 };
@@ -173,12 +173,15 @@ constexpr int warps_of(int DP, bool one_per_sm) { return (DP == 256 ? 2 : 4) * (
 constexpr int kPerSm = 2;
 inline int run_of(DecodeKind k) { return k.quant ? 32 : k.dtype == DCK_BF16 ? 16 : 8; }  // tokens of a warp's step
 
-// Visible tokens of sequence b and the first of them; 0 for invalid lengths.
-__device__ __forceinline__ int visible(const PagedDecodeArgs& a, int b, int& first, bool& bad) {
-  const int L = a.seq_len[b];
+// Visible tokens of a sequence of length L and the first of them; 0 for invalid lengths.
+__device__ __forceinline__ int visible_of(const PagedDecodeArgs& a, int L, int& first, bool& bad) {
   bad = L < 0 || L > a.max_len || L > kMaxLen || (L > 0 && (int64_t)a.v.by_page.div(L - 1) >= a.table_stride);
   first = a.window > 0 && L > a.window ? L - a.window : 0;
   return bad ? 0 : L - first;
+}
+// Of sequence b.
+__device__ __forceinline__ int visible(const PagedDecodeArgs& a, int b, int& first, bool& bad) {
+  return visible_of(a, a.seq_len[b], first, bad);
 }
 
 __device__ __forceinline__ float exp2_approx(float x) {
