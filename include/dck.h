@@ -565,6 +565,15 @@ dck_status dck_last_device_error(void* stream);
 int32_t dck_set_decode_kernel(int32_t which);
 
 /*
+ * dck_set_shared_way - how the calls over shared prefixes attend:
+ *   0 = automatic (by the bounds that the host knows)
+ *   1 = every row by itself
+ *   2 = what groups share once for all rows
+ * Returns this thread's previous value; other values change nothing.
+ */
+int32_t dck_set_shared_way(int32_t which);
+
+/*
  * dck_set_timing_events - timing hook of the decode calls
  * (dck_paged_decode_attention among them): `events` holds
  * n CUDA events (cudaEvent_t, owned by the caller, 2 <= n <= 16).  Each later

@@ -118,6 +118,7 @@ struct PagedDecodeArgs {
   // calls over shared prefixes: rows group_start[g] .. group_start[g + 1] - 1 share their first shared_len[g] tokens
   int32_t n_groups, max_own;
   const int32_t *group_start, *shared_len;
+  int32_t way;  // dck_set_shared_way
 };
 // What an attention call works on: the type of queries and outputs, and whether caches are 8-bit.
 struct DecodeKind {

@@ -181,6 +181,8 @@ size_t shared_workspace(const PagedView& v, DecodeKind kind, int32_t batch, int3
   return paged_shared_workspace(v, kind, batch, max_seq_len, max_own, sms);
 }
 
+thread_local int32_t t_shared_way = 0;  // dck_set_shared_way
+
 // The rows of a call that begin with the same tokens.
 struct Groups {
   int32_t max_own, n;
@@ -235,6 +237,7 @@ dck_status attend(const PagedView& v, DecodeKind kind, const void* q, int64_t q_
   a.max_own = groups ? groups->max_own : 0;
   a.group_start = groups ? groups->start : nullptr;
   a.shared_len = groups ? groups->shared : nullptr;
+  a.way = t_shared_way;
   a.ws = workspace;
   LaunchHook hook = thread_hook();
   a.hook = &hook;
@@ -383,6 +386,12 @@ dck_status dck_paged_append(const dck_paged_desc* desc, const dck_rope_table* ta
   if (st != DCK_OK) return st;
   return append(desc, nullptr, table, q, q_stride, k, k_stride, v, v_stride, n_tok, d_positions, d_slots, q_out, kcache,
                 nullptr, vcache, nullptr, stream);
+}
+
+int32_t dck_set_shared_way(int32_t which) {
+  const int32_t before = t_shared_way;
+  if (which >= 0 && which <= 2) t_shared_way = which;
+  return before;
 }
 
 dck_status dck_validate_quant_desc(const dck_quant_desc* desc) { return check_quant(desc); }

@@ -22,12 +22,7 @@ namespace {
 
 constexpr int kPlanThreads = 512;
 
-// What the plan is made from: the call's arrays, or (in its dry pass) some in shared memory.
-struct PlanInput {
-  const int32_t *seq_len, *group_start, *shared_len;
-  int B, n;
-};
-// What it works on: its records, in shared memory where they fit (kFew groups and rows), else where they go; tiles
+// What the plan works on: its records, in shared memory where they fit (kFew groups and rows), else where they go; tiles
 // of all groups, and of all rows, before each.
 constexpr int kFew = kPlanThreads;
 struct PlanState {
@@ -51,20 +46,21 @@ __device__ __forceinline__ RowView row_view(const PagedDecodeArgs& a, int len, i
 
 // A subgroup of LANES threads per group of rows at a time; true if d_group_start is not as it must be.
 template <int LANES>
-__device__ __forceinline__ bool plan_group(const Args& g, const PlanInput& in, const PlanState& s, int at, bool there, bool dry) {
+__device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, int at, bool there) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int lane = threadIdx.x % LANES;
   int start = 0, end = 0, said = 0;
-  if (there) start = in.group_start[at], end = in.group_start[at + 1], said = in.shared_len[at];
-  const bool wrong = there && (start < 0 || end < start || end > in.B || (at == 0 && start != 0) || (at == in.n - 1 && end != in.B));
+  if (there) start = a.group_start[at], end = a.group_start[at + 1], said = a.shared_len[at];
+  const bool wrong = there && (start < 0 || end < start || end > a.B || (at == 0 && start != 0) ||
+                               (at == x.n_groups - 1 && end != a.B));
   if (wrong) end = start;
   const int shared = max(said, 0), rows = end - start;
   if (said < 0 && lane == 0) atomicOr(a.err, kErrBadSeq);
   // the longest row, the first of them
   int longest = 0, row = start;
   for (int b = start + lane; b < end; b += LANES) {
-    const RowView r = row_view(a, in.seq_len[b], shared);
+    const RowView r = row_view(a, a.seq_len[b], shared);
     if (r.len > longest) longest = r.len, row = b;
   }
 #pragma unroll
@@ -75,7 +71,7 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanInput& in, c
   const int most = min(longest, shared), least = max(1, most - 256 - rows);
   int last = most, first = 0;
   for (int b = start + lane; b < end; b += LANES) {
-    const RowView r = row_view(a, in.seq_len[b], shared);
+    const RowView r = row_view(a, a.seq_len[b], shared);
     if (r.eff >= least) last = min(last, r.eff), first = max(first, r.first);
   }
 #pragma unroll
@@ -87,10 +83,10 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanInput& in, c
   const int64_t blocks = ((int64_t)rows * a.v.qpg + x.rows - 1) / x.rows;
   // what each row has of its own
   for (int b = start + lane; b < end; b += LANES) {
-    const RowView r = row_view(a, in.seq_len[b], rows > 1 ? shared : 0);
+    const RowView r = row_view(a, a.seq_len[b], rows > 1 ? shared : 0);
     RowPlan own;
     const bool takes_part = last > first && r.eff >= last && r.first <= first, bad = r.bad || r.len - r.eff > a.max_own;
-    if (bad && !dry) atomicOr(a.err, kErrBadSeq);
+    if (bad) atomicOr(a.err, kErrBadSeq);
     own.state = bad ? kEmpty : 0;
     own.group = takes_part && !bad ? at : -1;
     own.skip_at = takes_part ? first : 0;
@@ -166,120 +162,102 @@ __device__ __forceinline__ int last_of(const int* v, int n, int u) {
   return lo;
 }
 
-constexpr int kDry = 2;  // rows of the dry pass, in one group
-
 size_t plan_bytes(int groups, int rows) {
   const bool few = groups <= kFew && rows <= kFew;
-  return std::max((few ? groups * sizeof(GroupPlan) + rows * sizeof(RowPlan) : 0) + sizeof(int) * (groups + 1 + rows + 1),
-                  sizeof(GroupPlan) + kDry * sizeof(RowPlan) + sizeof(int) * (2 + kDry + 1));
+  return (few ? groups * sizeof(GroupPlan) + rows * sizeof(RowPlan) : 0) + sizeof(int) * (groups + 1 + rows + 1);
 }
 
-// One block.  While the launches before are still at work it makes a plan of two rows in shared memory, which is
-// stored nowhere: then the instructions are in the caches when the lengths are there (8 us a plan without, @@ with).
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Args g) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, n = x.n_groups;
   extern __shared__ __align__(16) uint8_t plan_memory[];
   __shared__ int64_t scratch[2][kPlanThreads / 32];
-  __shared__ int32_t dry_input[kDry + 3];
-  if (tid < kDry + 3) dry_input[tid] = tid < kDry ? min(tid + 64, a.max_len) : tid == kDry ? 0 : tid == kDry + 1 ? kDry : 64;
   pdl_launch_dependents();
+  pdl_wait();
+  const bool few = n <= kFew && a.B <= kFew;
+  PlanState s;
+  uint8_t* at = plan_memory;
+  s.groups = few ? reinterpret_cast<GroupPlan*>(at) : x.groups;
+  if (few) at += n * sizeof(GroupPlan);
+  s.own = few ? reinterpret_cast<RowPlan*>(at) : x.own;
+  if (few) at += a.B * sizeof(RowPlan);
+  s.units = reinterpret_cast<int*>(at);
+  s.tiles = s.units + n + 1;
+  int wrong = 0;
+  if (n <= 2 * kPlanThreads / 32) {
+    for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, s, i, true);
+  } else {
+    for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, s, i + tid / 8, i + tid / 8 < n);
+  }
+  wrong = __syncthreads_or(wrong);
+  if (!wrong) {
+    sum_before(s, n, a.B, scratch);
+    wrong = s.units[n] > kUnitLimit || (int64_t)s.tiles[a.B] * g.p.groups > kUnitLimit;
+    __syncthreads();
+  }
+  if (wrong) {  // every row is empty, of one tile
+    for (int b = tid; b <= a.B; b += kPlanThreads) {
+      if (b < a.B) s.own[b] = {0, 0, 0, 0, -1, kEmpty, 0, 0, 0, 0, {0, 0}};
+      s.tiles[b] = b;
+    }
+    for (int i = tid; i <= n; i += kPlanThreads) s.units[i] = 0;
+    if (tid == 0) atomicOr(a.err, kErrBadSeq);
+  }
   __syncthreads();
-#pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {
-    const bool dry = pass == 0;
-    PlanInput in = {dry_input, dry_input + kDry, dry_input + kDry + 2, kDry, 1};
-    if (!dry) {
-      pdl_wait();
-      in = {a.seq_len, a.group_start, a.shared_len, a.B, x.n_groups};
+  // where each CTA begins
+  const int units = s.units[n], own_tiles = s.tiles[a.B];
+  int n_items = min(x.n_items, units);
+  if (n == 1 && units) {
+    // Items that are all alike: whole CTAs for each, if that leaves out less than an eighth of them, so that none has the end
+    // of one and the beginning of another (3 us more where an end leaves 256 rows).
+    const int alike = units / s.groups[0].tiles, each = n_items / alike;
+    if (8 * each * alike >= 7 * n_items) n_items = each * alike;
+  }
+  const Ranges items(units, n_items);
+  for (int c = tid; c < x.n_items; c += kPlanThreads) {
+    ItemStart r;
+    r.n = 0;
+    if (c < items.n) {
+      const int u = items.begin(c);
+      r.n = items.begin(c + 1) - u;
+      r.g = last_of(s.units, n, u);
+      r.p = s.groups[r.g];
+      const int inside = u - s.units[r.g], item = inside / r.p.tiles, tile = inside - item * r.p.tiles;
+      r.hg = item / r.p.blocks;
+      r.block = item - r.hg * r.p.blocks;
+      r.token = r.p.first + tile * x.tile;
+      r.left = r.p.tiles - tile;
     }
-    const int n = in.n;
-    const bool few = n <= kFew && in.B <= kFew;
-    PlanState s;
-    uint8_t* at = plan_memory;
-    s.groups = few ? reinterpret_cast<GroupPlan*>(at) : x.groups;
-    if (few) at += n * sizeof(GroupPlan);
-    s.own = few ? reinterpret_cast<RowPlan*>(at) : x.own;
-    if (few) at += in.B * sizeof(RowPlan);
-    s.units = reinterpret_cast<int*>(at);
-    s.tiles = s.units + n + 1;
-    int wrong = 0;
-    if (n <= 2 * kPlanThreads / 32) {
-      for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, in, s, i, true, dry);
-    } else {
-      for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, in, s, i + tid / 8, i + tid / 8 < n, dry);
+    x.item_start[c] = r;
+  }
+  const int own_units = own_tiles * g.p.groups;
+  const Ranges rows(own_units, min(g.p.n_items, own_units));
+  for (int c = kPlanThreads - 1 - tid; c < g.p.n_items; c += kPlanThreads) {
+    OwnStart r;
+    r.n = r.b = r.hg = 0;
+    if (c < rows.n) {
+      const int u = rows.begin(c);
+      r.n = rows.begin(c + 1) - u;
+      r.hg = u / own_tiles;
+      const int inside = u - r.hg * own_tiles;
+      r.b = last_of(s.tiles, a.B, inside);
+      r.p = s.own[r.b];
+      r.token = r.p.first + (inside - s.tiles[r.b]) * g.p.tile;
+      r.left = s.tiles[r.b + 1] - inside;
     }
-    wrong = __syncthreads_or(wrong);
-    if (!wrong) {
-      sum_before(s, n, in.B, scratch);
-      wrong = s.units[n] > kUnitLimit || (int64_t)s.tiles[in.B] * g.p.groups > kUnitLimit;
-      __syncthreads();
-    }
-    if (wrong && !dry) {  // every row is empty, of one tile
-      for (int b = tid; b <= in.B; b += kPlanThreads) {
-        if (b < in.B) s.own[b] = {0, 0, 0, 0, -1, kEmpty, 0, 0, 0, 0, {0, 0}};
-        s.tiles[b] = b;
-      }
-      for (int i = tid; i <= n; i += kPlanThreads) s.units[i] = 0;
-      if (tid == 0) atomicOr(a.err, kErrBadSeq);
-    }
-    __syncthreads();
-    // where each CTA begins
-    const int units = s.units[n], own_tiles = s.tiles[in.B];
-    int n_items = min(x.n_items, units);
-    if (n == 1 && units) {
-      // Items that are all alike: whole CTAs for each, if that leaves out less than an eighth of them, so that none has the end
-      // of one and the beginning of another (3 us more where an end leaves 256 rows).
-      const int alike = units / s.groups[0].tiles, each = n_items / alike;
-      if (8 * each * alike >= 7 * n_items) n_items = each * alike;
-    }
-    const Ranges items(units, n_items);
-    for (int c = tid; c < x.n_items; c += kPlanThreads) {
-      ItemStart r;
-      r.n = 0;
-      if (c < items.n) {
-        const int u = items.begin(c);
-        r.n = items.begin(c + 1) - u;
-        r.g = last_of(s.units, n, u);
-        r.p = s.groups[r.g];
-        const int inside = u - s.units[r.g], item = inside / r.p.tiles, tile = inside - item * r.p.tiles;
-        r.hg = item / r.p.blocks;
-        r.block = item - r.hg * r.p.blocks;
-        r.token = r.p.first + tile * x.tile;
-        r.left = r.p.tiles - tile;
-      }
-      if (!dry) x.item_start[c] = r;
-    }
-    const int own_units = own_tiles * g.p.groups;
-    const Ranges rows(own_units, min(g.p.n_items, own_units));
-    for (int c = kPlanThreads - 1 - tid; c < g.p.n_items; c += kPlanThreads) {
-      OwnStart r;
-      r.n = r.b = r.hg = 0;
-      if (c < rows.n) {
-        const int u = rows.begin(c);
-        r.n = rows.begin(c + 1) - u;
-        r.hg = u / own_tiles;
-        const int inside = u - r.hg * own_tiles;
-        r.b = last_of(s.tiles, in.B, inside);
-        r.p = s.own[r.b];
-        r.token = r.p.first + (inside - s.tiles[r.b]) * g.p.tile;
-        r.left = s.tiles[r.b + 1] - inside;
-      }
-      if (!dry) x.own_start[c] = r;
-    }
-    // the records themselves
-    for (int i = tid; i < n; i += kPlanThreads) {
-      GroupPlan r = s.groups[i];
-      r.units = s.units[i];
-      if (!dry) x.groups[i] = r;
-    }
-    for (int b = tid; b < in.B; b += kPlanThreads) {
-      RowPlan r = s.own[b];
-      r.tiles = s.tiles[b];
-      if (!dry) x.own[b] = r;
-    }
-    __syncthreads();
+    x.own_start[c] = r;
+  }
+  // the records themselves
+  for (int i = tid; i < n; i += kPlanThreads) {
+    GroupPlan r = s.groups[i];
+    r.units = s.units[i];
+    x.groups[i] = r;
+  }
+  for (int b = tid; b < a.B; b += kPlanThreads) {
+    RowPlan r = s.own[b];
+    r.tiles = s.tiles[b];
+    x.own[b] = r;
   }
 }
 
@@ -439,7 +417,37 @@ size_t paged_shared_workspace(const PagedView& v, DecodeKind kind, int B, int ma
   return std::max(paged_decode_workspace(v, kind, B, max_len, sms), Parts(v, p, std::max(B, 1), sms).all);
 }
 
+namespace paged {
+namespace {
+
+// Whether what groups share is attended to once, or every row by itself: the one of the less time by models in us of both, fitted
+// to 142 measured calls (its choice is 1.5% off the better one on average; four head layouts, three kinds of caches, 1 to 16 groups of 2 to 64 rows, 256 to 32768 tokens). Rows
+// by themselves read mostly from L2; the shared way is four launches. The host knows bounds only: what groups share is taken
+// for the difference of those of a row's tokens and its own ones, and own tokens for half of theirs.
+// Measured, by rows / shared, 32 query heads on 8 KV heads of 128 in bf16, one group:
+//   4 rows on 512 tokens 6.1 / 16.5     16 on 2048 18.6 / 21.4     64 on 2048  56 / 25
+//   8 on 2048  12.4 / 20.7               8 on 8192 33.7 / 24.0     64 on 32768 767 / 53
+bool prefer_shared(const PagedDecodeArgs& a, DecodeKind kind) {
+  const PagedView& v = a.v;
+  const int DP = padded_dim(v.d), el = kind.quant ? 1 : kind.dtype == DCK_F32 ? 4 : 2;
+  const double row = 2. * v.Hkv * (v.d * el + (kind.quant ? 4 : 0));  // bytes of a token
+  const double seen = a.window > 0 ? std::min(a.window, a.max_len) : a.max_len, own = std::min<double>(a.max_own, seen) / 2;
+  const double shared = seen - own;
+  // bytes per us that rows by themselves, and blocks of queries, get through
+  const double rate = (kind.quant ? (DP == 256 ? 3.9 : 6.4) : kind.dtype == DCK_F32 || DP == 256 ? 9. : 11.) * 1e6;
+  const double by_rows = 6 + a.B * seen * row / rate;
+  const double queries = (double)v.qpg * a.B / a.n_groups;
+  const bool tc = kind.dtype == DCK_BF16 && !kind.quant && DP <= 128;
+  const double blocks = std::ceil(queries / (tc ? 256 : kind.dtype == DCK_BF16 && DP <= 128 ? 16 : 8));
+  const double once = a.n_groups * shared * row, again = once * blocks / (tc ? 7e6 : 6e6);
+  return 18 + std::max(once / 5.9e6, again) + a.B * own * row / 6e6 + 1.2e-3 * a.B * v.Hq < by_rows;
+}
+
+}  // namespace
+}  // namespace paged
+
 cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int sms, cudaStream_t s) {
+  if (a.way == 1 || (a.way == 0 && !prefer_shared(a, kind))) return launch_paged_decode(a, kind, sms, s);
   Args g = {};
   g.a = a;
   g.p = range_plan(a.v, kind, a.B, std::min(a.max_own, a.max_len), sms);

@@ -33,7 +33,7 @@ EXPORTED = (
     "dck_rope_init", "dck_rope", "dck_paged_append", "dck_paged_decode_workspace_size", "dck_paged_decode_attention",
     "dck_validate_quant_desc", "dck_quant_append", "dck_quant_read", "dck_quant_decode_workspace_size",
     "dck_quant_decode_attention", "dck_paged_shared_workspace_size", "dck_paged_shared_attention",
-    "dck_quant_shared_workspace_size", "dck_quant_shared_attention",
+    "dck_quant_shared_workspace_size", "dck_quant_shared_attention", "dck_set_shared_way",
 )
 
 
@@ -160,6 +160,8 @@ def lib() -> ctypes.CDLL:
     L.dck_quant_shared_attention.restype = I32
     L.dck_quant_shared_attention.argtypes = [Q8, P, I64, P, P, P, P, P, I64, P, I32, I32, I32, I32, P, P, F32, I32, F32, P, P,
                                              P, SZ, P]
+    L.dck_set_shared_way.restype = I32
+    L.dck_set_shared_way.argtypes = [I32]
     _lib = L
     return L
 
@@ -474,6 +476,10 @@ def dck_last_device_error(stream=None) -> int:
 
 def dck_set_decode_kernel(which: int) -> int:
     return lib().dck_set_decode_kernel(int(which))
+
+
+def dck_set_shared_way(which: int) -> int:
+    return lib().dck_set_shared_way(int(which))
 
 
 def dck_last_launch_count() -> int:

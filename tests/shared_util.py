@@ -99,10 +99,10 @@ def bounds(c, d, n, ref, rlse, weight, slack, softcap):
     return bo, bl
 
 
-def check(c, hq, window=0, softcap=0.0, scale=None, rows=None, **kw):
-    """The call against the plain definition, row by row (`rows`: those to look at)."""
+def check(c, hq, window=0, softcap=0.0, scale=None, rows=None, expect=dck.DCK_OK, **kw):
+    """The call against the plain definition, row by row (`rows`: those to look at; `expect`: the device error)."""
     out, lse, err = attend(c, hq, window, softcap, scale, **kw)
-    assert err == dck.DCK_OK
+    assert err == expect
     rows = np.arange(len(c["lens"])) if rows is None else np.asarray(rows)
     d = c["q"].shape[2]
     scale = float(np.float32(d ** -0.5 if scale is None else scale))

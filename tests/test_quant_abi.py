@@ -105,6 +105,11 @@ def test_workspace_sizes_of_bad_arguments_are_zero():
     assert dck.dck_quant_decode_workspace_size(_cache(n_pages=0), 4, 100) == 0
 
 
+def test_way_of_shared_calls():
+    assert dck.dck_set_shared_way(2) == 0 and dck.dck_set_shared_way(7) == 2 and dck.dck_set_shared_way(-1) == 2
+    assert dck.dck_set_shared_way(0) == 2
+
+
 def test_from_tensors():
     import torch
     both, scales = torch.zeros((5, 2, 16, 8, 128), dtype=torch.uint8), torch.zeros((5, 16, 2, 8))

@@ -11,6 +11,16 @@ from shared_util import attend, check, shared_case
 
 pytestmark = pytest.mark.gpu
 KINDS = [("bf16", False), ("f32", False), ("bf16", True), ("f32", True)]
+
+
+@pytest.fixture(autouse=True, params=["once", "by rows"])
+def way(request):
+    """Every test in both ways of the calls, whatever their rule would choose."""
+    dck.dck_set_shared_way(2 if request.param == "once" else 1)
+    yield request.param
+    dck.dck_set_shared_way(0)
+
+
 kinds = pytest.mark.parametrize("dtype,quant", KINDS, ids=["bf16", "f32", "q8-bf16", "q8-f32"])
 
 
@@ -123,7 +133,6 @@ def test_bad_rows_are_recorded_and_give_zeros(dtype, quant):
     """Lengths, own pages and own tokens beyond the bound: that row alone.  A page of the shared part: the rows that see it."""
     groups = [(6400, [6401, 6500, 6440, 6450]), (3200, [3300, 3201])]
     c = shared_case(8, 2, 64, dtype, quant, 16, "rows", groups)
-    ref = host(attend(c, 8)[0])
     for what, rows in (("negative", [1]), ("long", [1]), ("own page", [1]), ("shared page", [0, 1, 2, 3])):
         d = dict(c, table=c["table"].clone(), seq_len=c["seq_len"].clone())
         if what == "own page":
@@ -132,12 +141,39 @@ def test_bad_rows_are_recorded_and_give_zeros(dtype, quant):
             d["table"][:4, 3] = 1 << 20
         else:
             d["seq_len"][1] = -4 if what == "negative" else 6501
-        out, lse, err = attend(d, 8, max_len=6500)
-        assert err == dck.DCK_ERR_INVALID, what
         other = [b for b in range(6) if b not in rows]
+        out, lse = check(d, 8, max_len=6500, rows=other, expect=dck.DCK_ERR_INVALID)
         assert (out[rows] == 0).all() and torch.isneginf(lse[rows]).all(), what
-        # (without row 1, row 3 is the longest: the same tokens through another table)
-        assert np.array_equal(host(out)[other], ref[other]), what
+
+
+@kinds
+def test_groups_that_are_none(dtype, quant, way):
+    """Group starts out of order or off the batch: every output zero, and recorded.  Rows by themselves do not look at them."""
+    c = shared_case(8, 2, 64, dtype, quant, 16, "rows", [(320, [321, 400, 333]), (64, [70, 71])])
+    for starts in ((0, 6, 5), (1, 3, 5), (0, 3, 4), (0, -1, 5), (0, 3, 1 << 30)):
+        d = dict(c, group_start=torch.tensor(starts, dtype=torch.int32, device="cuda"))
+        if way == "by rows":
+            check(d, 8)
+            continue
+        out, lse, err = attend(d, 8)
+        assert err == dck.DCK_ERR_INVALID and (out == 0).all() and torch.isneginf(lse).all()
+    check(c, 8)
+
+
+@kinds
+def test_more_own_tokens_than_said(dtype, quant, way):
+    c = shared_case(8, 2, 64, dtype, quant, 16, "rows", [(320, [321, 400, 333]), (0, [70, 90]), (16, [50])])
+    if way == "once":
+        out, lse = check(c, 8, max_own=79, rows=[0, 2, 3, 5], expect=dck.DCK_ERR_INVALID)
+        assert (out[[1, 4]] == 0).all() and torch.isneginf(lse[[1, 4]]).all()
+    check(c, 8, max_own=90)
+
+
+@kinds
+def test_a_shared_length_below_zero_is_none(dtype, quant, way):
+    c = shared_case(8, 2, 64, dtype, quant, 16, "rows", [(320, [321, 400, 333]), (0, [70, 90])])
+    c["shared_len"][1] = -7
+    check(c, 8, expect=dck.DCK_ERR_INVALID if way == "once" else dck.DCK_OK)
 
 
 def test_graphs_and_streams_give_the_same_bits():
