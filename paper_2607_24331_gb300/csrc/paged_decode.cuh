@@ -70,13 +70,13 @@ struct ScoreScale {
 };
 
 // Calls over shared prefixes (paged_shared.cu): what the rows of group g see together, tokens [first, end), is attended
-// to for all of them at once, in items of a block of their queries and a head group, each cut into tiles; the items'
+// to for all of them at once, in items of a block of their queries on a KV head, each cut into tiles; the items'
 // tiles form one list, dealt to CTAs in equal ranges.
 struct alignas(16) GroupPlan {
   int start, rows;   // its rows
   int first, end;    // the tokens; none: end = first
   int table;         // the row whose block table they are read by
-  int tiles, blocks; // of an item; items per head group
+  int tiles, blocks; // of an item; items per KV head
   int units;         // tiles of all groups before
   int bad;           // a page outside the pool
   int pad[3];
@@ -95,7 +95,7 @@ constexpr int kEmpty = 1;
 // of that, and how many it has in all.
 struct alignas(16) ItemStart {
   GroupPlan p;
-  int g, hg, block, token, left, n, pad[2];
+  int g, head, block, token, left, n, pad[2];
 };
 struct alignas(16) OwnStart {
   RowPlan p;
@@ -121,20 +121,19 @@ struct Prefix {
   float *part_u, *part_ml;  // partial sums, as in Args, of what groups share: rows by row_of
   float *own_u, *own_ml;    // and of rows' own tokens: rows by own_row
   int n_groups, n_items;  // groups; CTAs that tiles are dealt to
-  int rows, wh, tile;     // queries of a block, heads of a head group, tokens of a tile
+  int rows, tile;         // queries of a block, tokens of a tile
   Divider by_qpg, by_rows;
 
   __device__ __forceinline__ int64_t own_row(const Plan& p, int B, int group, int b, int c, int w) const;
   // A number below B Hq of an item: every block has a query.
-  __device__ __forceinline__ int64_t item_id(int start, int blocks, int Hq, int hg, int block) const {
-    return (int64_t)start * Hq + (int64_t)hg * blocks + block;
+  __device__ __forceinline__ int64_t item_id(int start, int blocks, int Hq, int head, int block) const {
+    return (int64_t)start * Hq + (int64_t)head * blocks + block;
   }
-  // Where query `r` of the block `block` of head `w` of head group `hg` has the partial sum that CTA c leaves: items
-  // in order, CTAs that share one behind one another.  The next item of a CTA or the next CTA of an item is further on
-  // by all the rows that one of them can fill.  The group: rows from `start` on, `queries` on a KV head.
-  __device__ __forceinline__ int64_t row_of(int start, int queries, int Hq, int qpg, int hg, int block, int c, int w, int r) const {
-    const int here = min(rows, queries - block * rows);
-    return (int64_t)start * Hq + (int64_t)wh * ((int64_t)hg * queries + block * rows + (int64_t)c * rows) + w * here + r;
+  // Where query `r` of the block `block` of KV head `head` has the partial sum that CTA c leaves: items in order, CTAs that
+  // share one behind one another.  The next item of a CTA or the next CTA of an item is further on by all the rows
+  // that one of them can fill.  The group: rows from `start` on, `queries` on a KV head.
+  __device__ __forceinline__ int64_t row_of(int start, int queries, int Hq, int head, int block, int c, int r) const {
+    return (int64_t)start * Hq + (int64_t)head * queries + (int64_t)block * rows + (int64_t)c * rows + r;
   }
 };
 
@@ -171,6 +170,8 @@ inline int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // Warps of a CTA: two CTAs per SM fill its shared memory with rings, or one of twice the warps.
 constexpr int warps_of(int DP, bool one_per_sm) { return (DP == 256 ? 2 : 4) * (one_per_sm ? 2 : 1); }
 constexpr int kPerSm = 2;
+// (paged_shared.cuh) CTAs per SM of what groups share: three where 8-bit rows meet 16 queries.
+inline int prefix_per_sm(DecodeKind kind, int rows) { return kind.quant && rows > 8 ? 3 : kPerSm; }
 inline int run_of(DecodeKind k) { return k.quant ? 32 : k.dtype == DCK_BF16 ? 16 : 8; }  // tokens of a warp's step
 
 // Visible tokens of a sequence of length L and the first of them; 0 for invalid lengths.
@@ -399,30 +400,6 @@ struct LoaderBase {
                            have ? 16 : 0);
     }
   }
-  // The same of `count` queries from query q0 of a group's on, for KV head h.
-  __device__ __forceinline__ const char* query_of(const GroupPlan& p, int h, int q0, int row) const {
-    const int x = q0 + row, b = g.x.by_qpg.div(x), j = h * g.a.v.qpg + x - b * g.a.v.qpg;
-    return static_cast<const char*>(g.a.q) + ((int64_t)(p.start + b) * g.a.q_stride + (int64_t)j * g.a.v.d) * el;
-  }
-  __device__ __forceinline__ void copy_block(const GroupPlan& p, int h, int q0, int count, int at) const {
-    const uint32_t to = places + at * kPlace;
-    for (int x = lane; x < ROWS * kQChunks; x += 32) {
-      const int row = x / kQChunks, c = x % kQChunks;
-      const bool have = row < count && c * 16 < g.a.v.d * el;
-      cp_async16_or_zero(to + row * Z::kQRow + (c ^ (row & 7)) * 16, have ? query_of(p, h, q0, row) + c * 16 : g.a.q, have ? 16 : 0);
-    }
-  }
-  __device__ __forceinline__ void read_block(const GroupPlan& p, int h, int q0, int count, uint8_t* q_all, int warp, int at) const {
-    using T = typename Z::T;
-    T* to = reinterpret_cast<T*>(q_all + (warp * QS + at) * kPlace);
-    constexpr int per = 16 / el;
-    for (int x = lane; x < ROWS * Z::DP; x += 32) {
-      const int row = x / Z::DP, e = x % Z::DP;
-      to[row * Z::DP + ((e / per) ^ (row & 7)) * per + e % per] =
-          row < count && e < g.a.v.d ? reinterpret_cast<const T*>(query_of(p, h, q0, row))[e] : from_f32<T>(0.f);
-    }
-    __syncwarp();
-  }
   // The same by single elements, for queries off 16-byte boundaries.
   __device__ __forceinline__ void read_queries(const Queries& qs, int b, uint8_t* q_all, int warp, int at) const {
     using T = typename Z::T;
@@ -558,7 +535,8 @@ __device__ __forceinline__ void split_weights(float p0, float p1, uint32_t& hi, 
 template <class Z, bool PACK>
 struct TensorTile {
   static constexpr int kQ = PACK ? 1 : 2;  // query rows per lane
-  static constexpr int kRows = PACK ? 8 : 16;
+  static constexpr int kRows = PACK ? 8 : 16, kOperands = 16;
+  static __device__ __forceinline__ void lay_out(const uint8_t*, uint8_t*) {}
   float o[Z::DP / 8][4], m[kQ], l[kQ];
   uint32_t q[Z::DP / 16][2 * kQ];
 
@@ -714,7 +692,8 @@ struct TensorTile {
 // a token (no exchanges, but eight times the loads), 128.
 template <class Z, int ROWS>
 struct SimtTile {
-  static constexpr int kRows = ROWS;
+  static constexpr int kRows = ROWS, kOperands = 16;
+  static __device__ __forceinline__ void lay_out(const uint8_t*, uint8_t*) {}
   static constexpr int kOwn = Z::kChunks >= 32 ? Z::kChunks / 32 : 1;  // chunks per lane
   static constexpr int kSplit = Z::kChunks >= 32 ? 1 : 32 / Z::kChunks;  // lanes that share a chunk, by tokens
   static constexpr int kVals = ROWS > 4 ? ROWS / 4 : 1;                  // scores per lane

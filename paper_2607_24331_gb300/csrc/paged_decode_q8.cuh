@@ -148,15 +148,57 @@ __device__ __forceinline__ float2 shared8(uint32_t at) {
 // The order of a row's elements is free in <q, c>: lane l takes the 16 bytes of a key's chunk l % 4 (+ 4 j) in one
 // read, which are the operands of four k-steps.  Values go through ldmatrix.trans in pairs of codes, two elements
 // of two tokens in each word; of the two elements one goes to each of two MMAs.
-template <class Z, bool PACK>
+//
+// LAID_OUT: the queries stay in shared memory, as each lane's operands of each k-step in 16 bytes, and all warps of the CTA
+// read them from there: 32 registers fewer, so that three CTAs fit on an SM (16 bf16 queries of one KV head; a step is a chain
+// of short instructions, of which eight warps leave an SM's schedulers idle half of the time).
+template <class Z, bool PACK, bool LAID_OUT = false>
 struct QuantTile {
   static constexpr int kQ = PACK ? 1 : 2;  // query rows per lane
   static constexpr int kRows = PACK ? 8 : 16;
+  static constexpr int kStepBytes = 512, kUnits = Z::DP / 16 * kStepBytes;  // of a k-step's operands; where the rows' units begin
+  static constexpr int kOperands = LAID_OUT ? kUnits + kRows * 4 : 16;
+  static_assert(!LAID_OUT || !PACK, "16 queries");
   static constexpr bool kLow = std::is_same<typename Z::T, float>::value;  // queries of two terms
   static_assert(PACK || !kLow, "fp32 queries: low terms in rows 8-15");
   static constexpr int kTerms = PACK && !kLow ? 2 : 4;  // registers of a k-step's queries
   float o[Z::DP / 8][4], m[kQ], l[kQ], near[kQ], unit[kQ];  // near: reference of the weights, unit: of the queries
-  uint32_t q[Z::DP / 16][kTerms];
+  uint32_t q[LAID_OUT ? 1 : Z::DP / 16][kTerms], operands;
+
+  // The exponent e that brings a row of largest magnitude `top` (bits) to [2^14, 2^15) times 2^-e, where that is 2^-96 or more.
+  static __device__ __forceinline__ int exponent_of(uint32_t top) { return max((int)(top >> 23) - 127 - 14, -110); }
+  static __device__ __forceinline__ uint32_t finite_bits(float x) {
+    const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+    return u < 0x7f800000u ? u : 0u;
+  }
+  // LAID_OUT: rows at `place` to operands at `to`, by the whole CTA.  A thread has a row's chunk of 16 elements, four k-steps of
+  // lane 4 (row % 8) + chunk % 4.
+  static __device__ __forceinline__ void lay_out(const uint8_t* place, uint8_t* to) {
+    if constexpr (LAID_OUT) {
+      constexpr int kChunks = Z::DP / 16;
+      if (threadIdx.x >= kRows * kChunks) return;
+      const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
+      float x[16];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int e = chunk * 16 + i;
+        x[i] = to_f32(*reinterpret_cast<const typename Z::T*>(place + row * Z::kQRow + ((e / 8) ^ (row & 7)) * 16 + e % 8 * 2));
+        top = max(top, finite_bits(x[i]));
+      }
+#pragma unroll
+      for (int o = 1; o < kChunks; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
+      const int e = exponent_of(top);
+      const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+      if (chunk == 0) *reinterpret_cast<float*>(to + kUnits + row * 4) = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uint32_t* at = reinterpret_cast<uint32_t*>(to + (chunk / 4 * 4 + t) * kStepBytes + ((row & 7) * 4 + chunk % 4) * 16) + row / 8;
+        at[0] = half_pair(x[4 * t] * down, x[4 * t + 1] * down);
+        at[2] = half_pair(x[4 * t + 2] * down, x[4 * t + 3] * down);
+      }
+    }
+  }
 
   static __device__ __forceinline__ float query(uint32_t place, int row, int e) {  // element e of a row
     const uint32_t at = place + row * Z::kQRow;
@@ -170,23 +212,37 @@ struct QuantTile {
     return __uint_as_float((uint32_t)x << 16);
   }
 
-  __device__ __forceinline__ void begin(uint32_t place, int lane) {
-    const int c = lane & 3;
+  __device__ __forceinline__ void clear_sums() {
 #pragma unroll
     for (int x = 0; x < kQ; ++x) {
+      m[x] = near[x] = -CUDART_INF_F;
+      l[x] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < Z::DP / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+  }
+  __device__ __forceinline__ void begin(uint32_t place, int lane) {
+    const int c = lane & 3;
+    clear_sums();
+    if constexpr (LAID_OUT) {
+      operands = place + lane * 16;
+#pragma unroll
+      for (int x = 0; x < kQ; ++x) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(unit[x]) : "r"(place + kUnits + (lane / 4 + 8 * x) * 4));
+      return;
+    }
+#pragma unroll
+    for (int x = 0; x < (LAID_OUT ? 0 : kQ); ++x) {
       const int row = lane / 4 + 8 * x;
       uint32_t top = 0;
 #pragma unroll
       for (int k = 0; k < Z::DP / 16; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t u = __float_as_uint(query(place, row, 16 * (c + 4 * (k / 4)) + 4 * (k % 4) + i)) & 0x7fffffffu;
-          top = max(top, u < 0x7f800000u ? u : 0u);
+          top = max(top, finite_bits(query(place, row, 16 * (c + 4 * (k / 4)) + 4 * (k % 4) + i)));
         }
       top = max(top, __shfl_xor_sync(~0u, top, 1));
       top = max(top, __shfl_xor_sync(~0u, top, 2));
-      // largest magnitude in [2^14, 2^15), where it is 2^-96 or more
-      const int e = max((int)(top >> 23) - 127 - 14, -110);
+      const int e = exponent_of(top);
       const float down = __uint_as_float((uint32_t)(127 - e) << 23);
       unit[x] = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
@@ -205,11 +261,7 @@ struct QuantTile {
           q[k][(2 + x) % kTerms] = half_pair(y[2], y[3]);
         }
       }
-      m[x] = near[x] = -CUDART_INF_F;
-      l[x] = 0.f;
     }
-#pragma unroll
-    for (int n = 0; n < Z::DP / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
   }
 
   // The 32 tokens of a stage, the first `live` of them present (0 or fewer: none).
@@ -231,7 +283,14 @@ struct QuantTile {
           for (int t = 0; t < 4; ++t) {
             uint32_t b0, b1;
             open_codes(w[t], b0, b1);
-            const uint32_t(&y)[kTerms] = q[4 * j + t];
+            uint32_t y[kTerms];
+            if constexpr (LAID_OUT) {
+              const uint4 f = shared16(operands + (4 * j + t) * kStepBytes);
+              y[0] = f.x, y[1] = f.y, y[2 % kTerms] = f.z, y[3 % kTerms] = f.w;
+            } else {
+#pragma unroll
+              for (int i = 0; i < kTerms; ++i) y[i] = q[LAID_OUT ? 0 : 4 * j + t][i];
+            }
             if (PACK && !kLow) mma16816_f16(s[n], y[0], 0u, y[1], 0u, b0, b1);
             else mma16816_f16(s[n], y[0], y[1], y[2 % kTerms], y[3 % kTerms], b0, b1);
           }

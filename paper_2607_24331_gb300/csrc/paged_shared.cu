@@ -110,7 +110,7 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, in
   p.blocks = (int)blocks;
   p.bad = 0;
   s.groups[at] = p;
-  s.units[at] = (int)min((int64_t)p.tiles * blocks * (a.v.Hkv / x.wh), (int64_t)kUnitLimit + 1);
+  s.units[at] = (int)min((int64_t)p.tiles * blocks * a.v.Hkv, (int64_t)kUnitLimit + 1);
   return wrong;
 }
 
@@ -224,8 +224,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       r.g = last_of(s.units, n, u);
       r.p = s.groups[r.g];
       const int inside = u - s.units[r.g], item = inside / r.p.tiles, tile = inside - item * r.p.tiles;
-      r.hg = item / r.p.blocks;
-      r.block = item - r.hg * r.p.blocks;
+      r.head = item / r.p.blocks;
+      r.block = item - r.head * r.p.blocks;
       r.token = r.p.first + tile * x.tile;
       r.left = r.p.tiles - tile;
     }
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   const RowPlan own = load_record(x.own + b);
   const int h = x.by_qpg.div(j), q = j - h * qpg, chunk = by_rows.div(q), r = q - chunk * g.p.rows, vh = h * g.p.chunks + chunk;
   const int group = vh >> heads_log2, w = vh & (g.p.wh - 1);
-  const int row = (b - own.start) * qpg + q, block = x.by_rows.div(row), hg = h / x.wh;
+  const int row = (b - own.start) * qpg + q, block = x.by_rows.div(row);
   const bool shares = own.group >= 0;
   pdl_wait();
   bool bad = own.state == kEmpty;
@@ -287,14 +287,14 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   const CtaRange mine = x.own_ctas[(int64_t)group * a.B + b];
   CtaRange theirs = {0, -1};
   if (shares) {
-    theirs = x.item_ctas[x.item_id(own.start, own.blocks, a.v.Hq, hg, block)];
+    theirs = x.item_ctas[x.item_id(own.start, own.blocks, a.v.Hq, h, block)];
     // (numbers that are none: a CTA gave up waiting)
     bad |= x.groups[own.group].bad != 0 || theirs.first < 0 || theirs.first > theirs.last || theirs.last >= x.n_items;
   }
   const int n_own = own.end > own.first ? mine.last - mine.first + 1 : 0, n = bad ? 0 : n_own + theirs.last - theirs.first + 1;
   const int64_t own0 = x.own_row(g.p, a.B, group, b, mine.first, w) + r, own_step = (int64_t)g.p.wh * g.p.rows;
-  const int64_t part0 = x.row_of(own.start, own.rows * qpg, a.v.Hq, qpg, hg, block, theirs.first, h - hg * x.wh, row - block * x.rows);
-  const int64_t part_step = (int64_t)x.wh * x.rows;
+  const int64_t part0 = x.row_of(own.start, own.rows * qpg, a.v.Hq, h, block, theirs.first, row - block * x.rows);
+  const int64_t part_step = x.rows;
   const auto sums_of = [&](int i) {
     return i < n_own ? x.own_u + (own0 + i * own_step) * g.DP : x.part_u + (part0 + (i - n_own) * part_step) * g.DP;
   };
@@ -360,25 +360,22 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
 // How the shared part of a call is laid out.
 struct Layout {
   bool tc;  // on tcgen05
-  int rows, wh, tile, n_items;
+  int rows, tile, n_items;
 };
 Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int sms) {
   Layout l;
-  const int DP = padded_dim(v.d), warps = warps_of(DP, false);
+  const int DP = padded_dim(v.d);
   const int64_t queries = (int64_t)v.qpg * B / std::max(n_groups, 1);  // of a group, on average
   l.tc = kind.dtype == DCK_BF16 && !kind.quant && DP <= 128 && queries > 16;
   if (l.tc) {
     l.rows = 256;
     l.tile = 64;
-    l.wh = 1;
     l.n_items = std::max(1, sms - 1);  // the plan's block has the last SM while they get ready
     return l;
   }
   l.rows = kind.dtype == DCK_BF16 && DP <= 128 && queries > 8 ? 16 : 8;
-  l.wh = warps;
-  while (v.Hkv % l.wh) l.wh /= 2;
-  l.tile = warps / l.wh * run_of(kind);
-  l.n_items = std::min(kPerSm * sms, kMaxItems);
+  l.tile = warps_of(DP, false) * run_of(kind);
+  l.n_items = std::min(prefix_per_sm(kind, l.rows) * sms, kMaxItems);
   return l;
 }
 
@@ -386,7 +383,7 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
 struct Parts {
   size_t groups, own, item_start, own_start, item_ctas, own_ctas, part_ml, part_u, own_ml, own_u, all = 0;
   Parts(const PagedView& v, const Plan& p, int B, int sms) {
-    // (a CTA leaves 256 rows of an item, or each of two on an SM 16 for up to four heads)
+    // (a CTA leaves 256 rows of an item, or each of three on an SM 16)
     const size_t rows = (size_t)B * v.Hq + (size_t)sms * 256, DP = padded_dim(v.d);
     const size_t own_rows = ((size_t)p.groups * B + p.n_items) * p.wh * p.rows;
     const auto take = [&](size_t bytes) {
@@ -471,7 +468,6 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   g.x.n_groups = a.n_groups;
   g.x.n_items = l.n_items;
   g.x.rows = l.rows;
-  g.x.wh = l.wh;
   g.x.tile = l.tile;
   g.x.by_qpg = divider((uint32_t)a.v.qpg);
   g.x.by_rows = divider((uint32_t)l.rows);
@@ -483,7 +479,7 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   Args h = g;
   h.p.chunks = 1;
   h.p.by_chunks = divider(1);
-  h.p.wh = l.wh;
+  h.p.wh = 1;
   if (e == cudaSuccess)
     e = l.tc ? launch_prefix_tc(h, s) : kind.quant ? launch_prefix_q8(h, kind.dtype, s) : kind.dtype == DCK_F32 ? launch_prefix_f32(h, s) : launch_prefix_bf16(h, s);
   if (e == cudaSuccess)

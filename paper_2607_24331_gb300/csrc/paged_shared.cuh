@@ -1,5 +1,5 @@
 // Calls over shared prefixes: what the rows of a group see together, by per-warp rings as in
-// paged_decode.cuh (a tile of up to 16 or 8 queries per warp, of any rows of the group).
+// paged_decode.cuh (a tile of up to 16 or 8 queries, of any rows of the group).
 #pragma once
 
 #include "paged_decode.cuh"
@@ -10,7 +10,7 @@ namespace paged {
 // A position in the list of the items' tiles.
 struct ItemWalk {
   GroupPlan p;
-  int g, hg, block;
+  int g, head, block;
   int token, left;  // the tile's first token, and the tiles from it to the end of the item
 
   __device__ __forceinline__ void see(const Prefix& x, int at) {
@@ -21,15 +21,15 @@ struct ItemWalk {
   __device__ __forceinline__ int enter(const Prefix& x, int c) {
     const ItemStart s = load_record(x.item_start + c);
     p = s.p;
-    g = s.g, hg = s.hg, block = s.block, token = s.token, left = s.left;
+    g = s.g, head = s.head, block = s.block, token = s.token, left = s.left;
     return s.n;
   }
   // The next item.
-  __device__ __forceinline__ void leave(const Prefix& x, int head_groups) {
+  __device__ __forceinline__ void leave(const Prefix& x, int heads) {
     if (++block == p.blocks) {
       block = 0;
-      if (++hg == head_groups) {
-        hg = 0;
+      if (++head == heads) {
+        head = 0;
         do see(x, g + 1);
         while (p.tiles == 0);
       }
@@ -42,13 +42,13 @@ struct ItemWalk {
   __device__ __forceinline__ bool begins() const { return token == p.first; }
   // Notes that this CTA has a part of the item, its first or last.
   __device__ __forceinline__ void sign(const Prefix& x, int Hq, bool begun, bool ended) const {
-    CtaRange* r = x.item_ctas + x.item_id(p.start, p.blocks, Hq, hg, block);
+    CtaRange* r = x.item_ctas + x.item_id(p.start, p.blocks, Hq, head, block);
     if (begun) r->first = blockIdx.x;
     if (ended) r->last = blockIdx.x;
   }
-  // Where this CTA's sums of query r of head w go.
-  __device__ __forceinline__ int64_t row_of(const Prefix& x, int Hq, int qpg, int w, int r) const {
-    return x.row_of(p.start, p.rows * qpg, Hq, qpg, hg, block, blockIdx.x, w, r);
+  // Where this CTA's sums of its query r go.
+  __device__ __forceinline__ int64_t row_of(const Prefix& x, int Hq, int qpg, int r) const {
+    return x.row_of(p.start, p.rows * qpg, Hq, head, block, blockIdx.x, r);
   }
 };
 
@@ -100,63 +100,81 @@ __device__ __forceinline__ void leave_sums(uint8_t* raw, Shm& sh, const Tile& ti
 }
 
 template <class Z, class Tile>
-__global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid_constant__ Args g) {
+struct PrefixShared {  // after the rings
+  alignas(16) uint8_t q[Tile::kRows * Z::kQRow];  // the item's queries
+  alignas(16) uint8_t operands[Tile::kOperands];   // the same as a tile reads them from here, if it does
+  alignas(16) float mine[std::is_same<typename Z::T, float>::value && !Z::kQuant ? Z::NW * 8 * Tile::kRows : 4];  // fp32: a warp's weights
+  alignas(16) float2 ml[Z::NW][Tile::kRows];
+};
+
+// The item's queries to `to` (rows past them, and rows' ends, as zeros), by the whole CTA.
+template <class Z, int ROWS>
+__device__ __forceinline__ void read_item_queries(const Args& g, const ItemWalk& at, int count, uint8_t* to) {
+  using T = typename Z::T;
+  constexpr int el = sizeof(T), per = 16 / el, kChunks = Z::kQRow / 16;
+  const int qpg = g.a.v.qpg, d = g.a.v.d;
+  for (int i = threadIdx.x; i < ROWS * kChunks; i += Z::NW * 32) {
+    const int row = i / kChunks, c = i % kChunks, x = at.block * g.x.rows + row, b = g.x.by_qpg.div(x), j = at.head * qpg + x - b * qpg;
+    const T* from = static_cast<const T*>(g.a.q) + (int64_t)(at.p.start + b) * g.a.q_stride + (int64_t)j * d + c * per;
+    alignas(16) T v[per];
+    if (row < count && c * per < d) {
+      if (g.p.q_copied) {
+        *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(from);
+      } else {
+#pragma unroll
+        for (int k = 0; k < per; ++k) v[k] = from[k];
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < per; ++k) v[k] = from_f32<T>(0.f);
+    }
+    *reinterpret_cast<uint4*>(to + row * Z::kQRow + (c ^ (row & 7)) * 16) = *reinterpret_cast<const uint4*>(v);
+  }
+}
+
+// An item's tiles: its warps are runs of tokens, all with the same queries.  PER_SM: CTAs on an SM.
+template <class Z, class Tile, int PER_SM>
+__global__ void __launch_bounds__(Z::NW * 32, PER_SM) prefix_kernel(const __grid_constant__ Args g) {
   extern __shared__ __align__(128) uint8_t raw[];
-  using Shm = Shared<Z, Tile, false>;
+  using Shm = PrefixShared<Z, Tile>;
   Shm& sh = *reinterpret_cast<Shm*>(raw + Z::kRing);
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_heads = x.wh, n_runs = Z::NW / n_heads, wh = warp & (n_heads - 1), wt = warp / n_heads;
-  const int d = a.v.d, qpg = a.v.qpg, head_groups = a.v.Hkv / n_heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.v.d, qpg = a.v.qpg, heads = a.v.Hkv;
   pdl_wait();
   pdl_launch_dependents();  // the plan, and with it all that the own tokens' launch reads, is there
   ItemWalk ahead;
   int to_compute = ahead.enter(x, blockIdx.x);
   if (to_compute == 0) return;
-  const typename LoaderOf<Z, Tile::kRows, Shm::kPlaces>::type load(g, raw, sh.q, warp, lane, wh, wt);
+  const typename LoaderOf<Z, Tile::kRows, 1>::type load(g, raw, sh.q, warp, lane, 0, warp);
   load.clear(raw);
   ItemWalk at = ahead;
   int to_copy = to_compute, to_fetch = to_compute;
 
   // page numbers are read two tiles ahead of the copies
-  struct Next {
-    Pages pages;
-    GroupPlan p;
-    int block;  // of queries that come with the tile, or -1
-  };
-  Next next, next2;
-  bool first = true;
-  const auto fetch_next = [&](Next& n) {
+  Pages next = {0, -1, 0, -1}, next2 = {0, -1, 0, -1};
+  const auto fetch_next = [&]() {
     Walk w;
     w.token = ahead.token;
     w.len = ahead.p.end;
     w.b = ahead.p.table;
-    w.group = ahead.hg;
-    n.pages = load.fetch(w, false);
-    n.block = first ? ahead.block : -1;
-    if (first) n.p = ahead.p;
-    first = false;
+    w.group = ahead.head;
+    const Pages r = load.fetch(w, false);
     ahead.token += x.tile;
-    if (--to_fetch > 0 && --ahead.left == 0) {
-      ahead.leave(x, head_groups);
-      first = true;
-    }
+    if (--to_fetch > 0 && --ahead.left == 0) ahead.leave(x, heads);
+    return r;
   };
-  if (to_fetch > 0) fetch_next(next);
-  if (to_fetch > 0) fetch_next(next2);
+  if (to_fetch > 0) next = fetch_next();
+  if (to_fetch > 0) next2 = fetch_next();
   uint32_t outside = 0;
   int put = 0;
   const auto copy_next = [&]() {
     if (to_copy > 0) {
       --to_copy;
-      if (next.block >= 0 && g.p.q_copied)
-        load.copy_block(next.p, next.pages.group * n_heads + wh, next.block * x.rows,
-                        min(x.rows, next.p.rows * qpg - next.block * x.rows), put);
-      const bool bad = load.issue(next.pages, put);
+      const bool bad = load.issue(next, put);
       outside = (outside & ~(1u << put)) | (uint32_t)bad << put;
       next = next2;
-      if (to_fetch > 0) fetch_next(next2);
+      if (to_fetch > 0) next2 = fetch_next();
       put = put + 1 == Z::S ? 0 : put + 1;
     }
     cp_async_commit();
@@ -170,14 +188,21 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
   while (true) {
     __syncwarp();  // the stage that is filled next has been read
     copy_next();
-    cp_async_wait<Z::S - 1>();
-    __syncwarp();
-    if (fresh) {
+    if (fresh) {  // (the queries before are not in use any more: see leave_sums)
       count = at.count(x, qpg);
-      if (!g.p.q_copied) load.read_block(at.p, at.hg * n_heads + wh, at.block * x.rows, count, sh.q, warp, get);
-      tile.begin(load.places + get * load.kPlace, lane);
+      read_item_queries<Z, Tile::kRows>(g, at, count, sh.q);
+      __syncthreads();
+      if (Tile::kOperands > 16) {
+        Tile::lay_out(sh.q, sh.operands);
+        __syncthreads();
+        tile.begin((uint32_t)__cvta_generic_to_shared(sh.operands), lane);
+      } else {
+        tile.begin((uint32_t)__cvta_generic_to_shared(sh.q), lane);
+      }
       fresh = false;
     }
+    cp_async_wait<Z::S - 1>();
+    __syncwarp();
     bad |= outside >> get & 1;
     tile.step(load.ring + get * Z::kStage, at.p.end - at.token - load.run, lane, g.score, mine);
     const int used = get;
@@ -191,15 +216,14 @@ __global__ void __launch_bounds__(Z::NW * 32, kPerSm) prefix_kernel(const __grid
       atomicOr(&x.groups[at.g].bad, 1);
     }
     tile.finish();
-    leave_sums<Z>(raw, sh, tile, warp, lane, n_heads, n_runs, used, count, d, false, x.part_u, x.part_ml,
-                  at.row_of(x, a.v.Hq, qpg, wh, 0));
+    leave_sums<Z>(raw, sh, tile, warp, lane, 1, Z::NW, used, count, d, false, x.part_u, x.part_ml, at.row_of(x, a.v.Hq, qpg, 0));
     if (threadIdx.x == 0) at.sign(x, a.v.Hq, begun, at.left == 0);
     begun = true;
-    if (n_runs > 1) load.clear_stage(raw + (warp * Z::S + used) * Z::kStage);
+    load.clear_stage(raw + (warp * Z::S + used) * Z::kStage);
     if (last) break;
     bad = false;
     fresh = true;
-    at.leave(x, head_groups);
+    at.leave(x, heads);
   }
   cp_async_wait<0>();
 }
@@ -356,10 +380,12 @@ cudaError_t launch_own(const Args& g, cudaStream_t s) {
   return launch_part(own_kernel<Z, Tile>, ready, g.p.n_items, Z::NW * 32, Z::kRing + sizeof(Shared<Z, Tile, false>), g, s);
 }
 
-template <class Z, class Tile>
+template <class Z, class Tile, int PER_SM = kPerSm>
 cudaError_t launch_prefix(const Args& g, cudaStream_t s) {
   static std::atomic<uint64_t> ready{0};
-  return launch_part(prefix_kernel<Z, Tile>, ready, g.x.n_items, Z::NW * 32, Z::kRing + sizeof(Shared<Z, Tile, false>), g, s);
+  constexpr size_t smem = Z::kRing + sizeof(PrefixShared<Z, Tile>);
+  static_assert((smem + 1024) * PER_SM <= 233472, "an SM's shared memory");
+  return launch_part(prefix_kernel<Z, Tile, PER_SM>, ready, g.x.n_items, Z::NW * 32, smem, g, s);
 }
 
 }  // namespace paged

@@ -65,7 +65,7 @@ struct Segments {
     pair = false;
     n = 2;
     left = nth = 0;
-    at.p.start = at.p.rows = at.p.first = at.p.table = at.token = at.hg = at.block = at.left = 0;
+    at.p.start = at.p.rows = at.p.first = at.p.table = at.token = at.head = at.block = at.left = 0;
     at.p.end = 2 * kTok;
   }
   // The next item: the first real one once the plan is there.
@@ -137,7 +137,7 @@ struct Copier {
   __device__ __forceinline__ int64_t query(const ItemWalk& at, int from) const {
     const int qpg = g.a.v.qpg, r = from + 32 * w + lane;
     if (r >= at.count(g.x, qpg)) return -1;
-    const int x = at.block * g.x.rows + r, b = g.x.by_qpg.div(x), j = at.hg * qpg + x - b * qpg;
+    const int x = at.block * g.x.rows + r, b = g.x.by_qpg.div(x), j = at.head * qpg + x - b * qpg;
     return 2 * ((int64_t)(at.p.start + b) * g.a.q_stride + (int64_t)j * g.a.v.d);
   }
   // The same rows by single elements, for queries off 16-byte boundaries.
@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
       if (!ok) break;
       const bool pair = sg.pair, both = pair || sg.n > 1;
       const int count = dry ? 0 : sg.at.count(x, a.v.qpg), mine = pair ? s * kRows + r : r;
-      const int64_t row = sg.at.row_of(x, a.v.Hq, a.v.qpg, 0, mine);
+      const int64_t row = sg.at.row_of(x, a.v.Hq, a.v.qpg, mine);
       if (tid == 0 && !dry) sg.at.sign(x, a.v.Hq, sg.at.begins(), sg.n == sg.at.left);
       float* to = x.part_u + row * DP;
       float f0 = 1.f, f1 = 0.f;
@@ -472,8 +472,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
             atomicOr(&x.groups[sg.at.g].bad, 1);
           }
           const bool have = off[i] >= 0 && inside;
-          at[i][0] = have ? (int64_t)((uint64_t)page[i] * v.k_page_b + (uint64_t)off[i] * v.k_tok_b + (uint64_t)sg.at.hg * v.k_head_b) : -1;
-          at[i][1] = have ? (int64_t)((uint64_t)page[i] * v.v_page_b + (uint64_t)off[i] * v.v_tok_b + (uint64_t)sg.at.hg * v.v_head_b) : -1;
+          at[i][0] = have ? (int64_t)((uint64_t)page[i] * v.k_page_b + (uint64_t)off[i] * v.k_tok_b + (uint64_t)sg.at.head * v.k_head_b) : -1;
+          at[i][1] = have ? (int64_t)((uint64_t)page[i] * v.v_page_b + (uint64_t)off[i] * v.v_tok_b + (uint64_t)sg.at.head * v.v_head_b) : -1;
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) page[i] = page_of(k0 + kAhead + i, off[i]);
