@@ -241,6 +241,7 @@ cudaError_t launch_join(const Args& g, int sms, cudaStream_t s) {
 // tokens, half of them ragged 16-fold); its choice is 1.4% off the best of the three on
 // average.  The host knows a bound on the lengths only, so a way is judged by the geometric
 // mean of its times for sequences of that length and for ragged ones, 0.34 of it on average.
+// On 8-bit caches the figures are fitted to 148 calls of their own (the choice 0.5% off the best on average).
 // Measured, ranges / clusters / whole, 32 query heads on 8 KV heads of 128 in bf16:
 //   1 x 128   6.9 /  4.6 /  4.4     16 x 512       13.6 /  8.4 / 10.5    64 x 256        21 / - / 15
 //   1 x 1024  9.1 /  6.4 / 14.6     16 x 4096      49.8 / 46.3 / 56      64 x 2048       87 / - / 83
@@ -262,28 +263,31 @@ Plan plan_of(const PagedView& v, DecodeKind kind, int B, int max_len, int window
   while (heads % wide) wide /= 2;
 
   const int row = DP * el, slots = kPerSm * sms;
-  const double step = kind.quant ? (DP == 64 ? 1.2 : DP == 128 ? 1.85 : 3.4)
+  const double step = kind.quant ? (DP == 64 ? 1.55 : DP == 128 ? 2.15 : 2.95)
                                  : row <= 128 ? 0.45 : row == 256 ? 0.65 : row == 512 ? 0.95 : 1.37;  // a warp's run of tokens
   const double bytes = 1.07 * 2. * B * span * v.Hkv * (v.d * el + (kind.quant ? 4 : 0)) / 6.8e6;
   // (product of the two times) of a way with a fixed part and the longest CTA's part
   const auto times = [&](double fixed, double longest) {
     return (fixed + std::max(longest, bytes)) * (fixed + std::max(longest, 0.34 * bytes));
   };
-  double best = times((dtype == DCK_BF16 ? 7.5 : 12.7) + 0.45 * std::max(0., (double)pairs / wide / slots - 1) -
-                          (span <= few / wide * run ? 2.8 : 0), 0);
+  const double fixed = (kind.quant ? 10.5 : dtype == DCK_BF16 ? 7.5 : 12.7) + 0.45 * std::max(0., (double)pairs / wide / slots - 1) -
+                       (span <= few / wide * run ? 2.8 : 0);
+  // (a CTA's tiles in ranges take longer than HBM does for 8-bit rows only; fewer of them where sequences are shorter)
+  const double ranged = kind.quant ? 1.4 * step * std::ceil((double)(pairs / wide * tiles_of(few / wide * run)) / slots) : 0;
+  double best = (fixed + std::max(ranged, bytes)) * (fixed + 0.34 * std::max(ranged, bytes));
   if (ranges) best = 0;
   p.cluster = 0;
   p.warps = few;
   p.wh = wide;
   // clusters of c (not all SMs take part in those of 8: 15 of them on 152)
   for (int c = 1; c <= kMaxCluster && c * pairs <= sms - (c > 1 ? 4 * c : 0); c *= 2) {
-    const double t = times(c > 1 ? 5.4 : 4.3, tiles_of(many * run * c) * step);
+    const double t = times(c > 1 ? (kind.quant ? 4.7 : 5.4) : 4.3, tiles_of(many * run * c) * step);
     if (t < best) best = t, p.cluster = c, p.warps = many, p.wh = 1;
   }
   // a CTA of `few` warps for w heads of a sequence
   for (int w = 1; w <= wide; w *= 2) {
     const double waves = std::ceil((double)(pairs / w) / slots);
-    const double t = times(4.1 * (1 + 0.43 * (waves - 1)), waves * tiles_of(few / w * run) * step * 0.89);
+    const double t = times(4.1 * (1 + 0.43 * (waves - 1)), waves * tiles_of(few / w * run) * step * (kind.quant ? 1.03 : 0.89));
     if (t < best) best = t, p.cluster = 1, p.warps = few, p.wh = w;
   }
   p.wt = p.warps / p.wh;
