@@ -85,7 +85,7 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, in
   for (int b = start + lane; b < end; b += LANES) {
     const RowView r = row_view(a, a.seq_len[b], rows > 1 ? shared : 0);
     RowPlan own;
-    const bool takes_part = last > first && r.eff >= last && r.first <= first, bad = r.bad || r.len - r.eff > a.max_own;
+    const bool takes_part = last > first && r.eff >= last && r.first <= first, bad = r.bad || r.len - max(r.eff, r.first) > a.max_own;
     if (bad) atomicOr(a.err, kErrBadSeq);
     own.state = bad ? kEmpty : 0;
     own.group = takes_part && !bad ? at : -1;

@@ -206,3 +206,11 @@ def test_graphs_and_streams_give_the_same_bits():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, ref) and torch.equal(lse, rlse)
+
+
+@kinds
+@pytest.mark.parametrize("window", [1, 64, 100])
+def test_own_tokens_are_those_in_the_window(dtype, quant, window):
+    """max_own bounds the tokens beyond the shared ones that a row sees: with a window, no more than that."""
+    c = shared_case(8, 2, 64, dtype, quant, 16, "rows", [(320, [1000, 700, 333]), (0, [900])], window=window)
+    check(c, 8, window=window, max_own=window)
