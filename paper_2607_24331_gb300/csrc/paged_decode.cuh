@@ -104,11 +104,12 @@ struct alignas(16) OwnStart {
 struct CtaRange {  // of those that have tiles of an item, or of a (head group, row)
   int first, last;
 };
+// (past the L1, where a launch that does not wait for all before it may find what another call left)
 template <class S>
 __device__ __forceinline__ S load_record(const S* from) {
   S r;
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(S) / 16); ++i) reinterpret_cast<int4*>(&r)[i] = reinterpret_cast<const int4*>(from)[i];
+  for (int i = 0; i < (int)(sizeof(S) / 16); ++i) reinterpret_cast<int4*>(&r)[i] = __ldcg(reinterpret_cast<const int4*>(from) + i);
   return r;
 }
 struct Prefix {

@@ -274,6 +274,7 @@ __global__ void __launch_bounds__(Z::NW * 32, 3) own_kernel(const __grid_constan
   const int n_heads = g.p.wh, n_runs = g.p.wt, wh = warp & (n_heads - 1), wt = warp / n_heads;
   const int d = a.v.d;
   pdl_launch_dependents();  // (the shared part let this launch begin: the plan and all before it are complete)
+  __threadfence();          // what the L1 still has of earlier calls' tables and scales is not read
   OwnWalk ahead;
   int to_compute = ahead.enter(g, blockIdx.x);
   if (to_compute == 0) {

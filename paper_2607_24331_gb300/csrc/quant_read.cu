@@ -2,7 +2,7 @@
 // Bound by memory: (d + 4) bytes read and 2 or 4 d written per head's row.  A thread's unit is 16 codes (8 where the head
 // dim is no multiple of 16), read at once and written in 32-byte stores, whole sectors, where the output lies so; kInFlight
 // units are under way at a time.  (Units of 8 codes, 16-byte stores: 65536 x 8 heads of 128 in bf16, 407 MB, 90 us, bound by
-// instructions: most of a unit's are for its addresses; @@ us so.)
+// instructions: most of a unit's are for its addresses; 65 us so.)
 #include <cuda_fp16.h>
 
 #include <algorithm>
