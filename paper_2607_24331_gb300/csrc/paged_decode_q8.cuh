@@ -412,8 +412,10 @@ struct QuantTile {
       if (PACK) o[n][0] += o[n][2], o[n][1] += o[n][3];
 #pragma unroll
       for (int x = 0; x < kQ; ++x) {
-        const float f = near[x] == -CUDART_INF_F ? 0.f : exp2_approx(near[x] - m[x]);
-        o[n][2 * x] *= f, o[n][2 * x + 1] *= f;
+        // (by two powers: one may be below the least normal number, or above the largest, where the product is neither)
+        const float by = near[x] == -CUDART_INF_F ? -CUDART_INF_F : near[x] - m[x], half = floorf(by * 0.5f);
+        const float f = exp2_approx(half), rest = by == -CUDART_INF_F ? 0.f : exp2_approx(by - half);
+        o[n][2 * x] = o[n][2 * x] * f * rest, o[n][2 * x + 1] = o[n][2 * x + 1] * f * rest;
       }
     }
   }

@@ -186,3 +186,16 @@ def test_calls_repeat_bit_for_bit_in_a_graph_and_on_other_streams():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq", [4, 24])
+@pytest.mark.parametrize("exponent", [-126, -122, 102])
+def test_values_of_the_least_and_largest_scales(dtype, hq, exponent):
+    """Values whose powers of two alone are below the least normal number, or as large as the sums may be: 300 tokens of
+    values up to 448 2^102 with weights up to 2^8 before the division, 2^8.23 2^8.81 2^102 2^8 < 2^128.  (At 2^119 they are
+    not, and outputs were infinite: the interface says how large values may be.)"""
+    c = decode_case(hq, 2, 128, dtype, 16, "rows", (1, 40, 300), seed=exponent + 126)
+    c["v_scale"].fill_(2.0 ** exponent)
+    out, _ = _check(c, hq)
+    assert (out != 0).float().mean() > 0.9
