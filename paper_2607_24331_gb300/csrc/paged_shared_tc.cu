@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefix_tc_kernel(const __grid_con
           pk[i] = pack2(p.x, p.y);
           l = add2(l, p);
         }
-        tmem_st32(sb, pk);
+        if (!dry) tmem_st32(sb, pk);  // (after the item of nothing, real scores may lie there already)
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
