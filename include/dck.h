@@ -259,6 +259,8 @@ dck_status dck_decode_attention_noalloc(const dck_layer_desc* desc, const void* 
  *   dck_rope                    rotary positions, and the gradient through them
  *   dck_paged_append            new tokens' rotated keys and values into their rows
  *   dck_paged_decode_attention  one query per sequence over the pages
+ *   dck_quant_append, dck_quant_read, dck_quant_decode_attention  the same on pages of 8 bits
+ *   dck_paged_shared_attention, dck_quant_shared_attention  rows whose sequences begin alike
  * A page holds page_size consecutive tokens of one sequence; sequence b's token
  * t lies in page block_table[b][t / page_size] at offset t % page_size.  A slot
  * is page * page_size + offset; the slots of dck_page_update are also valid
@@ -503,7 +505,8 @@ dck_status dck_quant_read(const dck_quant_desc* desc, int32_t n_tok, const int64
  * dck_paged_decode_attention on an 8-bit cache: keys and values are code times scale.  Any finite scales >= 0 do,
  * powers of two or not.  Codes are multiplied exactly; queries are held to 2^-29 (bf16) or 2^-22 (fp32) of themselves,
  * or 2^-39 of their row's largest element, and weights to 2^-22 of themselves, or 2^-31 of the largest (2^-11 of
- * themselves on bf16 calls with more than 8 query heads on a KV head); all sums are fp32.  Otherwise as there.
+ * themselves on bf16 calls with more than 8 query heads on a KV head); all sums are fp32, of weights up to 2^8 that are
+ * divided at the end: 2^8 times the sum of a sequence's magnitudes has to be below 2^128.  Otherwise as there.
  */
 size_t dck_quant_decode_workspace_size(const dck_quant_desc* desc, int32_t batch, int32_t max_seq_len);
 dck_status dck_quant_decode_attention(const dck_quant_desc* desc, const void* q, int64_t q_stride, const void* kcache,
@@ -521,13 +524,20 @@ dck_status dck_quant_decode_attention(const dck_quant_desc* desc, const void* q,
  *   d_group_start  device int32 [n_groups + 1]: group g has rows d_group_start[g] .. d_group_start[g + 1] - 1;
  *                  0 first, batch last, none smaller than the one before
  *   d_shared_len   device int32 [n_groups]: the tokens that the rows of g share.  Of those a row sees the ones
- *                  below its length (and in its window): they lie, for all rows, where the block table of the group's
- *                  longest row (the first of them) has them.  Of groups of one row nothing counts as shared.
- *   max_own        upper bound on the tokens that a row sees beyond its group's shared ones, 1 .. 2^31 - 1
- * Other arguments as there.  Results differ from those calls' by roundings only.  A row with more than max_own tokens
- * of its own is treated like one with a bad length, a page outside the pool like one for every row that sees it; a
- * shared length below 0 counts as 0 and is recorded; where d_group_start is not as described, every output is zero with
- * lse = -inf, and it is recorded.  At most four launches; results do not depend on the order in which blocks run.
+ *                  below its length (and in its window); the block tables of all rows that see one have the same page
+ *                  for it, and the shared tokens are read by that of the group's longest row (the first of them).
+ *                  Of groups of one row nothing counts as shared.
+ *   max_own        upper bound on the tokens that a row sees beyond its group's shared ones (of groups of one row, on
+ *                  all that it sees), 1 .. 2^31 - 1
+ * Other arguments as there.  By batch, n_groups, max_seq_len, max_own and the descriptor a call attends to what
+ * groups share once, or, where that takes no longer, to every row by itself.  Results are those calls' up to roundings: on
+ * 16-bit caches the weights of the shared tokens may be one bf16 term (2^-8 of themselves), on 8-bit ones of bf16
+ * calls one fp16 term (2^-11).
+ * A page outside the pool counts like one for every row that sees it.  Where groups are attended to once, a row with more
+ * than max_own tokens of its own is treated like one with a bad length; a shared length below 0 counts as 0 and is
+ * recorded; where d_group_start is not as described, every output is zero with lse = -inf, and it is recorded.
+ * Rows by themselves do not look at any of the three.  At most four launches; results do not depend on the order in which
+ * blocks run.
  */
 size_t dck_paged_shared_workspace_size(const dck_paged_desc* desc, int32_t batch, int32_t max_seq_len, int32_t max_own);
 dck_status dck_paged_shared_attention(const dck_paged_desc* desc, const void* q, int64_t q_stride, const void* kcache,
