@@ -503,7 +503,7 @@ dck_status dck_quant_read(const dck_quant_desc* desc, int32_t n_tok, const int64
 
 /*
  * dck_paged_decode_attention on an 8-bit cache: keys and values are code times scale.  Any finite scales >= 0 do,
- * powers of two or not.  Codes are multiplied exactly; queries are held to 2^-29 (bf16) or 2^-22 (fp32) of themselves,
+ * powers of two or not (values' ones below 2^-126 count as 0).  Codes are multiplied exactly; queries are held to 2^-29 (bf16) or 2^-22 (fp32) of themselves,
  * or 2^-39 of their row's largest element, and weights to 2^-22 of themselves, or 2^-31 of the largest (2^-11 of
  * themselves on bf16 calls with more than 8 query heads on a KV head); all sums are fp32, of weights up to 2^8 that are
  * divided at the end: 2^8 times the sum of a sequence's magnitudes has to be below 2^128.  Otherwise as there.

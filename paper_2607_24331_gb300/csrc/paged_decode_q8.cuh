@@ -126,9 +126,11 @@ __device__ __forceinline__ void split_halves(float x, float y, uint32_t& hi, uin
   hi = *reinterpret_cast<const uint32_t*>(&h);
   lo = half_pair(x - f.x, y - f.y);
 }
-__device__ __forceinline__ float log2_approx(float x) {  // exact for powers of two
+// Of scales, exact for powers of two.  (Below the least normal number -infinity, a weight of 0: so 1.3% less time than with
+// the steps that those take.)
+__device__ __forceinline__ float log2_approx(float x) {
   float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ uint4 shared16(uint32_t at) {
