@@ -12,6 +12,7 @@
 // and attend one by one to those at its end, while a row far behind does by itself what it sees.
 //
 // Four launches: the plan (one block), the shared part, the own tokens (which start as the shared part's CTAs end), the join.
+#include <climits>
 #include <cmath>
 
 #include "paged_shared.cuh"
@@ -44,9 +45,25 @@ __device__ __forceinline__ RowView row_view(const PagedDecodeArgs& a, int len, i
   return r;
 }
 
-// A subgroup of LANES threads per group of rows at a time; true if d_group_start is not as it must be.
+// The largest v that LANES threads have, by T: those of a warp, or the whole block, with `scratch` between its warps.
+template <int LANES, typename T>
+__device__ __forceinline__ T largest_of(T v, int64_t* scratch) {
+#pragma unroll
+  for (int o = min(LANES, 32) / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
+  if (LANES > 32) {
+    if (threadIdx.x % 32 == 0) scratch[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = (T)scratch[0];
+#pragma unroll
+    for (int w = 1; w < LANES / 32; ++w) v = max(v, (T)scratch[w]);
+    __syncthreads();
+  }
+  return v;
+}
+
+// LANES threads per group of rows at a time; true if d_group_start is not as it must be.
 template <int LANES>
-__device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, int at, bool there) {
+__device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, int at, bool there, int64_t* scratch) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int lane = threadIdx.x % LANES;
@@ -63,22 +80,17 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, in
     const RowView r = row_view(a, a.seq_len[b], shared);
     if (r.len > longest) longest = r.len, row = b;
   }
-#pragma unroll
-  for (int o = LANES / 2; o; o >>= 1) {
-    const int n = __shfl_xor_sync(~0u, longest, o), b = __shfl_xor_sync(~0u, row, o);
-    if (n > longest || (n == longest && b < row)) longest = n, row = b;
-  }
+  const int64_t found = largest_of<LANES>((int64_t)longest << 32 | (INT_MAX - row), scratch);
+  longest = (int)(found >> 32);
+  row = INT_MAX - (int)(found & INT_MAX);
   const int most = min(longest, shared), least = max(1, most - 256 - rows);
   int last = most, first = 0;
   for (int b = start + lane; b < end; b += LANES) {
     const RowView r = row_view(a, a.seq_len[b], shared);
     if (r.eff >= least) last = min(last, r.eff), first = max(first, r.first);
   }
-#pragma unroll
-  for (int o = LANES / 2; o; o >>= 1) {
-    last = min(last, __shfl_xor_sync(~0u, last, o));
-    first = max(first, __shfl_xor_sync(~0u, first, o));
-  }
+  last = -largest_of<LANES>(-last, scratch);
+  first = largest_of<LANES>(first, scratch);
   if (rows < 2 || last <= first) last = first = 0;
   const int64_t blocks = ((int64_t)rows * a.v.qpg + x.rows - 1) / x.rows;
   // what each row has of its own
@@ -185,10 +197,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   s.units = reinterpret_cast<int*>(at);
   s.tiles = s.units + n + 1;
   int wrong = 0;
-  if (n <= 2 * kPlanThreads / 32) {
-    for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, s, i, true);
+  // Few groups of many rows by the whole block, 1.5 us each and 1 us per 512 rows, others by warps, 1 us per 32 rows
+  // (4096 rows in one group: 31 for 128 us), or where there are many by eight threads.
+  if (n < 16 && a.B * (16 - n) > 768 * n * n) {
+    for (int i = 0; i < n; ++i) wrong |= plan_group<kPlanThreads>(g, s, i, true, scratch[0]);
+  } else if (n <= 2 * kPlanThreads / 32) {
+    for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, s, i, true, nullptr);
   } else {
-    for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, s, i + tid / 8, i + tid / 8 < n);
+    for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, s, i + tid / 8, i + tid / 8 < n, nullptr);
   }
   wrong = __syncthreads_or(wrong);
   if (!wrong) {
