@@ -525,8 +525,7 @@ dck_status dck_quant_decode_attention(const dck_quant_desc* desc, const void* q,
  *                  0 first, batch last, none smaller than the one before
  *   d_shared_len   device int32 [n_groups]: the tokens that the rows of g share.  Of those a row sees the ones
  *                  below its length (and in its window); the block tables of all rows that see one have the same page
- *                  for it, and the shared tokens are read by that of the group's longest row (the first of them).
- *                  Of groups of one row nothing counts as shared.
+ *                  for it.  Of groups of one row nothing counts as shared.
  *   max_own        upper bound on the tokens that a row sees beyond its group's shared ones (of groups of one row, on
  *                  all that it sees), 1 .. 2^31 - 1
  * Other arguments as there.  By batch, n_groups, max_seq_len, max_own and the descriptor a call attends to what

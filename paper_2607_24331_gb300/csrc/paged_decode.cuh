@@ -70,7 +70,7 @@ struct ScoreScale {
 };
 
 // Calls over shared prefixes (paged_shared.cu): what the rows of group g see together, tokens [first, end), is attended
-// to for all of them at once, in items of a block of their queries on a KV head, each cut into tiles; the items'
+// to for all of them at once (of a long group, for parts of it: each like a group), in items of a block of their queries on a KV head, each cut into tiles; the items'
 // tiles form one list, dealt to CTAs in equal ranges.
 struct alignas(16) GroupPlan {
   int start, rows;   // its rows
@@ -122,6 +122,7 @@ struct Prefix {
   float *part_u, *part_ml;  // partial sums, as in Args, of what groups share: rows by row_of
   float *own_u, *own_ml;    // and of rows' own tokens: rows by own_row
   int n_groups, n_items;  // groups; CTAs that tiles are dealt to
+  int most_rows_log2, n_parts;  // of the rows of a group that is planned whole; places for groups and their parts
   int rows, tile;         // queries of a block, tokens of a tile
   Divider by_qpg, by_rows;
 

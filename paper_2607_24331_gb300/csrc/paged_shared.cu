@@ -12,7 +12,6 @@
 // and attend one by one to those at its end, while a row far behind does by itself what it sees.
 //
 // Four launches: the plan (one block), the shared part, the own tokens (which start as the shared part's CTAs end), the join.
-#include <climits>
 #include <cmath>
 
 #include "paged_shared.cuh"
@@ -22,6 +21,7 @@ namespace paged {
 namespace {
 
 constexpr int kPlanThreads = 512;
+constexpr int kLeastPartLog2 = 5, kMostPartLog2 = 7;  // rows that are planned together, at most (by layout_of)
 
 // What the plan works on: its records, in shared memory where they fit (kFew groups and rows), else where they go; tiles
 // of all groups, and of all rows, before each.
@@ -29,7 +29,7 @@ constexpr int kFew = kPlanThreads;
 struct PlanState {
   GroupPlan* groups;
   RowPlan* own;
-  int *units, *tiles;  // [n_groups + 1], [B + 1]
+  int *units, *tiles;  // [n_parts + 1], [B + 1]
 };
 
 // A row's first visible token, those it sees of the shared ones (0: none, or a bad length), and its length.
@@ -45,62 +45,90 @@ __device__ __forceinline__ RowView row_view(const PagedDecodeArgs& a, int len, i
   return r;
 }
 
-// The largest v that LANES threads have, by T: those of a warp, or the whole block, with `scratch` between its warps.
-template <int LANES, typename T>
-__device__ __forceinline__ T largest_of(T v, int64_t* scratch) {
-#pragma unroll
-  for (int o = min(LANES, 32) / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
-  if (LANES > 32) {
-    if (threadIdx.x % 32 == 0) scratch[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = (T)scratch[0];
-#pragma unroll
-    for (int w = 1; w < LANES / 32; ++w) v = max(v, (T)scratch[w]);
-    __syncthreads();
-  }
+// Group `at` of the call, its first row, its rows and their parts; `wrong`: d_group_start is not as it must be (no rows).
+struct GroupView {
+  int start, rows, parts;
+  bool wrong;
+};
+// Leaves a place empty that no part has, between this group's and the next one's (`speaks`: in one thread).
+__device__ __forceinline__ GroupView group_view(const Args& g, const PlanState& s, int at, bool speaks) {
+  const int start = g.a.group_start[at], end = g.a.group_start[at + 1];
+  GroupView v;
+  v.wrong = start < 0 || end < start || end > g.a.B || (at == 0 && start != 0) || (at == g.x.n_groups - 1 && end != g.a.B);
+  v.start = start;
+  v.rows = v.wrong ? 0 : end - start;
+  const int log2 = g.x.most_rows_log2;
+  v.parts = (v.rows + (1 << log2) - 1) >> log2;
+  const int past = at + (start >> log2) + v.parts;
+  if (speaks && !v.wrong && past < at + 1 + (end >> log2)) s.units[past] = s.groups[past].tiles = 0;
   return v;
 }
 
-// LANES threads per group of rows at a time; true if d_group_start is not as it must be.
+// Part `part` of group `at` (where `there`), planned by LANES threads; all groups of them in a warp at once.
 template <int LANES>
-__device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, int at, bool there, int64_t* scratch) {
+__device__ __forceinline__ void plan_part(const Args& g, const PlanState& s, int at, const GroupView& whole, int part, bool there) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
   const int lane = threadIdx.x % LANES;
+  there = there && part < whole.parts;
   int start = 0, end = 0, said = 0;
-  if (there) start = a.group_start[at], end = a.group_start[at + 1], said = a.shared_len[at];
-  const bool wrong = there && (start < 0 || end < start || end > a.B || (at == 0 && start != 0) ||
-                               (at == x.n_groups - 1 && end != a.B));
-  if (wrong) end = start;
+  if (there) {
+    start = whole.start, end = start + whole.rows;
+    if (whole.parts > 1) {
+      start = whole.start + part * whole.rows / whole.parts;
+      end = whole.start + (part + 1) * whole.rows / whole.parts;
+    }
+    said = a.shared_len[at];
+    if (said < 0 && lane == 0) atomicOr(a.err, kErrBadSeq);
+  }
   const int shared = max(said, 0), rows = end - start;
-  if (said < 0 && lane == 0) atomicOr(a.err, kErrBadSeq);
+  // all its rows' lengths at once, by a warp: a read takes longer than the rest of a row
+  constexpr int kKept = LANES == 32 ? (1 << kMostPartLog2) / 32 : 1;
+  int kept[kKept];
+#pragma unroll
+  for (int i = 0; i < kKept; ++i) kept[i] = start + lane + i * LANES < end ? a.seq_len[start + lane + i * LANES] : 0;
+  const auto each_row = [&](auto f) {
+    if (LANES == 32) {
+#pragma unroll
+      for (int i = 0; i < kKept; ++i)
+        if (start + lane + i * LANES < end) f(start + lane + i * LANES, kept[i]);
+    } else {
+      for (int b = start + lane; b < end; b += LANES) f(b, b == start + lane ? kept[0] : a.seq_len[b]);
+    }
+  };
   // the longest row, the first of them
   int longest = 0, row = start;
-  for (int b = start + lane; b < end; b += LANES) {
-    const RowView r = row_view(a, a.seq_len[b], shared);
+  each_row([&](int b, int len) {
+    const RowView r = row_view(a, len, shared);
     if (r.len > longest) longest = r.len, row = b;
+  });
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) {
+    const int n = __shfl_xor_sync(~0u, longest, o), b = __shfl_xor_sync(~0u, row, o);
+    if (n > longest || (n == longest && b < row)) longest = n, row = b;
   }
-  const int64_t found = largest_of<LANES>((int64_t)longest << 32 | (INT_MAX - row), scratch);
-  longest = (int)(found >> 32);
-  row = INT_MAX - (int)(found & INT_MAX);
   const int most = min(longest, shared), least = max(1, most - 256 - rows);
   int last = most, first = 0;
-  for (int b = start + lane; b < end; b += LANES) {
-    const RowView r = row_view(a, a.seq_len[b], shared);
+  each_row([&](int, int len) {
+    const RowView r = row_view(a, len, shared);
     if (r.eff >= least) last = min(last, r.eff), first = max(first, r.first);
+  });
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) {
+    last = min(last, __shfl_xor_sync(~0u, last, o));
+    first = max(first, __shfl_xor_sync(~0u, first, o));
   }
-  last = -largest_of<LANES>(-last, scratch);
-  first = largest_of<LANES>(first, scratch);
   if (rows < 2 || last <= first) last = first = 0;
   const int64_t blocks = ((int64_t)rows * a.v.qpg + x.rows - 1) / x.rows;
+  const int slot = at + (whole.start >> x.most_rows_log2) + part;
   // what each row has of its own
-  for (int b = start + lane; b < end; b += LANES) {
-    const RowView r = row_view(a, a.seq_len[b], rows > 1 ? shared : 0);
+  each_row([&](int b, int len) {
+    const RowView r = row_view(a, len, rows > 1 ? shared : 0);
     RowPlan own;
     const bool takes_part = last > first && r.eff >= last && r.first <= first, bad = r.bad || r.len - max(r.eff, r.first) > a.max_own;
     if (bad) atomicOr(a.err, kErrBadSeq);
     own.state = bad ? kEmpty : 0;
-    own.group = takes_part && !bad ? at : -1;
+    own.group = takes_part && !bad ? slot : -1;
     own.skip_at = takes_part ? first : 0;
     own.skip = takes_part ? last - first : 0;
     own.first = r.first;
@@ -110,8 +138,8 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, in
     own.blocks = (int)blocks;
     s.own[b] = own;
     s.tiles[b] = max(1, (own.end - own.first + g.p.tile - 1) / g.p.tile);
-  }
-  if (!there || lane) return wrong;
+  });
+  if (!there || lane) return;
   GroupPlan p;
   p.start = start;
   p.rows = rows;
@@ -121,9 +149,8 @@ __device__ __forceinline__ bool plan_group(const Args& g, const PlanState& s, in
   p.tiles = (last - first + x.tile - 1) / x.tile;
   p.blocks = (int)blocks;
   p.bad = 0;
-  s.groups[at] = p;
-  s.units[at] = (int)min((int64_t)p.tiles * blocks * a.v.Hkv, (int64_t)kUnitLimit + 1);
-  return wrong;
+  s.groups[slot] = p;
+  s.units[slot] = (int)min((int64_t)p.tiles * blocks * a.v.Hkv, (int64_t)kUnitLimit + 1);
 }
 
 // In place of units[0 .. n - 1] and tiles[0 .. m - 1] the sums of all before each, and of all in units[n] and tiles[m]:
@@ -182,34 +209,46 @@ size_t plan_bytes(int groups, int rows) {
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ Args g) {
   const PagedDecodeArgs& a = g.a;
   const Prefix& x = g.x;
-  const int tid = threadIdx.x, n = x.n_groups;
+  const int tid = threadIdx.x, n = x.n_groups, parts = x.n_parts;
   extern __shared__ __align__(16) uint8_t plan_memory[];
   __shared__ int64_t scratch[2][kPlanThreads / 32];
   pdl_launch_dependents();
   pdl_wait();
-  const bool few = n <= kFew && a.B <= kFew;
+  const bool few = parts <= kFew && a.B <= kFew;
   PlanState s;
   uint8_t* at = plan_memory;
   s.groups = few ? reinterpret_cast<GroupPlan*>(at) : x.groups;
-  if (few) at += n * sizeof(GroupPlan);
+  if (few) at += parts * sizeof(GroupPlan);
   s.own = few ? reinterpret_cast<RowPlan*>(at) : x.own;
   if (few) at += a.B * sizeof(RowPlan);
   s.units = reinterpret_cast<int*>(at);
-  s.tiles = s.units + n + 1;
+  s.tiles = s.units + parts + 1;
   int wrong = 0;
-  // Few groups of many rows by the whole block, 1.5 us each and 1 us per 512 rows, others by warps, 1 us per 32 rows
-  // (4096 rows in one group: 31 for 128 us), or where there are many by eight threads.
-  if (n < 16 && a.B * (16 - n) > 768 * n * n) {
-    for (int i = 0; i < n; ++i) wrong |= plan_group<kPlanThreads>(g, s, i, true, scratch[0]);
-  } else if (n <= 2 * kPlanThreads / 32) {
-    for (int i = tid / 32; i < n; i += kPlanThreads / 32) wrong |= plan_group<32>(g, s, i, true, nullptr);
+  if (n < 16 && n << (x.most_rows_log2 + 1) <= a.B) {  // few groups of many parts: a warp per part
+    for (int i = 0; i < n; ++i) {
+      const GroupView v = group_view(g, s, i, tid == 0);
+      wrong |= v.wrong;
+      for (int k = tid / 32; k < v.parts; k += kPlanThreads / 32) plan_part<32>(g, s, i, v, k, true);
+    }
+  } else if (n <= 2 * kPlanThreads / 32) {  // a warp per group
+    for (int i = tid / 32; i < n; i += kPlanThreads / 32) {
+      const GroupView v = group_view(g, s, i, tid % 32 == 0);
+      wrong |= v.wrong;
+      for (int k = 0; k < v.parts; ++k) plan_part<32>(g, s, i, v, k, true);
+    }
   } else {
-    for (int i = 0; i < n; i += kPlanThreads / 8) wrong |= plan_group<8>(g, s, i + tid / 8, i + tid / 8 < n, nullptr);
+    for (int i0 = 0; i0 < n; i0 += kPlanThreads / 8) {
+      const int i = i0 + tid / 8;
+      const GroupView v = i < n ? group_view(g, s, i, tid % 8 == 0) : GroupView{0, 0, 0, false};
+      wrong |= v.wrong;
+      const int most = __reduce_max_sync(~0u, v.parts);
+      for (int k = 0; k < most; ++k) plan_part<8>(g, s, i, v, k, i < n);
+    }
   }
   wrong = __syncthreads_or(wrong);
   if (!wrong) {
-    sum_before(s, n, a.B, scratch);
-    wrong = s.units[n] > kUnitLimit || (int64_t)s.tiles[a.B] * g.p.groups > kUnitLimit;
+    sum_before(s, parts, a.B, scratch);
+    wrong = s.units[parts] > kUnitLimit || (int64_t)s.tiles[a.B] * g.p.groups > kUnitLimit;
     __syncthreads();
   }
   if (wrong) {  // every row is empty, of one tile
@@ -217,14 +256,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       if (b < a.B) s.own[b] = {0, 0, 0, 0, -1, kEmpty, 0, 0, 0, 0, {0, 0}};
       s.tiles[b] = b;
     }
-    for (int i = tid; i <= n; i += kPlanThreads) s.units[i] = 0;
+    for (int i = tid; i <= parts; i += kPlanThreads) s.units[i] = 0;
     if (tid == 0) atomicOr(a.err, kErrBadSeq);
   }
   __syncthreads();
   // where each CTA begins
-  const int units = s.units[n], own_tiles = s.tiles[a.B];
+  const int units = s.units[parts], own_tiles = s.tiles[a.B];
   int n_items = min(x.n_items, units);
-  if (n == 1 && units) {
+  if (n == 1 && a.B <= 1 << x.most_rows_log2 && units) {
     // Items that are all alike: whole CTAs for each, if that leaves out less than an eighth of them, so that none has the end
     // of one and the beginning of another (3 us more where an end leaves 256 rows).
     const int alike = units / s.groups[0].tiles, each = n_items / alike;
@@ -237,7 +276,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     if (c < items.n) {
       const int u = items.begin(c);
       r.n = items.begin(c + 1) - u;
-      r.g = last_of(s.units, n, u);
+      r.g = last_of(s.units, parts, u);
       r.p = s.groups[r.g];
       const int inside = u - s.units[r.g], item = inside / r.p.tiles, tile = inside - item * r.p.tiles;
       r.head = item / r.p.blocks;
@@ -265,7 +304,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     x.own_start[c] = r;
   }
   // the records themselves
-  for (int i = tid; i < n; i += kPlanThreads) {
+  for (int i = tid; i < parts; i += kPlanThreads) {
     GroupPlan r = s.groups[i];
     r.units = s.units[i];
     x.groups[i] = r;
@@ -373,10 +412,17 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   }
 }
 
+// A group of more than 2^most_rows_log2 rows is planned in parts, each as a group of its own: the tokens of a long chunk that all its rows
+// see end where its first row does, and what its rows have of their own, by rows, grows as the square of its length. Parts of 256 queries, a
+// whole block on tcgen05, read the shared tokens no more often.  Part k of group i has place i + (start >> most_rows_log2) + k, so that
+// groups need not know of each other's parts.
+// Measured, 1024 tokens after 16384, in one part and so: 32 query heads on 8 KV heads of 128 in bf16 558 and 291 us; on 32
+// KV heads 1294 and 532; of 8 bits 1856 and 1517, and 3304 and 1734.
+
 // How the shared part of a call is laid out.
 struct Layout {
   bool tc;  // on tcgen05
-  int rows, tile, n_items;
+  int rows, tile, n_items, most_rows_log2;
 };
 Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int sms) {
   Layout l;
@@ -386,11 +432,14 @@ Layout layout_of(const PagedView& v, DecodeKind kind, int B, int n_groups, int s
   if (l.tc) {
     l.rows = 256;
     l.tile = 64;
+    l.most_rows_log2 = kLeastPartLog2;
+    while (l.most_rows_log2 < kMostPartLog2 && v.qpg << (l.most_rows_log2 + 1) <= 256) ++l.most_rows_log2;
     l.n_items = std::max(1, sms - 1);  // the plan's block has the last SM while they get ready
     return l;
   }
   l.rows = kind.dtype == DCK_BF16 && DP <= 128 && queries > 8 ? 16 : 8;
   l.tile = warps_of(DP, false) * run_of(kind);
+  l.most_rows_log2 = kLeastPartLog2;
   l.n_items = std::min(prefix_per_sm(kind, l.rows) * sms, kMaxItems);
   return l;
 }
@@ -407,7 +456,7 @@ struct Parts {
       all += align_up(bytes, 256);
       return at;
     };
-    groups = take((size_t)B * sizeof(GroupPlan));
+    groups = take((size_t)(B + (B >> kLeastPartLog2)) * sizeof(GroupPlan));
     own = take((size_t)B * sizeof(RowPlan));
     item_start = take(kMaxItems * sizeof(ItemStart));
     own_start = take(kMaxItems * sizeof(OwnStart));
@@ -482,6 +531,8 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   g.x.own_ml = reinterpret_cast<float*>(ws + parts.own_ml);
   g.x.own_u = reinterpret_cast<float*>(ws + parts.own_u);
   g.x.n_groups = a.n_groups;
+  g.x.most_rows_log2 = l.most_rows_log2;
+  g.x.n_parts = a.n_groups + (a.B >> l.most_rows_log2);
   g.x.n_items = l.n_items;
   g.x.rows = l.rows;
   g.x.tile = l.tile;
@@ -489,7 +540,7 @@ cudaError_t launch_paged_shared(const PagedDecodeArgs& a, DecodeKind kind, int s
   g.x.by_rows = divider((uint32_t)l.rows);
   static std::atomic<uint64_t> ready{0};
   cudaError_t e = allow_shared(plan_kernel, ready, plan_bytes(kFew, kFew));
-  if (e == cudaSuccess) e = launch_pdl(plan_kernel, 1, kPlanThreads, plan_bytes(a.n_groups, a.B), s, g);
+  if (e == cudaSuccess) e = launch_pdl(plan_kernel, 1, kPlanThreads, plan_bytes(g.x.n_parts, a.B), s, g);
   if (e == cudaSuccess) e = hook_launched(a.hook, s);
   // heads of the shared part are KV heads themselves
   Args h = g;

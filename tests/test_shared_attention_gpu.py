@@ -214,3 +214,15 @@ def test_own_tokens_are_those_in_the_window(dtype, quant, window):
     """max_own bounds the tokens beyond the shared ones that a row sees: with a window, no more than that."""
     c = shared_case(8, 2, 64, dtype, quant, 16, "rows", [(320, [1000, 700, 333]), (0, [900])], window=window)
     check(c, 8, window=window, max_own=window)
+
+
+@kinds
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (4, 4, 128), (16, 1, 64)])
+def test_groups_of_many_rows(dtype, quant, hq, hkv, d):
+    """Long chunks and prompts of many rows, planned in parts: odd sizes, between groups of one row, of none that sees anything
+    and of rows far apart."""
+    groups = [(5, [6]), _chunk(400, 257), (64, [64 + i * 7 % 50 for i in range(129)]), (0, [0, 0]), (640, [640 + i % 3 for i in range(65)]),
+              (0, [9]), (320, [i * 5 % 330 for i in range(193)])]
+    check(shared_case(hq, hkv, d, dtype, quant, 16, "rows", groups, seed=hq), hq)
+    check(shared_case(hq, hkv, d, dtype, quant, 16, "rows", groups[:2], window=100, seed=hq), hq, window=100)
+    check(shared_case(hq, hkv, d, dtype, quant, 16, "rows", [_chunk(600, 500)], seed=hq), hq)
