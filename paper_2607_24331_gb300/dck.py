@@ -479,6 +479,7 @@ def dck_set_decode_kernel(which: int) -> int:
 
 
 def dck_set_shared_way(which: int) -> int:
+    """0: shared calls choose by themselves; 1: every row by itself; 2: what groups share once.  The previous value."""
     return lib().dck_set_shared_way(int(which))
 
 
