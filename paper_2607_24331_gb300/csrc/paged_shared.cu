@@ -32,7 +32,8 @@ struct PlanState {
   int *units, *tiles;  // [n_parts + 1], [B + 1]
 };
 
-// A row's first visible token, those it sees of the shared ones (0: none, or a bad length), and its length.
+// A row's first visible token, those it sees of the shared ones (0: none), and its length. A bad row, by its length or by
+// more tokens of its own than the call says, has none at all: it may not decide for its group, by its length or by its table.
 struct RowView {
   int first, eff, len;
   bool bad;
@@ -40,8 +41,10 @@ struct RowView {
 __device__ __forceinline__ RowView row_view(const PagedDecodeArgs& a, int len, int shared) {
   RowView r;
   const int span = visible_of(a, len, r.first, r.bad);
-  r.len = r.bad ? r.first : span + r.first;
-  r.eff = r.bad ? 0 : min(r.len, shared);
+  r.len = span + r.first;
+  r.eff = min(r.len, shared);
+  r.bad |= r.len - max(r.eff, r.first) > a.max_own;
+  if (r.bad) r.first = r.len = r.eff = 0;
   return r;
 }
 
@@ -81,7 +84,7 @@ __device__ __forceinline__ void plan_part(const Args& g, const PlanState& s, int
     said = a.shared_len[at];
     if (said < 0 && lane == 0) atomicOr(a.err, kErrBadSeq);
   }
-  const int shared = max(said, 0), rows = end - start;
+  const int rows = end - start, shared = rows > 1 ? max(said, 0) : 0;
   // all its rows' lengths at once, by a warp: a read takes longer than the rest of a row
   constexpr int kKept = LANES == 32 ? (1 << kMostPartLog2) / 32 : 1;
   int kept[kKept];
@@ -123,16 +126,16 @@ __device__ __forceinline__ void plan_part(const Args& g, const PlanState& s, int
   const int slot = at + (whole.start >> x.most_rows_log2) + part;
   // what each row has of its own
   each_row([&](int b, int len) {
-    const RowView r = row_view(a, len, rows > 1 ? shared : 0);
+    const RowView r = row_view(a, len, shared);
     RowPlan own;
-    const bool takes_part = last > first && r.eff >= last && r.first <= first, bad = r.bad || r.len - max(r.eff, r.first) > a.max_own;
-    if (bad) atomicOr(a.err, kErrBadSeq);
-    own.state = bad ? kEmpty : 0;
-    own.group = takes_part && !bad ? slot : -1;
+    const bool takes_part = last > first && r.eff >= last && r.first <= first;
+    if (r.bad) atomicOr(a.err, kErrBadSeq);
+    own.state = r.bad ? kEmpty : 0;
+    own.group = takes_part ? slot : -1;
     own.skip_at = takes_part ? first : 0;
     own.skip = takes_part ? last - first : 0;
     own.first = r.first;
-    own.end = bad ? r.first : r.len - own.skip;
+    own.end = r.len - own.skip;
     own.start = start;
     own.rows = rows;
     own.blocks = (int)blocks;
