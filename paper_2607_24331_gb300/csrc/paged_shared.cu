@@ -486,13 +486,16 @@ namespace paged {
 namespace {
 
 // Whether what groups share is attended to once, or every row by itself: the one of the less time by models in us of both, fitted
-// to 142 measured calls (its choice is 1.5% off the better one on average; four head layouts, three kinds of caches, 1 to 16 groups of 2 to 64 rows, 256 to 32768 tokens). Rows
-// by themselves read mostly from L2; the shared way is four launches. The host knows bounds only: what groups share is taken
-// for the difference of those of a row's tokens and its own ones, and own tokens for half of theirs.
+// to 142 measured calls of groups and rows that are alike. Rows by themselves read mostly from L2; the shared way is four
+// launches. The host knows bounds only: rows are taken to be as long as they may, with half as many own tokens as they may
+// have and the rest shared, and groups to be of one size. Over 500 other calls (six head layouts, three kinds of caches, 1 to
+// 32 groups of 1 to 64 rows, chunks, windows, alike and ragged) the choice is 3% off the better one on average where max_own is
+// what rows have at most, 10% where it is no bound (max_seq_len), and up to 4 times in a single call.
 // Measured, by rows / shared, 32 query heads on 8 KV heads of 128 in bf16, one group:
 //   4 rows on 512 tokens 6.1 / 16.5     16 on 2048 18.6 / 21.4     64 on 2048  56 / 25
 //   8 on 2048  12.4 / 20.7               8 on 8192 33.7 / 24.0     64 on 32768 767 / 53
 bool prefer_shared(const PagedDecodeArgs& a, DecodeKind kind) {
+  if (a.n_groups == a.B) return false;  // rows of their own groups share nothing
   const PagedView& v = a.v;
   const int DP = padded_dim(v.d), el = kind.quant ? 1 : kind.dtype == DCK_F32 ? 4 : 2;
   const double row = 2. * v.Hkv * (v.d * el + (kind.quant ? 4 : 0));  // bytes of a token
@@ -505,7 +508,8 @@ bool prefer_shared(const PagedDecodeArgs& a, DecodeKind kind) {
   const bool tc = kind.dtype == DCK_BF16 && !kind.quant && DP <= 128;
   const double blocks = std::ceil(queries / (tc ? 256 : kind.dtype == DCK_BF16 && DP <= 128 ? 16 : 8));
   const double once = a.n_groups * shared * row, again = once * blocks / (tc ? 7e6 : 6e6);
-  return 18 + std::max(once / 5.9e6, again) + a.B * own * row / 6e6 + 1.2e-3 * a.B * v.Hq < by_rows;
+  // (own tokens are the same work as rows by themselves, without what those find in L2)
+  return 18 + std::max(once / 5.9e6, again) + a.B * own * row / std::min(6e6, rate) + 1.2e-3 * a.B * v.Hq < by_rows;
 }
 
 }  // namespace
