@@ -15,7 +15,7 @@ cudaError_t own(const Args& g, cudaStream_t s) {
 template <int DP, int S>
 cudaError_t prefix(const Args& g, cudaStream_t s) {
   using Z = Sizes<float, DP, warps_of(DP, false), S, 8>;
-  return g.x.rows <= 4 ? launch_prefix<Z, SimtTile<Z, 4>>(g, s) : launch_prefix<Z, SimtTile<Z, 8>>(g, s);
+  return launch_prefix<Z, SimtTile<Z, 8>>(g, s);  // (blocks of 8 queries: layout_of)
 }
 
 }  // namespace
