@@ -506,7 +506,8 @@ dck_status dck_quant_read(const dck_quant_desc* desc, int32_t n_tok, const int64
  * powers of two or not (values' ones below 2^-126 count as 0).  Codes are multiplied exactly; queries are held to 2^-29 (bf16) or 2^-22 (fp32) of themselves,
  * or 2^-39 of their row's largest element, and weights to 2^-22 of themselves, or 2^-31 of the largest (2^-11 of
  * themselves on bf16 calls with more than 8 query heads on a KV head); all sums are fp32, of weights up to 2^8 that are
- * divided at the end: 2^8 times the sum of a sequence's magnitudes has to be below 2^128.  Otherwise as there.
+ * divided at the end: 2^8 times the sum of a sequence's magnitudes has to be below 2^128, and a key's scale times the
+ * largest magnitude of a query's row below 2^142.  Otherwise as there.
  */
 size_t dck_quant_decode_workspace_size(const dck_quant_desc* desc, int32_t batch, int32_t max_seq_len);
 dck_status dck_quant_decode_attention(const dck_quant_desc* desc, const void* q, int64_t q_stride, const void* kcache,
@@ -529,14 +530,17 @@ dck_status dck_quant_decode_attention(const dck_quant_desc* desc, const void* q,
  *   max_own        upper bound on the tokens that a row sees beyond its group's shared ones (of groups of one row, on
  *                  all that it sees), 1 .. 2^31 - 1
  * Other arguments as there.  By batch, n_groups, max_seq_len, max_own and the descriptor a call attends to what
- * groups share once, or, where that takes no longer, to every row by itself.  Results are those calls' up to roundings: on
+ * groups share once, or, where models of both ways' times say that this takes no longer, to every row by itself (as it does to
+ * as many groups as rows: leave groups of no rows out of n_groups).  Results are those calls' up to roundings: on
  * 16-bit caches the weights of the shared tokens may be one bf16 term (2^-8 of themselves), on 8-bit ones of bf16
  * calls one fp16 term (2^-11).
  * A page outside the pool counts like one for every row that sees it.  Where groups are attended to once, a row with more
  * than max_own tokens of its own is treated like one with a bad length; a shared length below 0 counts as 0 and is
  * recorded; where d_group_start is not as described, every output is zero with lse = -inf, and it is recorded.
- * Rows by themselves do not look at any of the three.  At most four launches; results do not depend on the order in which
- * blocks run.
+ * Rows by themselves do not look at any of the three.  Neither the length nor the block table of a bad row reaches
+ * another row.  At most four launches; results do not depend on the order in which blocks run.
+ * The workspace, whichever way a call takes, is about 8 batch Hq d' bytes (d': head_dim rounded up to 64, 128 or 256) for
+ * partial sums, and 10 to 45 MB whatever the batch.
  */
 size_t dck_paged_shared_workspace_size(const dck_paged_desc* desc, int32_t batch, int32_t max_seq_len, int32_t max_own);
 dck_status dck_paged_shared_attention(const dck_paged_desc* desc, const void* q, int64_t q_stride, const void* kcache,

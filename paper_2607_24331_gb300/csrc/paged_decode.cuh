@@ -162,7 +162,7 @@ cudaError_t launch_q8(const Args& g, int dtype, cudaStream_t s);
 cudaError_t launch_prefix_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_prefix_f32(const Args& g, cudaStream_t s);
 cudaError_t launch_prefix_q8(const Args& g, int dtype, cudaStream_t s);
-cudaError_t launch_prefix_tc(const Args& g, cudaStream_t s);  // bf16, head dims up to 128: blocks of 128 queries
+cudaError_t launch_prefix_tc(const Args& g, cudaStream_t s);  // bf16, head dims up to 128: blocks of up to 256 queries
 cudaError_t launch_own_bf16(const Args& g, cudaStream_t s);
 cudaError_t launch_own_f32(const Args& g, cudaStream_t s);
 cudaError_t launch_own_q8(const Args& g, int dtype, cudaStream_t s);
@@ -266,7 +266,7 @@ struct Ranges {
 // What the plan keeps of the sequences in shared memory.
 struct Batch {
   int* prefix;  // [B + 1] exclusive prefix sums of the tile counts
-  int* len;     // [B] lengths, 0 for invalid ones (null: more than kKeptLens sequences, lengths from memory)
+  int* len;     // [B] lengths, of sequences that have tiles (null: more than kKeptLens sequences, lengths from memory)
 };
 constexpr int kKeptLens = 1024;
 

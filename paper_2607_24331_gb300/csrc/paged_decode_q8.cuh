@@ -8,8 +8,8 @@
 //
 // An e4m3 code is an fp16 number exactly (one conversion for two of them), so products run on
 // mma.sync m16n8k16 in fp16 with fp32 sums.  Queries are brought to 2^14 .. 2^15 by a power of two
-// per row first: of a bf16 query fp16 then keeps every element within 2^-29 of the row's largest, and
-// 2^-40 of that beyond; of an fp32 one two fp16 terms keep 2^-22.  Weights are two fp16 terms (2^-22), the low
+// per row first: of a bf16 query fp16 then holds every element down to 2^-29 of the row's largest as it is,
+// and smaller ones to 2^-39 of that (half of fp16's least step, 2^-25, of 2^14); of an fp32 one two fp16 terms keep 2^-22.  Weights are two fp16 terms (2^-22), the low
 // ones in the MMA's unused rows where up to 8 query heads share a KV head; with more of them one
 // term (2^-11, a quarter of what a bf16 output's rounding can be off by, and errors of many weights cancel).
 #pragma once

@@ -4,14 +4,16 @@
 // Mathematics: sums over disjoint sets of tokens join as sum_i 2^(m_i - M) (.)_i (paged_decode.cu), so a row's sums over
 // the tokens that its group shares may be formed elsewhere than those over its own.  The shared tokens are
 // attended to once per block of queries of the group's rows, whose queries on a KV head are the rows of one product;
-// each row's own tokens by a CTA or cluster as in a call by single rows, which then adds what the first left.
+// each row's own tokens by CTAs that tiles are dealt to in ranges, as in a call by single rows; a launch of its own joins what both
+// left.
 //
 // Which tokens: those that all the rows that take part see, so that the first part needs no mask (and what a row may not
 // see cannot reach it, infinities and NaN included).  A group's rows take part if they see nearly as many of the
 // shared tokens as the longest does, at most 256 and the number of rows fewer: a chunk's tokens all do,
 // and attend one by one to those at its end, while a row far behind does by itself what it sees.
 //
-// Four launches: the plan (one block), the shared part, the own tokens (which start as the shared part's CTAs end), the join.
+// Four launches: the plan (one block), the shared part, the own tokens (which do not wait for that: they take SMs as its CTAs
+// end), the join.
 #include <cmath>
 
 #include "paged_shared.cuh"
@@ -268,7 +270,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   int n_items = min(x.n_items, units);
   if (n == 1 && a.B <= 1 << x.most_rows_log2 && units) {
     // Items that are all alike: whole CTAs for each, if that leaves out less than an eighth of them, so that none has the end
-    // of one and the beginning of another (3 us more where an end leaves 256 rows).
+    // of one and the beginning of another (3 us more where an end leaves 256 rows).  For one group that is planned whole:
+    // items of several have as many tiles each as their group's tokens make.
     const int alike = units / s.groups[0].tiles, each = n_items / alike;
     if (8 * each * alike >= 7 * n_items) n_items = each * alike;
   }
